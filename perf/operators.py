@@ -190,9 +190,11 @@ def _prepare_distill(c, gen):
         idx = torch.where(seen, idx, -1)
     s["t_idx"], s["t_logit"] = idx.to(torch.int32).contiguous(), z.contiguous()
     s["weight"] = torch.rand(rows, generator=gen, device="cuda") / rows
-    s["loss"], s["lse"] = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
-    if c["mode"] == "backward":
-        s["lse"] = torch.logsumexp(s["logits"].float() / c["tau"], dim=1)
+    s["loss"], s["stats"] = torch.empty(rows, device="cuda"), torch.empty((rows, 2), device="cuda")
+    if c["mode"] == "backward":  # what the forward call left: a row's largest logit, and the log of its sum beside it
+        x = s["logits"].float() / c["tau"]
+        m = x.amax(dim=1)
+        s["stats"] = torch.stack([m, (x - torch.where(m == -math.inf, 0.0, m)[:, None]).exp().sum(dim=1).log()], dim=1)
     if c["mode"] != "loss":
         s["dlogits"] = _empty_rows(rows, V, c["type"], c["pad"])
     return s
@@ -232,11 +234,11 @@ def _plain_adapter_grad(s):
 
 
 def _log_p(x):
-    """(x - lse, lse) of rows in fp32; a row that holds nothing but -inf has lse = -inf and log p = -inf."""
-    m = x.amax(dim=1, keepdim=True)
-    m = torch.where(m == -math.inf, 0.0, m)
-    total = (x - m).exp().sum(dim=1, keepdim=True)
-    return torch.where(x == -math.inf, -math.inf, (x - m) - total.log()), m + total.log()
+    """(log p, [largest, log of the sum of exp(x - largest)]) of rows in fp32; -inf throughout where a row holds nothing else."""
+    top = x.amax(dim=1, keepdim=True)
+    m = torch.where(top == -math.inf, 0.0, top)
+    log_total = (x - m).exp().sum(dim=1, keepdim=True).log()
+    return torch.where(x == -math.inf, -math.inf, (x - m) - log_total), torch.cat([top, log_total], dim=1)
 
 
 def _plain_scores(s):
@@ -253,8 +255,8 @@ def _teacher(s, tau):
     """(q, log q, token, whether there is any) of the teacher's entries, in fp32."""
     there = s["t_idx"] >= 0
     z = torch.where(there, s["t_logit"] / tau, -math.inf)
-    logq, lse = _log_p(z)
-    return logq.exp(), torch.where(there, logq, 0.0), s["t_idx"].clamp(min=0).long(), lse > -math.inf
+    logq, stats = _log_p(z)
+    return logq.exp(), torch.where(there, logq, 0.0), s["t_idx"].clamp(min=0).long(), stats[:, 1:] > -math.inf
 
 
 def _plain_gradient(s, p, q, at, live):
@@ -267,12 +269,12 @@ def _plain_distill(s):
     x = s["logits"].float() / tau
     q, logq, at, live = _teacher(s, tau)
     if mode == "backward":
-        live = live & (s["lse"] > -math.inf)[:, None]
-        return {"dlogits": _plain_gradient(s, (x - s["lse"][:, None]).exp(), q, at, live)}
-    logp, lse = _log_p(x)
-    live = live & (lse > -math.inf)
+        m, log_total = s["stats"][:, :1], s["stats"][:, 1:]
+        return {"dlogits": _plain_gradient(s, ((x - m) - log_total).exp(), q, at, live & (log_total > -math.inf))}
+    logp, stats = _log_p(x)
+    live = live & (stats[:, 1:] > -math.inf)
     each = torch.where(live & (q > 0), q * (logq - logp.gather(1, at)), 0.0)
-    out = {"loss": tau * tau * each.sum(dim=1), "lse": lse[:, 0]}
+    out = {"loss": tau * tau * each.sum(dim=1), "stats": stats}
     if mode == "step":
         out["dlogits"] = _plain_gradient(s, logp.exp(), q, at, live)
     return out
@@ -319,10 +321,10 @@ def _own(s):
         ctx.wcc_token_scores(d, s["logits"], s["tokens"], s["logprob"], s["entropy"], s["top_idx"], s["top_logprob"])
         return {k: s[k] for k in ("logprob", "entropy", "top_idx", "top_logprob")}
     if s["case"]["mode"] == "backward":
-        ctx.wcc_distill_backward(d, s["logits"], s["t_idx"], s["t_logit"], s["lse"], s["weight"], s["dlogits"])
+        ctx.wcc_distill_backward(d, s["logits"], s["t_idx"], s["t_logit"], s["stats"], s["weight"], s["dlogits"])
         return {"dlogits": s["dlogits"]}
-    ctx.wcc_distill_forward(d, s["logits"], s["t_idx"], s["t_logit"], s["loss"], s["lse"], s["weight"], s.get("dlogits"))
-    return {k: s[k] for k in ("loss", "lse", "dlogits") if k in s}
+    ctx.wcc_distill_forward(d, s["logits"], s["t_idx"], s["t_logit"], s["loss"], s["stats"], s["weight"], s.get("dlogits"))
+    return {k: s[k] for k in ("loss", "stats", "dlogits") if k in s}
 
 
 def run(state):
@@ -351,7 +353,7 @@ def work(case):
     if c["kind"] == "scores":
         return {"bytes": n * size + rows * (12 + 8 * c["top"]), "flops": 5 * n}
     grad = c["mode"] != "loss"
-    return {"bytes": n * size * (2 if grad else 1) + rows * (16 + 8 * c["K"]), "flops": (6 if grad else 4) * n}
+    return {"bytes": n * size * (2 if grad else 1) + rows * (20 + 8 * c["K"]), "flops": (6 if grad else 4) * n}
 
 
 # --------------------------------------------------------------------------------------------
@@ -396,7 +398,7 @@ def _exact_distill(s):
     c = s["case"]
     tau, mode = c["tau"], c["mode"]
     x = s["logits"].double() / tau
-    lse = s["lse"].double() if mode == "backward" else torch.logsumexp(x, dim=1)
+    lse = s["stats"].double().sum(dim=1) if mode == "backward" else torch.logsumexp(x, dim=1)
     there = s["t_idx"] >= 0
     live = there.any(dim=1) & (lse > -math.inf)
     q = torch.softmax(torch.where(there, s["t_logit"].double() / tau, -math.inf), dim=1)
@@ -405,7 +407,9 @@ def _exact_distill(s):
     out = {}
     if mode != "backward":
         picked = torch.where(q > 0, x.gather(1, at) - lse[:, None], 0.0)
-        out = {"loss": tau ** 2 * (torch.special.xlogy(q, q) - q * picked).sum(dim=1), "lse": lse}
+        best = x.max(dim=1).values
+        out = {"loss": tau ** 2 * (torch.special.xlogy(q, q) - q * picked).sum(dim=1),
+               "stats": torch.stack([best, torch.where(best == -math.inf, -math.inf, lse - best)], dim=1)}
     if mode != "loss":
         p = torch.exp(x - lse[:, None])
         p.scatter_add_(1, at, -q)
