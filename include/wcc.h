@@ -293,6 +293,120 @@ wcc_status wcc_block_forward(wcc_ctx *ctx, const wcc_block_desc *desc, const voi
  * profiling is on (default 1). */
 wcc_status wcc_set_block_profile_layer(wcc_ctx *ctx, int layer);
 
+/* ==== the head of a model, on rows of tokens =================================================
+ * What follows a network's last map: a projection that many requests share, each with a
+ * low-rank adapter of its own; what is answered from its logits; and the loss that tunes a
+ * compressed network by an uncompressed one.  A row is a token (or a pixel of a map whose
+ * channels come last).
+ *
+ * Conventions where they differ from those at the top of this file: a matrix of tokens has a row
+ * stride in elements, at least its width, and is aligned to its elements only (so is every other
+ * tensor here); rows = 0 enqueues nothing but the zeros of a gradient.  bf16 results are
+ * rounded once, to nearest even, from fp32; sums, statistics of rows and gradients of adapters are
+ * fp32.  Sums are added in an order that depends on the descriptor alone, so equal calls give
+ * equal bits.  Nothing but what is said below depends on the contents of index tensors: a value
+ * outside its range counts as "none". */
+
+/* ---- one projection, an adapter for each row ---------------------------------------------------
+ * y[t,:] = W x[t,:] + s_a B_a (A_a x[t,:]),   a = adapter_of_row[t]; a outside [0, adapters)
+ * means W x[t,:] alone.
+ *   x [rows, C_in] stride ldx   w [C_out, C_in]   y [rows, C_out] stride ldy
+ *   a [adapters, rank, C_in]    b [adapters, C_out, rank]
+ *   ranks [adapters] int32, nullable: adapter i has the first ranks[i] of the `rank` lines its
+ *     memory holds (clamped to 0..rank; the others are not used, whatever they hold)
+ *   scale [adapters] fp32, nullable: s (else 1)
+ * All matrices have the one type of `dtype`.  The products with bf16 matrices are exact in fp32;
+ * A x keeps 16 significant bits of its sum on the way into B (and B^T dy into A). */
+typedef struct {
+  int64_t rows;            /* tokens, >= 0 and < 2^31                                            */
+  int32_t C_in, C_out;     /* 1 .. 2^20                                                           */
+  int32_t adapters;        /* >= 0                                                                */
+  int32_t rank;            /* 1 .. WCC_MAX_RANK (0 with no adapters)                              */
+  int32_t dtype;           /* WCC_F32 or WCC_BF16                                                */
+  int64_t ldx, ldy;        /* row strides of x and dx, of y and dy: < 2^31                        */
+} wcc_adapter_desc;
+#define WCC_MAX_RANK 128
+
+/* Workspace of the two calls below for this descriptor (a multiple of 256). */
+wcc_status wcc_adapter_workspace_bytes(const wcc_adapter_desc *desc, size_t *bytes);
+
+wcc_status wcc_adapter_forward(wcc_ctx *ctx, const wcc_adapter_desc *desc, const void *x,
+                               const void *w, const int32_t *adapter_of_row /*nullable: none*/,
+                               const void *a, const void *b, const int32_t *ranks /*nullable*/,
+                               const float *scale /*nullable*/, void *y, void *stream);
+
+/* The gradients of the call above for a gradient dy of y; W is frozen and has none:
+ *   dx[t,:] = W^T dy[t,:] + s_a A_a^T (B_a^T dy[t,:])                     (type of x, nullable)
+ *   da[i,:,:] = s_i sum_t (B_i^T dy[t,:]) x[t,:]^T   over the rows of adapter i  (fp32, nullable)
+ *   db[i,:,:] = s_i sum_t dy[t,:] (A_i x[t,:])^T                          (fp32, nullable)
+ * da and db are written whole (zeros for adapters without rows and for lines past ranks[i]).
+ * x may be NULL if da and db are, w if dx is. */
+wcc_status wcc_adapter_backward(wcc_ctx *ctx, const wcc_adapter_desc *desc, const void *x,
+                                const void *w, const int32_t *adapter_of_row, const void *a,
+                                const void *b, const int32_t *ranks, const float *scale,
+                                const void *dy, void *dx, float *da, float *db, void *stream);
+
+/* ---- what is answered from logits --------------------------------------------------------------
+ * Per row, with lse = log sum_v exp(logits[v]):
+ *   logprob   logits[token] - lse for the row's token (NaN for a token outside [0, V))
+ *   entropy   -sum_v p log p, p = exp(logits - lse), 0 log 0 = 0
+ *   top_idx, top_logprob [rows, top]  the `top` largest logits, falling, ties to the lower index
+ * logits of -inf are masked: p = 0, log p = -inf.  A row in which nothing is left has log p = -inf
+ * everywhere, entropy 0, and the first indices as its top.  With a NaN or +inf in the row its log
+ * probabilities and entropy are NaN; in the order NaN comes before +inf. */
+typedef struct {
+  int64_t rows;            /* >= 0 and < 2^31                                                     */
+  int32_t V;               /* logits a row, >= 1                                                  */
+  int32_t top;             /* alternatives, 0 .. min(V, WCC_MAX_TOP)                              */
+  int32_t dtype;           /* of the logits: WCC_F32 or WCC_BF16                                 */
+  int64_t ld;              /* row stride, >= V                                                    */
+} wcc_scores_desc;
+#define WCC_MAX_TOP 64
+
+wcc_status wcc_scores_workspace_bytes(const wcc_scores_desc *desc, size_t *bytes);
+wcc_status wcc_token_scores(wcc_ctx *ctx, const wcc_scores_desc *desc, const void *logits,
+                            const int32_t *tokens /*nullable with logprob*/,
+                            float *logprob /*nullable*/, float *entropy /*nullable*/,
+                            int32_t *top_idx /*nullable if top = 0*/,
+                            float *top_logprob /*nullable*/, void *stream);
+
+/* ---- distillation from a teacher's top logits --------------------------------------------------
+ * The teacher of a row is K pairs (t_idx, t_logit); a pair whose index is outside [0, V) or whose
+ * logit is -inf is none, pairs of equal index add up.  With q = softmax(t_logit / temperature)
+ * over the pairs, lse = log sum_v exp(logits[v] / temperature), log p = logits / temperature - lse:
+ *   loss[t] = temperature^2 sum_k q_k (log q_k - log p[t_idx_k])
+ *   dlogits[t,v] = weight[t] temperature (p[v] - sum_{k: t_idx_k = v} q_k)
+ * the gradient of sum_t weight[t] loss[t] (weight nullable: 1).  A row without a pair, and one whose
+ * logits are all -inf, has loss 0 and gradient 0; where p is 0 and q is not the loss is +inf.
+ * t_idx [rows, K] int32 and t_logit [rows, K] are contiguous. */
+typedef struct {
+  int64_t rows;            /* >= 0 and < 2^31                                                     */
+  int32_t V;               /* logits a row, >= 1                                                  */
+  int32_t K;               /* teacher's pairs a row, 1 .. WCC_MAX_TEACHER                         */
+  int32_t dtype;           /* of logits and dlogits: WCC_F32 or WCC_BF16                         */
+  int32_t t_dtype;         /* of t_logit: WCC_F32 or WCC_BF16                                    */
+  float temperature;       /* > 0, finite                                                         */
+  int64_t ld, ld_grad;     /* row strides of logits and dlogits, >= V                             */
+} wcc_distill_desc;
+#define WCC_MAX_TEACHER 256
+
+wcc_status wcc_distill_workspace_bytes(const wcc_distill_desc *desc, size_t *bytes);
+
+/* The loss, and with dlogits given its gradient in the same call, which reads a row once where the
+ * row fits a compute unit.  dlogits may be logits itself if ld_grad = ld.  stats [rows, 2] receives
+ * a row's largest m = max_v logits[v] / temperature and log sum_v exp(logits[v] / temperature - m),
+ * whose sum is lse: apart, they keep what a sum in fp32 loses beside a large m.  Both are -inf in a
+ * row that has nothing left. */
+wcc_status wcc_distill_forward(wcc_ctx *ctx, const wcc_distill_desc *desc, const void *logits,
+                               const int32_t *t_idx, const void *t_logit, float *loss,
+                               float *stats /*nullable*/, const float *weight /*nullable*/,
+                               void *dlogits /*nullable*/, void *stream);
+
+/* The gradient, from the stats that wcc_distill_forward gave. */
+wcc_status wcc_distill_backward(wcc_ctx *ctx, const wcc_distill_desc *desc, const void *logits,
+                                const int32_t *t_idx, const void *t_logit, const float *stats,
+                                const float *weight /*nullable*/, void *dlogits, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

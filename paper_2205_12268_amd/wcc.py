@@ -24,7 +24,10 @@ EXPORTS = ("wcc_create", "wcc_destroy", "wcc_workspace_bytes", "wcc_set_workspac
            "wcc_status_string", "wcc_set_profiling", "wcc_stage_times", "wcc_haar_fwd",
            "wcc_joint_topk", "wcc_gather_quant", "wcc_pointwise", "wcc_scatter_ihaar",
            "wcc_forward", "wcc_forward_static", "wcc_forward_fixed", "wcc_block_workspace_bytes", "wcc_depthwise3x3", "wcc_block_forward",
-           "wcc_set_block_profile_layer", "wcc_block_is_chained")
+           "wcc_set_block_profile_layer", "wcc_block_is_chained",
+           "wcc_adapter_workspace_bytes", "wcc_adapter_forward", "wcc_adapter_backward",
+           "wcc_scores_workspace_bytes", "wcc_token_scores",
+           "wcc_distill_workspace_bytes", "wcc_distill_forward", "wcc_distill_backward")
 
 
 class Desc(C.Structure):
@@ -41,6 +44,23 @@ class BlockDesc(C.Structure):
                 ("W", C.c_int32), ("levels", C.c_int32), ("keep_num", C.c_int64),
                 ("keep_den", C.c_int64), ("w_dtype", C.c_int32), ("act_quant_bits", C.c_int32),
                 ("act_dtype", C.c_int32), ("norm", C.c_int32)]
+
+
+class AdapterDesc(C.Structure):
+    """Mirror of ``wcc_adapter_desc``."""
+    _fields_ = [("rows", C.c_int64), ("C_in", C.c_int32), ("C_out", C.c_int32), ("adapters", C.c_int32),
+                ("rank", C.c_int32), ("dtype", C.c_int32), ("ldx", C.c_int64), ("ldy", C.c_int64)]
+
+
+class ScoresDesc(C.Structure):
+    """Mirror of ``wcc_scores_desc``."""
+    _fields_ = [("rows", C.c_int64), ("V", C.c_int32), ("top", C.c_int32), ("dtype", C.c_int32), ("ld", C.c_int64)]
+
+
+class DistillDesc(C.Structure):
+    """Mirror of ``wcc_distill_desc``."""
+    _fields_ = [("rows", C.c_int64), ("V", C.c_int32), ("K", C.c_int32), ("dtype", C.c_int32), ("t_dtype", C.c_int32),
+                ("temperature", C.c_float), ("ld", C.c_int64), ("ld_grad", C.c_int64)]
 
 
 class WccError(RuntimeError):
@@ -85,6 +105,15 @@ def lib():
         L.wcc_block_forward.argtypes = [vp, bp] + [vp] * 12
         L.wcc_set_block_profile_layer.argtypes = [vp, C.c_int]
         L.wcc_block_is_chained.argtypes = [bp]
+        sz = C.POINTER(C.c_size_t)
+        L.wcc_adapter_workspace_bytes.argtypes = [C.POINTER(AdapterDesc), sz]
+        L.wcc_adapter_forward.argtypes = [vp, C.POINTER(AdapterDesc)] + [vp] * 9
+        L.wcc_adapter_backward.argtypes = [vp, C.POINTER(AdapterDesc)] + [vp] * 12
+        L.wcc_scores_workspace_bytes.argtypes = [C.POINTER(ScoresDesc), sz]
+        L.wcc_token_scores.argtypes = [vp, C.POINTER(ScoresDesc)] + [vp] * 7
+        L.wcc_distill_workspace_bytes.argtypes = [C.POINTER(DistillDesc), sz]
+        L.wcc_distill_forward.argtypes = [vp, C.POINTER(DistillDesc)] + [vp] * 8
+        L.wcc_distill_backward.argtypes = [vp, C.POINTER(DistillDesc)] + [vp] * 7
         for name in EXPORTS:
             if name not in ("wcc_k", "wcc_status_string"):
                 getattr(L, name).restype = C.c_int
@@ -138,11 +167,64 @@ def block_workspace_bytes(desc: BlockDesc) -> int:
     return int(out.value)
 
 
+def make_adapter_desc(rows, C_in, C_out, adapters, rank, dtype, ldx=None, ldy=None) -> AdapterDesc:
+    return AdapterDesc(rows, C_in, C_out, adapters, rank, dtype, C_in if ldx is None else ldx, C_out if ldy is None else ldy)
+
+
+def make_scores_desc(rows, V, top, dtype, ld=None) -> ScoresDesc:
+    return ScoresDesc(rows, V, top, dtype, V if ld is None else ld)
+
+
+def make_distill_desc(rows, V, K, dtype, t_dtype=F32, temperature=1.0, ld=None, ld_grad=None) -> DistillDesc:
+    return DistillDesc(rows, V, K, dtype, t_dtype, temperature, V if ld is None else ld, V if ld_grad is None else ld_grad)
+
+
+def _workspace_of(desc) -> int:
+    call = {BlockDesc: "wcc_block_workspace_bytes", AdapterDesc: "wcc_adapter_workspace_bytes",
+            ScoresDesc: "wcc_scores_workspace_bytes", DistillDesc: "wcc_distill_workspace_bytes"}.get(type(desc), "wcc_workspace_bytes")
+    out = C.c_size_t(0)
+    _check(getattr(lib(), call)(C.byref(desc), C.byref(out)), call)
+    return int(out.value)
+
+
+def adapter_workspace_bytes(desc: AdapterDesc) -> int:
+    return _workspace_of(desc)
+
+
+def scores_workspace_bytes(desc: ScoresDesc) -> int:
+    return _workspace_of(desc)
+
+
+def distill_workspace_bytes(desc: DistillDesc) -> int:
+    return _workspace_of(desc)
+
+
 def _ptr(t):
     if t is None:
         return None
     assert t.is_cuda and t.is_contiguous(), "device tensors must be contiguous"
     return C.c_void_p(t.data_ptr())
+
+
+_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
+_TORCH = {F32: torch.float32, BF16: torch.bfloat16}
+
+
+def _rows(t, rows, width, ld, dtype):
+    """Address of a matrix of tokens: [rows, width] of the descriptor's type, rows `ld` elements apart."""
+    if t is None:
+        return None
+    assert t.is_cuda and tuple(t.shape) == (rows, width) and _DTYPES.get(t.dtype) == dtype, "not the descriptor's matrix"
+    assert (width <= 1 or t.stride(1) == 1) and (rows <= 1 or t.stride(0) == ld), "not the descriptor's row stride"
+    return t.data_ptr()
+
+
+def _whole(t, shape, dtype):
+    """Address of a contiguous tensor of this shape and torch type."""
+    if t is None:
+        return None
+    assert t.is_cuda and t.is_contiguous() and t.dtype == dtype and tuple(t.shape) == shape, "not the descriptor's tensor"
+    return t.data_ptr()
 
 
 def _stream():
@@ -171,7 +253,7 @@ class Context:
             pass
 
     def ensure_workspace(self, desc) -> int:
-        need = block_workspace_bytes(desc) if isinstance(desc, BlockDesc) else workspace_bytes(desc)
+        need = _workspace_of(desc)
         if self._ws is None or self._ws.numel() < need:
             self._ws = torch.empty(need, dtype=torch.uint8, device=f"cuda:{self.device}")
             _check(lib().wcc_set_workspace(self._h, _ptr(self._ws), self._ws.numel()),
@@ -243,3 +325,43 @@ class Context:
 
     def set_block_profile_layer(self, layer: int) -> None:
         _check(lib().wcc_set_block_profile_layer(self._h, int(layer)), "wcc_set_block_profile_layer")
+
+    # ---- the head of a model, on rows of tokens ----
+    def wcc_adapter_forward(self, desc, x, w, adapter_of_row, a, b, ranks, scale, y):
+        d, t = desc, _TORCH[desc.dtype]
+        _check(lib().wcc_adapter_forward(
+            self._h, C.byref(d), _rows(x, d.rows, d.C_in, d.ldx, d.dtype), _whole(w, (d.C_out, d.C_in), t),
+            _whole(adapter_of_row, (d.rows,), torch.int32), _whole(a, (d.adapters, d.rank, d.C_in), t),
+            _whole(b, (d.adapters, d.C_out, d.rank), t), _whole(ranks, (d.adapters,), torch.int32),
+            _whole(scale, (d.adapters,), torch.float32), _rows(y, d.rows, d.C_out, d.ldy, d.dtype), _stream()), "wcc_adapter_forward")
+
+    def wcc_adapter_backward(self, desc, x, w, adapter_of_row, a, b, ranks, scale, dy, dx=None, da=None, db=None):
+        d, t = desc, _TORCH[desc.dtype]
+        _check(lib().wcc_adapter_backward(
+            self._h, C.byref(d), _rows(x, d.rows, d.C_in, d.ldx, d.dtype), _whole(w, (d.C_out, d.C_in), t),
+            _whole(adapter_of_row, (d.rows,), torch.int32), _whole(a, (d.adapters, d.rank, d.C_in), t),
+            _whole(b, (d.adapters, d.C_out, d.rank), t), _whole(ranks, (d.adapters,), torch.int32),
+            _whole(scale, (d.adapters,), torch.float32), _rows(dy, d.rows, d.C_out, d.ldy, d.dtype),
+            _rows(dx, d.rows, d.C_in, d.ldx, d.dtype), _whole(da, (d.adapters, d.rank, d.C_in), torch.float32),
+            _whole(db, (d.adapters, d.C_out, d.rank), torch.float32), _stream()), "wcc_adapter_backward")
+
+    def wcc_token_scores(self, desc, logits, tokens=None, logprob=None, entropy=None, top_idx=None, top_logprob=None):
+        d, f = desc, torch.float32
+        _check(lib().wcc_token_scores(
+            self._h, C.byref(d), _rows(logits, d.rows, d.V, d.ld, d.dtype), _whole(tokens, (d.rows,), torch.int32),
+            _whole(logprob, (d.rows,), f), _whole(entropy, (d.rows,), f), _whole(top_idx, (d.rows, d.top), torch.int32),
+            _whole(top_logprob, (d.rows, d.top), f), _stream()), "wcc_token_scores")
+
+    def wcc_distill_forward(self, desc, logits, t_idx, t_logit, loss, stats=None, weight=None, dlogits=None):
+        d, f = desc, torch.float32
+        _check(lib().wcc_distill_forward(
+            self._h, C.byref(d), _rows(logits, d.rows, d.V, d.ld, d.dtype), _whole(t_idx, (d.rows, d.K), torch.int32),
+            _whole(t_logit, (d.rows, d.K), _TORCH[d.t_dtype]), _whole(loss, (d.rows,), f), _whole(stats, (d.rows, 2), f),
+            _whole(weight, (d.rows,), f), _rows(dlogits, d.rows, d.V, d.ld_grad, d.dtype), _stream()), "wcc_distill_forward")
+
+    def wcc_distill_backward(self, desc, logits, t_idx, t_logit, stats, weight, dlogits):
+        d, f = desc, torch.float32
+        _check(lib().wcc_distill_backward(
+            self._h, C.byref(d), _rows(logits, d.rows, d.V, d.ld, d.dtype), _whole(t_idx, (d.rows, d.K), torch.int32),
+            _whole(t_logit, (d.rows, d.K), _TORCH[d.t_dtype]), _whole(stats, (d.rows, 2), f), _whole(weight, (d.rows,), f),
+            _rows(dlogits, d.rows, d.V, d.ld_grad, d.dtype), _stream()), "wcc_distill_backward")
