@@ -46,20 +46,29 @@ __device__ __forceinline__ u32x4 pack<bf16_t>(const float *f) {
   return v;
 }
 
+// The thread's number, computed anew where it is called: without, the offsets of all vectors are made before the loop over the
+// rows and take more registers than the row.
+__device__ __forceinline__ int thread_here() {
+  int t = (int)threadIdx.x;
+  asm volatile("" : "+v"(t));
+  return t;
+}
+
 // n elements from p on into the registers, the rest -inf
 template <class T, int NT, int NV>
 __device__ __forceinline__ void load_slice(const T *p, int n, u32x4 (&v)[NV]) {
   constexpr int VE = VecOf<T>::N;
   constexpr uint32_t none = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+  const int tid = thread_here();
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int e = (i * NT + (int)threadIdx.x) * VE;
+    const int e = (i * NT + tid) * VE;
     if (e + VE <= n) v[i] = *reinterpret_cast<const u32x4_any *>(p + e);
     else v[i] = u32x4{none, none, none, none};
   }
   // the one vector that the end cuts
   const int last = n / VE;
-  if (n % VE != 0 && last % NT == (int)threadIdx.x) {
+  if (n % VE != 0 && last % NT == tid) {
     u32x4 c = {none, none, none, none};
 #pragma unroll
     for (int j = 0; j < VE - 1; ++j)
@@ -81,19 +90,27 @@ __device__ __forceinline__ void hold(u32x4 (&v)[NV]) {
   for (int i = 0; i < NV; ++i) asm volatile("" : "+v"(v[i]));
 }
 
-// VE elements of vector i to a slice of n elements at p
-template <class T, int NT>
-__device__ __forceinline__ void store_vec(T *p, int n, int i, const u32x4 &v) {
+// n elements of a slice to p: the vectors f(i) in order, i from 0 on.
+template <class T, int NT, int NV, class F>
+__device__ __forceinline__ void store_slice(T *p, int n, F f) {
   constexpr int VE = VecOf<T>::N;
-  const int e = (i * NT + (int)threadIdx.x) * VE;
-  if (e + VE <= n) {
-    *reinterpret_cast<u32x4_any *>(p + e) = v;
-  } else if (e < n) {
+  const int tid = thread_here();
+  u32x4 cut = {};
 #pragma unroll
-    for (int j = 0; j < VE; ++j)
-      if (e + j < n) {
-        if constexpr (sizeof(T) == 4) p[e + j] = __uint_as_float(v[j]);
-        else p[e + j] = (bf16_t)(v[j >> 1] >> (16 * (j & 1)));
+  for (int i = 0; i < NV; ++i) {
+    const u32x4 v = f(i);
+    const int e = (i * NT + tid) * VE;
+    if (e + VE <= n) *reinterpret_cast<u32x4_any *>(p + e) = v;
+    if (i == n / VE / NT) cut = v;
+    __builtin_amdgcn_sched_barrier(0);  // (interleaved, the results would not fit beside the row)
+  }
+  const int last = n / VE;
+  if (n % VE != 0 && last % NT == tid) {
+#pragma unroll
+    for (int j = 0; j < VE - 1; ++j)
+      if (last * VE + j < n) {
+        if constexpr (sizeof(T) == 4) p[last * VE + j] = __uint_as_float(cut[j]);
+        else p[last * VE + j] = (bf16_t)(cut[j >> 1] >> (16 * (j & 1)));
       }
   }
 }
