@@ -59,32 +59,22 @@ struct Thin {
 };
 
 // ---- 16 bytes of k of one line -------------------------------------------------------------------------------
-// `left` elements are there (any number; <= 0: none), the rest is 0.
+// `left` elements are there (any number; <= 0: none), the rest is 0; consecutive k are `sk` elements apart.
+template <class T>
+__device__ __forceinline__ u32x4 load_k_strided(const T *p, int64_t sk, int left) {
+  constexpr int VE = VecOf<T>::N;
+  uint32_t e[VE];
+#pragma unroll
+  for (int j = 0; j < VE; ++j) e[j] = j < left ? bits_of(p[j * sk]) : 0u;
+  if constexpr (sizeof(T) == 4) return u32x4{e[0], e[1], e[2], e[3]};
+  else return u32x4{e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16};
+}
+// the same where they are neighbours
 template <class T>
 __device__ __forceinline__ u32x4 load_k(const T *p, int left) {
   constexpr int VE = VecOf<T>::N;
   if (left >= VE) return *reinterpret_cast<const u32x4_any *>(p);
-  u32x4 v = {0, 0, 0, 0};
-#pragma unroll
-  for (int j = 0; j < VE - 1; ++j)
-    if (j < left) {
-      if constexpr (sizeof(T) == 4) v[j] = __float_as_uint(p[j]);
-      else v[j >> 1] |= (uint32_t)p[j] << (16 * (j & 1));
-    }
-  return v;
-}
-// the same where consecutive k are `sk` elements apart
-template <class T>
-__device__ __forceinline__ u32x4 load_k_strided(const T *p, int64_t sk, int left) {
-  constexpr int VE = VecOf<T>::N;
-  u32x4 v = {0, 0, 0, 0};
-#pragma unroll
-  for (int j = 0; j < VE; ++j)
-    if (j < left) {
-      if constexpr (sizeof(T) == 4) v[j] = __float_as_uint(p[j * sk]);
-      else v[j >> 1] |= (uint32_t)p[j * sk] << (16 * (j & 1));
-    }
-  return v;
+  return load_k_strided(p, 1, left);
 }
 // Two neighbouring lines at once where lines are contiguous and k is not: (line, line + 1) of each k is one load, the halves of
 // which go to the two lines.  `both`: the second line is there (it may be the end of memory).
@@ -93,18 +83,13 @@ typedef uint64_t u64_any __attribute__((aligned(4)));
 template <class T>
 __device__ __forceinline__ void load_k_pair(const T *p, int64_t sk, int left, bool both, u32x4 &f0, u32x4 &f1) {
   constexpr int VE = VecOf<T>::N;
-  f0 = f1 = u32x4{0, 0, 0, 0};
   if constexpr (sizeof(T) == 4) {
+    uint64_t v[4];
 #pragma unroll
-    for (int j = 0; j < VE; ++j)
-      if (j < left) {
-        if (both) {
-          const uint64_t v = *reinterpret_cast<const u64_any *>(p + j * sk);
-          f0[j] = (uint32_t)v, f1[j] = (uint32_t)(v >> 32);
-        } else {
-          f0[j] = __float_as_uint(p[j * sk]);
-        }
-      }
+    for (int j = 0; j < 4; ++j)
+      v[j] = j < left ? both ? *reinterpret_cast<const u64_any *>(p + j * sk) : (uint64_t)__float_as_uint(p[j * sk]) : 0;
+    f0 = u32x4{(uint32_t)v[0], (uint32_t)v[1], (uint32_t)v[2], (uint32_t)v[3]};
+    f1 = u32x4{(uint32_t)(v[0] >> 32), (uint32_t)(v[1] >> 32), (uint32_t)(v[2] >> 32), (uint32_t)(v[3] >> 32)};
   } else {
     uint32_t v[VE];
 #pragma unroll
@@ -145,17 +130,58 @@ struct PartsOf {
   static constexpr int Grad = sizeof(T) == 4 ? 1 : 3;  // into an fp32 gradient
 };
 
-// The rank lines of every row: [splits][rows][rank] fp32, summed over the splits (in their order) where they are used.
+// The rank lines of every row: [splits][rows][ld] fp32, ld a multiple of 8, summed over the splits (in their order) where they
+// are used.  Lines past an adapter's rank are 0 up to the next multiple of 8; rows without an adapter hold anything.
 struct Lines {
   float *p;
-  int splits;
-  int64_t stride;  // rows * rank
+  int splits, ld;
+  int64_t stride;  // rows * ld
   __device__ __forceinline__ float at(int64_t i) const {
     float v = p[i];
-    for (int s = 1; s < splits; ++s) v += p[s * stride + i];
+    for (int s = 1; s < splits; s += 4) {  // (four loads at a time: one by one each would wait for the last)
+      float w[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) w[u] = s + u < splits ? p[(s + u) * stride + i] : 0.f;
+      v += (w[0] + w[1]) + (w[2] + w[3]);
+    }
     return v;
   }
+  // eight lines from j (a multiple of 8) on
+  __device__ __forceinline__ void eight(int64_t t, int j, float (&v)[8]) const {
+    const float4 *q = reinterpret_cast<const float4 *>(p + t * ld + j);
+    float4 a = q[0], b = q[1];
+    auto add = [](const float4 &u, const float4 &w) { return make_float4(u.x + w.x, u.y + w.y, u.z + w.z, u.w + w.w); };
+    const int64_t step = stride >> 2;
+    int s = 1;
+    for (; s + 1 < splits; s += 2) {  // (the order of the splits; two at a time so that loads do not wait for each other)
+      const float4 c0 = q[s * step], d0 = q[s * step + 1], c1 = q[(s + 1) * step], d1 = q[(s + 1) * step + 1];
+      a = add(add(a, c0), c1), b = add(add(b, d0), d1);
+    }
+    if (s < splits) a = add(a, q[s * step]), b = add(b, q[s * step + 1]);
+    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+  }
 };
+
+// VE rank lines of one column of the thin operand from line j on, `left` of them there; what is past them meets zeros of h and
+// only has to be finite where the lines are.
+template <class T>
+__device__ __forceinline__ u32x4 thin_k(const Thin<T> &m, int a, int o, int j, int left) {
+  constexpr int VE = VecOf<T>::N;
+  const T *p = m.p + a * m.major + (int64_t)o * m.sc;
+  if (m.sj == 1) return load_k(p + j, left);
+  u32x4 v;
+  T e[VE];
+#pragma unroll
+  for (int i = 0; i < VE; ++i) e[i] = p[(int64_t)min(j + i, j + left - 1) * m.sj];
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __float_as_uint(e[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = (uint32_t)e[2 * i] | (uint32_t)e[2 * i + 1] << 16;
+  }
+  return v;
+}
 
 // One projection: y[t, o] = sum_k x[t, k] w(o, k) + sum_j m(a, j, o) h[t, j], w(o, k) at o * wo + k * wk (one of them is 1).
 template <class T>
@@ -172,7 +198,189 @@ struct Project {
   int64_t ldy;
 };
 
+// acc += the rank lines' product for the 32 rows from t0 on (lines of the result) and 32 outputs, o of each lane.  The sums of
+// each adapter among the rows apart: a row takes its own, whatever (infinities, NaN) other adapters hold.
+template <class T, int E>
+__device__ __forceinline__ void add_thin(const Low &low, const Thin<T> &m, const Lines &h, int64_t rows, int outs, int64_t t0,
+                                         const int (&o)[E], f32x16 (&acc)[E]) {
+  constexpr int VE = VecOf<T>::N, KS = StepOf<T>::K, P = PartsOf<T>::Out;
+  const int ln = threadIdx.x & 31, half = (threadIdx.x >> 5) & 1;
+  const int64_t t = min(t0 + ln, rows - 1);
+  const int id = t0 + ln < rows ? low.of(t) : -1;
+  uint32_t rest = (uint32_t)__ballot(id >= 0);
+  while (rest != 0) {
+    const int a = __builtin_amdgcn_readlane(id, __builtin_ctz(rest));
+    const uint32_t same = (uint32_t)__ballot(id == a);
+    rest &= ~same;
+    const int lines = low.lines(a);
+    f32x16 d[E] = {};
+    for (int j0 = 0; j0 < lines; j0 += KS) {
+      const int j = j0 + half * VE, left = lines - j;
+      u32x4 hf[P] = {}, mf[E] = {};
+      if (left > 0) {
+        float hv[8];
+        h.eight(t, j & ~7, hv);
+        if constexpr (VE == 4) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) hv[i] = half ? hv[4 + i] : hv[i];
+        }
+        split_to<T, P>(hv, hf);
+#pragma unroll
+        for (int e = 0; e < E; ++e) mf[e] = thin_k(m, a, min(o[e], outs - 1), j, left);
+      }
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+#pragma unroll
+        for (int q = P - 1; q >= 0; --q) d[e] = mma<T>(hf[q], mf[e], d[e]);
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[e][i] += same >> result_line(i, half) & 1 ? d[e][i] : 0.f;
+  }
+}
+
+// ---- making the rank lines --------------------------------------------------------------------------------------
+// h[t, j] = s_a sum_c m(a, j, c) x[t, c] for the rows of every adapter, in ranges of k.
+// Up to 64 rows: a wave takes 32 of them, a range of k and, of the distinct adapters among the rows, every groups-th.
+// More: a workgroup takes 128 rows and a range of k, brings the rows in the order of their adapters, and its waves take 32 of one
+// adapter at a time, so that rows in any order meet each adapter's lines once.
 template <class T>
-hipError_t launch_tiles(const Project<T> &p, hipStream_t s);
+struct ThinJob {
+  const T *x;
+  int64_t ldx, rows;
+  int width;
+  Thin<T> m;
+  Lines out;
+  int chunk, groups;
+  bool by_range;
+  int64_t units, blocks;  // blocks of four waves; units: of waves, not by_range
+};
+
+constexpr int kRange = 128;
+struct ThinLds {
+  int key[kRange], row[kRange], of[kRange], head[kRange], heads;
+};
+
+// the sums over k0 .. k1 of 32 rows (of the lane: xr, at its half's chunk) with 32 lines (mr)
+template <class T>
+__device__ __forceinline__ f32x16 thin_sums(const T *xr, const T *mr, int sc, int k0, int k1, int half) {
+  constexpr int VE = VecOf<T>::N, KS = StepOf<T>::K, U = 8;
+  f32x16 acc = {};
+  int k = k0;
+  for (; k + KS * U <= k1; k += KS * U) {
+    u32x4 xf[U], mf[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      xf[u] = *reinterpret_cast<const u32x4_any *>(xr + k + u * KS);
+      mf[u] = sc == 1 ? *reinterpret_cast<const u32x4_any *>(mr + k + u * KS)
+                      : load_k_strided(mr + (int64_t)(k + u * KS) * sc, sc, VE);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) acc = mma<T>(xf[u], mf[u], acc);
+  }
+  for (; k < k1; k += KS) {
+    const int left = k1 - k - half * VE;
+    const u32x4 xf = load_k(xr + k, left);
+    const u32x4 mf = sc == 1 ? load_k(mr + k, left) : load_k_strided(mr + (int64_t)k * sc, sc, left);
+    acc = mma<T>(xf, mf, acc);
+  }
+  return acc;
+}
+
+template <class T>
+__device__ __forceinline__ void thin_unit(const ThinJob<T> &g, const Low &low, int64_t unit) {
+  constexpr int VE = VecOf<T>::N;
+  const int lane = threadIdx.x & 63, ln = lane & 31, half = lane >> 5;
+  const int group = (int)(unit % g.groups), split = (int)(unit / g.groups % g.out.splits);
+  const int64_t t0 = unit / g.groups / g.out.splits * 32, t = t0 + ln;
+  const int id = t < g.rows ? low.of(t) : -1;
+  const int k0 = split * g.chunk, k1 = min(g.width, k0 + g.chunk);
+  const T *xr = g.x + min(t, g.rows - 1) * g.ldx + half * VE;
+  float *out = g.out.p + split * g.out.stride + t0 * g.out.ld;
+  uint32_t rest = (uint32_t)__ballot(id >= 0);  // (the halves of the wave hold the same rows)
+  for (int nth = 0; rest != 0; ++nth) {
+    const int a = __builtin_amdgcn_readlane(id, __builtin_ctz(rest));
+    const uint32_t same = (uint32_t)__ballot(id == a);
+    rest &= ~same;
+    if (nth % g.groups != group) continue;
+    const int lines = low.lines(a);
+    const float f = low.factor(a);
+    for (int j0 = 0; j0 < lines; j0 += 32) {
+      const T *mr = g.m.p + a * g.m.major + (int64_t)min(j0 + ln, lines - 1) * g.m.sj + (int64_t)(half * VE) * g.m.sc;
+      const f32x16 acc = thin_sums<T>(xr, mr, g.m.sc, k0, k1, half);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int row = result_line(i, half);
+        if ((same >> row & 1) && j0 + ln < g.out.ld) out[(int64_t)row * g.out.ld + j0 + ln] = j0 + ln < lines ? acc[i] * f : 0.f;
+      }
+    }
+  }
+}
+
+template <class T>
+__device__ __forceinline__ void thin_range(const ThinJob<T> &g, const Low &low, int64_t block, ThinLds &lds) {
+  constexpr int VE = VecOf<T>::N, none = 0x7fffffff;
+  const int tid = threadIdx.x, lane = tid & 63, ln = lane & 31, half = lane >> 5;
+  const int split = (int)(block % g.out.splits);
+  const int64_t base = block / g.out.splits * kRange;
+  if (tid < kRange) {
+    const int id = base + tid < g.rows ? low.of(base + tid) : -1;
+    lds.key[tid] = id < 0 ? none : id;
+  }
+  if (tid == 0) lds.heads = 0;
+  __syncthreads();
+  if (tid < kRange) {
+    const int key = lds.key[tid];
+    int less = 0, before = 0, equal = 0;
+    for (int i = 0; i < kRange; ++i) {
+      const int k = lds.key[i];
+      less += k < key;
+      equal += k == key;
+      before += k == key && i < tid;
+    }
+    lds.row[less + before] = tid;
+    lds.of[less + before] = key;
+    if (key != none && before % 32 == 0)  // (the order of the heads decides nothing)
+      lds.head[atomicAdd(&lds.heads, 1)] = (less + before) | min(equal - before, 32) << 16;
+  }
+  __syncthreads();
+  const int k0 = split * g.chunk, k1 = min(g.width, k0 + g.chunk), heads = lds.heads;
+  for (int h = tid >> 6; h < heads; h += 4) {
+    const int pos = __builtin_amdgcn_readfirstlane(lds.head[h]) & 0xffff, n = __builtin_amdgcn_readfirstlane(lds.head[h]) >> 16;
+    const int a = __builtin_amdgcn_readfirstlane(lds.of[pos]);
+    const int lines = low.lines(a);
+    const float f = low.factor(a);
+    const T *xr = g.x + (base + lds.row[pos + min(ln, n - 1)]) * g.ldx + half * VE;
+    float *out = g.out.p + split * g.out.stride + base * g.out.ld;
+    for (int j0 = 0; j0 < lines; j0 += 32) {
+      const T *mr = g.m.p + a * g.m.major + (int64_t)min(j0 + ln, lines - 1) * g.m.sj + (int64_t)(half * VE) * g.m.sc;
+      const f32x16 acc = thin_sums<T>(xr, mr, g.m.sc, k0, k1, half);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int q = result_line(i, half);
+        if (q < n && j0 + ln < g.out.ld) out[(int64_t)lds.row[pos + q] * g.out.ld + j0 + ln] = j0 + ln < lines ? acc[i] * f : 0.f;
+      }
+    }
+  }
+}
+
+// a workgroup of four waves
+template <class T>
+__device__ __forceinline__ void thin_block(const ThinJob<T> &g, const Low &low, int64_t block, void *lds) {
+  if (g.by_range) return thin_range<T>(g, low, block, *static_cast<ThinLds *>(lds));
+  const int64_t unit = block * 4 + (threadIdx.x >> 6);
+  if (unit < g.units) thin_unit<T>(g, low, unit);
+}
+
+template <class T>
+void launch_tiles(const Project<T> &p, hipStream_t s);  // adapter_tile.hip: anything
+// adapter_gemm.hip: rows that 16-byte loads can take
+bool gemm_takes(const Project<bf16_t> &p);
+int gemm_splits(int64_t rows, int width, int outs);  // ranges of k; 1: whole tiles
+void launch_gemm(const Project<bf16_t> &p, hipStream_t s);
+// the ranges' sums to part [splits][rows][outs], and the rank lines of one or two jobs beside
+void launch_gemm_split(const Project<bf16_t> &p, int splits, float *part, const ThinJob<bf16_t> &thin, const ThinJob<bf16_t> &other,
+                       hipStream_t s);
 
 }  // namespace wcc

@@ -15,64 +15,14 @@
 namespace wcc {
 namespace {
 
-// ---- the rank lines of rows -----------------------------------------------------------------------------------
-// A wave takes 32 rows, a range of k and, of the distinct adapters among the rows, every groups-th.
+// One or two jobs of rank lines by themselves, before whole tiles.
 template <class T>
-struct ThinJob {
-  const T *x;
-  int64_t ldx, rows;
-  int width;
-  Thin<T> m;
-  float *out;  // [splits][rows][rank]
-  int splits, chunk, groups;
-  int64_t units;
-};
-
-template <class T>
-__device__ __forceinline__ void thin_unit(const ThinJob<T> &g, const Low &low, int64_t unit) {
-  constexpr int VE = VecOf<T>::N, KS = StepOf<T>::K, U = 4;
-  const int lane = threadIdx.x & 63, ln = lane & 31, half = lane >> 5;
-  const int group = (int)(unit % g.groups), split = (int)(unit / g.groups % g.splits);
-  const int64_t t0 = unit / g.groups / g.splits * 32, t = t0 + ln;
-  const int id = t < g.rows ? low.of(t) : -1;
-  const int k0 = split * g.chunk, k1 = min(g.width, k0 + g.chunk);
-  const T *xr = g.x + min(t, g.rows - 1) * g.ldx + half * VE;
-  float *out = g.out + ((int64_t)split * g.rows + t0) * low.rank;
-  uint32_t rest = (uint32_t)__ballot(id >= 0);  // (the halves of the wave hold the same rows)
-  for (int nth = 0; rest != 0; ++nth) {
-    const int a = __builtin_amdgcn_readlane(id, __builtin_ctz(rest));
-    const uint32_t same = (uint32_t)__ballot(id == a);
-    rest &= ~same;
-    if (nth % g.groups != group) continue;
-    const int lines = low.lines(a);
-    const float f = low.factor(a);
-    for (int j0 = 0; j0 < lines; j0 += 32) {
-      const T *mr = g.m.p + a * g.m.major + (int64_t)min(j0 + ln, lines - 1) * g.m.sj + (int64_t)(half * VE) * g.m.sc;
-      f32x16 acc = {};
-      int k = k0;
-      for (; k + KS * U <= k1; k += KS * U) {
-        u32x4 xf[U], mf[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          xf[u] = *reinterpret_cast<const u32x4_any *>(xr + k + u * KS);
-          mf[u] = g.m.sc == 1 ? *reinterpret_cast<const u32x4_any *>(mr + k + u * KS)
-                              : load_k_strided(mr + (int64_t)(k + u * KS) * g.m.sc, g.m.sc, VE);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) acc = mma<T>(xf[u], mf[u], acc);
-      }
-      for (; k < k1; k += KS) {
-        const int left = k1 - k - half * VE;
-        const u32x4 xf = load_k(xr + k, left);
-        const u32x4 mf = g.m.sc == 1 ? load_k(mr + k, left) : load_k_strided(mr + (int64_t)k * g.m.sc, g.m.sc, left);
-        acc = mma<T>(xf, mf, acc);
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int row = result_line(i, half);
-        if ((same >> row & 1) && j0 + ln < lines) out[(int64_t)row * low.rank + j0 + ln] = acc[i] * f;
-      }
-    }
+__global__ __launch_bounds__(256) void adapter_lines_kernel(ThinJob<T> g1, ThinJob<T> g2, Low low) {
+  __shared__ ThinLds lds;
+  for (int64_t b = blockIdx.x; b < g1.blocks + g2.blocks; b += gridDim.x) {
+    if (b < g1.blocks) thin_block<T>(g1, low, b, &lds);
+    else thin_block<T>(g2, low, b - g1.blocks, &lds);
+    __syncthreads();
   }
 }
 
@@ -164,58 +114,122 @@ __device__ __forceinline__ void stream_block(const StreamJob<T> &g, int64_t bloc
     }
 }
 
-// First launch: blocks of the product with W, then waves of one or two jobs of rank lines.
+// First launch: workgroups of one or two jobs of rank lines (they take longest), then of the product with W.
 template <class T, int RT, bool NN>
 __global__ __launch_bounds__(256) void adapter_products_kernel(StreamJob<T> g, ThinJob<T> thin, ThinJob<T> thin2, Low low) {
   __shared__ float red[4 * 32 * RT * 72];
   const int64_t block = blockIdx.x;
-  if (block < g.blocks) return stream_block<T, RT, NN>(g, block, red);
-  const int64_t unit = (block - g.blocks) * 4 + (threadIdx.x >> 6);
-  if (unit < thin.units) return thin_unit<T>(thin, low, unit);
-  if (unit - thin.units < thin2.units) thin_unit<T>(thin2, low, unit - thin.units);
+  if (block < thin.blocks) return thin_block<T>(thin, low, block, red);
+  if (block < thin.blocks + thin2.blocks) return thin_block<T>(thin2, low, block - thin.blocks, red);
+  stream_block<T, RT, NN>(g, block - thin.blocks - thin2.blocks, red);
 }
 
-// Second launch: y[t, o] = the sum of the parts + sum_j m(a, j, o) h[t, j].  256 outputs x RB rows a workgroup.
-template <class T>
-__global__ __launch_bounds__(256) void adapter_finish_kernel(const float *__restrict__ part, int splits, int64_t rows, int outs,
-                                                             Low low, Thin<T> m, Lines h, T *__restrict__ y, int64_t ldy, int rb,
-                                                             int tiles_o, int64_t blocks) {
-  constexpr int VE = VecOf<T>::N;
-  __shared__ float hs[WCC_MAX_RANK];
-  for (int64_t b = blockIdx.x; b < blocks; b += gridDim.x) {
-    const int o = (int)(b % tiles_o) * 256 + (int)threadIdx.x;
-    const int64_t t0 = b / tiles_o * rb;
-    for (int64_t t = t0; t < min(t0 + rb, rows); ++t) {
-      const int a = low.of(t), lines = a >= 0 ? low.lines(a) : 0;
-      __syncthreads();
-      if ((int)threadIdx.x < lines) hs[threadIdx.x] = h.at(t * low.rank + threadIdx.x);
-      float v = 0.f;
-      if (o < outs)
-        for (int s = 0; s < splits; ++s) v += part[(s * rows + t) * outs + o];
-      __syncthreads();
-      if (o >= outs) continue;
-      if (lines > 0) {
-        const T *mr = m.p + a * m.major + (int64_t)o * m.sc;
-        float low_v = 0.f;
-        if (m.sj == 1) {
-          for (int j = 0; j < lines; j += VE) {
-            const u32x4 f = load_k(mr + j, lines - j);
+// The sum of the parts of one result, four loads at a time.
+__device__ __forceinline__ float sum_parts(const float *__restrict__ p, int splits, int64_t stride) {
+  float v = p[0];
+  for (int s = 1; s < splits; s += 4) {
+    float w[4];
 #pragma unroll
-            for (int i = 0; i < VE; ++i)
-              if (j + i < lines) low_v = fmaf(elem<T>(f, i), hs[j + i], low_v);
-          }
-        } else {
-          for (int j = 0; j < lines; ++j) low_v = fmaf(widen(mr[(int64_t)j * m.sj]), hs[j], low_v);
-        }
-        v += low_v;
-      }
-      y[t * ldy + o] = narrow<T>(v);
+    for (int u = 0; u < 4; ++u) w[u] = s + u < splits ? p[(s + u) * stride] : 0.f;
+    v += (w[0] + w[1]) + (w[2] + w[3]);
+  }
+  return v;
+}
+
+template <class T>
+struct FinishJob {
+  const float *part;
+  int splits, outs, tiles_o;
+  int64_t rows;
+  Thin<T> m;
+  Lines h;
+  T *y;
+  int64_t ldy, blocks;
+};
+
+// Second launch: y[t, o] = the sum of the parts + sum_j m(a, j, o) h[t, j].
+// Few rows, each likely with an adapter of its own: 256 outputs of a row a workgroup.
+template <class T>
+__global__ __launch_bounds__(256) void adapter_finish_row_kernel(FinishJob<T> g, Low low) {
+  constexpr int VE = VecOf<T>::N, Q = 32 / VE;
+  __shared__ float hs[WCC_MAX_RANK];
+  for (int64_t b = blockIdx.x; b < g.blocks; b += gridDim.x) {
+    const int o = (int)(b % g.tiles_o) * 256 + (int)threadIdx.x, oc = min(o, g.outs - 1);
+    const int64_t t = b / g.tiles_o;
+    const int a = low.of(t), lines = a >= 0 ? low.lines(a) : 0;
+    u32x4 mf[Q];  // the first 32 lines' loads go out together with the others
+#pragma unroll
+    for (int q = 0; q < Q; ++q) mf[q] = q * VE < lines ? thin_k(g.m, a, oc, q * VE, lines - q * VE) : u32x4{};
+    float v = sum_parts(g.part + t * g.outs + oc, g.splits, g.rows * g.outs);
+    if ((int)threadIdx.x < lines) hs[threadIdx.x] = g.h.at(t * g.h.ld + threadIdx.x);
+    __syncthreads();
+    float low_v = 0.f;
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
+#pragma unroll
+      for (int i = 0; i < VE; ++i)
+        if (q * VE + i < lines) low_v = fmaf(elem<T>(mf[q], i), hs[q * VE + i], low_v);
+    for (int j = 32; j < lines; j += VE) {
+      const u32x4 f = thin_k(g.m, a, oc, j, lines - j);
+#pragma unroll
+      for (int i = 0; i < VE; ++i)
+        if (j + i < lines) low_v = fmaf(elem<T>(f, i), hs[j + i], low_v);
     }
+    if (o < g.outs) g.y[t * g.ldy + o] = narrow<T>(v + low_v);
+    __syncthreads();
+  }
+}
+
+// More rows: 32 rows x 128 outputs a workgroup, the parts added up through LDS, 32 outputs a wave then.
+template <class T>
+__global__ __launch_bounds__(256) void adapter_finish_tile_kernel(FinishJob<T> g, Low low) {
+  constexpr int LD = 132;
+  __shared__ __align__(16) float sums[32][LD];
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, ln = lane & 31, half = lane >> 5;
+  for (int64_t b = blockIdx.x; b < g.blocks; b += gridDim.x) {
+    const int o0 = (int)(b % g.tiles_o) * 128, oq = o0 + (tid & 31) * 4;
+    const int64_t t0 = b / g.tiles_o * 32, stride = g.rows * g.outs;
+    f32x4_any v[4] = {};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float *p = g.part + min(t0 + (tid >> 5) + 8 * i, g.rows - 1) * g.outs + min(oq, g.outs - 1);
+      if (oq + 4 <= g.outs) {
+        int s = 0;
+        for (; s + 4 <= g.splits; s += 4) {
+          f32x4_any w[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) w[u] = *reinterpret_cast<const f32x4_any *>(p + (s + u) * stride);
+          v[i] += (w[0] + w[1]) + (w[2] + w[3]);
+        }
+        for (; s < g.splits; ++s) v[i] += *reinterpret_cast<const f32x4_any *>(p + s * stride);
+      } else {
+#pragma unroll
+        for (int q = 0; q < 3; ++q)
+          if (oq + q < g.outs) v[i][q] = sum_parts(p + q, g.splits, stride);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<float4 *>(&sums[(tid >> 5) + 8 * i][(tid & 31) * 4]) = make_float4(v[i][0], v[i][1], v[i][2], v[i][3]);
+    __syncthreads();
+    const int o[1] = {o0 + wv * 32 + ln};
+    f32x16 acc[1];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[0][i] = sums[result_line(i, half)][wv * 32 + ln];
+    if (low.of_row) add_thin<T, 1>(low, g.m, g.h, g.rows, g.outs, t0, o, acc);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int64_t t = t0 + result_line(i, half);
+      if (t < g.rows && o[0] < g.outs) g.y[t * g.ldy + o[0]] = narrow<T>(acc[0][i]);
+    }
+    __syncthreads();
   }
 }
 
 // ---- gradients of the adapters ------------------------------------------------------------------------------------
 // grad(a, j, c) = sum over the rows t of adapter a of h[t, j] x[t, c], at a * major + j * sj + c * sc.
+// A workgroup has an adapter, 512 columns, 32 lines and a range of rows.  It lists the rows that are the adapter's, 256 of the
+// range at a time, so that rows of many adapters in any order are read once in all.  The listed rows' h go to LDS as
+// operands (bf16: in three parts, which keep all 24 bits), x from memory: a lane has four columns of the rows of a step.
 template <class T>
 struct GradJob {
   const T *x;
@@ -231,130 +245,233 @@ struct GradJob {
   int64_t blocks;
 };
 
-// A workgroup has an adapter, 256 columns, 32 lines and a range of rows; it lists the rows that are the adapter's, so that rows
-// of many adapters in any order are read once in all.
+constexpr int kListed = 256 + 16;  // rows of a round, and what is left of the last step of the one before
+
 template <class T>
+struct GradLds {
+  static constexpr int P = PartsOf<T>::Grad;
+  T h[P][32][kListed];
+  int list[kListed], rest[16], counts[2][4];
+};
+
+// four columns (some of them past the width) of a row
+template <class T>
+__device__ __forceinline__ void load_four(const T *p, int left, uint32_t (&v)[(int)sizeof(T)]) {
+  if constexpr (sizeof(T) == 4) {
+    if (left >= 4) {
+      const u32x4 q = *reinterpret_cast<const u32x4_any *>(p);
+      v[0] = q[0], v[1] = q[1], v[2] = q[2], v[3] = q[3];
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = i < left ? __float_as_uint(p[i]) : 0u;
+    }
+  } else {
+    if (left >= 4) {
+      typedef uint64_t u64_2 __attribute__((aligned(2)));
+      const uint64_t q = *reinterpret_cast<const u64_2 *>(p);
+      v[0] = (uint32_t)q, v[1] = (uint32_t)(q >> 32);
+    } else {
+      v[0] = left > 0 ? (uint32_t)p[0] | (left > 1 ? (uint32_t)p[1] << 16 : 0u) : 0u;
+      v[1] = left > 2 ? (uint32_t)p[2] : 0u;
+    }
+  }
+}
+
+template <class T, bool FLIP>
 __device__ __forceinline__ void grad_block(const GradJob<T> &g, const Low &low, int64_t rows, int splits, int64_t range, int64_t block,
-                                           int *list, int *counts) {
-  constexpr int VE = VecOf<T>::N, KS = StepOf<T>::K, P = PartsOf<T>::Grad;
+                                           GradLds<T> &lds) {
+  constexpr int VE = VecOf<T>::N, KS = StepOf<T>::K, P = GradLds<T>::P, D = (int)sizeof(T);
   const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, ln = lane & 31, half = lane >> 5;
   const int tiles_j = (low.rank + 31) / 32;
   const int split = (int)(block % splits), j0 = (int)(block / splits % tiles_j) * 32;
   const int tile_c = (int)(block / splits / tiles_j % g.tiles_c), a = (int)(block / splits / tiles_j / g.tiles_c);
-  const int lines = low.lines(a), c = tile_c * 256 + wv * 64 + 2 * ln, j = j0 + ln;
-  const bool here = c < g.width, both = c + 1 < g.width;
+  const int lines = low.lines(a), cw = tile_c * 512 + wv * 128, c = cw + 4 * ln, left = g.width - c;
+  const bool busy = cw < g.width;
   const T *xc = g.x + min(c, g.width - 1);
   const int64_t t_end = min(rows, (split + 1) * range);
-  f32x16 acc[2] = {};
-  int have = 0, total = 0;
-  auto step = [&](int at, int n) {  // n (at most KS) listed rows from `at` on
-    float hv[VE];
-    u32x4 xf[2], hf[P];
-    uint32_t v32[VE];
-    uint64_t v64[VE];
+  f32x16 acc[4] = {};
+  int have = 0, total = 0, round = 0;
+
+  // the columns of the listed rows of step s; of a single step of n < KS rows the others are zeros
+  auto fetch = [&](int s, int n, uint32_t (&v)[VE][D]) {
+    const int at = s * KS + half * VE;
 #pragma unroll
     for (int i = 0; i < VE; ++i) {
-      const int q = half * VE + i;
-      hv[i] = 0.f;
-      v32[i] = 0, v64[i] = 0;
-      if (q < n) {
-        const int64_t t = list[at + q];
-        if (j < lines) hv[i] = g.h.at(t * low.rank + j);
-        const T *p = xc + t * g.ldx;
-        if constexpr (sizeof(T) == 4) v64[i] = both ? *reinterpret_cast<const u64_any *>(p) : here ? (uint64_t)__float_as_uint(*p) : 0;
-        else v32[i] = both ? *reinterpret_cast<const u32_any *>(p) : here ? (uint32_t)*p : 0;
+#pragma unroll
+      for (int d = 0; d < D; ++d) v[i][d] = 0u;
+      if (n >= KS || half * VE + i < n) load_four<T>(xc + (int64_t)lds.list[at + i] * g.ldx, left, v[i]);
+    }
+  };
+  auto multiply = [&](int s, const uint32_t (&v)[VE][D]) {
+    u32x4 hf[P];
+#pragma unroll
+    for (int p = 0; p < P; ++p) hf[p] = *reinterpret_cast<const u32x4 *>(&lds.h[p][ln][s * KS + half * VE]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      u32x4 xf;
+      if constexpr (D == 4) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) xf[i] = v[i][e];
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          xf[i] = __builtin_amdgcn_perm(v[2 * i + 1][e >> 1], v[2 * i][e >> 1], e & 1 ? 0x07060302 : 0x05040100);
+      }
+#pragma unroll
+      for (int p = P - 1; p >= 0; --p) acc[e] = FLIP ? mma<T>(xf, hf[p], acc[e]) : mma<T>(hf[p], xf, acc[e]);
+    }
+  };
+  // the operands of listed rows from..to of h; zeros to the end of their step
+  auto stage = [&](int from, int to) {
+    const int end = (to + KS - 1) / KS * KS;
+    for (int i = from * 32 + tid; i < end * 32; i += 256) {
+      const int q = i >> 5, line = i & 31;
+      float v = 0.f;
+      if (q < to && j0 + line < lines) v = g.h.at((int64_t)lds.list[q] * g.h.ld + j0 + line);
+      if constexpr (D == 4) {
+        lds.h[0][line][q] = v;
+      } else {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+          const bf16_t b = narrow<bf16_t>(v);
+          lds.h[p][line][q] = b;
+          v -= widen(b);
+        }
       }
     }
-    if constexpr (sizeof(T) == 4) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) xf[0][i] = (uint32_t)v64[i], xf[1][i] = (uint32_t)(v64[i] >> 32);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        xf[0][i] = __builtin_amdgcn_perm(v32[2 * i + 1], v32[2 * i], 0x05040100);
-        xf[1][i] = __builtin_amdgcn_perm(v32[2 * i + 1], v32[2 * i], 0x07060302);
-      }
-    }
-    split_to<T, P>(hv, hf);
-#pragma unroll
-    for (int e = 0; e < 2; ++e)
-#pragma unroll
-      for (int p = P - 1; p >= 0; --p) acc[e] = mma<T>(hf[p], xf[e], acc[e]);
   };
   if (j0 < lines) {
-    for (int64_t t0 = split * range; t0 < t_end; t0 += 256) {
+    for (int64_t t0 = split * range; t0 < t_end; t0 += 256, round ^= 1) {
       const int64_t t = t0 + tid;
       const bool mine = t < t_end && low.of(t) == a;
       const uint64_t vote = __ballot(mine);
-      if (lane == 0) counts[wv] = __popcll(vote);
+      if (lane == 0) lds.counts[round][wv] = __popcll(vote);
       __syncthreads();
       int before = have, all = have;
+#pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int n = counts[i];
+        const int n = lds.counts[round][i];
         if (i < wv) before += n;
         all += n;
       }
-      if (mine) list[before + __popcll(vote & ((1ull << lane) - 1))] = (int)t;
+      if (all == have) continue;  // (the other counts are written next)
+      if (mine) lds.list[before + __popcll(vote & ((1ull << lane) - 1))] = (int)t;
       __syncthreads();
       total += all - have;
       const int full = all / KS * KS;
-      for (int at = 0; at < full; at += KS) step(at, KS);
-      have = all - full;
-      __syncthreads();
-      if (tid < have) counts[4 + tid] = list[full + tid];
-      __syncthreads();
-      if (tid < have) list[tid] = counts[4 + tid];
-      // (the next round's first barrier comes before the list is read)
+      if (full > 0) {
+        // (two steps' columns are on their way while h is staged, and while the two before are multiplied)
+        uint32_t v0[VE][D], v1[VE][D];
+        const int steps = full / KS;
+        if (busy) {
+          fetch(0, KS, v0);
+          if (steps > 1) fetch(1, KS, v1);
+        }
+        stage(0, full);
+        __syncthreads();
+        if (busy)
+          for (int s = 0; s < steps; s += 2) {
+            multiply(s, v0);
+            if (s + 2 < steps) fetch(s + 2, KS, v0);
+            if (s + 1 < steps) multiply(s + 1, v1);
+            if (s + 3 < steps) fetch(s + 3, KS, v1);
+          }
+        __syncthreads();
+        have = all - full;
+        if (tid < have) lds.rest[tid] = lds.list[full + tid];
+        __syncthreads();
+        if (tid < have) lds.list[tid] = lds.rest[tid];
+      } else {
+        have = all;
+      }
     }
     __syncthreads();
-    if (have > 0) step(0, have);
+    if (have > 0) {
+      uint32_t v0[VE][D];
+      if (busy) fetch(0, have, v0);
+      stage(0, have);
+      __syncthreads();
+      if (busy) multiply(0, v0);
+    }
   }
   if (splits > 1) {
-    if (g.found && tile_c == 0 && j0 == 0 && tid == 0) g.found[(int64_t)split * low.n + a] = total;
+    if (tile_c == 0 && j0 == 0 && tid == 0) g.found[(int64_t)split * low.n + a] = total;
     if (total == 0) return;
   }
+  if (!busy) return;
   float *out = g.out + (splits > 1 ? split * g.size : 0) + a * g.major;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    const int line = j0 + result_line(i, half);
-    if (line >= low.rank) continue;
+    const int q = result_line(i, half);
 #pragma unroll
-    for (int e = 0; e < 2; ++e)
-      if (c + e < g.width) out[(int64_t)line * g.sj + (int64_t)(c + e) * g.sc] = line < lines ? acc[e][i] : 0.f;
+    for (int e = 0; e < 4; ++e) {
+      const int line = j0 + (FLIP ? ln : q), col = cw + 4 * (FLIP ? q : ln) + e;
+      if (line < low.rank && col < g.width) out[(int64_t)line * g.sj + (int64_t)col * g.sc] = line < lines ? acc[e][i] : 0.f;
+    }
   }
 }
 
+// dA's blocks, then dB's (whose lines are the contiguous ones: its results lie the other way round)
 template <class T>
 __global__ __launch_bounds__(256) void adapter_grad_kernel(GradJob<T> ga, GradJob<T> gb, Low low, int64_t rows, int splits, int64_t range) {
-  __shared__ int list[256 + 16], counts[4 + 16];
+  __shared__ __align__(16) GradLds<T> lds;
   for (int64_t b = blockIdx.x; b < ga.blocks + gb.blocks; b += gridDim.x) {
-    if (b < ga.blocks) grad_block<T>(ga, low, rows, splits, range, b, list, counts);
-    else grad_block<T>(gb, low, rows, splits, range, b - ga.blocks, list, counts);
+    if (b < ga.blocks) grad_block<T, false>(ga, low, rows, splits, range, b, lds);
+    else grad_block<T, true>(gb, low, rows, splits, range, b - ga.blocks, lds);
     __syncthreads();
   }
 }
 
-// The ranges' sums as one, in their order; lines past an adapter's rank are 0.
+// The ranges' sums as one, in their order; lines past an adapter's rank are 0.  A workgroup has 1024 entries of an adapter and
+// lists the ranges that have rows of it first.
 struct JoinJob {
   const float *part;
   float *out;
   int64_t size, major;
-  int sj, sc;
+  int sj, sc, tiles;
 };
+constexpr int kRanges = 1024;
 __global__ __launch_bounds__(256) void adapter_grad_join_kernel(JoinJob ja, JoinJob jb, Low low, int splits,
                                                                 const int32_t *__restrict__ found) {
-  const int64_t total = ja.size + jb.size, step = (int64_t)gridDim.x * 256;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += step) {
-    const bool first = i < ja.size;
+  __shared__ int list[kRanges], counts[4];
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  const int64_t blocks = (int64_t)(ja.tiles + jb.tiles) * low.n;
+  for (int64_t b = blockIdx.x; b < blocks; b += gridDim.x) {
+    const int a = (int)(b / (ja.tiles + jb.tiles)), tile = (int)(b % (ja.tiles + jb.tiles));
+    const bool first = tile < ja.tiles;
     const JoinJob &g = first ? ja : jb;
-    const int64_t at = first ? i : i - ja.size;
-    const int a = (int)(at / g.major);
-    const int in = (int)(at - a * g.major), j = g.sj == 1 ? in % low.rank : in / g.sj;
-    float v = 0.f;
-    if (j < low.lines(a))
-      for (int s = 0; s < splits; ++s)
-        if (found[(int64_t)s * low.n + a] > 0) v += g.part[s * g.size + at];
-    g.out[at] = v;
+    int n = 0;
+    for (int s0 = 0; s0 < splits; s0 += 256) {
+      const int s = s0 + tid;
+      const bool has = s < splits && found[(int64_t)s * low.n + a] > 0;
+      const uint64_t vote = __ballot(has);
+      if (lane == 0) counts[wv] = __popcll(vote);
+      __syncthreads();
+      int before = n;
+      for (int i = 0; i < wv; ++i) before += counts[i];
+      if (has) list[before + __popcll(vote & ((1ull << lane) - 1))] = s;
+      n += counts[0] + counts[1] + counts[2] + counts[3];
+      __syncthreads();
+    }
+    const int lines = low.lines(a);
+    const int64_t at0 = (int64_t)(first ? tile : tile - ja.tiles) * 1024;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int64_t in = at0 + i * 256 + tid;
+      if (in >= g.major) break;
+      const int j = g.sj == 1 ? (int)(in % low.rank) : (int)(in / g.sj);
+      const float *p = g.part + a * g.major + in;
+      float v = 0.f;
+      if (j < lines)
+        for (int s = 0; s < n; s += 4) {
+          float w[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) w[u] = s + u < n ? p[list[s + u] * g.size] : 0.f;
+          v += (w[0] + w[1]) + (w[2] + w[3]);
+        }
+      g.out[a * g.major + in] = v;
+    }
+    __syncthreads();
   }
 }
 
@@ -364,51 +481,60 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // k of a range is a multiple of 64 bf16 / 32 fp32 elements (four waves' steps)
 int step4(const wcc_adapter_desc &d) { return d.dtype == WCC_BF16 ? 64 : 32; }
+int lines_ld(const wcc_adapter_desc &d) { return (d.rank + 7) / 8 * 8; }
 
-// Ranges of k for the rank lines: about a thousand waves.
-int thin_splits(const wcc_adapter_desc &d, int width) {
-  const int64_t tiles = ceil_div(d.rows, 32);
-  return (int)std::clamp<int64_t>(ceil_div(1024, std::max<int64_t>(tiles, 1)), 1, std::clamp<int64_t>(width / 256, 1, 16));
-}
-size_t lines_bytes(const wcc_adapter_desc &d, int width) {
-  return align256((size_t)thin_splits(d, width) * d.rows * d.rank * 4);
-}
-
-// The product with W for few rows: whether, and ranges of k.
-struct StreamPlan {
-  bool taken;
+// How y = x W^T is made.  Few rows, and whatever 16-byte loads cannot take up to a thousand tiles: streamed; else LDS tiles
+// (bf16: adapter_gemm.hip), in ranges of k where the tiles alone would leave compute units without work.
+struct Plan {
+  enum { kStream, kTiles, kGemm, kGemmSplit } route;
   int rt, splits, chunk, tiles_o;
-  int64_t blocks;
+  int64_t blocks;  // of the stream
+  bool parts() const { return route == kStream || route == kGemmSplit; }
 };
-StreamPlan stream_plan(const wcc_adapter_desc &d, int width, int outs) {
-  StreamPlan p{};
-  p.rt = d.rows <= 32 ? 1 : 2;
+Plan plan_of(const wcc_adapter_desc &d, int width, int outs, bool aligned) {
+  Plan p{};
+  const int64_t rows = std::max<int64_t>(d.rows, 1);
+  p.rt = rows <= 32 ? 1 : 2;
   p.tiles_o = (int)ceil_div(outs, 64);
-  const int64_t tiles = ceil_div(d.rows, 32 * p.rt) * p.tiles_o;
-  p.taken = tiles <= 1024;
-  const int unit = 4 * step4(d);
-  const int64_t splits = std::clamp<int64_t>(ceil_div(512, std::max<int64_t>(tiles, 1)), 1, std::min<int64_t>(ceil_div(width, unit), 16));
-  p.chunk = (int)(ceil_div(ceil_div(width, splits), unit) * unit);
-  p.splits = (int)ceil_div(width, p.chunk);
-  p.blocks = tiles * p.splits;
+  const int64_t tiles = ceil_div(rows, 32 * p.rt) * p.tiles_o;
+  if (aligned && rows > 64) {
+    p.splits = gemm_splits(rows, width, outs);
+    p.route = p.splits > 1 ? Plan::kGemmSplit : Plan::kGemm;
+  } else if (tiles <= 1024) {
+    p.route = Plan::kStream;
+    const int unit = 4 * step4(d);
+    const int64_t splits = std::clamp<int64_t>(ceil_div(512, tiles), 1, std::min<int64_t>(ceil_div(width, unit), 16));
+    p.chunk = (int)(ceil_div(ceil_div(width, splits), unit) * unit);
+    p.splits = (int)ceil_div(width, p.chunk);
+    p.blocks = tiles * p.splits;
+  } else {
+    p.route = Plan::kTiles;
+  }
   return p;
 }
-size_t parts_bytes(const wcc_adapter_desc &d, const StreamPlan &p, int outs) {
-  return p.taken ? align256((size_t)p.splits * d.rows * outs * 4) : 0;
+// Ranges of k of the rank lines, of 256 at least: as many as give two workgroups a compute unit, 16 at most (8 for many rows, where
+// every tile adds them up again).
+int thin_splits(const wcc_adapter_desc &d, int width) {
+  const int64_t rows = std::max<int64_t>(d.rows, 1), most = std::clamp<int64_t>(width / 256, 1, rows <= 64 ? 16 : 8);
+  return (int)std::clamp<int64_t>(ceil_div(512, ceil_div(rows, kRange)), 1, most);
+}
+size_t lines_bytes(const wcc_adapter_desc &d, int width) { return align256((size_t)thin_splits(d, width) * d.rows * lines_ld(d) * 4); }
+size_t parts_bytes(const wcc_adapter_desc &d, const Plan &p, int outs) {
+  return p.parts() ? align256((size_t)p.splits * d.rows * outs * 4) : 0;
 }
 
-// Ranges of rows for the gradients: enough workgroups even where a range has rows of one adapter only, 64 MB of sums at most.
+// Ranges of rows for the gradients: the sums of the ranges no more than twice what x takes, 64 rows at least in a range.
 struct GradPlan {
   int splits;
   int64_t range;
 };
 GradPlan grad_plan(const wcc_adapter_desc &d) {
-  const int64_t tiles = ceil_div(std::min(d.C_in, d.C_out), 256);
-  const int64_t bytes = (int64_t)d.adapters * d.rank * (d.C_in + d.C_out) * 4;
-  int64_t splits = std::clamp<int64_t>(ceil_div(512, tiles), 1, std::max<int64_t>(ceil_div(d.rows, 256), 1));
-  if (bytes > 0) splits = std::clamp<int64_t>(splits, 1, std::max<int64_t>(((int64_t)64 << 20) / bytes, 1));
+  const int64_t size = d.dtype == WCC_BF16 ? 2 : 4, lines = std::max<int64_t>((int64_t)d.adapters * d.rank, 1);
+  const int64_t tiles = ceil_div(d.C_in, 512) + ceil_div(d.C_out, 512);
+  int64_t splits = std::min(ceil_div(d.rows, 64), d.rows * size / (2 * lines));
+  splits = std::clamp<int64_t>(splits, 1, std::clamp<int64_t>(1024 / tiles, 1, kRanges));
   GradPlan p;
-  p.range = std::max<int64_t>(ceil_div(ceil_div(d.rows, splits), 256) * 256, 256);
+  p.range = std::max<int64_t>(ceil_div(ceil_div(d.rows, splits), 64) * 64, 64);
   p.splits = (int)std::max<int64_t>(ceil_div(d.rows, p.range), 1);
   return p;
 }
@@ -425,32 +551,23 @@ ThinJob<T> thin_job(const wcc_adapter_desc &d, const AdapterArgs &g, bool back, 
   j.rows = d.rows;
   j.width = back ? d.C_out : d.C_in;
   j.m = back ? Thin<T>{(const T *)g.b, co * r, 1, (int)r} : Thin<T>{(const T *)g.a, r * ci, (int)ci, 1};
-  j.out = out;
-  const int splits = thin_splits(d, j.width);
-  j.chunk = (int)(ceil_div(ceil_div(j.width, splits), step4(d)) * step4(d));
-  j.splits = (int)ceil_div(j.width, j.chunk);
-  j.groups = (int)std::clamp<int64_t>(std::min<int64_t>(d.adapters, 32), 1, d.rows <= 512 ? 32 : 4);
-  j.units = ceil_div(d.rows, 32) * j.splits * j.groups;
+  j.chunk = (int)(ceil_div(ceil_div(j.width, thin_splits(d, j.width)), step4(d)) * step4(d));
+  j.out = Lines{out, (int)ceil_div(j.width, j.chunk), lines_ld(d), d.rows * lines_ld(d)};
+  j.by_range = d.rows > 64;
+  j.groups = std::clamp(d.adapters, 1, 32);
+  j.units = ceil_div(d.rows, 32) * j.out.splits * j.groups;
+  j.blocks = j.by_range ? ceil_div(d.rows, kRange) * j.out.splits : ceil_div(j.units, 4);
   return j;
 }
+
 template <class T>
-Lines lines_of(const wcc_adapter_desc &d, const ThinJob<T> &j) {
-  return Lines{j.out, std::max(j.splits, 1), d.rows * d.rank};
+void launch_lines(const ThinJob<T> &g1, const ThinJob<T> &g2, const Low &low, hipStream_t s) {
+  if (g1.blocks + g2.blocks > 0)
+    adapter_lines_kernel<T><<<(unsigned)std::min<int64_t>(g1.blocks + g2.blocks, 1 << 20), 256, 0, s>>>(g1, g2, low);
 }
 
 template <class T>
-__global__ __launch_bounds__(256) void adapter_lines_kernel(ThinJob<T> thin, ThinJob<T> thin2, Low low) {
-  const int64_t step = (int64_t)gridDim.x * 4;
-  for (int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); unit < thin.units + thin2.units; unit += step) {
-    if (unit < thin.units) thin_unit<T>(thin, low, unit);
-    else thin_unit<T>(thin2, low, unit - thin.units);
-  }
-}
-
-// y = x W^T + h m (back: dx from dy), with another job of rank lines beside (the forward ones, for dB)
-template <class T>
-hipError_t project(const wcc_adapter_desc &d, const AdapterArgs &g, bool back, const ThinJob<T> &thin, const ThinJob<T> &other, float *part,
-                   hipStream_t s) {
+Project<T> project_of(const wcc_adapter_desc &d, const AdapterArgs &g, bool back) {
   const int64_t ci = d.C_in, co = d.C_out, r = d.rank;
   Project<T> p{};
   p.x = (const T *)(back ? g.dy : g.x);
@@ -463,53 +580,69 @@ hipError_t project(const wcc_adapter_desc &d, const AdapterArgs &g, bool back, c
   p.wk = back ? ci : 1;
   p.low = low_of(d, g);
   p.m = back ? Thin<T>{(const T *)g.a, r * ci, (int)ci, 1} : Thin<T>{(const T *)g.b, co * r, 1, (int)r};
-  p.h = lines_of(d, thin);
   p.y = (T *)g.y;
   p.ldy = back ? d.ldx : d.ldy;
-  const StreamPlan sp = stream_plan(d, p.width, p.outs);
-  const int64_t thin_blocks = ceil_div(thin.units + other.units, 4);
-  if (!sp.taken) {
-    if (thin_blocks > 0) adapter_lines_kernel<T><<<(unsigned)std::min<int64_t>(thin_blocks, 1 << 20), 256, 0, s>>>(thin, other, p.low);
+  return p;
+}
+template <class T>
+bool aligned(const Project<T> &p) {
+  if constexpr (sizeof(T) == 2) return gemm_takes(p);
+  return false;
+}
+
+// y = x W^T + h m (back: dx from dy), with another job of rank lines beside (the forward ones, for dB)
+template <class T>
+void project(Project<T> p, const Plan &pl, const ThinJob<T> &thin, const ThinJob<T> &other, float *part, hipStream_t s) {
+  p.h = thin.out;
+  if (!pl.parts()) {
+    launch_lines(thin, other, p.low, s);
+    if constexpr (sizeof(T) == 2) {
+      if (pl.route == Plan::kGemm) return launch_gemm(p, s);
+    }
     return launch_tiles(p, s);
   }
-  const StreamJob<T> job{p.x, p.ldx, p.rows, p.width, p.outs, p.w, ci, part, sp.splits, sp.chunk, sp.tiles_o, sp.blocks};
-  const unsigned blocks = (unsigned)(sp.blocks + thin_blocks);
-  if (back) {
-    if (sp.rt == 1) adapter_products_kernel<T, 1, true><<<blocks, 256, 0, s>>>(job, thin, other, p.low);
-    else adapter_products_kernel<T, 2, true><<<blocks, 256, 0, s>>>(job, thin, other, p.low);
+  if (pl.route == Plan::kGemmSplit) {
+    if constexpr (sizeof(T) == 2) launch_gemm_split(p, pl.splits, part, thin, other, s);
   } else {
-    if (sp.rt == 1) adapter_products_kernel<T, 1, false><<<blocks, 256, 0, s>>>(job, thin, other, p.low);
-    else adapter_products_kernel<T, 2, false><<<blocks, 256, 0, s>>>(job, thin, other, p.low);
+    const bool nn = p.wk != 1;
+    const StreamJob<T> job{p.x, p.ldx, p.rows, p.width, p.outs, p.w, nn ? p.wk : p.wo, part, pl.splits, pl.chunk, pl.tiles_o, pl.blocks};
+    const unsigned blocks = (unsigned)(pl.blocks + thin.blocks + other.blocks);
+    if (nn) {
+      if (pl.rt == 1) adapter_products_kernel<T, 1, true><<<blocks, 256, 0, s>>>(job, thin, other, p.low);
+      else adapter_products_kernel<T, 2, true><<<blocks, 256, 0, s>>>(job, thin, other, p.low);
+    } else {
+      if (pl.rt == 1) adapter_products_kernel<T, 1, false><<<blocks, 256, 0, s>>>(job, thin, other, p.low);
+      else adapter_products_kernel<T, 2, false><<<blocks, 256, 0, s>>>(job, thin, other, p.low);
+    }
   }
-  const int tiles_o = (int)ceil_div(p.outs, 256);
-  const int rb = (int)std::clamp<int64_t>(d.rows * tiles_o / 512, 1, 16);
-  const int64_t fin = ceil_div(d.rows, rb) * tiles_o;
-  adapter_finish_kernel<T><<<(unsigned)std::min<int64_t>(fin, 1 << 20), 256, 0, s>>>(part, sp.splits, d.rows, p.outs, p.low, p.m, p.h, p.y,
-                                                                                    p.ldy, rb, tiles_o, fin);
-  return hipGetLastError();
+  const bool by_row = p.rows <= 64;
+  const int tiles_o = (int)ceil_div(p.outs, by_row ? 256 : 128);
+  const FinishJob<T> f{part, pl.splits, p.outs, tiles_o, p.rows, p.m, p.h, p.y, p.ldy, ceil_div(p.rows, by_row ? 1 : 32) * tiles_o};
+  if (by_row) adapter_finish_row_kernel<T><<<(unsigned)std::min<int64_t>(f.blocks, 1 << 20), 256, 0, s>>>(f, p.low);
+  else adapter_finish_tile_kernel<T><<<(unsigned)std::min<int64_t>(f.blocks, 1 << 20), 256, 0, s>>>(f, p.low);
 }
 
 template <class T>
 hipError_t forward(const wcc_adapter_desc &d, const AdapterArgs &g, hipStream_t s) {
-  const ThinJob<T> thin = thin_job<T>(d, g, false, (float *)g.ws);
-  return project<T>(d, g, false, thin, ThinJob<T>{}, (float *)(g.ws + lines_bytes(d, d.C_in)), s);
+  const Project<T> p = project_of<T>(d, g, false);
+  const Plan pl = plan_of(d, d.C_in, d.C_out, aligned(p));
+  project<T>(p, pl, thin_job<T>(d, g, false, (float *)g.ws), ThinJob<T>{}, (float *)(g.ws + lines_bytes(d, d.C_in)), s);
+  return hipGetLastError();
 }
 
 template <class T>
 hipError_t backward(const wcc_adapter_desc &d, const AdapterArgs &g, hipStream_t s) {
   char *at = g.ws;
   auto take = [&](size_t bytes) { char *p = at; at += bytes; return p; };
-  float *h = (float *)take(lines_bytes(d, d.C_in)), *gr = (float *)take(lines_bytes(d, d.C_out));
-  float *part = (float *)take(parts_bytes(d, stream_plan(d, d.C_out, d.C_in), d.C_in));
+  const Project<T> p = project_of<T>(d, g, true);
+  const Low low = p.low;
+  const Plan pl = plan_of(d, d.C_out, d.C_in, aligned(p));
+  float *gr = (float *)take(lines_bytes(d, d.C_out)), *h = (float *)take(lines_bytes(d, d.C_in));
+  float *part = (float *)take(g.y ? parts_bytes(d, pl, d.C_in) : 0);
   const ThinJob<T> back = g.y || g.da ? thin_job<T>(d, g, true, gr) : ThinJob<T>{};
   const ThinJob<T> fore = g.db ? thin_job<T>(d, g, false, h) : ThinJob<T>{};
-  const Low low = low_of(d, g);
-  if (g.y) {
-    const hipError_t e = project<T>(d, g, true, back, fore, part, s);
-    if (e != hipSuccess) return e;
-  } else if (back.units + fore.units > 0) {
-    adapter_lines_kernel<T><<<(unsigned)std::min<int64_t>(ceil_div(back.units + fore.units, 4), 1 << 20), 256, 0, s>>>(back, fore, low);
-  }
+  if (g.y) project<T>(p, pl, back, fore, part, s);
+  else launch_lines(back, fore, low, s);
   if (!g.da && !g.db) return hipGetLastError();
   const GradPlan gp = grad_plan(d);
   const int64_t ci = d.C_in, co = d.C_out, r = d.rank, na = d.adapters * r * ci, nb = d.adapters * r * co;
@@ -519,19 +652,20 @@ hipError_t backward(const wcc_adapter_desc &d, const AdapterArgs &g, hipStream_t
   const int tiles_j = (int)ceil_div(r, 32);
   GradJob<T> ja{}, jb{};
   if (g.da) {
-    const int tiles = (int)ceil_div(ci, 256);
-    ja = GradJob<T>{(const T *)g.x, d.ldx, d.C_in, lines_of(d, back), gp.splits > 1 ? pa : g.da, na, r * ci, (int)ci, 1, found, tiles,
+    const int tiles = (int)ceil_div(ci, 512);
+    ja = GradJob<T>{(const T *)g.x, d.ldx, d.C_in, back.out, gp.splits > 1 ? pa : g.da, na, r * ci, (int)ci, 1, found, tiles,
                     (int64_t)tiles * tiles_j * d.adapters * gp.splits};
   }
   if (g.db) {
-    const int tiles = (int)ceil_div(co, 256);
-    jb = GradJob<T>{(const T *)g.dy, d.ldy, d.C_out, lines_of(d, fore), gp.splits > 1 ? pb : g.db, nb, co * r, 1, (int)r, found, tiles,
+    const int tiles = (int)ceil_div(co, 512);
+    jb = GradJob<T>{(const T *)g.dy, d.ldy, d.C_out, fore.out, gp.splits > 1 ? pb : g.db, nb, co * r, 1, (int)r, found, tiles,
                     (int64_t)tiles * tiles_j * d.adapters * gp.splits};
   }
   adapter_grad_kernel<T><<<(unsigned)std::min<int64_t>(ja.blocks + jb.blocks, 1 << 20), 256, 0, s>>>(ja, jb, low, d.rows, gp.splits, gp.range);
   if (gp.splits > 1) {
-    const JoinJob a{pa, g.da, g.da ? na : 0, r * ci, (int)ci, 1}, b{pb, g.db, g.db ? nb : 0, co * r, 1, (int)r};
-    adapter_grad_join_kernel<<<(unsigned)std::min<int64_t>(ceil_div(a.size + b.size, 256), 1 << 20), 256, 0, s>>>(a, b, low, gp.splits, found);
+    const JoinJob a{pa, g.da, na, r * ci, (int)ci, 1, g.da ? (int)ceil_div(r * ci, 1024) : 0};
+    const JoinJob b{pb, g.db, nb, co * r, 1, (int)r, g.db ? (int)ceil_div(co * r, 1024) : 0};
+    adapter_grad_join_kernel<<<(unsigned)std::min<int64_t>((int64_t)(a.tiles + b.tiles) * d.adapters, 1 << 20), 256, 0, s>>>(a, b, low, gp.splits, found);
   }
   return hipGetLastError();
 }
@@ -539,12 +673,17 @@ hipError_t backward(const wcc_adapter_desc &d, const AdapterArgs &g, hipStream_t
 }  // namespace
 
 size_t adapter_bytes(const wcc_adapter_desc &d) {
-  const StreamPlan f = stream_plan(d, d.C_in, d.C_out), b = stream_plan(d, d.C_out, d.C_in);
   const GradPlan gp = grad_plan(d);
-  const size_t lines = lines_bytes(d, d.C_in), sums = (size_t)d.adapters * d.rank * 4;
-  const size_t back = lines + lines_bytes(d, d.C_out) + parts_bytes(d, b, d.C_in) + align256((size_t)gp.splits * d.adapters * 4) +
-                      (gp.splits > 1 ? align256(gp.splits * sums * d.C_in) + align256(gp.splits * sums * d.C_out) : 0);
-  return std::max(lines + parts_bytes(d, f, d.C_out), back);
+  const size_t sums = (size_t)d.adapters * d.rank * 4;
+  const size_t grads = align256((size_t)gp.splits * d.adapters * 4) +
+                       (gp.splits > 1 ? align256(gp.splits * sums * d.C_in) + align256(gp.splits * sums * d.C_out) : 0);
+  size_t most = 0;
+  for (const bool fits : {false, true}) {  // (alignment is known with the pointers)
+    const bool al = fits && d.dtype == WCC_BF16;
+    most = std::max(most, parts_bytes(d, plan_of(d, d.C_in, d.C_out, al), d.C_out));
+    most = std::max(most, parts_bytes(d, plan_of(d, d.C_out, d.C_in, al), d.C_in) + lines_bytes(d, d.C_out) + grads);
+  }
+  return lines_bytes(d, d.C_in) + most;
 }
 
 hipError_t launch_adapter_forward(const wcc_adapter_desc &d, const AdapterArgs &g, hipStream_t s) {

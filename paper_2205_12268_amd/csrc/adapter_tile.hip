@@ -4,8 +4,7 @@
 // while one is multiplied.  LDS rows are 144 bytes apart, which spreads the 16-byte reads of 32 rows over all banks.
 // Where W's outputs are contiguous and not its k (the gradient of x), a thread loads pairs of outputs of eight (four) k and
 // exchanges halves, so that LDS holds the same rows of k either way.
-// The thin product of the rank lines comes last, adapter by adapter among the 32 rows of a matrix-core tile, into registers
-// of its own: a row takes the sums of its own adapter only, whatever (infinities, NaN) other adapters hold.
+// The thin product of the rank lines comes last (add_thin).
 #include "adapter.h"
 
 namespace wcc {
@@ -22,42 +21,6 @@ __device__ __forceinline__ void tile_of(int64_t b, int64_t tiles, int64_t tiles_
   const int64_t high = min(tiles_t - first, (int64_t)8);
   tt = first + in % high;
   to = (int)(in / high);
-}
-
-// acc += the rank lines' product for the 32 rows from t0 on and 32 outputs at o of each lane.
-template <class T, int E>
-__device__ __forceinline__ void add_thin(const Project<T> &p, int64_t t0, const int (&o)[E], f32x16 (&acc)[E]) {
-  constexpr int VE = VecOf<T>::N, KS = StepOf<T>::K, P = PartsOf<T>::Out;
-  const int ln = threadIdx.x & 31, half = (threadIdx.x >> 5) & 1;
-  const int64_t t = t0 + ln;
-  const int id = t < p.rows ? p.low.of(t) : -1;
-  uint32_t rest = (uint32_t)__ballot(id >= 0);
-  while (rest != 0) {
-    const int a = __builtin_amdgcn_readlane(id, __builtin_ctz(rest));
-    const uint32_t same = (uint32_t)__ballot(id == a);
-    rest &= ~same;
-    const int lines = p.low.lines(a);
-    f32x16 d[E] = {};
-    for (int j0 = 0; j0 < lines; j0 += KS) {
-      const int j = j0 + half * VE, left = lines - j;
-      float hv[VE];
-#pragma unroll
-      for (int i = 0; i < VE; ++i) hv[i] = i < left && id == a ? p.h.at(t * p.low.rank + j + i) : 0.f;
-      u32x4 hf[P];
-      split_to<T, P>(hv, hf);
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const T *mr = p.m.p + a * p.m.major + (int64_t)min(o[e], p.outs - 1) * p.m.sc + (int64_t)j * p.m.sj;
-        const u32x4 mf = p.m.sj == 1 ? load_k(mr, left) : load_k_strided(mr, p.m.sj, left);
-#pragma unroll
-        for (int q = P - 1; q >= 0; --q) d[e] = mma<T>(hf[q], mf, d[e]);
-      }
-    }
-#pragma unroll
-    for (int e = 0; e < E; ++e)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) acc[e][i] += same >> result_line(i, half) & 1 ? d[e][i] : 0.f;
-  }
 }
 
 template <class T, bool NN>
@@ -140,7 +103,7 @@ __global__ __launch_bounds__(256, 2) void project_tile_kernel(Project<T> p, int6
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
       const int64_t tr = t0 + wm * 64 + r * 32;
-      if (p.low.of_row) add_thin<T, 2>(p, tr, o, acc[r]);
+      if (p.low.of_row) add_thin<T, 2>(p.low, p.m, p.h, p.rows, p.outs, tr, o, acc[r]);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int64_t t = tr + result_line(i, half);
@@ -156,15 +119,14 @@ __global__ __launch_bounds__(256, 2) void project_tile_kernel(Project<T> p, int6
 }  // namespace
 
 template <class T>
-hipError_t launch_tiles(const Project<T> &p, hipStream_t s) {
+void launch_tiles(const Project<T> &p, hipStream_t s) {
   const int64_t tiles_t = (p.rows + kTile - 1) / kTile;
   const int tiles_o = (p.outs + kTile - 1) / kTile;
   const unsigned blocks = (unsigned)std::min<int64_t>(tiles_t * tiles_o, 1 << 20);
   if (p.wk == 1) project_tile_kernel<T, false><<<blocks, 256, 0, s>>>(p, tiles_t, tiles_o);
   else project_tile_kernel<T, true><<<blocks, 256, 0, s>>>(p, tiles_t, tiles_o);
-  return hipGetLastError();
 }
-template hipError_t launch_tiles<bf16_t>(const Project<bf16_t> &, hipStream_t);
-template hipError_t launch_tiles<float>(const Project<float> &, hipStream_t);
+template void launch_tiles<bf16_t>(const Project<bf16_t> &, hipStream_t);
+template void launch_tiles<float>(const Project<float> &, hipStream_t);
 
 }  // namespace wcc
