@@ -1,12 +1,16 @@
 // The projection for many rows of bf16: the matrix cores fed from LDS, which loads go to straight from memory.
 //
-// A workgroup has BT rows x BO outputs, stages of 64 k, two of them in LDS: while one is multiplied, the other's loads
-// (16 bytes a lane, into LDS without passing registers) are in flight.  LDS has no padding (such a load writes 1 KiB in a row),
-// so the 16-byte chunks of a line are exchanged by a key of the line, at the load by choosing which chunk of memory a lane
-// asks for: the 16 lines that a read takes at once are then on different banks.
+// A workgroup of four waves has BT rows x BO outputs and two stages of 64 k in LDS; loads (16 bytes a lane) go there without
+// passing registers.  A wave's operands of a whole stage fit its registers beside the results, so a stage's half of LDS is
+// free after a quarter of its products: from there on the loads of the stage after the next go out, one between every three
+// products.  Two barriers a stage: LDS is read; the next stage is there.
+// LDS has no padding (such a load writes 1 KiB in a row), so the 16-byte chunks of a line are exchanged by a key of the line, at
+// the load by choosing which chunk of memory a lane asks for: the 16 lines that a read takes at once are on different banks.
 // Where W's outputs are contiguous and not its k (NN), LDS holds lines of k and the reads transpose 4 x 16 blocks.
-// The first operand of the matrix cores is W, the second x: a lane has one row's results, four neighbouring outputs at a time.
-// Chunks past the end of k, and outputs past the last (NN), are loaded from 16 bytes of zeros.
+// The first operand of the matrix cores is W, the second x: a lane has one row's results, four neighbouring outputs at a time,
+// which leave through LDS as whole lines.
+// The last stages, which the end of k cuts, are not overlapped; chunks past the end (and, NN, past the last output) come from 16
+// bytes of zeros.
 #include "adapter.h"
 
 namespace wcc {
@@ -14,15 +18,14 @@ namespace {
 
 __device__ const uint4 kZeros = {0, 0, 0, 0};
 
-typedef __attribute__((address_space(3))) unsigned char lds_byte;
 typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4;
 
-__device__ __forceinline__ void to_lds(const bf16_t *from, unsigned char *to) {
+__device__ __forceinline__ void to_lds(const void *from, unsigned char *to) {
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
                                    (__attribute__((address_space(3))) void *)to, 16, 0, 0);
 }
 
-constexpr int kK = 64;  // k of a stage: lines of 128 bytes
+constexpr int kK = 64, Line = kK * 2, Chunks = kK / 8, PerLoad = 1024 / Line;  // k of a stage; bytes and chunks of a line, lines of a load
 
 // (see adapter_tile.hip)
 __device__ __forceinline__ void tile_of(int64_t b, int64_t tiles, int64_t tiles_t, int tiles_o, int64_t &tt, int &to) {
@@ -34,64 +37,115 @@ __device__ __forceinline__ void tile_of(int64_t b, int64_t tiles, int64_t tiles_
   to = (int)(in / high);
 }
 
-template <int BT, int BO, int WT, int WO, bool NN>
+// FULL: a tile lies within the rows and outputs (the last ones are moved back, over others, whose results they repeat).
+template <int BT, int BO, bool NN, bool FULL>
 struct Gemm {
-  static constexpr int Waves = WT * WO, Threads = Waves * 64;
-  static constexpr int ET = BT / WT / 32, EO = BO / WO / 32;       // 32 x 32 results of a wave
-  static constexpr int XB = BT * kK * 2, WB = BO * kK * 2;         // bytes of a stage
+  static constexpr int WT = 2, WO = 2, Waves = WT * WO;
+  static constexpr int ET = BT / WT / 32, EO = BO / WO / 32;            // 32 x 32 results of a wave
+  static constexpr int XB = BT * kK * 2, WB = BO * kK * 2;              // bytes of a stage
   static constexpr int XL = XB / 1024 / Waves, WL = WB / 1024 / Waves;  // loads of a wave
+  static constexpr int C = BO / 8, R = 64 / C;                          // NN: chunks of a line of k, lines of a load
+  __device__ static __forceinline__ int key(int line) { return (line >> 1) & 7; }
 
+  // Where a wave's loads begin.  Load i is at x + i * x_step + k, and a lane's place in it depends on i's last bit alone; without
+  // FULL the rows are held to the last one, each load's by itself.
   struct Loader {
-    const bf16_t *x[XL], *w[WL];
-    int xk[XL], wk[WL];  // first k of the lane's chunk (NN: of w, the line of k), or far off where there is none
-    int64_t w_step;
+    const char *x, *w;
+    int64_t x_step, w_step, w_stage;  // bytes between loads; NN: between stages
+    uint32_t xo[2], wo[2];
+    const char *xr[FULL ? 1 : XL], *wr[FULL || NN ? 1 : WL];
+    int o_left;                       // NN: outputs from o0 on
   };
 
   __device__ static __forceinline__ void aim(const Project<bf16_t> &p, int64_t t0, int o0, int k0, Loader &l) {
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-#pragma unroll
-    for (int i = 0; i < XL; ++i) {
-      const int row = (wv * XL + i) * 8 + (lane >> 3), chunk = (lane & 7) ^ ((row >> 1) & 7);
-      l.x[i] = p.x + min(t0 + row, p.rows - 1) * p.ldx + k0 + chunk * 8;
-      l.xk[i] = chunk * 8;
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    l.x = reinterpret_cast<const char *>(p.x + (t0 + wv * XL * PerLoad) * p.ldx + k0);
+    l.x_step = (int64_t)PerLoad * p.ldx * 2;
+    l.o_left = p.outs - o0;
+    if constexpr (NN) {
+      l.w = reinterpret_cast<const char *>(p.w + (int64_t)(k0 + wv * WL * R) * p.wk + o0);
+      l.w_step = R * p.wk * 2;
+      l.w_stage = kK * p.wk * 2;
+    } else {
+      l.w = reinterpret_cast<const char *>(p.w + (int64_t)(o0 + wv * WL * PerLoad) * p.wo + k0);
+      l.w_step = PerLoad * p.wo * 2;
+      l.w_stage = Line;
     }
 #pragma unroll
-    for (int i = 0; i < WL; ++i) {
+    for (int b = 0; b < 2; ++b) {
+      const int row = b * PerLoad + lane / Chunks, chunk = (lane % Chunks) ^ key(row);
+      l.xo[b] = (uint32_t)((lane / Chunks) * p.ldx * 2 + chunk * 16);
+      if constexpr (NN) l.wo[b] = (uint32_t)((lane / C) * p.wk * 2 + ((lane % C) ^ (((b * R + lane / C) & 3) * 4)) * 16);
+      else l.wo[b] = (uint32_t)((lane / Chunks) * p.wo * 2 + chunk * 16);
+    }
+    if constexpr (!FULL) {
+#pragma unroll
+      for (int i = 0; i < XL; ++i) {
+        const int row = (wv * XL + i) * PerLoad + lane / Chunks, chunk = (lane % Chunks) ^ key(row);
+        l.xr[i] = reinterpret_cast<const char *>(p.x + min(t0 + row, p.rows - 1) * p.ldx + k0 + chunk * 8);
+      }
       if constexpr (!NN) {
-        const int row = (wv * WL + i) * 8 + (lane >> 3), chunk = (lane & 7) ^ ((row >> 1) & 7);
-        l.w[i] = p.w + (int64_t)min(o0 + row, p.outs - 1) * p.wo + k0 + chunk * 8;
-        l.wk[i] = chunk * 8;
-      } else {
-        constexpr int C = BO / 8, R = 64 / C;  // chunks of a line, lines of a load
-        const int row = (wv * WL + i) * R + lane / C, chunk = (lane % C) ^ ((row & 3) * 4);
-        const int o = o0 + chunk * 8;
-        l.w[i] = p.w + (int64_t)(k0 + row) * p.wk + o;
-        l.wk[i] = o < p.outs ? row : 1 << 30;
+#pragma unroll
+        for (int i = 0; i < WL; ++i) {
+          const int row = (wv * WL + i) * PerLoad + lane / Chunks, chunk = (lane % Chunks) ^ key(row);
+          l.wr[i] = reinterpret_cast<const char *>(p.w + (int64_t)min(o0 + row, p.outs - 1) * p.wo + k0 + chunk * 8);
+        }
       }
     }
-    l.w_step = NN ? kK * p.wk : kK;
   }
 
-  // the stage that begins at k
-  __device__ static __forceinline__ void load(Loader &l, int k, int end, unsigned char *xs, unsigned char *ws) {
+  __device__ static __forceinline__ const char *x_at(const Loader &l, int i, int stage) {
+    if constexpr (FULL) return l.x + i * l.x_step + (int64_t)stage * Line + l.xo[i & 1];
+    else return l.xr[i] + (int64_t)stage * Line;
+  }
+  __device__ static __forceinline__ const char *w_at(const Loader &l, int i, int stage) {
+    if constexpr (FULL || NN) return l.w + i * l.w_step + stage * l.w_stage + l.wo[i & 1];
+    else return l.wr[i] + (int64_t)stage * Line;
+  }
+  // NN without FULL: whether the lane's chunk of load i lies before the last output
+  __device__ static __forceinline__ bool w_there(const Loader &l, int i) {
+    const int lane = threadIdx.x & 63, row = (i & 1) * R + lane / C;
+    return ((lane % C) ^ ((row & 3) * 4)) * 8 < l.o_left;
+  }
+
+  // loads from..to of a stage all of whose k are there
+  template <int from, int to>
+  __device__ static __forceinline__ void load(const Loader &l, int stage, unsigned char *xs, unsigned char *ws) {
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const bf16_t *zeros = reinterpret_cast<const bf16_t *>(&kZeros);
+#pragma unroll
+    for (int i = from; i < to; ++i) {
+      if (i < XL) {
+        to_lds(x_at(l, i, stage), xs + (wv * XL + i) * 1024);
+      } else {
+        const char *at = w_at(l, i - XL, stage);
+        if constexpr (NN && !FULL) at = w_there(l, i - XL) ? at : reinterpret_cast<const char *>(&kZeros);
+        to_lds(at, ws + (wv * WL + i - XL) * 1024);
+      }
+    }
+  }
+  // a stage of which `left` k are there (a multiple of 8)
+  __device__ static __forceinline__ void load_cut(const Loader &l, int stage, int left, unsigned char *xs, unsigned char *ws) {
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const char *zeros = reinterpret_cast<const char *>(&kZeros);
 #pragma unroll
     for (int i = 0; i < XL; ++i) {
-      to_lds(k + l.xk[i] < end ? l.x[i] : zeros, xs + (wv * XL + i) * 1024);
-      l.x[i] += kK;
+      const int chunk = (lane % Chunks) ^ key(i * PerLoad + lane / Chunks);  // (a wave's first line is a multiple of 16)
+      to_lds(chunk * 8 < left ? x_at(l, i, stage) : zeros, xs + (wv * XL + i) * 1024);
     }
 #pragma unroll
     for (int i = 0; i < WL; ++i) {
-      to_lds(k + l.wk[i] < end ? l.w[i] : zeros, ws + (wv * WL + i) * 1024);
-      l.w[i] += l.w_step;
+      bool there;
+      if constexpr (NN) there = (wv * WL + i) * R + lane / C < left && w_there(l, i);
+      else there = ((lane % Chunks) ^ key(i * PerLoad + lane / Chunks)) * 8 < left;
+      to_lds(there ? w_at(l, i, stage) : zeros, ws + (wv * WL + i) * 1024);
     }
   }
 
   __device__ static __forceinline__ u32x4 line(const unsigned char *s, int row, int chunk) {
-    return *reinterpret_cast<const u32x4 *>(s + row * 128 + ((chunk ^ ((row >> 1) & 7)) << 4));
+    return *reinterpret_cast<const u32x4 *>(s + row * Line + ((chunk ^ key(row)) << 4));
   }
-  // 32 outputs from o on, 16 k from k on, of lines of k
+  // 32 outputs from o on, 16 k from k on, of lines of k: within 16 lanes, lane 4j + q supplies four outputs of k + j, and lane 4q + e
+  // receives the e-th of them for j = 0..3
   __device__ static __forceinline__ u32x4 across(const unsigned char *s, int o, int k) {
     const int lane = threadIdx.x & 63, g = lane >> 4, q = lane & 15;
     const int n = o + (g & 1) * 16 + (q & 3) * 4, kk = k + (g >> 1) * 8 + (q >> 2);
@@ -108,26 +162,111 @@ struct Gemm {
     return v;
   }
 
-  __device__ static __forceinline__ void multiply(const unsigned char *xs, const unsigned char *ws, f32x16 (&acc)[EO][ET]) {
+  struct Operands {
+    u32x4 x[ET], w[EO];
+  };
+  __device__ static __forceinline__ void fetch(const unsigned char *xs, const unsigned char *ws, int step, Operands &f) {
     const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, ln = lane & 31, half = lane >> 5;
     const int tw = (wv / WO) * (ET * 32), ow = (wv % WO) * (EO * 32);
-    u32x4 xf[2][ET], wf[2][EO];
-    auto fetch = [&](int ks) {
 #pragma unroll
-      for (int e = 0; e < EO; ++e)
-        wf[ks & 1][e] = NN ? across(ws, ow + e * 32, ks * 16) : line(ws, ow + e * 32 + ln, ks * 2 + half);
+    for (int e = 0; e < EO; ++e) f.w[e] = NN ? across(ws, ow + e * 32, step * 16) : line(ws, ow + e * 32 + ln, step * 2 + half);
 #pragma unroll
-      for (int r = 0; r < ET; ++r) xf[ks & 1][r] = line(xs, tw + r * 32 + ln, ks * 2 + half);
-    };
-    fetch(0);
+    for (int r = 0; r < ET; ++r) f.x[r] = line(xs, tw + r * 32 + ln, step * 2 + half);
+  }
+  __device__ static __forceinline__ void multiply(const Operands &f, f32x16 (&acc)[EO][ET]) {
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) {
-      if (ks < 3) fetch(ks + 1);
+    for (int e = 0; e < EO; ++e)
 #pragma unroll
-      for (int e = 0; e < EO; ++e)
+      for (int r = 0; r < ET; ++r) acc[e][r] = mma<bf16_t>(f.w[e], f.x[r], acc[e][r]);
+  }
+  // The barrier by itself (a fence would wait for all loads); the clobbers keep the reads of LDS on their sides of it.
+  __device__ static __forceinline__ void barrier() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  }
+  // all but the last n loads of every wave have arrived
+  template <int n>
+  __device__ static __forceinline__ void arrived() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(n) : "memory");
+    barrier();
+  }
+  // The order of a step: its reads of LDS two at a time between the first products (the rest of which hide the last one's way),
+  // its loads between the others, as far apart as they get: a load takes 16 cycles on its way out, a product 32.
+  template <int reads, int loads>
+  __device__ static __forceinline__ void spread() {
+    constexpr int M = ET * EO, N = (reads + 1) / 2;
 #pragma unroll
-        for (int r = 0; r < ET; ++r) acc[e][r] = mma<bf16_t>(wf[ks & 1][e], xf[ks & 1][r], acc[e][r]);
-      __builtin_amdgcn_sched_barrier(0);  // (the reads of one step ahead, no more: registers)
+    for (int i = 0; i < N; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      if (i < M) __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    }
+    constexpr int each = loads > 0 && M > N ? (M - N) / loads : 0;
+#pragma unroll
+    for (int i = 0; i < loads; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+      if (each > 0) __builtin_amdgcn_sched_group_barrier(0x008, each, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, M, 0);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  // The stage in (xs, ws), whose first two steps' operands are on their way to f; the next one is in (xn, wn), and `later` is loaded
+  // where this one was.
+  __device__ static __forceinline__ void stage(const Loader &l, int later, unsigned char *xs, unsigned char *ws, const unsigned char *xn,
+                                               const unsigned char *wn, Operands (&f)[4], f32x16 (&acc)[EO][ET]) {
+    constexpr int Reads = ET + EO * (NN ? 2 : 1), L = XL + WL, L1 = (L + 2) / 3, L2 = 2 * L1;
+    fetch(xs, ws, 2, f[2]);
+    fetch(xs, ws, 3, f[3]);
+    multiply(f[0], acc);
+    spread<2 * Reads, 0>();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    barrier();
+    load<0, L1>(l, later, xs, ws);
+    multiply(f[1], acc);
+    spread<0, L1>();
+    load<L1, L2>(l, later, xs, ws);
+    multiply(f[2], acc);
+    spread<0, L2 - L1>();
+    arrived<L2>();
+    fetch(xn, wn, 0, f[0]);
+    fetch(xn, wn, 1, f[1]);
+    load<L2, L>(l, later, xs, ws);
+    multiply(f[3], acc);
+    spread<2 * Reads, L - L2>();
+  }
+
+  // acc += x W^T over k0 .. k1
+  __device__ static __forceinline__ void run(const Project<bf16_t> &p, int64_t t0, int o0, int k0, int k1, unsigned char *xs0,
+                                             unsigned char *ws0, unsigned char *xs1, unsigned char *ws1, f32x16 (&acc)[EO][ET]) {
+    constexpr int L = XL + WL;
+    Loader l;
+    aim(p, t0, o0, k0, l);
+    const int pairs = (k1 - k0) / (2 * kK);
+    Operands f[4];
+    if (pairs > 0) {
+      load<0, L>(l, 0, xs0, ws0);
+      load<0, L>(l, 1, xs1, ws1);
+      arrived<L>();
+      fetch(xs0, ws0, 0, f[0]);
+      fetch(xs0, ws0, 1, f[1]);
+      const int last = 2 * pairs - 1;  // (what would be loaded beyond it is loaded again, for nothing)
+      for (int s = 0; s < last; s += 2) {
+        stage(l, min(s + 2, last), xs0, ws0, xs1, ws1, f, acc);
+        stage(l, min(s + 3, last), xs1, ws1, xs0, ws0, f, acc);
+      }
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // nothing is on its way to LDS from here on
+      barrier();
+    }
+    for (int s = 2 * pairs, left = k1 - k0 - s * kK; left > 0; ++s, left -= kK) {
+      load_cut(l, s, left, xs0, ws0);
+      arrived<0>();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        fetch(xs0, ws0, i, f[0]);
+        multiply(f[0], acc);
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      barrier();
     }
   }
 
@@ -164,79 +303,72 @@ struct Gemm {
         for (int i = 0; i < 16; ++i) acc[e][r][i] += id == a ? d[e][i] : 0.f;
     }
   }
+
+  // The wave's results to y, rows from tw and outputs from ow on, through its part of LDS: a row's 8-byte pieces are exchanged by a
+  // key of the row (even, so that pairs of them stay together).
+  __device__ static __forceinline__ void store(const Project<bf16_t> &p, int64_t tw, int ow, const f32x16 (&acc)[EO][ET], unsigned char *lds) {
+    constexpr int Row = EO * 64, Pieces = Row / 8, Lanes = Row / 16, Rows = 64 / Lanes;  // bytes of a row; rows of a store
+    const int lane = threadIdx.x & 63, ln = lane & 31, half = lane >> 5;
+    auto twist = [](int row) { return row % (Pieces / 2) * 2; };
+#pragma unroll
+    for (int r = 0; r < ET; ++r) {
+#pragma unroll
+      for (int e = 0; e < EO; ++e)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          const int row = r * 32 + ln, piece = e * 8 + (i >> 1) + half;
+          const uint2 v = {(uint32_t)narrow<bf16_t>(acc[e][r][i]) | (uint32_t)narrow<bf16_t>(acc[e][r][i + 1]) << 16,
+                           (uint32_t)narrow<bf16_t>(acc[e][r][i + 2]) | (uint32_t)narrow<bf16_t>(acc[e][r][i + 3]) << 16};
+          *reinterpret_cast<uint2 *>(lds + row * Row + ((piece ^ twist(row)) << 3)) = v;
+        }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    // (a wave reads what it wrote itself: LDS is in order)
+#pragma unroll 4
+    for (int r0 = 0; r0 < ET * 32; r0 += Rows) {
+      const int row = r0 + lane / Lanes, c = lane % Lanes, o = ow + c * 8;
+      const u32x4 v = *reinterpret_cast<const u32x4 *>(lds + row * Row + (((2 * c) ^ twist(row)) << 3));
+      bf16_t *y = p.y + (tw + row) * p.ldy + o;
+      if (FULL || (tw + row < p.rows && o + 8 <= p.outs)) {
+        *reinterpret_cast<u32x4_any *>(y) = v;
+      } else if (tw + row < p.rows) {
+#pragma unroll
+        for (int q = 0; q < 7; ++q)
+          if (o + q < p.outs) y[q] = (bf16_t)(v[q >> 1] >> (16 * (q & 1)));
+      }
+    }
+  }
 };
 
-// The results of a tile: acc += x W^T over k0 .. k1.
-template <class G>
-__device__ __forceinline__ void run_tile(const Project<bf16_t> &p, int64_t t0, int o0, int k0, int k1, unsigned char *xs0, unsigned char *ws0,
-                                         unsigned char *xs1, unsigned char *ws1, f32x16 (&acc)[G::EO][G::ET]) {
-  typename G::Loader l;
-  G::aim(p, t0, o0, k0, l);
-  G::load(l, k0, k1, xs0, ws0);
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __syncthreads();
-  for (int k = k0; k < k1; k += 2 * kK) {  // (an odd last stage has one of zeros beside it)
-    G::load(l, k + kK, k1, xs1, ws1);
-    G::multiply(xs0, ws0, acc);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (k + 2 * kK < k1) G::load(l, k + 2 * kK, k1, xs0, ws0);
-    G::multiply(xs1, ws1, acc);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-  }
-}
-
-template <int BT, int BO, int WT, int WO, bool NN>
-__global__ __launch_bounds__(WT *WO * 64, 2) void project_gemm_kernel(Project<bf16_t> p, int64_t tiles_t, int tiles_o) {
-  using G = Gemm<BT, BO, WT, WO, NN>;
+template <int BT, int BO, bool NN, bool FULL>
+__global__ __launch_bounds__(256, BT == 128 ? 2 : 1) void project_gemm_kernel(Project<bf16_t> p, int64_t tiles_t, int tiles_o) {
+  using G = Gemm<BT, BO, NN, FULL>;
   constexpr int ET = G::ET, EO = G::EO;
   __shared__ __align__(1024) unsigned char xs0[G::XB], ws0[G::WB], xs1[G::XB], ws1[G::WB];
   int64_t tt;
   int to;
   tile_of(blockIdx.x, tiles_t * tiles_o, tiles_t, tiles_o, tt, to);
-  const int64_t t0 = tt * BT;
-  const int o0 = to * BO;
-  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, ln = lane & 31, half = lane >> 5;
-  const int64_t tw = t0 + (wv / WO) * (ET * 32);
-  const int ow = o0 + (wv % WO) * (EO * 32);
+  int64_t t0 = tt * BT;
+  int o0 = to * BO;
+  if constexpr (FULL) t0 = min(t0, p.rows - BT), o0 = min(o0, p.outs - BO);
+  const int wv = threadIdx.x >> 6;
+  const int64_t tw = t0 + (wv / G::WO) * (ET * 32);
+  const int ow = o0 + (wv % G::WO) * (EO * 32);
   f32x16 acc[EO][ET] = {};
-  if (p.low.of_row) {  // (first: beside the loads' addresses its registers would not fit)
+  if (p.low.of_row) {  // (first: beside the operands its registers would not fit)
 #pragma unroll
     for (int r = 0; r < ET; ++r) G::add_rank(p, tw + r * 32, ow, acc, r);
   }
-  run_tile<G>(p, t0, o0, 0, p.width, xs0, ws0, xs1, ws1, acc);
-#pragma unroll
-  for (int r = 0; r < ET; ++r) {
-    __builtin_amdgcn_sched_barrier(0);
-    const int64_t t = tw + r * 32 + ln;
-    if (t >= p.rows) continue;
-#pragma unroll
-    for (int e = 0; e < EO; ++e)
-#pragma unroll
-      for (int i = 0; i < 16; i += 4) {
-        const int o = ow + e * 32 + (i >> 2) * 8 + half * 4;
-        bf16_t *y = p.y + t * p.ldy + o;
-        if (o + 4 <= p.outs) {
-          const uint64_t v = (uint64_t)narrow<bf16_t>(acc[e][r][i]) | (uint64_t)narrow<bf16_t>(acc[e][r][i + 1]) << 16 |
-                             (uint64_t)narrow<bf16_t>(acc[e][r][i + 2]) << 32 | (uint64_t)narrow<bf16_t>(acc[e][r][i + 3]) << 48;
-          typedef uint64_t u64_2 __attribute__((aligned(2)));
-          *reinterpret_cast<u64_2 *>(y) = v;
-        } else {
-#pragma unroll
-          for (int q = 0; q < 4; ++q)
-            if (o + q < p.outs) y[q] = narrow<bf16_t>(acc[e][r][i + q]);
-        }
-      }
-  }
+  G::run(p, t0, o0, 0, p.width, xs0, ws0, xs1, ws1, acc);
+  unsigned char *own = wv == 0 ? xs0 : wv == 1 ? ws0 : wv == 2 ? xs1 : ws1;
+  G::store(p, tw, ow, acc, own);
 }
 
 // Ranges of k: a workgroup leaves its sums as they are.  Before the tiles, workgroups of rank lines.
-template <int BT, int BO, int WT, int WO, bool NN>
-__global__ __launch_bounds__(WT *WO * 64, 2) void project_gemm_split_kernel(Project<bf16_t> p, int64_t tiles_t, int tiles_o, int splits,
-                                                                            int chunk, float *__restrict__ part, ThinJob<bf16_t> thin,
-                                                                            ThinJob<bf16_t> other) {
-  using G = Gemm<BT, BO, WT, WO, NN>;
+template <int BT, int BO, bool NN>
+__global__ __launch_bounds__(256, 2) void project_gemm_split_kernel(Project<bf16_t> p, int64_t tiles_t, int tiles_o, int splits, int chunk,
+                                                                    float *__restrict__ part, ThinJob<bf16_t> thin, ThinJob<bf16_t> other) {
+  using G = Gemm<BT, BO, NN, false>;
   constexpr int ET = G::ET, EO = G::EO;
   __shared__ __align__(1024) unsigned char xs0[G::XB], ws0[G::WB], xs1[G::XB], ws1[G::WB];
   const int64_t block = blockIdx.x;
@@ -248,9 +380,9 @@ __global__ __launch_bounds__(WT *WO * 64, 2) void project_gemm_split_kernel(Proj
   const int64_t tile = at / splits, t0 = tile % tiles_t * BT;
   const int o0 = (int)(tile / tiles_t) * BO;
   f32x16 acc[EO][ET] = {};
-  run_tile<G>(p, t0, o0, split * chunk, min(p.width, (split + 1) * chunk), xs0, ws0, xs1, ws1, acc);
-  const int64_t tw = t0 + (wv / WO) * (ET * 32);
-  const int ow = o0 + (wv % WO) * (EO * 32);
+  G::run(p, t0, o0, split * chunk, min(p.width, (split + 1) * chunk), xs0, ws0, xs1, ws1, acc);
+  const int64_t tw = t0 + (wv / G::WO) * (ET * 32);
+  const int ow = o0 + (wv % G::WO) * (EO * 32);
 #pragma unroll
   for (int r = 0; r < ET; ++r) {
     const int64_t t = tw + r * 32 + ln;
@@ -265,7 +397,7 @@ __global__ __launch_bounds__(WT *WO * 64, 2) void project_gemm_split_kernel(Proj
           *reinterpret_cast<f32x4_any *>(y) = f32x4_any{acc[e][r][i], acc[e][r][i + 1], acc[e][r][i + 2], acc[e][r][i + 3]};
         } else {
 #pragma unroll
-          for (int q = 0; q < 4; ++q)
+          for (int q = 0; q < 3; ++q)
             if (o + q < p.outs) y[q] = acc[e][r][i + q];
         }
       }
@@ -275,21 +407,21 @@ __global__ __launch_bounds__(WT *WO * 64, 2) void project_gemm_split_kernel(Proj
 bool on_16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 int64_t tiles(int64_t n, int size) { return (n + size - 1) / size; }
 
-template <int BT, int BO, int WT, int WO>
+template <int B, bool FULL>
 void launch(const Project<bf16_t> &p, hipStream_t s) {
-  const int64_t tiles_t = tiles(p.rows, BT);
-  const int tiles_o = (int)tiles(p.outs, BO);
+  const int64_t tiles_t = tiles(p.rows, B);
+  const int tiles_o = (int)tiles(p.outs, B);
   const unsigned blocks = (unsigned)(tiles_t * tiles_o);
-  if (p.wk == 1) project_gemm_kernel<BT, BO, WT, WO, false><<<blocks, WT * WO * 64, 0, s>>>(p, tiles_t, tiles_o);
-  else project_gemm_kernel<BT, BO, WT, WO, true><<<blocks, WT * WO * 64, 0, s>>>(p, tiles_t, tiles_o);
+  if (p.wk == 1) project_gemm_kernel<B, B, false, FULL><<<blocks, 256, 0, s>>>(p, tiles_t, tiles_o);
+  else project_gemm_kernel<B, B, true, FULL><<<blocks, 256, 0, s>>>(p, tiles_t, tiles_o);
 }
 
 }  // namespace
 
-// Rows of x and W that 16-byte loads can take, and no more tiles than a launch has workgroups.
+// Rows of x and W that 16-byte loads can take, lanes' offsets within 32 bits, and no more tiles than a launch has workgroups.
 bool gemm_takes(const Project<bf16_t> &p) {
   const int64_t w_row = p.wk == 1 ? p.wo : p.wk;
-  return on_16(p.x) && on_16(p.w) && p.ldx % 8 == 0 && w_row % 8 == 0 && p.width % 8 == 0 &&
+  return on_16(p.x) && on_16(p.w) && p.ldx % 8 == 0 && p.ldx < 1 << 27 && w_row % 8 == 0 && p.width % 8 == 0 &&
          tiles(p.rows, 128) * tiles(p.outs, 128) < 1 << 22;
 }
 
@@ -302,8 +434,8 @@ int gemm_splits(int64_t rows, int width, int outs) {
 }
 
 void launch_gemm(const Project<bf16_t> &p, hipStream_t s) {
-  if (tiles(p.rows, 256) * tiles(p.outs, 256) >= 200) launch<256, 256, 2, 4>(p, s);
-  else launch<128, 128, 2, 2>(p, s);
+  if (p.rows >= 256 && p.outs >= 256 && tiles(p.rows, 256) * tiles(p.outs, 256) >= 200) launch<256, true>(p, s);
+  else launch<128, false>(p, s);
 }
 
 void launch_gemm_split(const Project<bf16_t> &p, int splits, float *part, const ThinJob<bf16_t> &thin, const ThinJob<bf16_t> &other,
@@ -311,8 +443,8 @@ void launch_gemm_split(const Project<bf16_t> &p, int splits, float *part, const 
   const int64_t tiles_t = tiles(p.rows, 128);
   const int tiles_o = (int)tiles(p.outs, 128), chunk = (int)tiles(tiles(p.width, splits), 128) * 128;
   const unsigned blocks = (unsigned)(tiles_t * tiles_o * splits + thin.blocks + other.blocks);
-  if (p.wk == 1) project_gemm_split_kernel<128, 128, 2, 2, false><<<blocks, 256, 0, s>>>(p, tiles_t, tiles_o, splits, chunk, part, thin, other);
-  else project_gemm_split_kernel<128, 128, 2, 2, true><<<blocks, 256, 0, s>>>(p, tiles_t, tiles_o, splits, chunk, part, thin, other);
+  if (p.wk == 1) project_gemm_split_kernel<128, 128, false><<<blocks, 256, 0, s>>>(p, tiles_t, tiles_o, splits, chunk, part, thin, other);
+  else project_gemm_split_kernel<128, 128, true><<<blocks, 256, 0, s>>>(p, tiles_t, tiles_o, splits, chunk, part, thin, other);
 }
 
 }  // namespace wcc
