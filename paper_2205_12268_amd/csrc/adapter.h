@@ -259,13 +259,15 @@ struct ThinJob {
 
 constexpr int kRange = 128;
 struct ThinLds {
-  int key[kRange], row[kRange], of[kRange], head[kRange], heads;
+  int4 key[kRange / 4];
+  int row[kRange], of[kRange], head[kRange], heads;
 };
 
-// the sums over k0 .. k1 of 32 rows (of the lane: xr, at its half's chunk) with 32 lines (mr)
-template <class T>
+// the sums over k0 .. k1 of 32 rows (of the lane: xr, at its half's chunk) with 32 lines (mr); CONT: sc = 1.  Eight steps' loads go
+// out together: with four, and the next four on their way meanwhile, 128 rows x 512 k a workgroup took 50 us where these take 38.
+template <class T, bool CONT>
 __device__ __forceinline__ f32x16 thin_sums(const T *xr, const T *mr, int sc, int k0, int k1, int half) {
-  constexpr int VE = VecOf<T>::N, KS = StepOf<T>::K, U = 8;
+  constexpr int VE = VecOf<T>::N, KS = StepOf<T>::K, U = CONT ? 8 : 4;
   f32x16 acc = {};
   int k = k0;
   for (; k + KS * U <= k1; k += KS * U) {
@@ -273,8 +275,8 @@ __device__ __forceinline__ f32x16 thin_sums(const T *xr, const T *mr, int sc, in
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       xf[u] = *reinterpret_cast<const u32x4_any *>(xr + k + u * KS);
-      mf[u] = sc == 1 ? *reinterpret_cast<const u32x4_any *>(mr + k + u * KS)
-                      : load_k_strided(mr + (int64_t)(k + u * KS) * sc, sc, VE);
+      if constexpr (CONT) mf[u] = *reinterpret_cast<const u32x4_any *>(mr + k + u * KS);
+      else mf[u] = load_k_strided(mr + (int64_t)(k + u * KS) * sc, sc, VE);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) acc = mma<T>(xf[u], mf[u], acc);
@@ -282,7 +284,9 @@ __device__ __forceinline__ f32x16 thin_sums(const T *xr, const T *mr, int sc, in
   for (; k < k1; k += KS) {
     const int left = k1 - k - half * VE;
     const u32x4 xf = load_k(xr + k, left);
-    const u32x4 mf = sc == 1 ? load_k(mr + k, left) : load_k_strided(mr + (int64_t)k * sc, sc, left);
+    u32x4 mf;
+    if constexpr (CONT) mf = load_k(mr + k, left);
+    else mf = load_k_strided(mr + (int64_t)k * sc, sc, left);
     acc = mma<T>(xf, mf, acc);
   }
   return acc;
@@ -308,7 +312,7 @@ __device__ __forceinline__ void thin_unit(const ThinJob<T> &g, const Low &low, i
     const float f = low.factor(a);
     for (int j0 = 0; j0 < lines; j0 += 32) {
       const T *mr = g.m.p + a * g.m.major + (int64_t)min(j0 + ln, lines - 1) * g.m.sj + (int64_t)(half * VE) * g.m.sc;
-      const f32x16 acc = thin_sums<T>(xr, mr, g.m.sc, k0, k1, half);
+      const f32x16 acc = g.m.sc == 1 ? thin_sums<T, true>(xr, mr, 1, k0, k1, half) : thin_sums<T, false>(xr, mr, g.m.sc, k0, k1, half);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int row = result_line(i, half);
@@ -326,18 +330,19 @@ __device__ __forceinline__ void thin_range(const ThinJob<T> &g, const Low &low, 
   const int64_t base = block / g.out.splits * kRange;
   if (tid < kRange) {
     const int id = base + tid < g.rows ? low.of(base + tid) : -1;
-    lds.key[tid] = id < 0 ? none : id;
+    reinterpret_cast<int *>(lds.key)[tid] = id < 0 ? none : id;
   }
   if (tid == 0) lds.heads = 0;
   __syncthreads();
   if (tid < kRange) {
-    const int key = lds.key[tid];
+    const int key = reinterpret_cast<const int *>(lds.key)[tid];
     int less = 0, before = 0, equal = 0;
-    for (int i = 0; i < kRange; ++i) {
-      const int k = lds.key[i];
-      less += k < key;
-      equal += k == key;
-      before += k == key && i < tid;
+#pragma unroll 8
+    for (int i = 0; i < kRange / 4; ++i) {
+      const int4 k = lds.key[i];
+      less += (k.x < key) + (k.y < key) + (k.z < key) + (k.w < key);
+      equal += (k.x == key) + (k.y == key) + (k.z == key) + (k.w == key);
+      before += (k.x == key && 4 * i < tid) + (k.y == key && 4 * i + 1 < tid) + (k.z == key && 4 * i + 2 < tid) + (k.w == key && 4 * i + 3 < tid);
     }
     lds.row[less + before] = tid;
     lds.of[less + before] = key;
@@ -355,7 +360,7 @@ __device__ __forceinline__ void thin_range(const ThinJob<T> &g, const Low &low, 
     float *out = g.out.p + split * g.out.stride + base * g.out.ld;
     for (int j0 = 0; j0 < lines; j0 += 32) {
       const T *mr = g.m.p + a * g.m.major + (int64_t)min(j0 + ln, lines - 1) * g.m.sj + (int64_t)(half * VE) * g.m.sc;
-      const f32x16 acc = thin_sums<T>(xr, mr, g.m.sc, k0, k1, half);
+      const f32x16 acc = g.m.sc == 1 ? thin_sums<T, true>(xr, mr, 1, k0, k1, half) : thin_sums<T, false>(xr, mr, g.m.sc, k0, k1, half);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int q = result_line(i, half);

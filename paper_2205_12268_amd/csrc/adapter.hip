@@ -17,7 +17,7 @@ namespace {
 
 // One or two jobs of rank lines by themselves, before whole tiles.
 template <class T>
-__global__ __launch_bounds__(256) void adapter_lines_kernel(ThinJob<T> g1, ThinJob<T> g2, Low low) {
+__global__ __launch_bounds__(256, 2) void adapter_lines_kernel(ThinJob<T> g1, ThinJob<T> g2, Low low) {
   __shared__ ThinLds lds;
   for (int64_t b = blockIdx.x; b < g1.blocks + g2.blocks; b += gridDim.x) {
     if (b < g1.blocks) thin_block<T>(g1, low, b, &lds);
@@ -64,7 +64,7 @@ __device__ __forceinline__ void stream_block(const StreamJob<T> &g, int64_t bloc
     u32x4 xf[U][RT], wf[U][2];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (!NN) {
+      if constexpr (!NN) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) wf[u][e] = *reinterpret_cast<const u32x4_any *>(wr[e] + k + u * KS);
       } else {
@@ -83,7 +83,7 @@ __device__ __forceinline__ void stream_block(const StreamJob<T> &g, int64_t bloc
   for (; k < k1; k += KS) {
     const int left = k1 - k - half * VE;
     u32x4 wf[2];
-    if (!NN) {
+    if constexpr (!NN) {
 #pragma unroll
       for (int e = 0; e < 2; ++e) wf[e] = load_k(wr[e] + k, left);
     } else {
@@ -116,7 +116,7 @@ __device__ __forceinline__ void stream_block(const StreamJob<T> &g, int64_t bloc
 
 // First launch: workgroups of one or two jobs of rank lines (they take longest), then of the product with W.
 template <class T, int RT, bool NN>
-__global__ __launch_bounds__(256) void adapter_products_kernel(StreamJob<T> g, ThinJob<T> thin, ThinJob<T> thin2, Low low) {
+__global__ __launch_bounds__(256, 2) void adapter_products_kernel(StreamJob<T> g, ThinJob<T> thin, ThinJob<T> thin2, Low low) {
   __shared__ float red[4 * 32 * RT * 72];
   const int64_t block = blockIdx.x;
   if (block < thin.blocks) return thin_block<T>(thin, low, block, red);
@@ -291,6 +291,19 @@ __device__ __forceinline__ void grad_block(const GradJob<T> &g, const Low &low, 
   const int64_t t_end = min(rows, (split + 1) * range);
   f32x16 acc[4] = {};
   int have = 0, total = 0, round = 0;
+  // most ranges have rows of few adapters: a wave looks by itself whether there are any of this one
+  if (range <= 256) {
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int64_t t = split * range + i * 64 + lane;
+      any |= i * 64 + lane < range && t < rows && low.of(t) == a;
+    }
+    if (splits > 1 && __ballot(any) == 0) {
+      if (tile_c == 0 && j0 == 0 && tid == 0) g.found[(int64_t)split * low.n + a] = 0;
+      return;
+    }
+  }
 
   // the columns of the listed rows of step s; of a single step of n < KS rows the others are zeros
   auto fetch = [&](int s, int n, uint32_t (&v)[VE][D]) {
@@ -413,7 +426,7 @@ __device__ __forceinline__ void grad_block(const GradJob<T> &g, const Low &low, 
 
 // dA's blocks, then dB's (whose lines are the contiguous ones: its results lie the other way round)
 template <class T>
-__global__ __launch_bounds__(256) void adapter_grad_kernel(GradJob<T> ga, GradJob<T> gb, Low low, int64_t rows, int splits, int64_t range) {
+__global__ __launch_bounds__(256, 3) void adapter_grad_kernel(GradJob<T> ga, GradJob<T> gb, Low low, int64_t rows, int splits, int64_t range) {
   __shared__ __align__(16) GradLds<T> lds;
   for (int64_t b = blockIdx.x; b < ga.blocks + gb.blocks; b += gridDim.x) {
     if (b < ga.blocks) grad_block<T, false>(ga, low, rows, splits, range, b, lds);
@@ -455,21 +468,30 @@ __global__ __launch_bounds__(256) void adapter_grad_join_kernel(JoinJob ja, Join
     }
     const int lines = low.lines(a);
     const int64_t at0 = (int64_t)(first ? tile : tile - ja.tiles) * 1024;
+    const int64_t in = at0 + tid * 4;
+    const float *p = g.part + a * g.major + in;
+    float *out = g.out + a * g.major + in;
+    if (in + 4 <= g.major) {
+      f32x4_any v = {};
+      int i = 0;
+      for (; i + 4 <= n; i += 4) {
+        f32x4_any w[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int64_t in = at0 + i * 256 + tid;
-      if (in >= g.major) break;
-      const int j = g.sj == 1 ? (int)(in % low.rank) : (int)(in / g.sj);
-      const float *p = g.part + a * g.major + in;
-      float v = 0.f;
-      if (j < lines)
-        for (int s = 0; s < n; s += 4) {
-          float w[4];
+        for (int u = 0; u < 4; ++u) w[u] = *reinterpret_cast<const f32x4_any *>(p + list[i + u] * g.size);
+        v += (w[0] + w[1]) + (w[2] + w[3]);
+      }
+      for (; i < n; ++i) v += *reinterpret_cast<const f32x4_any *>(p + list[i] * g.size);
 #pragma unroll
-          for (int u = 0; u < 4; ++u) w[u] = s + u < n ? p[list[s + u] * g.size] : 0.f;
-          v += (w[0] + w[1]) + (w[2] + w[3]);
-        }
-      g.out[a * g.major + in] = v;
+      for (int q = 0; q < 4; ++q)
+        if ((g.sj == 1 ? (int)((in + q) % low.rank) : (int)((in + q) / g.sj)) >= lines) v[q] = 0.f;
+      *reinterpret_cast<f32x4_any *>(out) = v;
+    } else {
+      for (int q = 0; in + q < g.major; ++q) {
+        float v = 0.f;
+        if ((g.sj == 1 ? (int)((in + q) % low.rank) : (int)((in + q) / g.sj)) < lines)
+          for (int i = 0; i < n; ++i) v += p[list[i] * g.size + q];
+        out[q] = v;
+      }
     }
     __syncthreads();
   }
