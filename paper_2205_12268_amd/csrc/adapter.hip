@@ -19,9 +19,12 @@ namespace {
 template <class T>
 __global__ __launch_bounds__(256, 2) void adapter_lines_kernel(ThinJob<T> g1, ThinJob<T> g2, Low low) {
   __shared__ ThinLds lds;
+  constexpr int room = sizeof(T) == 2 ? 16384 : 16;
+  __shared__ __align__(1024) unsigned char x0[room], m0[room], x1[room], m1[room];
+  const ThinStages st{x0, m0, x1, m1};
   for (int64_t b = blockIdx.x; b < g1.blocks + g2.blocks; b += gridDim.x) {
-    if (b < g1.blocks) thin_block<T>(g1, low, b, &lds);
-    else thin_block<T>(g2, low, b - g1.blocks, &lds);
+    if (b < g1.blocks) thin_block<T>(g1, low, b, lds, st);
+    else thin_block<T>(g2, low, b - g1.blocks, lds, st);
     __syncthreads();
   }
 }
@@ -119,8 +122,13 @@ template <class T, int RT, bool NN>
 __global__ __launch_bounds__(256, 2) void adapter_products_kernel(StreamJob<T> g, ThinJob<T> thin, ThinJob<T> thin2, Low low) {
   __shared__ float red[4 * 32 * RT * 72];
   const int64_t block = blockIdx.x;
-  if (block < thin.blocks) return thin_block<T>(thin, low, block, red);
-  if (block < thin.blocks + thin2.blocks) return thin_block<T>(thin2, low, block - thin.blocks, red);
+  if (block < thin.blocks + thin2.blocks) {
+    __shared__ ThinLds lds;
+    const ThinStages st{};
+    if (block < thin.blocks) thin_block<T>(thin, low, block, lds, st);
+    else thin_block<T>(thin2, low, block - thin.blocks, lds, st);
+    return;
+  }
   stream_block<T, RT, NN>(g, block - thin.blocks - thin2.blocks, red);
 }
 
@@ -215,7 +223,7 @@ __global__ __launch_bounds__(256) void adapter_finish_tile_kernel(FinishJob<T> g
     f32x16 acc[1];
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[0][i] = sums[result_line(i, half)][wv * 32 + ln];
-    if (low.of_row) add_thin<T, 1>(low, g.m, g.h, g.rows, g.outs, t0, o, acc);
+    if (low.of_row) add_thin<T, 1, true>(low, g.m, g.h, g.rows, g.outs, t0, o, acc);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const int64_t t = t0 + result_line(i, half);
@@ -519,9 +527,9 @@ Plan plan_of(const wcc_adapter_desc &d, int width, int outs, bool aligned) {
   p.rt = rows <= 32 ? 1 : 2;
   p.tiles_o = (int)ceil_div(outs, 64);
   const int64_t tiles = ceil_div(rows, 32 * p.rt) * p.tiles_o;
-  if (aligned && rows > 64) {
+  if (aligned) {
     p.splits = gemm_splits(rows, width, outs);
-    p.route = p.splits > 1 ? Plan::kGemmSplit : Plan::kGemm;
+    p.route = p.splits > 1 || rows <= 64 ? Plan::kGemmSplit : Plan::kGemm;
   } else if (tiles <= 1024) {
     p.route = Plan::kStream;
     const int unit = 4 * step4(d);
@@ -564,7 +572,7 @@ GradPlan grad_plan(const wcc_adapter_desc &d) {
 Low low_of(const wcc_adapter_desc &d, const AdapterArgs &g) { return Low{g.of_row, g.ranks, g.scale, d.adapters, d.rank}; }
 
 template <class T>
-ThinJob<T> thin_job(const wcc_adapter_desc &d, const AdapterArgs &g, bool back, float *out) {
+ThinJob<T> thin_job(const wcc_adapter_desc &d, const AdapterArgs &g, bool back, bool lds, float *out) {
   ThinJob<T> j{};
   if (!g.of_row) return j;
   const int64_t ci = d.C_in, co = d.C_out, r = d.rank;
@@ -576,9 +584,13 @@ ThinJob<T> thin_job(const wcc_adapter_desc &d, const AdapterArgs &g, bool back, 
   j.chunk = (int)(ceil_div(ceil_div(j.width, thin_splits(d, j.width)), step4(d)) * step4(d));
   j.out = Lines{out, (int)ceil_div(j.width, j.chunk), lines_ld(d), d.rows * lines_ld(d)};
   j.by_range = d.rows > 64;
-  j.groups = std::clamp(d.adapters, 1, 32);
+  auto whole = [](const void *p, int64_t stride) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && stride % 8 == 0; };
+  j.through_lds = lds && j.by_range && sizeof(T) == 2 && j.width % 8 == 0 && whole(j.x, j.ldx) && whole(j.m.p, back ? r : ci);
+  const int64_t ranges = ceil_div(d.rows, kRange) * j.out.splits;
+  // (up to 64 rows a wave an adapter, more: workgroups for two a compute unit, but not where few adapters leave them idle)
+  j.groups = j.by_range ? (int)std::clamp<int64_t>(512 / ranges, 1, std::min<int64_t>(8, ceil_div(d.adapters, 4))) : std::clamp(d.adapters, 1, 32);
   j.units = ceil_div(d.rows, 32) * j.out.splits * j.groups;
-  j.blocks = j.by_range ? ceil_div(d.rows, kRange) * j.out.splits : ceil_div(j.units, 4);
+  j.blocks = j.by_range ? ranges * j.groups : ceil_div(j.units, 4);
   return j;
 }
 
@@ -648,7 +660,7 @@ template <class T>
 hipError_t forward(const wcc_adapter_desc &d, const AdapterArgs &g, hipStream_t s) {
   const Project<T> p = project_of<T>(d, g, false);
   const Plan pl = plan_of(d, d.C_in, d.C_out, aligned(p));
-  project<T>(p, pl, thin_job<T>(d, g, false, (float *)g.ws), ThinJob<T>{}, (float *)(g.ws + lines_bytes(d, d.C_in)), s);
+  project<T>(p, pl, thin_job<T>(d, g, false, pl.route != Plan::kStream, (float *)g.ws), ThinJob<T>{}, (float *)(g.ws + lines_bytes(d, d.C_in)), s);
   return hipGetLastError();
 }
 
@@ -659,10 +671,11 @@ hipError_t backward(const wcc_adapter_desc &d, const AdapterArgs &g, hipStream_t
   const Project<T> p = project_of<T>(d, g, true);
   const Low low = p.low;
   const Plan pl = plan_of(d, d.C_out, d.C_in, aligned(p));
+  const bool lds = !g.y || pl.route != Plan::kStream;  // (the streaming launch has none to spare)
   float *gr = (float *)take(lines_bytes(d, d.C_out)), *h = (float *)take(lines_bytes(d, d.C_in));
   float *part = (float *)take(g.y ? parts_bytes(d, pl, d.C_in) : 0);
-  const ThinJob<T> back = g.y || g.da ? thin_job<T>(d, g, true, gr) : ThinJob<T>{};
-  const ThinJob<T> fore = g.db ? thin_job<T>(d, g, false, h) : ThinJob<T>{};
+  const ThinJob<T> back = g.y || g.da ? thin_job<T>(d, g, true, lds, gr) : ThinJob<T>{};
+  const ThinJob<T> fore = g.db ? thin_job<T>(d, g, false, lds, h) : ThinJob<T>{};
   if (g.y) project<T>(p, pl, back, fore, part, s);
   else launch_lines(back, fore, low, s);
   if (!g.da && !g.db) return hipGetLastError();

@@ -16,16 +16,7 @@
 namespace wcc {
 namespace {
 
-__device__ const uint4 kZeros = {0, 0, 0, 0};
-
-typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4;
-
-__device__ __forceinline__ void to_lds(const void *from, unsigned char *to) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
-                                   (__attribute__((address_space(3))) void *)to, 16, 0, 0);
-}
-
-constexpr int kK = 64, Line = kK * 2, Chunks = kK / 8, PerLoad = 1024 / Line;  // k of a stage; bytes and chunks of a line, lines of a load
+constexpr int Line = kLine, Chunks = kChunks, PerLoad = 1024 / Line;  // lines of a load
 
 // (see adapter_tile.hip)
 __device__ __forceinline__ void tile_of(int64_t b, int64_t tiles, int64_t tiles_t, int tiles_o, int64_t &tt, int &to) {
@@ -38,14 +29,13 @@ __device__ __forceinline__ void tile_of(int64_t b, int64_t tiles, int64_t tiles_
 }
 
 // FULL: a tile lies within the rows and outputs (the last ones are moved back, over others, whose results they repeat).
-template <int BT, int BO, bool NN, bool FULL>
+template <int BT, int BO, int WT, bool NN, bool FULL>
 struct Gemm {
-  static constexpr int WT = 2, WO = 2, Waves = WT * WO;
+  static constexpr int Waves = 4, WO = Waves / WT;
   static constexpr int ET = BT / WT / 32, EO = BO / WO / 32;            // 32 x 32 results of a wave
   static constexpr int XB = BT * kK * 2, WB = BO * kK * 2;              // bytes of a stage
   static constexpr int XL = XB / 1024 / Waves, WL = WB / 1024 / Waves;  // loads of a wave
   static constexpr int C = BO / 8, R = 64 / C;                          // NN: chunks of a line of k, lines of a load
-  __device__ static __forceinline__ int key(int line) { return (line >> 1) & 7; }
 
   // Where a wave's loads begin.  Load i is at x + i * x_step + k, and a lane's place in it depends on i's last bit alone; without
   // FULL the rows are held to the last one, each load's by itself.
@@ -73,7 +63,7 @@ struct Gemm {
     }
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      const int row = b * PerLoad + lane / Chunks, chunk = (lane % Chunks) ^ key(row);
+      const int row = b * PerLoad + lane / Chunks, chunk = (lane % Chunks) ^ chunk_key(row);
       l.xo[b] = (uint32_t)((lane / Chunks) * p.ldx * 2 + chunk * 16);
       if constexpr (NN) l.wo[b] = (uint32_t)((lane / C) * p.wk * 2 + ((lane % C) ^ (((b * R + lane / C) & 3) * 4)) * 16);
       else l.wo[b] = (uint32_t)((lane / Chunks) * p.wo * 2 + chunk * 16);
@@ -81,13 +71,13 @@ struct Gemm {
     if constexpr (!FULL) {
 #pragma unroll
       for (int i = 0; i < XL; ++i) {
-        const int row = (wv * XL + i) * PerLoad + lane / Chunks, chunk = (lane % Chunks) ^ key(row);
+        const int row = (wv * XL + i) * PerLoad + lane / Chunks, chunk = (lane % Chunks) ^ chunk_key(row);
         l.xr[i] = reinterpret_cast<const char *>(p.x + min(t0 + row, p.rows - 1) * p.ldx + k0 + chunk * 8);
       }
       if constexpr (!NN) {
 #pragma unroll
         for (int i = 0; i < WL; ++i) {
-          const int row = (wv * WL + i) * PerLoad + lane / Chunks, chunk = (lane % Chunks) ^ key(row);
+          const int row = (wv * WL + i) * PerLoad + lane / Chunks, chunk = (lane % Chunks) ^ chunk_key(row);
           l.wr[i] = reinterpret_cast<const char *>(p.w + (int64_t)min(o0 + row, p.outs - 1) * p.wo + k0 + chunk * 8);
         }
       }
@@ -129,23 +119,19 @@ struct Gemm {
     const char *zeros = reinterpret_cast<const char *>(&kZeros);
 #pragma unroll
     for (int i = 0; i < XL; ++i) {
-      const int chunk = (lane % Chunks) ^ key(i * PerLoad + lane / Chunks);  // (a wave's first line is a multiple of 16)
+      const int chunk = (lane % Chunks) ^ chunk_key((wv * XL + i) * PerLoad + lane / Chunks);
       to_lds(chunk * 8 < left ? x_at(l, i, stage) : zeros, xs + (wv * XL + i) * 1024);
     }
 #pragma unroll
     for (int i = 0; i < WL; ++i) {
       bool there;
       if constexpr (NN) there = (wv * WL + i) * R + lane / C < left && w_there(l, i);
-      else there = ((lane % Chunks) ^ key(i * PerLoad + lane / Chunks)) * 8 < left;
+      else there = ((lane % Chunks) ^ chunk_key((wv * WL + i) * PerLoad + lane / Chunks)) * 8 < left;
       to_lds(there ? w_at(l, i, stage) : zeros, ws + (wv * WL + i) * 1024);
     }
   }
 
-  __device__ static __forceinline__ u32x4 line(const unsigned char *s, int row, int chunk) {
-    return *reinterpret_cast<const u32x4 *>(s + row * Line + ((chunk ^ key(row)) << 4));
-  }
-  // 32 outputs from o on, 16 k from k on, of lines of k: within 16 lanes, lane 4j + q supplies four outputs of k + j, and lane 4q + e
-  // receives the e-th of them for j = 0..3
+  // 32 outputs from o on, 16 k from k on, of lines of k
   __device__ static __forceinline__ u32x4 across(const unsigned char *s, int o, int k) {
     const int lane = threadIdx.x & 63, g = lane >> 4, q = lane & 15;
     const int n = o + (g & 1) * 16 + (q & 3) * 4, kk = k + (g >> 1) * 8 + (q >> 2);
@@ -153,10 +139,7 @@ struct Gemm {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int row = kk + h * 4;
-      const unsigned char *at = s + row * (BO * 2) + (((n >> 3) ^ ((row & 3) * 4)) << 4) + (n & 7) * 2;
-      const bf16x4 r = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
-          (__attribute__((address_space(3))) bf16x4 *)(__attribute__((address_space(3))) void *)at);
-      const uint2 u = __builtin_bit_cast(uint2, r);
+      const uint2 u = turned(s + row * (BO * 2) + (((n >> 3) ^ ((row & 3) * 4)) << 4) + (n & 7) * 2);
       v[2 * h] = u.x, v[2 * h + 1] = u.y;
     }
     return v;
@@ -169,9 +152,9 @@ struct Gemm {
     const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, ln = lane & 31, half = lane >> 5;
     const int tw = (wv / WO) * (ET * 32), ow = (wv % WO) * (EO * 32);
 #pragma unroll
-    for (int e = 0; e < EO; ++e) f.w[e] = NN ? across(ws, ow + e * 32, step * 16) : line(ws, ow + e * 32 + ln, step * 2 + half);
+    for (int e = 0; e < EO; ++e) f.w[e] = NN ? across(ws, ow + e * 32, step * 16) : chunk_of(ws, ow + e * 32 + ln, step * 2 + half);
 #pragma unroll
-    for (int r = 0; r < ET; ++r) f.x[r] = line(xs, tw + r * 32 + ln, step * 2 + half);
+    for (int r = 0; r < ET; ++r) f.x[r] = chunk_of(xs, tw + r * 32 + ln, step * 2 + half);
   }
   __device__ static __forceinline__ void multiply(const Operands &f, f32x16 (&acc)[EO][ET]) {
 #pragma unroll
@@ -274,40 +257,6 @@ struct Gemm {
     }
   }
 
-  // As adapter.h's add_thin, with rows and outputs exchanged: a lane's own row is t0 + lane % 32.
-  __device__ static __forceinline__ void add_rank(const Project<bf16_t> &p, int64_t t0, int o0, f32x16 (&acc)[EO][ET], int r) {
-    constexpr int P = PartsOf<bf16_t>::Out;
-    const int ln = threadIdx.x & 31, half = (threadIdx.x >> 5) & 1;
-    const int64_t t = min(t0 + ln, p.rows - 1);
-    const int id = t0 + ln < p.rows ? p.low.of(t) : -1;
-    uint32_t rest = (uint32_t)__ballot(id >= 0);
-    while (rest != 0) {
-      const int a = __builtin_amdgcn_readlane(id, __builtin_ctz(rest));
-      rest &= ~(uint32_t)__ballot(id == a);
-      const int lines = p.low.lines(a);
-      f32x16 d[EO] = {};
-      for (int j0 = 0; j0 < lines; j0 += 16) {
-        const int j = j0 + half * 8, left = lines - j;
-        u32x4 hf[P] = {}, mf[EO] = {};
-        if (left > 0) {
-          float hv[8];
-          p.h.eight(t, j, hv);
-          split_to<bf16_t, P>(hv, hf);
-#pragma unroll
-          for (int e = 0; e < EO; ++e) mf[e] = thin_k(p.m, a, min(o0 + e * 32 + ln, p.outs - 1), j, left);
-        }
-#pragma unroll
-        for (int e = 0; e < EO; ++e)
-#pragma unroll
-          for (int q = P - 1; q >= 0; --q) d[e] = mma<bf16_t>(mf[e], hf[q], d[e]);
-      }
-#pragma unroll
-      for (int e = 0; e < EO; ++e)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) acc[e][r][i] += id == a ? d[e][i] : 0.f;
-    }
-  }
-
   // The wave's results to y, rows from tw and outputs from ow on, through its part of LDS: a row's 8-byte pieces are exchanged by a
   // key of the row (even, so that pairs of them stay together).
   __device__ static __forceinline__ void store(const Project<bf16_t> &p, int64_t tw, int ow, const f32x16 (&acc)[EO][ET], unsigned char *lds) {
@@ -346,7 +295,7 @@ struct Gemm {
 
 template <int BT, int BO, bool NN, bool FULL>
 __global__ __launch_bounds__(256, BT == 128 ? 2 : 1) void project_gemm_kernel(Project<bf16_t> p, int64_t tiles_t, int tiles_o) {
-  using G = Gemm<BT, BO, NN, FULL>;
+  using G = Gemm<BT, BO, 2, NN, FULL>;
   constexpr int ET = G::ET, EO = G::EO;
   __shared__ __align__(1024) unsigned char xs0[G::XB], ws0[G::WB], xs1[G::XB], ws1[G::WB];
   int64_t tt;
@@ -361,7 +310,15 @@ __global__ __launch_bounds__(256, BT == 128 ? 2 : 1) void project_gemm_kernel(Pr
   f32x16 acc[EO][ET] = {};
   if (p.low.of_row) {  // (first: beside the operands its registers would not fit)
 #pragma unroll
-    for (int r = 0; r < ET; ++r) G::add_rank(p, tw + r * 32, ow, acc, r);
+    for (int r = 0; r < ET; ++r) {
+      int o[EO];
+      f32x16 sums[EO] = {};
+#pragma unroll
+      for (int e = 0; e < EO; ++e) o[e] = ow + e * 32 + (threadIdx.x & 31);
+      add_thin<bf16_t, EO, false>(p.low, p.m, p.h, p.rows, p.outs, tw + r * 32, o, sums);
+#pragma unroll
+      for (int e = 0; e < EO; ++e) acc[e][r] = sums[e];
+    }
   }
   G::run(p, t0, o0, 0, p.width, xs0, ws0, xs1, ws1, acc);
   unsigned char *own = wv == 0 ? xs0 : wv == 1 ? ws0 : wv == 2 ? xs1 : ws1;
@@ -369,16 +326,21 @@ __global__ __launch_bounds__(256, BT == 128 ? 2 : 1) void project_gemm_kernel(Pr
 }
 
 // Ranges of k: a workgroup leaves its sums as they are.  Before the tiles, workgroups of rank lines.
-template <int BT, int BO, bool NN>
+template <int BT, int BO, int WT, bool NN>
 __global__ __launch_bounds__(256, 2) void project_gemm_split_kernel(Project<bf16_t> p, int64_t tiles_t, int tiles_o, int splits, int chunk,
                                                                     float *__restrict__ part, ThinJob<bf16_t> thin, ThinJob<bf16_t> other) {
-  using G = Gemm<BT, BO, NN, false>;
+  using G = Gemm<BT, BO, WT, NN, false>;
   constexpr int ET = G::ET, EO = G::EO;
   __shared__ __align__(1024) unsigned char xs0[G::XB], ws0[G::WB], xs1[G::XB], ws1[G::WB];
   const int64_t block = blockIdx.x;
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, ln = lane & 31, half = lane >> 5;
-  if (block < thin.blocks) return thin_block<bf16_t>(thin, p.low, block, xs0);
-  if (block < thin.blocks + other.blocks) return thin_block<bf16_t>(other, p.low, block - thin.blocks, xs0);
+  if (block < thin.blocks + other.blocks) {
+    __shared__ ThinLds lds;
+    const ThinStages st{xs0, ws0, xs1, ws1};
+    if (block < thin.blocks) thin_block<bf16_t>(thin, p.low, block, lds, st);
+    else thin_block<bf16_t>(other, p.low, block - thin.blocks, lds, st);
+    return;
+  }
   const int64_t at = block - thin.blocks - other.blocks;
   const int split = (int)(at % splits);
   const int64_t tile = at / splits, t0 = tile % tiles_t * BT;
@@ -429,10 +391,15 @@ bool gemm_takes(const Project<bf16_t> &p) {
          tiles(p.rows, 128) * tiles(p.outs, 128) < 1 << 22;
 }
 
+// Tiles in ranges of k: 32, 64 or 128 rows by 128 outputs.
+int split_rows(int64_t rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
+
+// Whole tiles where they give three quarters of the compute units work; else ranges of 256 k at least, and two (few rows: what counts
+// is W on its way) workgroups a compute unit.
 int gemm_splits(int64_t rows, int width, int outs) {
-  const int64_t n = tiles(rows, 128) * tiles(outs, 128);
-  if (n >= 192) return 1;
-  const int64_t want = std::min<int64_t>((384 + n - 1) / n, std::max(width / 256, 1));
+  const int64_t n = tiles(rows, split_rows(rows)) * tiles(outs, 128);
+  if (rows > 64 && n >= 192) return 1;
+  const int64_t want = std::min<int64_t>(((rows > 64 ? 384 : 512) + n - 1) / n, std::max(width / 256, 1));
   const int64_t chunk = tiles(tiles(width, (int)std::min<int64_t>(want, 16)), 128) * 128;
   return (int)tiles(width, (int)chunk);
 }
@@ -442,13 +409,21 @@ void launch_gemm(const Project<bf16_t> &p, hipStream_t s) {
   else launch<128, false>(p, s);
 }
 
-void launch_gemm_split(const Project<bf16_t> &p, int splits, float *part, const ThinJob<bf16_t> &thin, const ThinJob<bf16_t> &other,
-                       hipStream_t s) {
-  const int64_t tiles_t = tiles(p.rows, 128);
+template <int BT, int WT>
+void launch_split(const Project<bf16_t> &p, int splits, float *part, const ThinJob<bf16_t> &thin, const ThinJob<bf16_t> &other, hipStream_t s) {
+  const int64_t tiles_t = tiles(p.rows, BT);
   const int tiles_o = (int)tiles(p.outs, 128), chunk = (int)tiles(tiles(p.width, splits), 128) * 128;
   const unsigned blocks = (unsigned)(tiles_t * tiles_o * splits + thin.blocks + other.blocks);
-  if (p.wk == 1) project_gemm_split_kernel<128, 128, false><<<blocks, 256, 0, s>>>(p, tiles_t, tiles_o, splits, chunk, part, thin, other);
-  else project_gemm_split_kernel<128, 128, true><<<blocks, 256, 0, s>>>(p, tiles_t, tiles_o, splits, chunk, part, thin, other);
+  if (p.wk == 1) project_gemm_split_kernel<BT, 128, WT, false><<<blocks, 256, 0, s>>>(p, tiles_t, tiles_o, splits, chunk, part, thin, other);
+  else project_gemm_split_kernel<BT, 128, WT, true><<<blocks, 256, 0, s>>>(p, tiles_t, tiles_o, splits, chunk, part, thin, other);
+}
+
+void launch_gemm_split(const Project<bf16_t> &p, int splits, float *part, const ThinJob<bf16_t> &thin, const ThinJob<bf16_t> &other,
+                       hipStream_t s) {
+  const int rows = split_rows(p.rows);
+  if (rows == 32) launch_split<32, 1>(p, splits, part, thin, other, s);
+  else if (rows == 64) launch_split<64, 1>(p, splits, part, thin, other, s);
+  else launch_split<128, 2>(p, splits, part, thin, other, s);
 }
 
 }  // namespace wcc

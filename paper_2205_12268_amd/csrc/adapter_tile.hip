@@ -103,7 +103,7 @@ __global__ __launch_bounds__(256, 2) void project_tile_kernel(Project<T> p, int6
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
       const int64_t tr = t0 + wm * 64 + r * 32;
-      if (p.low.of_row) add_thin<T, 2>(p.low, p.m, p.h, p.rows, p.outs, tr, o, acc[r]);
+      if (p.low.of_row) add_thin<T, 2, true>(p.low, p.m, p.h, p.rows, p.outs, tr, o, acc[r]);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int64_t t = tr + result_line(i, half);
