@@ -119,6 +119,11 @@ __device__ __forceinline__ void store_slice(T *p, int n, F f) {
 struct Larger {
   __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
 };
+// (NaN if one of them is)
+__device__ __forceinline__ float largest_of(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+struct Largest {
+  __device__ __forceinline__ float operator()(float a, float b) const { return largest_of(a, b); }
+};
 struct Sum {
   __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
 };

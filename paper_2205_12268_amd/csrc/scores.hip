@@ -96,8 +96,9 @@ __global__ __launch_bounds__(NT, 4) void scores_slice_kernel(const T *__restrict
     for (int i = 0; i < NV; ++i) {
       float vm = elem<T>(v[i], 0);
 #pragma unroll
-      for (int j = 1; j < VE; ++j) vm = fmaxf(vm, elem<T>(v[i], j));
-      if (vm > mine) mine = vm, at = i;
+      for (int j = 1; j < VE; ++j) vm = largest_of(vm, elem<T>(v[i], j));
+      if (vm > mine) at = i;
+      mine = largest_of(mine, vm);
     }
     uint64_t my_key = 0;  // largest element, start of its vector
     if constexpr (TOP) {
@@ -105,19 +106,32 @@ __global__ __launch_bounds__(NT, 4) void scores_slice_kernel(const T *__restrict
       best[tid] = my_key;
       if (tid == 0) n_holder = n_cand = 0;
     }
-    const float m = block_all<NT>(mine, fpart[0], Larger());
+    const float m = block_all<NT>(mine, fpart[0], Largest());
     const float base = m == -INFINITY ? 0.f : m;
     hold(v);
 
-    float s[2] = {0.f, 0.f}, e[2] = {0.f, 0.f};
+    // To base 2: d = (x - m) log2(e).  One fma a logit, x log2(e) - c with c = m log2(e) rounded, whose error `off`, the same for
+    // all, is taken off the sums; a large m, beside which it would not be small, has the subtraction first, from memory.
+    // (E: 0 times -inf; 2^-200 is 0.)
+    float s[2] = {0.f, 0.f}, e[2] = {0.f, 0.f}, off = 0.f;
+    if (fabsf(base) < 1024.f) {
+      const float c = base * kLog2e;
+      off = fmaf(base, kLog2e, -c);
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+      for (int i = 0; i < NV; ++i)
 #pragma unroll
-      for (int j = 0; j < VE; ++j) {
-        const float d = (elem<T>(v[i], j) - base) * kLog2e, p = __builtin_amdgcn_exp2f(d);
-        s[j & 1] += p;
-        e[j & 1] = fmaf(p, fmaxf(d, -200.f), e[j & 1]);  // (0 times -inf; 2^-200 is 0)
+        for (int j = 0; j < VE; ++j) {
+          const float d = largest_of(fmaf(elem<T>(v[i], j), kLog2e, -c), -200.f), p = __builtin_amdgcn_exp2f(d);
+          s[j & 1] += p;
+          e[j & 1] = fmaf(p, d, e[j & 1]);
+        }
+    } else {
+      for (int i = tid; i < n; i += NT) {
+        const float d = largest_of((widen(r[i]) - base) * kLog2e, -200.f), p = __builtin_amdgcn_exp2f(d);
+        s[0] += p;
+        e[0] = fmaf(p, d, e[0]);
       }
+    }
     float st = wave_all(s[0] + s[1], Sum()), et = wave_all(e[0] + e[1], Sum());
     if constexpr (NT > 64) {
       if (lane == 0) fpart[1][wv] = st, fpart[2][wv] = et;
@@ -138,6 +152,8 @@ __global__ __launch_bounds__(NT, 4) void scores_slice_kernel(const T *__restrict
 #pragma unroll
       for (int i = 1; i < NW; ++i) st += fpart[1][i], et += fpart[2][i];
     }
+    st = fmaf(st, -off * kLn2, st);
+    et = fmaf(et, -off * kLn2, et) - off * st;
     if (tid == 0) {
       if (slices == 1) write_scalars(out, t, r, V, base, st, et);
       else part[w] = Part{m, st, et, 0.f};
@@ -214,14 +230,19 @@ __global__ __launch_bounds__(256) void scores_join_kernel(const T *__restrict__ 
   for (int64_t t = blockIdx.x; t < rows; t += gridDim.x) {
     const Part *p = part + t * slices;
     float m = -INFINITY;
-    for (int i = tid; i < slices; i += 256) m = fmaxf(m, p[i].m);
+    for (int i = tid; i < slices; i += 256) m = largest_of(m, p[i].m);
     const int64_t total = (int64_t)slices * top;
     const uint64_t *ks = keys + t * total;
-    uint64_t mine = 0;
-    for (int64_t i = tid; i < total; i += 256) mine = max(mine, ks[i]);
+    constexpr int H = 8;  // keys of a thread that are loaded together, and held: all of them of 2048
+    uint64_t held[H], mine = 0;
+#pragma unroll
+    for (int i = 0; i < H; ++i) held[i] = i * 256 + tid < total ? ks[i * 256 + tid] : 0;
+#pragma unroll
+    for (int i = 0; i < H; ++i) mine = max(mine, held[i]);
+    for (int64_t i = H * 256 + tid; i < total; i += 256) mine = max(mine, ks[i]);
     best[tid] = mine;
     if (tid == 0) n_cand = 0;
-    m = block_all<256>(m, fpart[0], Larger());
+    m = block_all<256>(m, fpart[0], Largest());
     const float base = m == -INFINITY ? 0.f : m;
     float s = 0.f, e = 0.f;
     for (int i = tid; i < slices; i += 256) {
@@ -242,13 +263,16 @@ __global__ __launch_bounds__(256) void scores_join_kernel(const T *__restrict__ 
       }
       __syncthreads();
       const uint64_t b = bound;
-      if (mine >= b)
-        for (int64_t i = tid; i < total; i += 256) {
-          const uint64_t k = ks[i];
-          if (k == 0 || k < b) continue;
-          const int slot = atomicAdd(&n_cand, 1);
-          if (slot < kCandidates) cand[slot] = k;
-        }
+      auto keep = [&](uint64_t k) {
+        if (k == 0 || k < b) return;
+        const int slot = atomicAdd(&n_cand, 1);
+        if (slot < kCandidates) cand[slot] = k;
+      };
+      if (mine >= b) {
+#pragma unroll
+        for (int i = 0; i < H; ++i) keep(held[i]);
+        for (int64_t i = H * 256 + tid; i < total; i += 256) keep(ks[i]);
+      }
       __syncthreads();
       const int found = n_cand;
       const float log_s = logf(s);
@@ -285,21 +309,29 @@ __global__ __launch_bounds__(256) void scores_join_kernel(const T *__restrict__ 
   }
 }
 
-// Slices: as few as a workgroup's registers allow where there are rows enough to fill the card, else so many that there
-// are two workgroups a compute unit, of one vector a thread at least.
+// Slices: as few as a workgroup's registers allow where there are rows enough to fill the card, else so many that there are two
+// workgroups a compute unit, of one vector a thread at least; and of those counts and the next ones the one that leaves the
+// fewest places of vectors empty (200 rows of 50001 fp32 logits: 20.5 us in three slices with half of theirs empty).
 SlicePlan plan(const wcc_scores_desc &d) {
   const int ve = d.dtype == WCC_BF16 ? 8 : 4;
-  const int64_t vecs = (d.V + ve - 1) / ve;
-  int64_t want = (vecs + 512 * 16 - 1) / (512 * 16);
-  if (d.rows * want < 512) want = std::max(want, std::min((512 + d.rows - 1) / d.rows, vecs / 256));
-  want = std::max<int64_t>(want, 1);
-  const int64_t each = (vecs + want - 1) / want;
-  SlicePlan p;
-  p.length = (int)std::min<int64_t>(each * ve, d.V);
-  p.slices = (int)((d.V + p.length - 1) / p.length);
-  p.nt = each <= 64 * 4 ? 64 : each <= 256 * 16 ? 256 : 512;
-  p.nv = 1;
-  while ((int64_t)p.nt * p.nv < each) p.nv *= 2;
+  const int64_t vecs = ((int64_t)d.V + ve - 1) / ve;
+  int64_t least = (vecs + 512 * 16 - 1) / (512 * 16);
+  if (d.rows * least < 512) least = std::max(least, std::min((512 + d.rows - 1) / d.rows, vecs / 256));
+  least = std::max<int64_t>(least, 1);
+  SlicePlan p{};
+  int64_t cost = 0;
+  for (int64_t want = least; want <= (least == 1 ? 1 : 2 * least); ++want) {
+    const int64_t each = (vecs + want - 1) / want;
+    const int nt = want == 1 && each <= 64 * 4 ? 64 : each <= 256 * 16 ? 256 : 512;
+    int nv = 1;
+    while ((int64_t)nt * nv < each) nv *= 2;
+    const int64_t places = want * nt * nv;
+    if (p.nt != 0 && places >= cost) continue;
+    cost = places;
+    p.length = (int)std::min<int64_t>(each * ve, d.V);
+    p.slices = (int)((d.V + p.length - 1) / p.length);
+    p.nt = nt, p.nv = nv;
+  }
   return p;
 }
 
@@ -325,6 +357,7 @@ void launch(const wcc_scores_desc &d, const ScoresArgs &g, hipStream_t s) {
     case 6401: launch_slices<T, 64, 1>(d, g, p, o, part, keys, s); break;
     case 6402: launch_slices<T, 64, 2>(d, g, p, o, part, keys, s); break;
     case 6404: launch_slices<T, 64, 4>(d, g, p, o, part, keys, s); break;
+    case 25601: launch_slices<T, 256, 1>(d, g, p, o, part, keys, s); break;
     case 25602: launch_slices<T, 256, 2>(d, g, p, o, part, keys, s); break;
     case 25604: launch_slices<T, 256, 4>(d, g, p, o, part, keys, s); break;
     case 25608: launch_slices<T, 256, 8>(d, g, p, o, part, keys, s); break;
