@@ -74,7 +74,8 @@ typedef enum {
   WCC_ERR_WORKSPACE = 5,   /* no workspace attached, or it is too small / misaligned      */
   WCC_ERR_UNSUPPORTED = 6, /* valid request this build has no kernel for                  */
   WCC_ERR_HIP = 7,         /* the HIP runtime reported an error                           */
-  WCC_ERR_ALIGN = 8        /* a tensor pointer is not 16-byte aligned                     */
+  WCC_ERR_ALIGN = 8        /* a tensor pointer is not 16-byte aligned (the operators on rows
+                              of tokens at the end of this file: not to its elements)     */
 } wcc_status;
 
 typedef enum { WCC_F32 = 0, WCC_BF16 = 1, WCC_I8 = 2, WCC_I4 = 3 } wcc_dtype;

@@ -324,7 +324,7 @@ constexpr int64_t kGridMost = 1 << 20;
 // slicing would not help; else slices of up to 256 x 8 vectors, two workgroups a compute unit at least.
 SlicePlan plan(const wcc_distill_desc &d, bool backward) {
   const int ve = d.dtype == WCC_BF16 ? 8 : 4;
-  const int64_t vecs = (d.V + ve - 1) / ve;
+  const int64_t vecs = ((int64_t)d.V + ve - 1) / ve;
   SlicePlan p{1, d.V, 0, 1};
   if (!backward && vecs <= 1024 * 16 && (d.rows >= 128 || vecs <= 512)) {
     p.nt = vecs <= 64 * 4 ? 64 : vecs <= 256 * 16 ? 256 : vecs <= 512 * 16 ? 512 : 1024;
@@ -336,7 +336,7 @@ SlicePlan plan(const wcc_distill_desc &d, bool backward) {
   want = std::max<int64_t>(want, 1);
   const int64_t each = (vecs + want - 1) / want;
   p.length = (int)std::min<int64_t>(each * ve, d.V);
-  p.slices = (int)((d.V + p.length - 1) / p.length);
+  p.slices = (int)(((int64_t)d.V + p.length - 1) / p.length);
   p.nt = each <= 64 * 4 ? 64 : 256;
   while ((int64_t)p.nt * p.nv < each) p.nv *= 2;
   return p;

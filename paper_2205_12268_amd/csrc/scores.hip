@@ -329,7 +329,7 @@ SlicePlan plan(const wcc_scores_desc &d) {
     if (p.nt != 0 && places >= cost) continue;
     cost = places;
     p.length = (int)std::min<int64_t>(each * ve, d.V);
-    p.slices = (int)((d.V + p.length - 1) / p.length);
+    p.slices = (int)(((int64_t)d.V + p.length - 1) / p.length);
     p.nt = nt, p.nv = nv;
   }
   return p;
