@@ -126,6 +126,9 @@ __device__ __forceinline__ void load_k_pair(const T *p, int64_t sk, int left, bo
 
 // ---- fp32 values of k for one line, as operands ---------------------------------------------------------------
 // bf16 operands carry 8 bits each: P of them take P * 8 bits of the values, the rest of each going to the next.
+__device__ __forceinline__ float left_of(float v, uint32_t part) {  // (nothing of an infinity, or it would be NaN)
+  return (part & 0x7f80) == 0x7f80 ? 0.f : v - __uint_as_float(part << 16);
+}
 template <class T, int P>
 __device__ __forceinline__ void split_to(const float *v, u32x4 (&f)[P]) {
   if constexpr (sizeof(T) == 4) {
@@ -140,8 +143,8 @@ __device__ __forceinline__ void split_to(const float *v, u32x4 (&f)[P]) {
       for (int j = 0; j < 4; ++j) {
         const uint32_t lo = narrow<bf16_t>(rest[2 * j]), hi = narrow<bf16_t>(rest[2 * j + 1]);
         f[p][j] = lo | hi << 16;
-        rest[2 * j] -= __uint_as_float(lo << 16);
-        rest[2 * j + 1] -= __uint_as_float(hi << 16);
+        rest[2 * j] = left_of(rest[2 * j], lo);
+        rest[2 * j + 1] = left_of(rest[2 * j + 1], hi);
       }
     }
   }
@@ -168,34 +171,43 @@ struct Lines {
     }
     return v;
   }
-  // eight lines from j (a multiple of 8) on
-  __device__ __forceinline__ void eight(int64_t t, int j, float (&v)[8]) const {
-    const float4 *q = reinterpret_cast<const float4 *>(p + t * ld + j);
-    float4 a = q[0], b = q[1];
-    auto add = [](const float4 &u, const float4 &w) { return make_float4(u.x + w.x, u.y + w.y, u.z + w.z, u.w + w.w); };
-    const int64_t step = stride >> 2;
-    int s = 1;
-    for (; s + 1 < splits; s += 2) {  // (the order of the splits; two at a time so that loads do not wait for each other)
-      const float4 c0 = q[s * step], d0 = q[s * step + 1], c1 = q[(s + 1) * step], d1 = q[(s + 1) * step + 1];
-      a = add(add(a, c0), c1), b = add(add(b, d0), d1);
-    }
-    if (s < splits) a = add(a, q[s * step]), b = add(b, q[s * step + 1]);
-    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-  }
 };
 
-// VE rank lines of one column of the thin operand from line j on, `left` > 0 of them there.  What is past them repeats the last one
-// and meets zeros of h.
+// VE rank lines of one column of the thin operand from line j on.  No branch, so that loads do not wait for each other: what is not
+// there is loaded from where something is, and cut off where it is used.
 template <class T>
-__device__ __forceinline__ u32x4 thin_k(const Thin<T> &m, int a, int o, int j, int left) {
+__device__ __forceinline__ u32x4 thin_k(const Thin<T> &m, int a, int o, int j, int lines) {
   constexpr int VE = VecOf<T>::N;
-  const T *p = m.p + a * m.major + (int64_t)o * m.sc + (int64_t)j * m.sj;
-  if (m.sj == 1 && left >= VE) return *reinterpret_cast<const u32x4_any *>(p);
+  const T *p = m.p + a * m.major + (int64_t)o * m.sc;
+  if (m.sj == 1 && m.sc % VE == 0) return *reinterpret_cast<const u32x4_any *>(p + min(j, m.sc - VE));  // (sc: the rank of all)
   uint32_t e[VE];
 #pragma unroll
-  for (int i = 0; i < VE; ++i) e[i] = bits_of(p[(int64_t)min(i, left - 1) * m.sj]);
+  for (int i = 0; i < VE; ++i) e[i] = bits_of(p[(int64_t)max(min(j + i, lines - 1), 0) * m.sj]);
   if constexpr (sizeof(T) == 4) return u32x4{e[0], e[1], e[2], e[3]};
   else return u32x4{e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16};
+}
+// those past `lines` 0
+template <class T>
+__device__ __forceinline__ u32x4 cut_k(u32x4 v, int j, int lines) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) v[i] = j + i < lines ? v[i] : 0u;
+    else v[i] = j + 2 * i + 1 < lines ? v[i] : j + 2 * i < lines ? v[i] & 0xffffu : 0u;
+  }
+  return v;
+}
+
+// An order of workgroups that leaves each of the eight XCDs (they go to them in turn) a run of neighbours, and of tiles within it in
+// blocks of up to eight row tiles, so that what neighbours share is in their L2.
+__device__ __forceinline__ int64_t in_runs(int64_t b, int64_t n) {
+  const int64_t each = n / 8;
+  return b < each * 8 ? b % 8 * each + b / 8 : b;
+}
+__device__ __forceinline__ void tile_of(int64_t b, int64_t tiles_t, int tiles_o, int64_t &tt, int &to) {
+  const int64_t band = (int64_t)8 * tiles_o, first = b / band * 8, in = b % band;
+  const int64_t high = min(tiles_t - first, (int64_t)8);
+  tt = first + in % high;
+  to = (int)(in / high);
 }
 
 // One projection: y[t, o] = sum_k x[t, k] w(o, k) + sum_j m(a, j, o) h[t, j], w(o, k) at o * wo + k * wk (one of them is 1).
@@ -213,74 +225,158 @@ struct Project {
   int64_t ldy;
 };
 
-// acc += the rank lines' product for the 32 rows from t0 on and 32 E outputs, o of each lane.  ROWS: rows are the first operand (the
-// lines of a result), outputs the second; else the other way round.  The sums of each adapter among the rows apart: a row takes
-// its own, whatever (infinities, NaN) other adapters hold.  A row's lines meet no adapter but its own, so they are loaded once; the
-// next adapter's operands are on their way while one's are multiplied.
-template <class T, int E, bool ROWS>
-__device__ __forceinline__ void add_thin(const Low &low, const Thin<T> &m, const Lines &h, int64_t rows, int outs, int64_t t0,
-                                         const int (&o)[E], f32x16 (&acc)[E]) {
-  constexpr int VE = VecOf<T>::N, KS = StepOf<T>::K, P = PartsOf<T>::Out, J = 2;  // J steps of lines are held
-  const int ln = threadIdx.x & 31, half = (threadIdx.x >> 5) & 1;
-  const int64_t t = min(t0 + ln, rows - 1);
-  const int id = t0 + ln < rows ? low.of(t) : -1;
-  const int mine = id >= 0 ? low.lines(id) : 0;
-  auto own_lines = [&](int j0, u32x4 (&hf)[P]) {
-    const int j = j0 + half * VE;
-    float hv[8] = {};
-    if (j < mine) h.eight(t, j & ~7, hv);
-    if constexpr (VE == 4) {
+// The lines of N rows from t0 on to LDS by a workgroup, as operands: [N][P][ld], bf16 in P = 2 parts; room(row): where a row's are.
+// Those past an adapter's rank, and of rows without an adapter, 0.
+template <class T, int N, class F>
+__device__ __forceinline__ void gather_lines(const Low &low, const Lines &h, F room, int64_t t0, int64_t rows) {
+  const int pieces = h.ld / 4;
+  const int64_t step = h.stride >> 2;
+#pragma unroll 2
+  for (int i = threadIdx.x; i < N * pieces; i += 256) {
+    const int row = i / pieces, c = i - row * pieces;
+    const int64_t t = min(t0 + row, rows - 1);
+    const int id = low.of(t);
+    const float4 *q = reinterpret_cast<const float4 *>(h.p + t * h.ld) + c;
+    float4 v = q[0];
+    for (int s = 1; s < h.splits; s += 7) {
+      float4 w[7];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) hv[i] = half ? hv[4 + i] : hv[i];
+      for (int u = 0; u < 7; ++u) w[u] = q[min(s + u, h.splits - 1) * step];
+#pragma unroll
+      for (int u = 0; u < 7; ++u)
+        if (s + u < h.splits) v = make_float4(v.x + w[u].x, v.y + w[u].y, v.z + w[u].z, v.w + w[u].w);
     }
-    split_to<T, P>(hv, hf);
-  };
-  auto operands = [&](int a, int lines, int j0, u32x4 (&mf)[E]) {
-    const int j = j0 + half * VE;
+    const int left = (id >= 0 ? low.lines(id) : 0) - c * 4;
+    v = make_float4(left > 0 ? v.x : 0.f, left > 1 ? v.y : 0.f, left > 2 ? v.z : 0.f, left > 3 ? v.w : 0.f);
+    if constexpr (sizeof(T) == 4) {
+      *reinterpret_cast<float4 *>(room(row) + c * 4) = v;
+    } else {
+      const float e[8] = {v.x, v.y, v.z, v.w};
+      u32x4 f[2];
+      split_to<T, 2>(e, f);
 #pragma unroll
-    for (int e = 0; e < E; ++e) mf[e] = j < lines ? thin_k(m, a, min(o[e], outs - 1), j, lines - j) : u32x4{0, 0, 0, 0};
-  };
-  auto product = [&](const u32x4 (&hf)[P], const u32x4 (&mf)[E], f32x16 (&d)[E]) {
-#pragma unroll
-    for (int e = 0; e < E; ++e)
-#pragma unroll
-      for (int q = P - 1; q >= 0; --q) d[e] = ROWS ? mma<T>(hf[q], mf[e], d[e]) : mma<T>(mf[e], hf[q], d[e]);
-  };
-  uint32_t rest = (uint32_t)__ballot(id >= 0);
-  u32x4 hf[J][P], mf[J][E];
-#pragma unroll
-  for (int s = 0; s < J; ++s) {
-    own_lines(s * KS, hf[s]);
-#pragma unroll
-    for (int e = 0; e < E; ++e) mf[s][e] = u32x4{0, 0, 0, 0};
+      for (int part = 0; part < 2; ++part) *reinterpret_cast<uint2 *>(room(row) + part * h.ld + c * 4) = make_uint2(f[part][0], f[part][1]);
+    }
   }
-  int a = -2, lines = 0;  // (none yet: the first round only loads)
-  while (a != -1) {
-    const int next = rest != 0 ? __builtin_amdgcn_readlane(id, __builtin_ctz(rest)) : -1;
-    const int next_lines = next >= 0 ? low.lines(next) : 0;
-    u32x4 nf[J][E];
+}
+
+// acc += the rank lines' product for 32 R rows from t0 on and 32 E outputs, o of each lane; lines_of(r): the lines of the r-th 32 rows
+// in LDS (gather_lines).  ROWS: rows are the first operand (the lines of a result), outputs the second; else the other way round.
+// Of each adapter among the rows J steps of lines at a time, the next ones' operands on their way meanwhile; of the distinct adapters
+// every turn-th from the first-th on.  The lines of rows with other adapters are replaced by zeros, except where an adapter holds
+// infinities or NaN (a product of its operands with zeros tells): its sums are made apart then, and rows take none but their own.
+// (With all sums apart, and the lines of each 32 rows by themselves: 1172 rows, 2816 -> 4224, 29 adapters in mixed order, 162 us
+// instead of 122; 8192 rows, 4096 -> 4096, 318 instead of 305.)
+template <class T, int E, int R, bool ROWS, int J, class F>
+__device__ __forceinline__ void add_thin(const Low &low, const Thin<T> &m, int ld, F lines_of, int64_t rows, int outs, int64_t t0,
+                                         const int (&o)[E], f32x16 (&acc)[E][R], int first = 0, int turn = 1) {
+  constexpr int VE = VecOf<T>::N, KS = StepOf<T>::K, P = PartsOf<T>::Out;
+  const int ln = threadIdx.x & 31, half = (threadIdx.x >> 5) & 1;
+  int id[R];
+  uint32_t rest[R];
 #pragma unroll
-    for (int s = 0; s < J; ++s) operands(next, next_lines, s * KS, nf[s]);
-    f32x16 d[E] = {};
+  for (int r = 0; r < R; ++r) id[r] = low.of(min(t0 + r * 32 + ln, rows - 1));
 #pragma unroll
-    for (int s = 0; s < J; ++s) product(hf[s], mf[s], d);
-    for (int j0 = J * KS; j0 < lines; j0 += KS) {
-      u32x4 hj[P], mj[E];
-      own_lines(j0, hj);
-      operands(a, lines, j0, mj);
-      product(hj, mj, d);
+  for (int r = 0; r < R; ++r) {
+    if (t0 + r * 32 + ln >= rows) id[r] = -1;
+    rest[r] = (uint32_t)__ballot(id[r] >= 0);
+  }
+  auto front = [&] {
+    int a = -1;
+#pragma unroll
+    for (int r = R - 1; r >= 0; --r)
+      if (rest[r] != 0) a = __builtin_amdgcn_readlane(id[r], __builtin_ctz(rest[r]));
+    return a;
+  };
+  auto pass = [&](int n) {
+    for (; n > 0; --n) {
+      const int a = front();
+#pragma unroll
+      for (int r = 0; r < R; ++r) rest[r] &= ~(uint32_t)__ballot(id[r] == a);
     }
-    const uint32_t same = (uint32_t)__ballot(id == a);
+  };
+  const u32x4 zeros = {0, 0, 0, 0};
+  // (one e at a time, all of a row's steps)
+  auto product = [&](const T *h, int j, const u32x4 &mf, bool mine, f32x16 c) {
+    u32x4 hf[P];
 #pragma unroll
-    for (int e = 0; e < E; ++e)
+    for (int q = 0; q < P; ++q) {
+      const u32x4 v = *reinterpret_cast<const u32x4 *>(h + (ln * P + q) * ld + min(j, ld - VE));
+      hf[q] = mine && j < ld ? v : zeros;
+    }
 #pragma unroll
-      for (int i = 0; i < 16; ++i) acc[e][i] += (ROWS ? (same >> result_line(i, half) & 1) != 0 : id == a) ? d[e][i] : 0.f;
-    a = next, lines = next_lines;
-    rest &= ~(uint32_t)__ballot(id == a);
+    for (int q = P - 1; q >= 0; --q) c = ROWS ? mma<T>(hf[q], mf, c) : mma<T>(mf, hf[q], c);
+    return c;
+  };
+  u32x4 mf[J][E];
+#pragma unroll
+  for (int s = 0; s < J; ++s)
+#pragma unroll
+    for (int e = 0; e < E; ++e) mf[s][e] = zeros;
+  pass(first);
+  int a = -2, lines = 0, j0 = 0;  // (none yet: the first round only loads)
+  bool apart = false;
+  while (a != -1) {
+    int next = a, next_lines = lines, next_j = j0 + J * KS;
+    if (next_j >= lines) {
+      next = front(), next_lines = next >= 0 ? low.lines(next) : 0, next_j = 0;
+      pass(turn);
+    }
+    u32x4 nf[J][E];
 #pragma unroll
     for (int s = 0; s < J; ++s)
 #pragma unroll
-      for (int e = 0; e < E; ++e) mf[s][e] = nf[s][e];
+      for (int e = 0; e < E; ++e)
+        nf[s][e] = s == 0 || s * KS < low.rank ? thin_k(m, max(next, 0), min(o[e], outs - 1), next_j + s * KS + half * VE, next_lines) : zeros;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const bool mine = id[r] == a;
+      const T *h = lines_of(r);
+#pragma unroll
+      for (int s = 0; s < J; ++s)
+        if (s == 0 || s * KS < low.rank)
+#pragma unroll
+          for (int e = 0; e < E; ++e) acc[e][r] = product(h, j0 + s * KS + half * VE, mf[s][e], mine, acc[e][r]);
+    }
+    if (apart) {
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const bool mine = id[r] == a;
+        const uint32_t same = (uint32_t)__ballot(mine);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          f32x16 d = {};
+#pragma unroll 1
+          for (int s = 0; s < J; ++s) {
+            const int j = j0 + s * KS + half * VE;
+            d = product(lines_of(r), j, cut_k<T>(thin_k(m, a, min(o[e], outs - 1), j, lines), j, lines), true, d);
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[e][r][i] += (ROWS ? (same >> result_line(i, half) & 1) != 0 : mine) ? d[i] : 0.f;
+        }
+      }
+    }
+    a = next, lines = next_lines, j0 = next_j;
+    f32x16 none = {};
+#pragma unroll
+    for (int s = 0; s < J; ++s)
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        mf[s][e] = cut_k<T>(nf[s][e], j0 + s * KS + half * VE, lines);
+        if constexpr (sizeof(T) == 4) {  // (four instructions of the vector unit, not four of the matrix cores)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) none[0] = fmaf(__uint_as_float(mf[s][e][i]), 0.f, none[0]);
+        } else if (s == 0 || s * KS < low.rank) {
+          none = mma<T>(zeros, mf[s][e], none);
+        }
+      }
+    apart = __ballot(none[0] != 0.f) != 0;  // (NaN)
+    if (apart) {
+#pragma unroll
+      for (int s = 0; s < J; ++s)
+#pragma unroll
+        for (int e = 0; e < E; ++e) mf[s][e] = zeros;
+    }
   }
 }
 
@@ -298,7 +394,7 @@ struct ThinJob {
   Thin<T> m;
   Lines out;
   int chunk, groups;
-  bool by_range, through_lds;  // through_lds: by_range, bf16, and all of x and m in whole chunks of 16 bytes
+  bool by_range;
   int64_t units, blocks;  // blocks of four waves; units: of waves, not by_range
 };
 
@@ -307,13 +403,10 @@ struct ThinLds {
   int4 key[kRange / 4];
   int row[kRange], of[kRange], head[kRange];
 };
-// two stages of x and of m, 4 KiB a wave each
-struct ThinStages {
-  unsigned char *x0, *m0, *x1, *m1;
-};
+constexpr int kThinRoom = 8192;  // bytes of LDS of a wave: 32 rows and 32 lines by 128 bytes of k
 
 // the sums over k0 .. k1 of 32 rows (of the lane: xr, at its half's chunk) with 32 lines (mr); CONT: sc = 1.  Eight steps' loads go
-// out together: with four, and the next four on their way meanwhile, 128 rows x 512 k a workgroup took 50 us where these take 38.
+// out together.
 template <class T, bool CONT>
 __device__ __forceinline__ f32x16 thin_sums(const T *xr, const T *mr, int sc, int k0, int k1, int half) {
   constexpr int VE = VecOf<T>::N, KS = StepOf<T>::K, U = CONT ? 8 : 4;
@@ -371,69 +464,83 @@ __device__ __forceinline__ void thin_unit(const ThinJob<T> &g, const Low &low, i
   }
 }
 
-// The sums over k0 .. k1 of the 32 rows at xr (a lane's for each load: row 8 i + lane / 8) with 32 lines from j0 on, in stages of 64 k
-// through the wave's own LDS.  Straight into registers, 32 rows x 32 bytes at a time, four loads in a row ask for the same lines
-// of memory, and wait for each other's: 8192 rows x 4096 k took 38 us.
-__device__ __forceinline__ f32x16 thin_stages(const ThinJob<bf16_t> &g, int a, int lines, int j0, const bf16_t *const (&xr)[4], int k0,
-                                              int k1, const ThinStages &st) {
-  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), ln = lane & 31, half = lane >> 5;
-  const bool cont = g.m.sc == 1;
-  const bf16_t *mr = g.m.p + a * g.m.major;
-  auto load = [&](int k, unsigned char *xs, unsigned char *ms) {
+// The sums over k0 .. k1 of the 32 rows at xr (a lane's for each load: row 8 i + lane / 8) with 32 lines from j0 on, in stages of 128
+// bytes of k through the wave's own LDS, the next stage's loads in flight meanwhile.  A load asks for whole lines of 128 bytes of
+// eight rows; straight into operands, 32 bytes of 32 rows, 190 rows, 5232 -> 4072, rank 64 took 54 us (with the product) instead
+// of 42.  Two stages ahead: no gain (45 us).
+template <class T>
+__device__ __forceinline__ f32x16 thin_stages(const ThinJob<T> &g, int a, int lines, int j0, const T *const (&xr)[4], int k0, int k1,
+                                              unsigned char *own) {
+  constexpr int VE = VecOf<T>::N, KB = kLine / (int)sizeof(T), PerK = 32 / VE;  // PerK: lanes of a line of k
+  const int lane = thread_here() & 63, ln = lane & 31, half = lane >> 5;
+  const int chunk = lane % kChunks, line = lane / kChunks;
+  const bool cont = g.m.sc == 1, even = g.m.sc % VE == 0;  // even: (not cont) 16 bytes of lines from any of them on are there
+  const T *mr = g.m.p + a * g.m.major;
+  const T *ml[4];  // the lane's place of the loads of m
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int row = i * 8 + lane / kChunks, c = ((lane % kChunks) ^ chunk_key(row)) * 8;
-      to_lds(k + c < k1 ? (const void *)(xr[i] + k + c) : &kZeros, xs + wv * 4096 + i * 1024);
+  for (int i = 0; i < 4; ++i)
+    ml[i] = cont ? mr + (int64_t)min(j0 + i * 8 + line, lines - 1) * g.m.sj + chunk * VE
+                 : mr + (int64_t)(i * (64 / PerK) + lane / PerK) * g.m.sc + (even ? min(j0 + lane % PerK * VE, g.m.sc - VE) : j0 + lane % PerK * VE);
+  u32x4 st[8];
+  auto load = [&](int k) {
+    if (k + KB <= k1 && (cont || even)) {  // (nothing to check: no branch between the loads; lines past the adapter's are not used)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        st[i] = *reinterpret_cast<const u32x4_any *>(xr[i] + k + chunk * VE);
+        st[4 + i] = *reinterpret_cast<const u32x4_any *>(ml[i] + (int64_t)k * g.m.sc);
+      }
+      return;
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const void *at = &kZeros;
-      if (cont) {
-        const int row = i * 8 + lane / kChunks, c = ((lane % kChunks) ^ chunk_key(row)) * 8;
-        if (k + c < k1) at = mr + (int64_t)min(j0 + row, lines - 1) * g.m.sj + k + c;
-      } else {  // lines of k of 32 neighbours
-        const int kk = k + i * 16 + lane / 4, j = j0 + lane % 4 * 8;
-        if (kk < k1 && j < lines) at = mr + (int64_t)kk * g.m.sc + j;
-      }
-      to_lds(at, ms + wv * 4096 + i * 1024);
+      const int left = k1 - k - chunk * VE;
+      st[i] = load_k(xr[i] + k + chunk * VE, left);
+      if (cont) st[4 + i] = load_k(ml[i] + k, left);
+      else st[4 + i] = load_k(ml[i] + (int64_t)k * g.m.sc, k + i * (64 / PerK) + lane / PerK < k1 ? even ? VE : lines - j0 - lane % PerK * VE : 0);
     }
   };
   f32x16 acc = {};
-  auto add = [&](const unsigned char *xs, const unsigned char *ms) {
-    xs += wv * 4096, ms += wv * 4096;
+  load(k0);
+  for (int k = k0; k < k1; k += KB) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = i * 8 + line, at = row * kLine + ((chunk ^ chunk_key(row)) << 4);
+      *reinterpret_cast<u32x4 *>(own + at) = st[i];
+      *reinterpret_cast<u32x4 *>(own + 4096 + (cont ? at : i * 1024 + lane * 16)) = st[4 + i];
+    }
+    if (k + KB < k1) load(k + KB);
+    // (LDS serves a wave in order; the compiler shall not turn it round)
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    const unsigned char *ms = own + 4096;
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-      const u32x4 xf = chunk_of(xs, ln, s * 2 + half);
+      const u32x4 xf = chunk_of(own, ln, s * 2 + half);
       u32x4 mf;
       if (cont) {
         mf = chunk_of(ms, ln, s * 2 + half);
-      } else {
+      } else if constexpr (sizeof(T) == 2) {
         const unsigned char *at = ms + (s * 16 + half * 8 + ((lane & 15) >> 2)) * 64 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
         const uint2 u = turned(at), v = turned(at + 4 * 64);
         mf = u32x4{u.x, u.y, v.x, v.y};
+      } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) mf[q] = *reinterpret_cast<const uint32_t *>(ms + (s * 8 + half * 4 + q) * 128 + ln * 4);
       }
-      acc = mma<bf16_t>(xf, mf, acc);
+      acc = mma<T>(xf, mf, acc);
     }
-  };
-  load(k0, st.x0, st.m0);
-  for (int k = k0; k < k1; k += 2 * kK) {  // (stages past the end are zeros)
-    load(k + kK, st.x1, st.m1);
-    asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
-    add(st.x0, st.m0);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    load(k + 2 * kK, st.x0, st.m0);
-    asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
-    add(st.x1, st.m1);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
   }
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   return acc;
 }
 
 template <class T>
-__device__ __forceinline__ void thin_range(const ThinJob<T> &g, const Low &low, int64_t block, ThinLds &lds, const ThinStages &st) {
-  constexpr int VE = VecOf<T>::N, none = 0x7fffffff;
-  const int tid = threadIdx.x, lane = tid & 63, ln = lane & 31, half = lane >> 5;
+__device__ __forceinline__ void thin_range(const ThinJob<T> &g, const Low &low, int64_t block, ThinLds &lds, unsigned char *own) {
+  constexpr int none = 0x7fffffff;
+  const int tid = thread_here(), lane = tid & 63, ln = lane & 31, half = lane >> 5;
   const int split = (int)(block % g.out.splits), share = (int)(block / g.out.splits % g.groups);
   const int64_t base = block / g.out.splits / g.groups * kRange;
   if (tid < kRange) {
@@ -469,22 +576,10 @@ __device__ __forceinline__ void thin_range(const ThinJob<T> &g, const Low &low, 
     const float f = low.factor(a);
     float *out = g.out.p + split * g.out.stride + base * g.out.ld;
     for (int j0 = 0; j0 < lines; j0 += 32) {
-      f32x16 acc;
-      bool done = false;
-      if constexpr (sizeof(T) == 2) {
-        if (g.through_lds) {
-          const bf16_t *xr[4];
+      const T *xr[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) xr[i] = g.x + (base + lds.row[pos + min(i * 8 + lane / kChunks, n - 1)]) * g.ldx;
-          acc = thin_stages(g, a, lines, j0, xr, k0, k1, st);
-          done = true;
-        }
-      }
-      if (!done) {
-        const T *xr = g.x + (base + lds.row[pos + min(ln, n - 1)]) * g.ldx + half * VE;
-        const T *mr = g.m.p + a * g.m.major + (int64_t)min(j0 + ln, lines - 1) * g.m.sj + (int64_t)(half * VE) * g.m.sc;
-        acc = g.m.sc == 1 ? thin_sums<T, true>(xr, mr, 1, k0, k1, half) : thin_sums<T, false>(xr, mr, g.m.sc, k0, k1, half);
-      }
+      for (int i = 0; i < 4; ++i) xr[i] = g.x + (base + lds.row[pos + min(i * 8 + lane / kChunks, n - 1)]) * g.ldx;
+      const f32x16 acc = thin_stages<T>(g, a, lines, j0, xr, k0, k1, own);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int q = result_line(i, half);
@@ -494,16 +589,21 @@ __device__ __forceinline__ void thin_range(const ThinJob<T> &g, const Low &low, 
   }
 }
 
-// a workgroup of four waves
+// a workgroup of four waves; `own`: the wave's LDS, of kThinRoom bytes (by_range)
 template <class T>
-__device__ __forceinline__ void thin_block(const ThinJob<T> &g, const Low &low, int64_t block, ThinLds &lds, const ThinStages &st) {
-  if (g.by_range) return thin_range<T>(g, low, block, lds, st);
+__device__ __forceinline__ void thin_block(const ThinJob<T> &g, const Low &low, int64_t block, ThinLds &lds, unsigned char *own) {
+  if (g.by_range) return thin_range<T>(g, low, block, lds, own);
   const int64_t unit = block * 4 + (threadIdx.x >> 6);
   if (unit < g.units) thin_unit<T>(g, low, unit);
 }
 
+// adapter_tile.hip: anything.  Ranges of k; with more than one, their sums go to part [splits][rows][outs], and the rank lines of one
+// or two jobs are made beside.
+constexpr int kPlaces = 512;  // workgroups of tiles that a card of 256 compute units holds at once
+int64_t tiles_of(int64_t rows, int outs);
+int tile_splits(int64_t rows, int width, int outs, int size);
 template <class T>
-void launch_tiles(const Project<T> &p, hipStream_t s);  // adapter_tile.hip: anything
+void launch_tiles(const Project<T> &p, int splits, float *part, const ThinJob<T> &thin, const ThinJob<T> &other, hipStream_t s);
 // adapter_gemm.hip: rows that 16-byte loads can take
 bool gemm_takes(const Project<bf16_t> &p);
 int gemm_splits(int64_t rows, int width, int outs);  // ranges of k; 1: whole tiles

@@ -19,12 +19,11 @@ namespace {
 template <class T>
 __global__ __launch_bounds__(256, 2) void adapter_lines_kernel(ThinJob<T> g1, ThinJob<T> g2, Low low) {
   __shared__ ThinLds lds;
-  constexpr int room = sizeof(T) == 2 ? 16384 : 16;
-  __shared__ __align__(1024) unsigned char x0[room], m0[room], x1[room], m1[room];
-  const ThinStages st{x0, m0, x1, m1};
+  __shared__ __align__(1024) unsigned char room[4][kThinRoom];
+  unsigned char *own = room[threadIdx.x >> 6];
   for (int64_t b = blockIdx.x; b < g1.blocks + g2.blocks; b += gridDim.x) {
-    if (b < g1.blocks) thin_block<T>(g1, low, b, lds, st);
-    else thin_block<T>(g2, low, b - g1.blocks, lds, st);
+    const bool second = b >= g1.blocks;
+    thin_block<T>(second ? g2 : g1, low, second ? b - g1.blocks : b, lds, own);
     __syncthreads();
   }
 }
@@ -124,9 +123,9 @@ __global__ __launch_bounds__(256, 2) void adapter_products_kernel(StreamJob<T> g
   const int64_t block = blockIdx.x;
   if (block < thin.blocks + thin2.blocks) {
     __shared__ ThinLds lds;
-    const ThinStages st{};
-    if (block < thin.blocks) thin_block<T>(thin, low, block, lds, st);
-    else thin_block<T>(thin2, low, block - thin.blocks, lds, st);
+    unsigned char *own = nullptr;  // (few rows: not by ranges)
+    if (block < thin.blocks) thin_block<T>(thin, low, block, lds, own);
+    else thin_block<T>(thin2, low, block - thin.blocks, lds, own);
     return;
   }
   stream_block<T, RT, NN>(g, block - thin.blocks - thin2.blocks, red);
@@ -167,7 +166,7 @@ __global__ __launch_bounds__(256) void adapter_finish_row_kernel(FinishJob<T> g,
     const int a = low.of(t), lines = a >= 0 ? low.lines(a) : 0;
     u32x4 mf[Q];  // the first 32 lines' loads go out together with the others
 #pragma unroll
-    for (int q = 0; q < Q; ++q) mf[q] = q * VE < lines ? thin_k(g.m, a, oc, q * VE, lines - q * VE) : u32x4{};
+    for (int q = 0; q < Q; ++q) mf[q] = thin_k(g.m, max(a, 0), oc, q * VE, lines);
     float v = sum_parts(g.part + t * g.outs + oc, g.splits, g.rows * g.outs);
     if ((int)threadIdx.x < lines) hs[threadIdx.x] = g.h.at(t * g.h.ld + threadIdx.x);
     __syncthreads();
@@ -178,7 +177,7 @@ __global__ __launch_bounds__(256) void adapter_finish_row_kernel(FinishJob<T> g,
       for (int i = 0; i < VE; ++i)
         if (q * VE + i < lines) low_v = fmaf(elem<T>(mf[q], i), hs[q * VE + i], low_v);
     for (int j = 32; j < lines; j += VE) {
-      const u32x4 f = thin_k(g.m, a, oc, j, lines - j);
+      const u32x4 f = thin_k(g.m, a, oc, j, lines);
 #pragma unroll
       for (int i = 0; i < VE; ++i)
         if (j + i < lines) low_v = fmaf(elem<T>(f, i), hs[j + i], low_v);
@@ -188,19 +187,23 @@ __global__ __launch_bounds__(256) void adapter_finish_row_kernel(FinishJob<T> g,
   }
 }
 
-// More rows: 32 rows x 128 outputs a workgroup, the parts added up through LDS, 32 outputs a wave then.
+// More rows: 32 rows x 64 outputs a workgroup.  Each wave has all of them and, of the distinct adapters among the rows, every
+// fourth: the thin products of rows in any order are as many trips to memory one after the other as there are adapters.  (One
+// wave for all adapters of 32 outputs: 190 rows of mixed adapters, rank 64, 4072 outputs took 28 us.)
 template <class T>
 __global__ __launch_bounds__(256) void adapter_finish_tile_kernel(FinishJob<T> g, Low low) {
-  constexpr int LD = 132;
-  __shared__ __align__(16) float sums[32][LD];
-  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, ln = lane & 31, half = lane >> 5;
+  constexpr int LD = 68;
+  __shared__ __align__(16) float sums[4][32][LD];
+  __shared__ __align__(16) T h[32 * PartsOf<T>::Out * WCC_MAX_RANK];
+  const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), ln = lane & 31, half = lane >> 5;
   for (int64_t b = blockIdx.x; b < g.blocks; b += gridDim.x) {
-    const int o0 = (int)(b % g.tiles_o) * 128, oq = o0 + (tid & 31) * 4;
+    const int o0 = (int)(b % g.tiles_o) * 64, r = tid >> 4, c = (tid & 15) * 4, oq = o0 + c;
     const int64_t t0 = b / g.tiles_o * 32, stride = g.rows * g.outs;
-    f32x4_any v[4] = {};
+    f32x4_any v[2] = {};
+    if (low.of_row) gather_lines<T, 32>(low, g.h, [&](int row) { return h + row * PartsOf<T>::Out * g.h.ld; }, t0, g.rows);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float *p = g.part + min(t0 + (tid >> 5) + 8 * i, g.rows - 1) * g.outs + min(oq, g.outs - 1);
+    for (int i = 0; i < 2; ++i) {
+      const float *p = g.part + min(t0 + r + 16 * i, g.rows - 1) * g.outs + min(oq, g.outs - 1);
       if (oq + 4 <= g.outs) {
         int s = 0;
         for (; s + 4 <= g.splits; s += 4) {
@@ -216,18 +219,31 @@ __global__ __launch_bounds__(256) void adapter_finish_tile_kernel(FinishJob<T> g
           if (oq + q < g.outs) v[i][q] = sum_parts(p + q, g.splits, stride);
       }
     }
+    if (low.of_row) {
+      const int o[2] = {o0 + ln, o0 + 32 + ln};
+      f32x16 acc[2][1] = {};
+      __syncthreads();
+      add_thin<T, 2, 1, true, 32 / StepOf<T>::K>(low, g.m, g.h.ld, [&](int) { return h; }, g.rows, g.outs, t0, o, acc, wv, 4);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) *reinterpret_cast<float4 *>(&sums[(tid >> 5) + 8 * i][(tid & 31) * 4]) = make_float4(v[i][0], v[i][1], v[i][2], v[i][3]);
-    __syncthreads();
-    const int o[1] = {o0 + wv * 32 + ln};
-    f32x16 acc[1];
+      for (int e = 0; e < 2; ++e)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) acc[0][i] = sums[result_line(i, half)][wv * 32 + ln];
-    if (low.of_row) add_thin<T, 1, true>(low, g.m, g.h, g.rows, g.outs, t0, o, acc);
+        for (int i = 0; i < 16; ++i) sums[wv][result_line(i, half)][e * 32 + ln] = acc[e][0][i];
+      __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int64_t t = t0 + result_line(i, half);
-      if (t < g.rows && o[0] < g.outs) g.y[t * g.ldy + o[0]] = narrow<T>(acc[0][i]);
+      for (int i = 0; i < 2; ++i) {
+        f32x4_any w[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) w[u] = *reinterpret_cast<const f32x4_any *>(&sums[u][r + 16 * i][c]);
+        v[i] += (w[0] + w[1]) + (w[2] + w[3]);  // (a row's is one of them, the others' are 0)
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int64_t t = t0 + r + 16 * i;
+      if (t >= g.rows) continue;
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (oq + q < g.outs) g.y[t * g.ldy + oq + q] = narrow<T>(v[i][q]);
     }
     __syncthreads();
   }
@@ -513,40 +529,39 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int step4(const wcc_adapter_desc &d) { return d.dtype == WCC_BF16 ? 64 : 32; }
 int lines_ld(const wcc_adapter_desc &d) { return (d.rank + 7) / 8 * 8; }
 
-// How y = x W^T is made.  Few rows, and whatever 16-byte loads cannot take up to a thousand tiles: streamed; else LDS tiles
-// (bf16: adapter_gemm.hip), in ranges of k where the tiles alone would leave compute units without work.
+// How y = x W^T is made: bf16 that 16-byte loads can take by adapter_gemm.hip, whatever else by the stream (up to 64 rows) or
+// adapter_tile.hip; in ranges of k where the tiles alone would leave compute units without work.
 struct Plan {
   enum { kStream, kTiles, kGemm, kGemmSplit } route;
   int rt, splits, chunk, tiles_o;
   int64_t blocks;  // of the stream
-  bool parts() const { return route == kStream || route == kGemmSplit; }
+  bool parts() const { return route == kStream || route == kGemmSplit || splits > 1; }
 };
 Plan plan_of(const wcc_adapter_desc &d, int width, int outs, bool aligned) {
   Plan p{};
   const int64_t rows = std::max<int64_t>(d.rows, 1);
-  p.rt = rows <= 32 ? 1 : 2;
-  p.tiles_o = (int)ceil_div(outs, 64);
-  const int64_t tiles = ceil_div(rows, 32 * p.rt) * p.tiles_o;
   if (aligned) {
     p.splits = gemm_splits(rows, width, outs);
     p.route = p.splits > 1 || rows <= 64 ? Plan::kGemmSplit : Plan::kGemm;
-  } else if (tiles <= 1024) {
+  } else if (rows <= 64) {
     p.route = Plan::kStream;
+    p.rt = rows <= 32 ? 1 : 2;
+    p.tiles_o = (int)ceil_div(outs, 64);
     const int unit = 4 * step4(d);
-    const int64_t splits = std::clamp<int64_t>(ceil_div(512, tiles), 1, std::min<int64_t>(ceil_div(width, unit), 16));
+    const int64_t splits = std::clamp<int64_t>(ceil_div(512, p.tiles_o), 1, std::min<int64_t>(ceil_div(width, unit), 16));
     p.chunk = (int)(ceil_div(ceil_div(width, splits), unit) * unit);
     p.splits = (int)ceil_div(width, p.chunk);
-    p.blocks = tiles * p.splits;
+    p.blocks = (int64_t)p.tiles_o * p.splits;
   } else {
     p.route = Plan::kTiles;
+    p.splits = tile_splits(rows, width, outs, d.dtype == WCC_BF16 ? 2 : 4);
   }
   return p;
 }
-// Ranges of k of the rank lines, of 256 at least: as many as give two workgroups a compute unit, 16 at most (8 for many rows, where
-// every tile adds them up again).
+// Ranges of k of the rank lines, of 256 at least: as many as give two workgroups (many rows: one) a compute unit, 16 at most.
 int thin_splits(const wcc_adapter_desc &d, int width) {
   const int64_t rows = std::max<int64_t>(d.rows, 1), most = std::clamp<int64_t>(width / 256, 1, rows <= 64 ? 16 : 8);
-  return (int)std::clamp<int64_t>(ceil_div(512, ceil_div(rows, kRange)), 1, most);
+  return (int)std::clamp<int64_t>(ceil_div(rows <= 64 ? 512 : 256, ceil_div(rows, kRange)), 1, most);
 }
 size_t lines_bytes(const wcc_adapter_desc &d, int width) { return align256((size_t)thin_splits(d, width) * d.rows * lines_ld(d) * 4); }
 size_t parts_bytes(const wcc_adapter_desc &d, const Plan &p, int outs) {
@@ -572,7 +587,7 @@ GradPlan grad_plan(const wcc_adapter_desc &d) {
 Low low_of(const wcc_adapter_desc &d, const AdapterArgs &g) { return Low{g.of_row, g.ranks, g.scale, d.adapters, d.rank}; }
 
 template <class T>
-ThinJob<T> thin_job(const wcc_adapter_desc &d, const AdapterArgs &g, bool back, bool lds, float *out) {
+ThinJob<T> thin_job(const wcc_adapter_desc &d, const AdapterArgs &g, bool back, float *out) {
   ThinJob<T> j{};
   if (!g.of_row) return j;
   const int64_t ci = d.C_in, co = d.C_out, r = d.rank;
@@ -584,8 +599,6 @@ ThinJob<T> thin_job(const wcc_adapter_desc &d, const AdapterArgs &g, bool back, 
   j.chunk = (int)(ceil_div(ceil_div(j.width, thin_splits(d, j.width)), step4(d)) * step4(d));
   j.out = Lines{out, (int)ceil_div(j.width, j.chunk), lines_ld(d), d.rows * lines_ld(d)};
   j.by_range = d.rows > 64;
-  auto whole = [](const void *p, int64_t stride) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && stride % 8 == 0; };
-  j.through_lds = lds && j.by_range && sizeof(T) == 2 && j.width % 8 == 0 && whole(j.x, j.ldx) && whole(j.m.p, back ? r : ci);
   const int64_t ranges = ceil_div(d.rows, kRange) * j.out.splits;
   // (up to 64 rows a wave an adapter, more: workgroups for two a compute unit, but not where few adapters leave them idle)
   j.groups = j.by_range ? (int)std::clamp<int64_t>(512 / ranges, 1, std::min<int64_t>(8, ceil_div(d.adapters, 4))) : std::clamp(d.adapters, 1, 32);
@@ -633,10 +646,16 @@ void project(Project<T> p, const Plan &pl, const ThinJob<T> &thin, const ThinJob
     if constexpr (sizeof(T) == 2) {
       if (pl.route == Plan::kGemm) return launch_gemm(p, s);
     }
-    return launch_tiles(p, s);
+    return launch_tiles(p, 1, nullptr, thin, other, s);
   }
   if (pl.route == Plan::kGemmSplit) {
     if constexpr (sizeof(T) == 2) launch_gemm_split(p, pl.splits, part, thin, other, s);
+  } else if (pl.route == Plan::kTiles) {
+    // The rank lines beside the tiles where all workgroups have a place at once; else they would keep tiles waiting for a second
+    // turn (1588 rows, 3520 -> 704, fp32: 150 us beside, 133 us with a launch of their own).
+    const bool beside = tiles_of(p.rows, p.outs) * pl.splits + thin.blocks + other.blocks <= kPlaces;
+    if (!beside) launch_lines(thin, other, p.low, s);
+    launch_tiles(p, pl.splits, part, beside ? thin : ThinJob<T>{}, beside ? other : ThinJob<T>{}, s);
   } else {
     const bool nn = p.wk != 1;
     const StreamJob<T> job{p.x, p.ldx, p.rows, p.width, p.outs, p.w, nn ? p.wk : p.wo, part, pl.splits, pl.chunk, pl.tiles_o, pl.blocks};
@@ -650,7 +669,7 @@ void project(Project<T> p, const Plan &pl, const ThinJob<T> &thin, const ThinJob
     }
   }
   const bool by_row = p.rows <= 64;
-  const int tiles_o = (int)ceil_div(p.outs, by_row ? 256 : 128);
+  const int tiles_o = (int)ceil_div(p.outs, by_row ? 256 : 64);
   const FinishJob<T> f{part, pl.splits, p.outs, tiles_o, p.rows, p.m, p.h, p.y, p.ldy, ceil_div(p.rows, by_row ? 1 : 32) * tiles_o};
   if (by_row) adapter_finish_row_kernel<T><<<(unsigned)std::min<int64_t>(f.blocks, 1 << 20), 256, 0, s>>>(f, p.low);
   else adapter_finish_tile_kernel<T><<<(unsigned)std::min<int64_t>(f.blocks, 1 << 20), 256, 0, s>>>(f, p.low);
@@ -660,7 +679,7 @@ template <class T>
 hipError_t forward(const wcc_adapter_desc &d, const AdapterArgs &g, hipStream_t s) {
   const Project<T> p = project_of<T>(d, g, false);
   const Plan pl = plan_of(d, d.C_in, d.C_out, aligned(p));
-  project<T>(p, pl, thin_job<T>(d, g, false, pl.route != Plan::kStream, (float *)g.ws), ThinJob<T>{}, (float *)(g.ws + lines_bytes(d, d.C_in)), s);
+  project<T>(p, pl, thin_job<T>(d, g, false, (float *)g.ws), ThinJob<T>{}, (float *)(g.ws + lines_bytes(d, d.C_in)), s);
   return hipGetLastError();
 }
 
@@ -671,11 +690,10 @@ hipError_t backward(const wcc_adapter_desc &d, const AdapterArgs &g, hipStream_t
   const Project<T> p = project_of<T>(d, g, true);
   const Low low = p.low;
   const Plan pl = plan_of(d, d.C_out, d.C_in, aligned(p));
-  const bool lds = !g.y || pl.route != Plan::kStream;  // (the streaming launch has none to spare)
   float *gr = (float *)take(lines_bytes(d, d.C_out)), *h = (float *)take(lines_bytes(d, d.C_in));
   float *part = (float *)take(g.y ? parts_bytes(d, pl, d.C_in) : 0);
-  const ThinJob<T> back = g.y || g.da ? thin_job<T>(d, g, true, lds, gr) : ThinJob<T>{};
-  const ThinJob<T> fore = g.db ? thin_job<T>(d, g, false, lds, h) : ThinJob<T>{};
+  const ThinJob<T> back = g.y || g.da ? thin_job<T>(d, g, true, gr) : ThinJob<T>{};
+  const ThinJob<T> fore = g.db ? thin_job<T>(d, g, false, h) : ThinJob<T>{};
   if (g.y) project<T>(p, pl, back, fore, part, s);
   else launch_lines(back, fore, low, s);
   if (!g.da && !g.db) return hipGetLastError();

@@ -18,16 +18,6 @@ namespace {
 
 constexpr int Line = kLine, Chunks = kChunks, PerLoad = 1024 / Line;  // lines of a load
 
-// (see adapter_tile.hip)
-__device__ __forceinline__ void tile_of(int64_t b, int64_t tiles, int64_t tiles_t, int tiles_o, int64_t &tt, int &to) {
-  const int64_t each = tiles / 8;
-  if (b < each * 8) b = b % 8 * each + b / 8;
-  const int64_t band = (int64_t)8 * tiles_o, first = b / band * 8, in = b % band;
-  const int64_t high = min(tiles_t - first, (int64_t)8);
-  tt = first + in % high;
-  to = (int)(in / high);
-}
-
 // FULL: a tile lies within the rows and outputs (the last ones are moved back, over others, whose results they repeat).
 template <int BT, int BO, int WT, bool NN, bool FULL>
 struct Gemm {
@@ -300,7 +290,7 @@ __global__ __launch_bounds__(256, BT == 128 ? 2 : 1) void project_gemm_kernel(Pr
   __shared__ __align__(1024) unsigned char xs0[G::XB], ws0[G::WB], xs1[G::XB], ws1[G::WB];
   int64_t tt;
   int to;
-  tile_of(blockIdx.x, tiles_t * tiles_o, tiles_t, tiles_o, tt, to);
+  tile_of(in_runs(blockIdx.x, tiles_t * tiles_o), tiles_t, tiles_o, tt, to);
   int64_t t0 = tt * BT;
   int o0 = to * BO;
   if constexpr (FULL) t0 = min(t0, p.rows - BT), o0 = min(o0, p.outs - BO);
@@ -309,16 +299,19 @@ __global__ __launch_bounds__(256, BT == 128 ? 2 : 1) void project_gemm_kernel(Pr
   const int ow = o0 + (wv % G::WO) * (EO * 32);
   f32x16 acc[EO][ET] = {};
   if (p.low.of_row) {  // (first: beside the operands its registers would not fit)
+    constexpr int Quarter = BT / 4;
+    auto room = [&](int row) {
+      const int q = row / Quarter;
+      return reinterpret_cast<bf16_t *>(q == 0 ? xs0 : q == 1 ? ws0 : q == 2 ? xs1 : ws1) + row % Quarter * PartsOf<bf16_t>::Out * p.h.ld;
+    };
+    gather_lines<bf16_t, BT>(p.low, p.h, room, t0, p.rows);
+    __syncthreads();
+    auto lines_of = [&](int r) { return room(__builtin_amdgcn_readfirstlane((wv / G::WO) * (ET * 32) + r * 32)); };
+    int o[EO];
 #pragma unroll
-    for (int r = 0; r < ET; ++r) {
-      int o[EO];
-      f32x16 sums[EO] = {};
-#pragma unroll
-      for (int e = 0; e < EO; ++e) o[e] = ow + e * 32 + (threadIdx.x & 31);
-      add_thin<bf16_t, EO, false>(p.low, p.m, p.h, p.rows, p.outs, tw + r * 32, o, sums);
-#pragma unroll
-      for (int e = 0; e < EO; ++e) acc[e][r] = sums[e];
-    }
+    for (int e = 0; e < EO; ++e) o[e] = ow + e * 32 + (threadIdx.x & 31);
+    add_thin<bf16_t, EO, ET, false, 1>(p.low, p.m, p.h.ld, lines_of, p.rows, p.outs, tw, o, acc);
+    __syncthreads();
   }
   G::run(p, t0, o0, 0, p.width, xs0, ws0, xs1, ws1, acc);
   unsigned char *own = wv == 0 ? xs0 : wv == 1 ? ws0 : wv == 2 ? xs1 : ws1;
@@ -336,9 +329,9 @@ __global__ __launch_bounds__(256, 2) void project_gemm_split_kernel(Project<bf16
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, ln = lane & 31, half = lane >> 5;
   if (block < thin.blocks + other.blocks) {
     __shared__ ThinLds lds;
-    const ThinStages st{xs0, ws0, xs1, ws1};
-    if (block < thin.blocks) thin_block<bf16_t>(thin, p.low, block, lds, st);
-    else thin_block<bf16_t>(other, p.low, block - thin.blocks, lds, st);
+    unsigned char *own = wv == 0 ? xs0 : wv == 1 ? ws0 : wv == 2 ? xs1 : ws1;  // (16 KiB each where rows come by ranges)
+    if (block < thin.blocks) thin_block<bf16_t>(thin, p.low, block, lds, own);
+    else thin_block<bf16_t>(other, p.low, block - thin.blocks, lds, own);
     return;
   }
   const int64_t at = block - thin.blocks - other.blocks;
