@@ -521,6 +521,26 @@ __global__ __launch_bounds__(256) void adapter_grad_join_kernel(JoinJob ja, Join
   }
 }
 
+// ---- rows that 16-byte loads cannot take --------------------------------------------------------------------------
+// A copy of a bf16 matrix, its rows `chunks` whole chunks of 8 long, what is past its width and its rows 0.
+struct PackJob {
+  const bf16_t *from;
+  int64_t ld, rows, rows_to;
+  int width, chunks;
+  bf16_t *to;
+};
+
+__global__ __launch_bounds__(256) void adapter_pack_kernel(PackJob g1, PackJob g2) {
+  const int64_t n1 = g1.rows_to * g1.chunks, n = n1 + g2.rows_to * g2.chunks;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const bool second = i >= n1;
+    const PackJob &g = second ? g2 : g1;
+    const int64_t at = second ? i - n1 : i, row = at / g.chunks;
+    const int c = (int)(at - row * g.chunks) * 8;
+    reinterpret_cast<u32x4 *>(g.to)[at] = load_k(g.from + row * g.ld + c, row < g.rows ? g.width - c : 0);
+  }
+}
+
 // ---- host ------------------------------------------------------------------------------------------------------------
 size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -541,7 +561,7 @@ Plan plan_of(const wcc_adapter_desc &d, int width, int outs, bool aligned) {
   Plan p{};
   const int64_t rows = std::max<int64_t>(d.rows, 1);
   if (aligned) {
-    p.splits = gemm_splits(rows, width, outs);
+    p.splits = gemm_splits(rows, (width + 7) / 8 * 8, outs);
     p.route = p.splits > 1 || rows <= 64 ? Plan::kGemmSplit : Plan::kGemm;
   } else if (rows <= 64) {
     p.route = Plan::kStream;
@@ -558,14 +578,38 @@ Plan plan_of(const wcc_adapter_desc &d, int width, int outs, bool aligned) {
   }
   return p;
 }
-// Ranges of k of the rank lines, of 256 at least: as many as give two workgroups (many rows: one) a compute unit, 16 at most.
+// Ranges of k of the rank lines, of 256 at least: as many as give two workgroups (many rows: one) a compute unit, 16 at most; 8 where
+// more than four adapters share many rows among groups of workgroups (512 rows, 4096 -> 4096, 24 adapters, with the product: 24 us
+// with 8, 32 with 16; 190 rows, 5232 -> 4072, 4 adapters: 42 and 35).
 int thin_splits(const wcc_adapter_desc &d, int width) {
-  const int64_t rows = std::max<int64_t>(d.rows, 1), most = std::clamp<int64_t>(width / 256, 1, rows <= 64 ? 16 : 8);
+  const int64_t rows = std::max<int64_t>(d.rows, 1), most = std::clamp<int64_t>(width / 256, 1, rows <= 64 || d.adapters <= 4 ? 16 : 8);
   return (int)std::clamp<int64_t>(ceil_div(rows <= 64 ? 512 : 256, ceil_div(rows, kRange)), 1, most);
 }
 size_t lines_bytes(const wcc_adapter_desc &d, int width) { return align256((size_t)thin_splits(d, width) * d.rows * lines_ld(d) * 4); }
 size_t parts_bytes(const wcc_adapter_desc &d, const Plan &p, int outs) {
   return p.parts() ? align256((size_t)p.splits * d.rows * outs * 4) : 0;
+}
+
+// Copies of x (back: dy) and W that 16-byte loads can take, where the strides do not allow them: then the products go through
+// adapter_gemm.hip.  From 2^32 of them on, and if W is copied from 512 rows on: the copies take 4 to 7 us, and W's the time of twice
+// its bytes (rows 3 further apart: 1172 rows, 2816 -> 4224, 29 adapters, 121 us without and 100 with; 777 rows, 1000 -> 1537,
+// 34 and 39).
+struct Packs {
+  bool x, w;
+  int width, outs;  // of the copies
+  size_t x_bytes, w_bytes;
+};
+Packs packs_of(const wcc_adapter_desc &d, bool back) {
+  const int width = back ? d.C_out : d.C_in, outs = back ? d.C_in : d.C_out;
+  const int64_t ld = back ? d.ldy : d.ldx;
+  Packs k{};
+  k.width = (width + 7) / 8 * 8, k.outs = back ? (outs + 7) / 8 * 8 : outs;
+  k.x = ld % 8 != 0 || k.width != width;
+  k.w = k.width != width || k.outs != outs;
+  if (d.dtype != WCC_BF16 || d.rows <= 64 || (k.w && d.rows < 512) || d.rows * width < ((int64_t)1 << 32) / outs) k.x = k.w = false;
+  if (k.x) k.x_bytes = align256((size_t)d.rows * k.width * 2);
+  if (k.w) k.w_bytes = align256((size_t)k.width * k.outs * 2);
+  return k;
 }
 
 // Ranges of rows for the gradients: the sums of the ranges no more than twice what x takes, 64 rows at least in a range.
@@ -637,6 +681,29 @@ bool aligned(const Project<T> &p) {
   return false;
 }
 
+// p on copies, where they let 16-byte loads take it; `at`: their place
+void pack(Project<bf16_t> &p, const wcc_adapter_desc &d, bool back, char *at, hipStream_t s) {
+  const Packs k = packs_of(d, back);
+  if (!k.x && !k.w) return;
+  Project<bf16_t> q = p;
+  PackJob jx{}, jw{};
+  if (k.x) {
+    q.x = (const bf16_t *)at, q.ldx = k.width;
+    jx = PackJob{p.x, p.ldx, p.rows, p.rows, p.width, k.width / 8, (bf16_t *)at};
+    at += k.x_bytes;
+  }
+  if (k.w) {
+    q.w = (const bf16_t *)at;
+    (back ? q.wk : q.wo) = back ? k.outs : k.width;
+    jw = back ? PackJob{p.w, p.wk, p.width, k.width, p.outs, k.outs / 8, (bf16_t *)at} : PackJob{p.w, p.wo, p.outs, p.outs, p.width, k.width / 8, (bf16_t *)at};
+  }
+  q.width = k.width;
+  if (!gemm_takes(q)) return;  // (what is not copied begins between 16 bytes)
+  p = q;
+  const int64_t n = jx.rows_to * jx.chunks + jw.rows_to * jw.chunks;
+  adapter_pack_kernel<<<(unsigned)std::min<int64_t>(ceil_div(n, 256), 1 << 14), 256, 0, s>>>(jx, jw);
+}
+
 // y = x W^T + h m (back: dx from dy), with another job of rank lines beside (the forward ones, for dB)
 template <class T>
 void project(Project<T> p, const Plan &pl, const ThinJob<T> &thin, const ThinJob<T> &other, float *part, hipStream_t s) {
@@ -677,9 +744,14 @@ void project(Project<T> p, const Plan &pl, const ThinJob<T> &thin, const ThinJob
 
 template <class T>
 hipError_t forward(const wcc_adapter_desc &d, const AdapterArgs &g, hipStream_t s) {
-  const Project<T> p = project_of<T>(d, g, false);
-  const Plan pl = plan_of(d, d.C_in, d.C_out, aligned(p));
-  project<T>(p, pl, thin_job<T>(d, g, false, (float *)g.ws), ThinJob<T>{}, (float *)(g.ws + lines_bytes(d, d.C_in)), s);
+  char *at = g.ws;
+  auto take = [&](size_t bytes) { char *p = at; at += bytes; return p; };
+  const Packs k = packs_of(d, false);
+  float *h = (float *)take(lines_bytes(d, d.C_in));
+  char *copies = take(k.x_bytes + k.w_bytes);
+  Project<T> p = project_of<T>(d, g, false);
+  if constexpr (sizeof(T) == 2) pack(p, d, false, copies, s);
+  project<T>(p, plan_of(d, d.C_in, d.C_out, aligned(p)), thin_job<T>(d, g, false, h), ThinJob<T>{}, (float *)at, s);
   return hipGetLastError();
 }
 
@@ -687,10 +759,15 @@ template <class T>
 hipError_t backward(const wcc_adapter_desc &d, const AdapterArgs &g, hipStream_t s) {
   char *at = g.ws;
   auto take = [&](size_t bytes) { char *p = at; at += bytes; return p; };
-  const Project<T> p = project_of<T>(d, g, true);
+  Project<T> p = project_of<T>(d, g, true);
   const Low low = p.low;
-  const Plan pl = plan_of(d, d.C_out, d.C_in, aligned(p));
   float *gr = (float *)take(lines_bytes(d, d.C_out)), *h = (float *)take(lines_bytes(d, d.C_in));
+  const Packs k = packs_of(d, true);
+  char *copies = take(k.x_bytes + k.w_bytes);
+  if constexpr (sizeof(T) == 2) {
+    if (g.y) pack(p, d, true, copies, s);
+  }
+  const Plan pl = plan_of(d, d.C_out, d.C_in, aligned(p));
   float *part = (float *)take(g.y ? parts_bytes(d, pl, d.C_in) : 0);
   const ThinJob<T> back = g.y || g.da ? thin_job<T>(d, g, true, gr) : ThinJob<T>{};
   const ThinJob<T> fore = g.db ? thin_job<T>(d, g, false, h) : ThinJob<T>{};
@@ -730,11 +807,12 @@ size_t adapter_bytes(const wcc_adapter_desc &d) {
   const size_t sums = (size_t)d.adapters * d.rank * 4;
   const size_t grads = align256((size_t)gp.splits * d.adapters * 4) +
                        (gp.splits > 1 ? align256(gp.splits * sums * d.C_in) + align256(gp.splits * sums * d.C_out) : 0);
+  const Packs fore = packs_of(d, false), back = packs_of(d, true);
   size_t most = 0;
   for (const bool fits : {false, true}) {  // (alignment is known with the pointers)
     const bool al = fits && d.dtype == WCC_BF16;
-    most = std::max(most, parts_bytes(d, plan_of(d, d.C_in, d.C_out, al), d.C_out));
-    most = std::max(most, parts_bytes(d, plan_of(d, d.C_out, d.C_in, al), d.C_in) + lines_bytes(d, d.C_out) + grads);
+    most = std::max(most, parts_bytes(d, plan_of(d, d.C_in, d.C_out, al), d.C_out) + fore.x_bytes + fore.w_bytes);
+    most = std::max(most, parts_bytes(d, plan_of(d, d.C_out, d.C_in, al), d.C_in) + lines_bytes(d, d.C_out) + grads + back.x_bytes + back.w_bytes);
   }
   return lines_bytes(d, d.C_in) + most;
 }

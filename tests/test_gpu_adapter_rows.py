@@ -24,6 +24,7 @@ MANY = [  # type, rows, width, outputs, adapters, rank, padding, shift, order
     ("bf16", 4001, 200, 3528, 5, 16, 0, 0, "runs"), ("bf16", 4001, 328, 3528, 3, 40, 8, 8, "mixed"),
     ("bf16", 1500, 264, 2056, 30, 24, 0, 0, "mixed"), ("bf16", 1500, 136, 2051, 4, 128, 0, 0, "runs"),
     ("bf16", 2200, 75, 1801, 6, 8, 3, 1, "mixed"), ("f32", 2200, 72, 1800, 6, 20, 0, 0, "mixed"), ("f32", 1300, 2100, 500, 4, 24, 0, 0, "mixed"),
+    ("bf16", 2304, 1003, 1900, 4, 16, 1, 1, "mixed"), ("bf16", 1500, 1600, 1800, 12, 24, 3, 0, "runs"),  # (copied: rows and W, rows)
     ("bf16", 700, 1111, 333, 9, 16, 1, 0, "runs"), ("f32", 700, 1111, 333, 9, 7, 1, 0, "mixed"), ("bf16", 190, 2048, 1032, 3, 64, 0, 0, "mixed"),
 ]
 
@@ -46,7 +47,7 @@ def test_backward_of_many_rows(ctx, case):
 
 
 APART = [("bf16", 20, 256, 136, 3, 8), ("f32", 20, 129, 63, 3, 5), ("bf16", 100, 512, 264, 4, 16), ("bf16", 100, 511, 263, 4, 24), ("f32", 100, 300, 200, 3, 24),
-         ("bf16", 1500, 136, 2056, 6, 40), ("bf16", 2200, 75, 1801, 3, 8), ("f32", 2200, 72, 1800, 5, 12), ("bf16", 4001, 72, 3528, 4, 16)]
+         ("bf16", 1500, 136, 2056, 6, 40), ("bf16", 2200, 75, 1801, 3, 8), ("bf16", 2304, 1003, 1900, 4, 16), ("f32", 2200, 72, 1800, 5, 12), ("bf16", 4001, 72, 3528, 4, 16)]
 
 
 @pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
