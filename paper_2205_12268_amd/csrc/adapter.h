@@ -330,6 +330,7 @@ __device__ __forceinline__ void add_thin(const Low &low, const Thin<T> &m, int l
         nf[s][e] = s == 0 || s * KS < low.rank ? thin_k(m, max(next, 0), min(o[e], outs - 1), next_j + s * KS + half * VE, next_lines) : zeros;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
+      if (a < 0) break;
       const bool mine = id[r] == a;
       const T *h = lines_of(r);
 #pragma unroll

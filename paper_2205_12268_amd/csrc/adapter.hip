@@ -5,11 +5,9 @@
 //   backward  g[t,j] = s_a sum_o B_a[o,j] dy[t,o],   dx[t,c] = sum_o W[o,c] dy[t,o]  + sum_j A_a[j,c] g[t,j]
 //   gradients dA_a[j,c] = sum_t g[t,j] x[t,c],       dB_a[o,j] = sum_t h[t,j] dy[t,o]
 //
-// Few rows: what has to be read is W and the adapters, once, and what counts is how many loads are in flight.  The first
-// launch has the product with W, cut along k over waves and workgroups, each wave's operands straight from memory into
-// registers, and in further workgroups the rank lines (they are but more lines that x meets).  The second adds the partial
-// sums, the thin product with h and rounds.  Many rows: the rank lines, then tiles through LDS with the thin product in
-// their last step (adapter_tile.hip).
+// What is left out of the product with W by the first launch, in ranges of k, a second one adds up, with the thin product, and rounds;
+// whole tiles need one launch for the rank lines and one for all else.  Up to 64 rows what has to be read is W and the adapters, once,
+// and what counts is how many loads are in flight; from some hundred rows on it is the matrix cores.  Which way a call goes: plan_of.
 #include "adapter.h"
 
 namespace wcc {
@@ -28,7 +26,7 @@ __global__ __launch_bounds__(256, 2) void adapter_lines_kernel(ThinJob<T> g1, Th
   }
 }
 
-// ---- the product with W for few rows ----------------------------------------------------------------------------
+// ---- the product with W for few rows: fp32, and bf16 that 16-byte loads cannot take ---------------------------------
 // 32 RT rows x 64 outputs x a range of k a workgroup; each of its four waves has a quarter of the range and all results.
 // NN: W's outputs are contiguous, not its k.
 template <class T>
@@ -189,9 +187,10 @@ __global__ __launch_bounds__(256) void adapter_finish_row_kernel(FinishJob<T> g,
 
 // More rows: 32 rows x 64 outputs a workgroup.  Each wave has all of them and, of the distinct adapters among the rows, every
 // fourth: the thin products of rows in any order are as many trips to memory one after the other as there are adapters.  (One
-// wave for all adapters of 32 outputs: 190 rows of mixed adapters, rank 64, 4072 outputs took 28 us.)
+// wave for all adapters of 32 outputs: 190 rows of mixed adapters, rank 64, 4072 outputs took 28 us, this 17.)  Bound by those trips:
+// three workgroups a compute unit at the cost of a few spilled registers, 777 rows x 1537 outputs 11 us (with two 17).
 template <class T>
-__global__ __launch_bounds__(256) void adapter_finish_tile_kernel(FinishJob<T> g, Low low) {
+__global__ __launch_bounds__(256, 3) void adapter_finish_tile_kernel(FinishJob<T> g, Low low) {
   constexpr int LD = 68;
   __shared__ __align__(16) float sums[4][32][LD];
   __shared__ __align__(16) T h[32 * PartsOf<T>::Out * WCC_MAX_RANK];
@@ -223,7 +222,7 @@ __global__ __launch_bounds__(256) void adapter_finish_tile_kernel(FinishJob<T> g
       const int o[2] = {o0 + ln, o0 + 32 + ln};
       f32x16 acc[2][1] = {};
       __syncthreads();
-      add_thin<T, 2, 1, true, 32 / StepOf<T>::K>(low, g.m, g.h.ld, [&](int) { return h; }, g.rows, g.outs, t0, o, acc, wv, 4);
+      add_thin<T, 2, 1, true, 2>(low, g.m, g.h.ld, [&](int) { return h; }, g.rows, g.outs, t0, o, acc, wv, 4);
 #pragma unroll
       for (int e = 0; e < 2; ++e)
 #pragma unroll
@@ -550,7 +549,8 @@ int step4(const wcc_adapter_desc &d) { return d.dtype == WCC_BF16 ? 64 : 32; }
 int lines_ld(const wcc_adapter_desc &d) { return (d.rank + 7) / 8 * 8; }
 
 // How y = x W^T is made: bf16 that 16-byte loads can take by adapter_gemm.hip, whatever else by the stream (up to 64 rows) or
-// adapter_tile.hip; in ranges of k where the tiles alone would leave compute units without work.
+// adapter_tile.hip; in ranges of k where the tiles alone would leave compute units without work.  (fp32, stream and tiles: 64 rows,
+// 2048 -> 2048 25 and 30 us, 40 rows, 1024 -> 512 15 and 18; 1588 rows, 3520 -> 704 157 and 142.)
 struct Plan {
   enum { kStream, kTiles, kGemm, kGemmSplit } route;
   int rt, splits, chunk, tiles_o;
@@ -735,7 +735,7 @@ void project(Project<T> p, const Plan &pl, const ThinJob<T> &thin, const ThinJob
       else adapter_products_kernel<T, 2, false><<<blocks, 256, 0, s>>>(job, thin, other, p.low);
     }
   }
-  const bool by_row = p.rows <= 64;
+  const bool by_row = p.rows <= 64;  // (64 rows, 2048 -> 2048, 4 adapters, by row and by tiles: bf16 15.2 and 18.1 us, fp32 24.7 and 28.2)
   const int tiles_o = (int)ceil_div(p.outs, by_row ? 256 : 64);
   const FinishJob<T> f{part, pl.splits, p.outs, tiles_o, p.rows, p.m, p.h, p.y, p.ldy, ceil_div(p.rows, by_row ? 1 : 32) * tiles_o};
   if (by_row) adapter_finish_row_kernel<T><<<(unsigned)std::min<int64_t>(f.blocks, 1 << 20), 256, 0, s>>>(f, p.low);

@@ -11,6 +11,9 @@
 // which leave through LDS as whole lines.
 // The last stages, which the end of k cuts, are not overlapped; chunks past the end (and, NN, past the last output) come from 16
 // bytes of zeros.
+// Bound by the matrix cores and what feeds them: 8192 rows, 4096 -> 4096 267 us (1.03 PFLOP/s), the other order of W 248 (1.11), 8192 in
+// all three 0.93 ms (1.18 PFLOP/s); 128 x 128 tiles 1024 rows, 4096 -> 4096 57 us.  The adapters before it, in mixed order, add 17 us
+// there.  Not kept: four stages of 32 k (300 us), bands of 4 or 16 row tiles (270 to 277), a priority for waves that multiply.
 #include "adapter.h"
 
 namespace wcc {
@@ -388,7 +391,8 @@ bool gemm_takes(const Project<bf16_t> &p) {
 int split_rows(int64_t rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
 
 // Whole tiles where they give three quarters of the compute units work; else ranges of 256 k at least, and two (few rows: what counts
-// is W on its way) workgroups a compute unit.
+// is W on its way) workgroups a compute unit.  (1024 rows, with 4 adapters, whole and in ranges: 4096 -> 1536 62 and 36 us, 4096 -> 3200
+// 63 and 72, 1024 -> 3200 34 and 43.)
 int gemm_splits(int64_t rows, int width, int outs) {
   const int64_t n = tiles(rows, split_rows(rows)) * tiles(outs, 128);
   if (rows > 64 && n >= 192) return 1;
@@ -397,6 +401,8 @@ int gemm_splits(int64_t rows, int width, int outs) {
   return (int)tiles(width, (int)chunk);
 }
 
+// 256 x 256 tiles, of which a compute unit holds one, where three quarters of them have one.  (4 adapters, 256 and 128: 4096 rows,
+// 4096 -> 4096 172 and 187 us; 2048 rows, 4096 -> 2048, which gives 64, 133 and 69.)
 void launch_gemm(const Project<bf16_t> &p, hipStream_t s) {
   if (p.rows >= 256 && p.outs >= 256 && tiles(p.rows, 256) * tiles(p.outs, 256) >= 200) launch<256, true>(p, s);
   else launch<128, false>(p, s);
