@@ -578,11 +578,11 @@ Plan plan_of(const wcc_adapter_desc &d, int width, int outs, bool aligned) {
   }
   return p;
 }
-// Ranges of k of the rank lines, of 256 at least: as many as give two workgroups (many rows: one) a compute unit, 16 at most; 8 where
+// Ranges of k of the rank lines, of 256 (many rows: 128) at least: as many as give two workgroups (many rows: one) a compute unit, 16 at most; 8 where
 // more than four adapters share many rows among groups of workgroups (512 rows, 4096 -> 4096, 24 adapters, with the product: 24 us
 // with 8, 32 with 16; 190 rows, 5232 -> 4072, 4 adapters: 42 and 35).
 int thin_splits(const wcc_adapter_desc &d, int width) {
-  const int64_t rows = std::max<int64_t>(d.rows, 1), most = std::clamp<int64_t>(width / 256, 1, rows <= 64 || d.adapters <= 4 ? 16 : 8);
+  const int64_t rows = std::max<int64_t>(d.rows, 1), most = std::clamp<int64_t>(width / (rows <= 64 ? 256 : 128), 1, rows <= 64 || d.adapters <= 4 ? 16 : 8);
   return (int)std::clamp<int64_t>(ceil_div(rows <= 64 ? 512 : 256, ceil_div(rows, kRange)), 1, most);
 }
 size_t lines_bytes(const wcc_adapter_desc &d, int width) { return align256((size_t)thin_splits(d, width) * d.rows * lines_ld(d) * 4); }
