@@ -265,8 +265,9 @@ __device__ __forceinline__ void gather_lines(const Low &low, const Lines &h, F r
 // Of each adapter among the rows J steps of lines at a time, the next ones' operands on their way meanwhile; of the distinct adapters
 // every turn-th from the first-th on.  The lines of rows with other adapters are replaced by zeros, except where an adapter holds
 // infinities or NaN (a product of its operands with zeros tells): its sums are made apart then, and rows take none but their own.
-// (With all sums apart, and the lines of each 32 rows by themselves: 1172 rows, 2816 -> 4224, 29 adapters in mixed order, 162 us
-// instead of 122; 8192 rows, 4096 -> 4096, 318 instead of 305.)
+// (With all sums apart, and the lines of each 32 rows by themselves: 8192 rows, 4096 -> 4096, 8 adapters of rank 32 in runs 318 us
+// instead of 292.  With the additions for operands that are not finite in the one loop, whose results then moved between the
+// registers of the vector unit and of the matrix cores: 4096 rows, 4096 -> 4096, 24 adapters in mixed order 244 us instead of 195.)
 template <class T, int E, int R, bool ROWS, int J, class F>
 __device__ __forceinline__ void add_thin(const Low &low, const Thin<T> &m, int ld, F lines_of, int64_t rows, int outs, int64_t t0,
                                          const int (&o)[E], f32x16 (&acc)[E][R], int first = 0, int turn = 1) {
@@ -313,9 +314,25 @@ __device__ __forceinline__ void add_thin(const Low &low, const Thin<T> &m, int l
   for (int s = 0; s < J; ++s)
 #pragma unroll
     for (int e = 0; e < E; ++e) mf[s][e] = zeros;
+  // NaN if any of J steps' operands are not finite
+  auto checked = [&](const u32x4 (&f)[J][E]) {
+    f32x16 none = {};
+#pragma unroll
+    for (int s = 0; s < J; ++s)
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        if constexpr (sizeof(T) == 4) {  // (four instructions of the vector unit, not four of the matrix cores)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) none[0] = fmaf(__uint_as_float(f[s][e][i]), 0.f, none[0]);
+        } else if (s == 0 || s * KS < low.rank) {
+          none = mma<T>(zeros, f[s][e], none);
+        }
+      }
+    return __ballot(none[0] != 0.f) != 0;
+  };
   pass(first);
   int a = -2, lines = 0, j0 = 0;  // (none yet: the first round only loads)
-  bool apart = false;
+  bool some_apart = false;
   while (a != -1) {
     int next = a, next_lines = lines, next_j = j0 + J * KS;
     if (next_j >= lines) {
@@ -339,7 +356,37 @@ __device__ __forceinline__ void add_thin(const Low &low, const Thin<T> &m, int l
 #pragma unroll
           for (int e = 0; e < E; ++e) acc[e][r] = product(h, j0 + s * KS + half * VE, mf[s][e], mine, acc[e][r]);
     }
-    if (apart) {
+    a = next, lines = next_lines, j0 = next_j;
+#pragma unroll
+    for (int s = 0; s < J; ++s)
+#pragma unroll
+      for (int e = 0; e < E; ++e) mf[s][e] = cut_k<T>(nf[s][e], j0 + s * KS + half * VE, lines);
+    if (checked(mf)) {
+      some_apart = true;
+#pragma unroll
+      for (int s = 0; s < J; ++s)
+#pragma unroll
+        for (int e = 0; e < E; ++e) mf[s][e] = zeros;
+    }
+  }
+  if (!some_apart) return;
+  // (a loop of its own: the vector unit's additions in the loop above would keep the results out of the matrix cores' registers)
+#pragma unroll
+  for (int r = 0; r < R; ++r) rest[r] = (uint32_t)__ballot(id[r] >= 0);
+  pass(first);
+#pragma unroll 1
+  for (a = front(); a != -1; a = front()) {
+    lines = low.lines(a);
+#pragma unroll 1
+    for (j0 = 0; j0 < lines; j0 += J * KS) {
+#pragma unroll
+      for (int s = 0; s < J; ++s)
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const int j = j0 + s * KS + half * VE;
+          mf[s][e] = cut_k<T>(thin_k(m, a, min(o[e], outs - 1), j, lines), j, lines);
+        }
+      if (!checked(mf)) continue;
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         const bool mine = id[r] == a;
@@ -347,37 +394,14 @@ __device__ __forceinline__ void add_thin(const Low &low, const Thin<T> &m, int l
 #pragma unroll
         for (int e = 0; e < E; ++e) {
           f32x16 d = {};
-#pragma unroll 1
-          for (int s = 0; s < J; ++s) {
-            const int j = j0 + s * KS + half * VE;
-            d = product(lines_of(r), j, cut_k<T>(thin_k(m, a, min(o[e], outs - 1), j, lines), j, lines), true, d);
-          }
+#pragma unroll
+          for (int s = 0; s < J; ++s) d = product(lines_of(r), j0 + s * KS + half * VE, mf[s][e], true, d);
 #pragma unroll
           for (int i = 0; i < 16; ++i) acc[e][r][i] += (ROWS ? (same >> result_line(i, half) & 1) != 0 : mine) ? d[i] : 0.f;
         }
       }
     }
-    a = next, lines = next_lines, j0 = next_j;
-    f32x16 none = {};
-#pragma unroll
-    for (int s = 0; s < J; ++s)
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        mf[s][e] = cut_k<T>(nf[s][e], j0 + s * KS + half * VE, lines);
-        if constexpr (sizeof(T) == 4) {  // (four instructions of the vector unit, not four of the matrix cores)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) none[0] = fmaf(__uint_as_float(mf[s][e][i]), 0.f, none[0]);
-        } else if (s == 0 || s * KS < low.rank) {
-          none = mma<T>(zeros, mf[s][e], none);
-        }
-      }
-    apart = __ballot(none[0] != 0.f) != 0;  // (NaN)
-    if (apart) {
-#pragma unroll
-      for (int s = 0; s < J; ++s)
-#pragma unroll
-        for (int e = 0; e < E; ++e) mf[s][e] = zeros;
-    }
+    pass(turn);
   }
 }
 
