@@ -304,8 +304,9 @@ wcc_status wcc_set_block_profile_layer(wcc_ctx *ctx, int layer);
  * stride in elements, at least its width, and is aligned to its elements only (so is every other
  * tensor here); rows = 0 enqueues nothing but the zeros of a gradient.  bf16 results are
  * rounded once, to nearest even, from fp32; sums, statistics of rows and gradients of adapters are
- * fp32.  Sums are added in an order that depends on the descriptor alone, so equal calls give
- * equal bits.  Nothing but what is said below depends on the contents of index tensors: a value
+ * fp32.  Sums are added in an order that depends on the descriptor and on the alignment of the
+ * tensors (and, for an adapter that holds infinities or NaN, on that), so equal calls give equal
+ * bits.  What is not finite in a row or an adapter reaches no other row's results.  Nothing but what is said below depends on the contents of index tensors: a value
  * outside its range counts as "none". */
 
 /* ---- one projection, an adapter for each row ---------------------------------------------------

@@ -186,9 +186,9 @@ __global__ __launch_bounds__(256) void adapter_finish_row_kernel(FinishJob<T> g,
 }
 
 // More rows: 32 rows x 64 outputs a workgroup.  Each wave has all of them and, of the distinct adapters among the rows, every
-// fourth: the thin products of rows in any order are as many trips to memory one after the other as there are adapters.  (One
-// wave for all adapters of 32 outputs: 190 rows of mixed adapters, rank 64, 4072 outputs took 28 us, this 17.)  Bound by those trips:
-// three workgroups a compute unit at the cost of a few spilled registers, 777 rows x 1537 outputs 11 us (with two 17).
+// fourth: the thin products of rows in any order are as many trips to memory one after the other as there are adapters, and those
+// trips are what bounds it.  (One wave for all adapters of 32 outputs: 190 rows of mixed adapters, rank 64, 4072 outputs took 28 us,
+// this 17.  Three workgroups a compute unit: 777 rows x 1537 outputs 11 us, with two 17.)
 template <class T>
 __global__ __launch_bounds__(256, 3) void adapter_finish_tile_kernel(FinishJob<T> g, Low low) {
   constexpr int LD = 68;
