@@ -22,6 +22,7 @@ def ctx():
 
 MANY = [  # type, rows, width, outputs, adapters, rank, padding, shift, order
     ("bf16", 4001, 200, 3528, 5, 16, 0, 0, "runs"), ("bf16", 4001, 328, 3528, 3, 40, 8, 8, "mixed"),
+    ("bf16", 4001, 72, 3528, 2, 128, 0, 0, "runs"), ("f32", 2200, 72, 1800, 2, 128, 0, 0, "mixed"),
     ("bf16", 1500, 264, 2056, 30, 24, 0, 0, "mixed"), ("bf16", 1500, 136, 2051, 4, 128, 0, 0, "runs"),
     ("bf16", 2200, 75, 1801, 6, 8, 3, 1, "mixed"), ("f32", 2200, 72, 1800, 6, 20, 0, 0, "mixed"), ("f32", 1300, 2100, 500, 4, 24, 0, 0, "mixed"),
     ("bf16", 2304, 1003, 1900, 4, 16, 1, 1, "mixed"), ("bf16", 1500, 1600, 1800, 12, 24, 3, 0, "runs"),  # (copied: rows and W, rows)
