@@ -162,9 +162,11 @@ __global__ __launch_bounds__(256) void adapter_finish_row_kernel(FinishJob<T> g,
     const int o = (int)(b % g.tiles_o) * 256 + (int)threadIdx.x, oc = min(o, g.outs - 1);
     const int64_t t = b / g.tiles_o;
     const int a = low.of(t), lines = a >= 0 ? low.lines(a) : 0;
-    u32x4 mf[Q];  // the first 32 lines' loads go out together with the others
+    u32x4 mf[Q] = {};
+    if (low.of_row) {  // the first 32 lines' loads go out together with the others (without adapters there may be nothing at m.p)
 #pragma unroll
-    for (int q = 0; q < Q; ++q) mf[q] = thin_k(g.m, max(a, 0), oc, q * VE, lines);
+      for (int q = 0; q < Q; ++q) mf[q] = thin_k(g.m, max(a, 0), oc, q * VE, lines);
+    }
     float v = sum_parts(g.part + t * g.outs + oc, g.splits, g.rows * g.outs);
     if ((int)threadIdx.x < lines) hs[threadIdx.x] = g.h.at(t * g.h.ld + threadIdx.x);
     __syncthreads();
