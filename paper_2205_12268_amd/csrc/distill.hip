@@ -333,8 +333,9 @@ SlicePlan plan(const wcc_distill_desc &d, bool backward) {
     while ((int64_t)p.nt * p.nv < vecs) p.nv *= 2;
     return p;
   }
+  const int64_t rows = std::max<int64_t>(d.rows, 1);
   int64_t want = (vecs + 256 * 8 - 1) / (256 * 8);
-  if (d.rows * want < 512) want = std::max(want, std::min((512 + d.rows - 1) / d.rows, vecs / 256));
+  if (rows * want < 512) want = std::max(want, std::min((512 + rows - 1) / rows, vecs / 256));
   want = std::max<int64_t>(want, 1);
   const int64_t each = (vecs + want - 1) / want;
   p.length = (int)std::min<int64_t>(each * ve, d.V);

@@ -319,8 +319,9 @@ __global__ __launch_bounds__(256) void scores_join_kernel(const T *__restrict__ 
 SlicePlan plan(const wcc_scores_desc &d) {
   const int ve = d.dtype == WCC_BF16 ? 8 : 4;
   const int64_t vecs = ((int64_t)d.V + ve - 1) / ve;
+  const int64_t rows = std::max<int64_t>(d.rows, 1);
   int64_t least = (vecs + 512 * 16 - 1) / (512 * 16);
-  if (d.rows * least < 512) least = std::max(least, std::min((512 + d.rows - 1) / d.rows, vecs / 256));
+  if (rows * least < 512) least = std::max(least, std::min((512 + rows - 1) / rows, vecs / 256));
   least = std::max<int64_t>(least, 1);
   SlicePlan p{};
   int64_t cost = 0;
