@@ -21,7 +21,8 @@ namespace {
 
 constexpr int Line = kLine, Chunks = kChunks, PerLoad = 1024 / Line;  // lines of a load
 
-// FULL: a tile lies within the rows and outputs (the last ones are moved back, over others, whose results they repeat).
+// FULL: a tile lies within the rows and outputs (the last ones are moved back, over others, whose results they repeat).  With NN,
+// outputs count up to whole chunks of 8 there, which W's rows hold: its loads begin at a chunk.
 template <int BT, int BO, int WT, bool NN, bool FULL>
 struct Gemm {
   static constexpr int Waves = 4, WO = Waves / WT;
@@ -275,9 +276,9 @@ struct Gemm {
       const int row = r0 + lane / Lanes, c = lane % Lanes, o = ow + c * 8;
       const u32x4 v = *reinterpret_cast<const u32x4 *>(lds + row * Row + (((2 * c) ^ twist(row)) << 3));
       bf16_t *y = p.y + (tw + row) * p.ldy + o;
-      if (FULL || (tw + row < p.rows && o + 8 <= p.outs)) {
+      if ((FULL || tw + row < p.rows) && ((FULL && !NN) || o + 8 <= p.outs)) {
         *reinterpret_cast<u32x4_any *>(y) = v;
-      } else if (tw + row < p.rows) {
+      } else if (FULL || tw + row < p.rows) {
 #pragma unroll
         for (int q = 0; q < 7; ++q)
           if (o + q < p.outs) y[q] = (bf16_t)(v[q >> 1] >> (16 * (q & 1)));
@@ -296,7 +297,7 @@ __global__ __launch_bounds__(256, BT == 128 ? 2 : 1) void project_gemm_kernel(Pr
   tile_of(in_runs(blockIdx.x, tiles_t * tiles_o), tiles_t, tiles_o, tt, to);
   int64_t t0 = tt * BT;
   int o0 = to * BO;
-  if constexpr (FULL) t0 = min(t0, p.rows - BT), o0 = min(o0, p.outs - BO);
+  if constexpr (FULL) t0 = min(t0, p.rows - BT), o0 = min(o0, (NN ? (p.outs + 7) / 8 * 8 : p.outs) - BO);
   const int wv = threadIdx.x >> 6;
   const int64_t tw = t0 + (wv / G::WO) * (ET * 32);
   const int ow = o0 + (wv % G::WO) * (EO * 32);
