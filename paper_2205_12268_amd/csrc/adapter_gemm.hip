@@ -21,8 +21,9 @@ namespace {
 
 constexpr int Line = kLine, Chunks = kChunks, PerLoad = 1024 / Line;  // lines of a load
 
-// FULL: a tile lies within the rows and outputs (the last ones are moved back, over others, whose results they repeat).  With NN,
-// outputs count up to whole chunks of 8 there, which W's rows hold: its loads begin at a chunk.
+// FULL: a tile lies within the rows and outputs (the last ones are moved back, over others: rows, whose results they repeat, are
+// stored twice, outputs by the one tile whose they are, since where an adapter is not finite the order of its sums goes by all outputs
+// of a wave).  With NN, outputs count up to whole chunks of 8 there, which W's rows hold: its loads begin at a chunk.
 template <int BT, int BO, int WT, bool NN, bool FULL>
 struct Gemm {
   static constexpr int Waves = 4, WO = Waves / WT;
@@ -251,9 +252,10 @@ struct Gemm {
     }
   }
 
-  // The wave's results to y, rows from tw and outputs from ow on, through its part of LDS: a row's 8-byte pieces are exchanged by a
-  // key of the row (even, so that pairs of them stay together).
-  __device__ static __forceinline__ void store(const Project<bf16_t> &p, int64_t tw, int ow, const f32x16 (&acc)[EO][ET], unsigned char *lds) {
+  // The wave's results to y, rows from tw and outputs from ow on, without those before `from`, through its part of LDS: a row's 8-byte
+  // pieces are exchanged by a key of the row (even, so that pairs of them stay together).
+  __device__ static __forceinline__ void store(const Project<bf16_t> &p, int64_t tw, int ow, int from, const f32x16 (&acc)[EO][ET],
+                                               unsigned char *lds) {
     constexpr int Row = EO * 64, Pieces = Row / 8, Lanes = Row / 16, Rows = 64 / Lanes;  // bytes of a row; rows of a store
     const int lane = threadIdx.x & 63, ln = lane & 31, half = lane >> 5;
     auto twist = [](int row) { return row % (Pieces / 2) * 2; };
@@ -276,12 +278,12 @@ struct Gemm {
       const int row = r0 + lane / Lanes, c = lane % Lanes, o = ow + c * 8;
       const u32x4 v = *reinterpret_cast<const u32x4 *>(lds + row * Row + (((2 * c) ^ twist(row)) << 3));
       bf16_t *y = p.y + (tw + row) * p.ldy + o;
-      if ((FULL || tw + row < p.rows) && ((FULL && !NN) || o + 8 <= p.outs)) {
+      if ((FULL || tw + row < p.rows) && (!FULL || o >= from) && ((FULL && !NN) || o + 8 <= p.outs)) {
         *reinterpret_cast<u32x4_any *>(y) = v;
       } else if (FULL || tw + row < p.rows) {
 #pragma unroll
-        for (int q = 0; q < 7; ++q)
-          if (o + q < p.outs) y[q] = (bf16_t)(v[q >> 1] >> (16 * (q & 1)));
+        for (int q = 0; q < 8; ++q)
+          if ((!FULL || o + q >= from) && o + q < p.outs) y[q] = (bf16_t)(v[q >> 1] >> (16 * (q & 1)));
       }
     }
   }
@@ -297,6 +299,7 @@ __global__ __launch_bounds__(256, BT == 128 ? 2 : 1) void project_gemm_kernel(Pr
   tile_of(in_runs(blockIdx.x, tiles_t * tiles_o), tiles_t, tiles_o, tt, to);
   int64_t t0 = tt * BT;
   int o0 = to * BO;
+  const int from = o0;
   if constexpr (FULL) t0 = min(t0, p.rows - BT), o0 = min(o0, (NN ? (p.outs + 7) / 8 * 8 : p.outs) - BO);
   const int wv = threadIdx.x >> 6;
   const int64_t tw = t0 + (wv / G::WO) * (ET * 32);
@@ -319,7 +322,7 @@ __global__ __launch_bounds__(256, BT == 128 ? 2 : 1) void project_gemm_kernel(Pr
   }
   G::run(p, t0, o0, 0, p.width, xs0, ws0, xs1, ws1, acc);
   unsigned char *own = wv == 0 ? xs0 : wv == 1 ? ws0 : wv == 2 ? xs1 : ws1;
-  G::store(p, tw, ow, acc, own);
+  G::store(p, tw, ow, from, acc, own);
 }
 
 // Ranges of k: a workgroup leaves its sums as they are.  Before the tiles, workgroups of rank lines.
