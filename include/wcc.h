@@ -380,8 +380,8 @@ wcc_status wcc_token_scores(wcc_ctx *ctx, const wcc_scores_desc *desc, const voi
  *   dlogits[t,v] = weight[t] temperature (p[v] - sum_{k: t_idx_k = v} q_k)
  * the gradient of sum_t weight[t] loss[t] (weight nullable: 1).  A row without a pair, and one whose
  * logits are all -inf, has loss 0 and gradient 0; where p is 0 and q is not the loss is +inf.
- * (logits / temperature below fp32's range count as -inf; above it they are as +inf, whose results,
- * like those of NaN, are NaN or unspecified.)
+ * (logits / temperature and t_logit / temperature below fp32's range count as -inf; above it they are
+ * as +inf, whose results, like those of NaN, are NaN or unspecified.)
  * t_idx [rows, K] int32 and t_logit [rows, K] are contiguous. */
 typedef struct {
   int64_t rows;            /* >= 0 and < 2^31                                                     */

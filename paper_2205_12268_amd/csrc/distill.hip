@@ -38,9 +38,9 @@ struct Pairs {
       log_q[p] = -INFINITY;  // (the logit, until solve())
       if (k < te.K) {
         const int i = te.idx[t * te.K + k];
-        const float z = te.bf16 ? widen(static_cast<const bf16_t *>(te.logit)[t * te.K + k])
-                                : static_cast<const float *>(te.logit)[t * te.K + k];
-        if ((uint32_t)i < (uint32_t)V && z != -INFINITY) at[p] = i, log_q[p] = z * inv_tau;
+        const float z = (te.bf16 ? widen(static_cast<const bf16_t *>(te.logit)[t * te.K + k])
+                                 : static_cast<const float *>(te.logit)[t * te.K + k]) * inv_tau;
+        if ((uint32_t)i < (uint32_t)V && z != -INFINITY) at[p] = i, log_q[p] = z;
       }
     }
   }
