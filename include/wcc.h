@@ -399,14 +399,16 @@ wcc_status wcc_distill_workspace_bytes(const wcc_distill_desc *desc, size_t *byt
 /* The loss, and with dlogits given its gradient in the same call, which reads a row once where the
  * row fits a compute unit.  dlogits may be logits itself if ld_grad = ld.  stats [rows, 2] receives
  * a row's largest m = max_v logits[v] / temperature and log sum_v exp(logits[v] / temperature - m),
- * whose sum is lse: apart, they keep what a sum in fp32 loses beside a large m.  Both are -inf in a
- * row that has nothing left. */
+ * whose sum is lse: apart, they keep what a sum in fp32 loses beside a large m.  (m is rounded, the
+ * second relative to it as it is written; from |m| = 2^28 on relative to the quotient itself.)  Both are
+ * -inf in a row that has nothing left. */
 wcc_status wcc_distill_forward(wcc_ctx *ctx, const wcc_distill_desc *desc, const void *logits,
                                const int32_t *t_idx, const void *t_logit, float *loss,
                                float *stats /*nullable*/, const float *weight /*nullable*/,
                                void *dlogits /*nullable*/, void *stream);
 
-/* The gradient, from the stats that wcc_distill_forward gave. */
+/* The gradient, from the stats that wcc_distill_forward gave.  (From |m| = 2^28 on logits / temperature
+ * are taken as fp32 has them, in steps of 32 and more: values that round alike count as equal.) */
 wcc_status wcc_distill_backward(wcc_ctx *ctx, const wcc_distill_desc *desc, const void *logits,
                                 const int32_t *t_idx, const void *t_logit, const float *stats,
                                 const float *weight /*nullable*/, void *dlogits, void *stream);

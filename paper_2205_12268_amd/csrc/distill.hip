@@ -128,6 +128,11 @@ __device__ __forceinline__ float largest(const u32x4 (&v)[NV], float *part) {
   return block_all<NT>(m, part, Larger());
 }
 
+// m = largest / temperature from here on: its rounding to fp32 moves exponents by up to 32 and more, which the log of the sum cannot
+// carry (at 1e38 it would leave nothing else of it).  The log of the sum is then relative to the largest logit itself, and from the
+// stats a logit's exponent is the difference of quotients rounded alike: 0 at the largest, exact to fp32's steps (32 and more) at others.
+constexpr float kFar = 268435456.f;  // 2^28
+
 struct Row {
   float *loss, *stats;
   const float *weight;
@@ -152,9 +157,9 @@ __device__ __forceinline__ void write_loss(const Row &o, int64_t t, const Pairs<
     if (o.loss) o.loss[t] = o.tau * o.tau * l;
     if (o.stats) {
       // (m is rounded; what that takes off goes to the other one, whose sum is then relative to m as it is written)
-      const float m = mx * o.inv_tau;
+      const float m = S == 0.f ? -INFINITY : mx / o.tau;
       o.stats[2 * t] = m;
-      o.stats[2 * t + 1] = S == 0.f ? -INFINITY : log_s + fmaf(base, o.inv_tau, -m);
+      o.stats[2 * t + 1] = S == 0.f ? -INFINITY : fabsf(m) >= kFar ? log_s : log_s + fmaf(base, o.inv_tau, -m);
     }
   }
 }
@@ -292,13 +297,19 @@ __global__ __launch_bounds__(NT, 4) void distill_grad_kernel(const T *x, int64_t
     const bool live = pr.some && S != 0.f;
     const float f = out.tau * (out.weight ? out.weight[t] : 1.f);
     T *o = dx + t * ldg + first;
-    write_p<T, NT, NV>(o, n, v, ex, f / S, live);
+    const bool far = !parts && live && fabsf(ex.b) >= kFar;
+    auto far_p = [&](float z) { return __builtin_amdgcn_exp2f((z / out.tau - ex.b) * kLog2e); };
+    if (far) {
+      for (int i = threadIdx.x; i < n; i += NT) o[i] = narrow<T>(f / S * far_p(widen(r[i])));  // (r may be o: an element at a time)
+    } else {
+      write_p<T, NT, NV>(o, n, v, ex, f / S, live);
+    }
     __syncthreads();
 #pragma unroll
     for (int p = 0; p < Pr::P; ++p) {
       const int i = pr.at[p] - first;
       if (pr.at[p] >= 0 && i >= 0 && i < n && live)
-        o[i] = narrow<T>(f * (__builtin_amdgcn_exp2f(ex(own[p])) / S - mass[p]));
+        o[i] = narrow<T>(f * ((far ? far_p(own[p]) : __builtin_amdgcn_exp2f(ex(own[p]))) / S - mass[p]));
     }
     __syncthreads();
   }
