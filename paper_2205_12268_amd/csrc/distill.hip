@@ -291,25 +291,32 @@ __global__ __launch_bounds__(NT, 4) void distill_grad_kernel(const T *x, int64_t
     } else {
       ex = Exponent{out.inv_tau, out.stats[2 * t], kLog2e};
       S = expf(out.stats[2 * t + 1]);
+      if (fabsf(ex.b) >= kFar) {  // (the differences take the logits' places: bf16 ones are 0 or beyond -2^18, which rounding leaves so)
+        auto apart = [&](float z) { return z / out.tau - ex.b; };
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          float d[VecOf<T>::N];
+#pragma unroll
+          for (int j = 0; j < VecOf<T>::N; ++j) d[j] = apart(elem<T>(v[i], j));
+          v[i] = pack<T>(d);
+        }
+#pragma unroll
+        for (int p = 0; p < Pr::P; ++p) own[p] = apart(own[p]);
+        ex = Exponent{1.f, 0.f, kLog2e};
+      }
     }
     float mass[Pr::P];
     masses<NT>(pr, te.K, at_s, q_s, mass);
     const bool live = pr.some && S != 0.f;
     const float f = out.tau * (out.weight ? out.weight[t] : 1.f);
     T *o = dx + t * ldg + first;
-    const bool far = !parts && live && fabsf(ex.b) >= kFar;
-    auto far_p = [&](float z) { return __builtin_amdgcn_exp2f((z / out.tau - ex.b) * kLog2e); };
-    if (far) {
-      for (int i = threadIdx.x; i < n; i += NT) o[i] = narrow<T>(f / S * far_p(widen(r[i])));  // (r may be o: an element at a time)
-    } else {
-      write_p<T, NT, NV>(o, n, v, ex, f / S, live);
-    }
+    write_p<T, NT, NV>(o, n, v, ex, f / S, live);
     __syncthreads();
 #pragma unroll
     for (int p = 0; p < Pr::P; ++p) {
       const int i = pr.at[p] - first;
       if (pr.at[p] >= 0 && i >= 0 && i < n && live)
-        o[i] = narrow<T>(f * ((far ? far_p(own[p]) : __builtin_amdgcn_exp2f(ex(own[p]))) / S - mass[p]));
+        o[i] = narrow<T>(f * (__builtin_amdgcn_exp2f(ex(own[p])) / S - mass[p]));
     }
     __syncthreads();
   }
