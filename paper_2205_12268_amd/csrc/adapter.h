@@ -6,6 +6,8 @@
 // which is all that matters).
 #pragma once
 
+#include <type_traits>
+
 #include "head.h"
 #include "rows.h"
 
@@ -128,6 +130,16 @@ __device__ __forceinline__ void load_k_pair(const T *p, int64_t sk, int left, bo
 // bf16 operands carry 8 bits each: P of them take P * 8 bits of the values, the rest of each going to the next.
 __device__ __forceinline__ float left_of(float v, uint32_t part) {  // (nothing of an infinity, or it would be NaN)
   return (part & 0x7f80) == 0x7f80 ? 0.f : v - __uint_as_float(part << 16);
+}
+// bf16 operands with 0 in the place of infinities and NaN: what meets parts past the first, which are 0 where the first has all of a
+// value, so that an infinity by a value is not made NaN by its parts
+__device__ __forceinline__ u32x4 finite_of(u32x4 v) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if ((v[i] & 0x7f80u) == 0x7f80u) v[i] &= 0xffff0000u;
+    if ((v[i] & 0x7f800000u) == 0x7f800000u) v[i] &= 0xffffu;
+  }
+  return v;
 }
 template <class T, int P>
 __device__ __forceinline__ void split_to(const float *v, u32x4 (&f)[P]) {
@@ -298,7 +310,7 @@ __device__ __forceinline__ void add_thin(const Low &low, const Thin<T> &m, int l
   };
   const u32x4 zeros = {0, 0, 0, 0};
   // (one e at a time, all of a row's steps)
-  auto product = [&](const T *h, int j, const u32x4 &mf, bool mine, f32x16 c) {
+  auto product = [&](auto apart, const T *h, int j, const u32x4 &mf, bool mine, f32x16 c) {
     u32x4 hf[P];
 #pragma unroll
     for (int q = 0; q < P; ++q) {
@@ -306,7 +318,16 @@ __device__ __forceinline__ void add_thin(const Low &low, const Thin<T> &m, int l
       hf[q] = mine && j < ld ? v : zeros;
     }
 #pragma unroll
-    for (int q = P - 1; q >= 0; --q) c = ROWS ? mma<T>(hf[q], mf, c) : mma<T>(mf, hf[q], c);
+    for (int q = P - 1; q >= 0; --q) {
+      u32x4 m = mf;
+      if constexpr (apart && P > 1) {
+        if (q > 0) {
+          asm volatile("" : "+v"(m));  // (made where it is used: kept for all rows' products, it would cost registers of the loop above)
+          m = finite_of(m);
+        }
+      }
+      c = ROWS ? mma<T>(hf[q], m, c) : mma<T>(m, hf[q], c);
+    }
     return c;
   };
   u32x4 mf[J][E];
@@ -354,7 +375,7 @@ __device__ __forceinline__ void add_thin(const Low &low, const Thin<T> &m, int l
       for (int s = 0; s < J; ++s)
         if (s == 0 || s * KS < low.rank)
 #pragma unroll
-          for (int e = 0; e < E; ++e) acc[e][r] = product(h, j0 + s * KS + half * VE, mf[s][e], mine, acc[e][r]);
+          for (int e = 0; e < E; ++e) acc[e][r] = product(std::false_type{}, h, j0 + s * KS + half * VE, mf[s][e], mine, acc[e][r]);
     }
     a = next, lines = next_lines, j0 = next_j;
 #pragma unroll
@@ -395,7 +416,7 @@ __device__ __forceinline__ void add_thin(const Low &low, const Thin<T> &m, int l
         for (int e = 0; e < E; ++e) {
           f32x16 d = {};
 #pragma unroll
-          for (int s = 0; s < J; ++s) d = product(lines_of(r), j0 + s * KS + half * VE, mf[s][e], true, d);
+          for (int s = 0; s < J; ++s) d = product(std::true_type{}, lines_of(r), j0 + s * KS + half * VE, mf[s][e], true, d);
 #pragma unroll
           for (int i = 0; i < 16; ++i) acc[e][r][i] += (ROWS ? (same >> result_line(i, half) & 1) != 0 : mine) ? d[i] : 0.f;
         }

@@ -276,7 +276,7 @@ template <class T>
 struct GradLds {
   static constexpr int P = PartsOf<T>::Grad;
   T h[P][32][kListed];
-  int list[kListed], rest[16], counts[2][4];
+  int list[kListed], rest[16], counts[2][4], odd[2][4];
 };
 
 // four columns (some of them past the width) of a row
@@ -302,8 +302,10 @@ __device__ __forceinline__ void load_four(const T *p, int left, uint32_t (&v)[(i
   }
 }
 
-template <class T, bool FLIP>
-__device__ __forceinline__ void grad_block(const GradJob<T> &g, const Low &low, int64_t rows, int splits, int64_t range, int64_t block,
+// AGAIN: an infinity of x meets no part of a line past the first, which is 0 where the first has all of it (infinity times 0 is NaN).
+// Whether sums of the wave are not finite: then the workgroup has to do the block so (bf16).
+template <class T, bool FLIP, bool AGAIN>
+__device__ __forceinline__ bool grad_block(const GradJob<T> &g, const Low &low, int64_t rows, int splits, int64_t range, int64_t block,
                                            GradLds<T> &lds) {
   constexpr int VE = VecOf<T>::N, KS = StepOf<T>::K, P = GradLds<T>::P, D = (int)sizeof(T);
   const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, ln = lane & 31, half = lane >> 5;
@@ -326,7 +328,7 @@ __device__ __forceinline__ void grad_block(const GradJob<T> &g, const Low &low, 
     }
     if (splits > 1 && __ballot(any) == 0) {
       if (tile_c == 0 && j0 == 0 && tid == 0) g.found[(int64_t)split * low.n + a] = 0;
-      return;
+      return false;
     }
   }
 
@@ -356,7 +358,10 @@ __device__ __forceinline__ void grad_block(const GradJob<T> &g, const Low &low, 
           xf[i] = __builtin_amdgcn_perm(v[2 * i + 1][e >> 1], v[2 * i][e >> 1], e & 1 ? 0x07060302 : 0x05040100);
       }
 #pragma unroll
-      for (int p = P - 1; p >= 0; --p) acc[e] = FLIP ? mma<T>(xf, hf[p], acc[e]) : mma<T>(hf[p], xf, acc[e]);
+      for (int p = P - 1; p >= 0; --p) {
+        const u32x4 xp = AGAIN && p > 0 ? finite_of(xf) : xf;
+        acc[e] = FLIP ? mma<T>(xp, hf[p], acc[e]) : mma<T>(hf[p], xp, acc[e]);
+      }
     }
   };
   // the operands of listed rows from..to of h; zeros to the end of their step
@@ -373,7 +378,7 @@ __device__ __forceinline__ void grad_block(const GradJob<T> &g, const Low &low, 
         for (int p = 0; p < P; ++p) {
           const bf16_t b = narrow<bf16_t>(v);
           lds.h[p][line][q] = b;
-          v -= widen(b);
+          v = left_of(v, b);
         }
       }
     }
@@ -434,9 +439,9 @@ __device__ __forceinline__ void grad_block(const GradJob<T> &g, const Low &low, 
   }
   if (splits > 1) {
     if (tile_c == 0 && j0 == 0 && tid == 0) g.found[(int64_t)split * low.n + a] = total;
-    if (total == 0) return;
+    if (total == 0) return false;
   }
-  if (!busy) return;
+  if (!busy) return false;
   float *out = g.out + (splits > 1 ? split * g.size : 0) + a * g.major;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
@@ -447,16 +452,35 @@ __device__ __forceinline__ void grad_block(const GradJob<T> &g, const Low &low, 
       if (line < low.rank && col < g.width) out[(int64_t)line * g.sj + (int64_t)col * g.sc] = line < lines ? acc[e][i] : 0.f;
     }
   }
+  float none[4] = {};
+  if constexpr (P > 1 && !AGAIN) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) none[e] = fmaf(acc[e][i], 0.f, none[e]);
+  }
+  return __ballot((none[0] + none[1]) + (none[2] + none[3]) != 0.f) != 0;
 }
 
 // dA's blocks, then dB's (whose lines are the contiguous ones: its results lie the other way round)
 template <class T>
 __global__ __launch_bounds__(256, 3) void adapter_grad_kernel(GradJob<T> ga, GradJob<T> gb, Low low, int64_t rows, int splits, int64_t range) {
   __shared__ __align__(16) GradLds<T> lds;
-  for (int64_t b = blockIdx.x; b < ga.blocks + gb.blocks; b += gridDim.x) {
-    if (b < ga.blocks) grad_block<T, false>(ga, low, rows, splits, range, b, lds);
-    else grad_block<T, true>(gb, low, rows, splits, range, b - ga.blocks, lds);
+  int turn = 0;
+  for (int64_t b = blockIdx.x; b < ga.blocks + gb.blocks; b += gridDim.x, turn ^= 1) {
+    const bool odd = b < ga.blocks ? grad_block<T, false, false>(ga, low, rows, splits, range, b, lds)
+                                   : grad_block<T, true, false>(gb, low, rows, splits, range, b - ga.blocks, lds);
+    if constexpr (GradLds<T>::P > 1) {
+      if ((threadIdx.x & 63) == 0) lds.odd[turn][threadIdx.x >> 6] = odd;
+    }
     __syncthreads();
+    if constexpr (GradLds<T>::P > 1) {
+      const int *all = lds.odd[turn];
+      if ((all[0] | all[1] | all[2] | all[3]) == 0) continue;
+      if (b < ga.blocks) grad_block<T, false, true>(ga, low, rows, splits, range, b, lds);
+      else grad_block<T, true, true>(gb, low, rows, splits, range, b - ga.blocks, lds);
+      __syncthreads();
+    }
   }
 }
 
