@@ -389,7 +389,7 @@ typedef struct {
   int32_t K;               /* teacher's pairs a row, 1 .. WCC_MAX_TEACHER                         */
   int32_t dtype;           /* of logits and dlogits: WCC_F32 or WCC_BF16                         */
   int32_t t_dtype;         /* of t_logit: WCC_F32 or WCC_BF16                                    */
-  float temperature;       /* > 0, finite                                                         */
+  float temperature;       /* > 0, finite, and log2(e) / temperature finite (from 4.25e-39 on)    */
   int64_t ld, ld_grad;     /* row strides of logits and dlogits, >= V                             */
 } wcc_distill_desc;
 #define WCC_MAX_TEACHER 256

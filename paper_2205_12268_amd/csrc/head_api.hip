@@ -41,7 +41,8 @@ wcc_status check(const wcc_distill_desc *d) {
   if (!real_type(d->dtype) || !real_type(d->t_dtype)) return WCC_ERR_DTYPE;
   if (d->rows < 0 || d->rows > kMostRows || d->V < 1 || d->K < 1) return WCC_ERR_SHAPE;
   if (bad_stride(d->ld, d->V) || bad_stride(d->ld_grad, d->V)) return WCC_ERR_SHAPE;
-  if (!(d->temperature > 0.f) || !std::isfinite(d->temperature) || !std::isfinite(1.f / d->temperature)) return WCC_ERR_SHAPE;
+  // (exponents are made with log2(e) / temperature)
+  if (!(d->temperature > 0.f) || !std::isfinite(d->temperature) || !std::isfinite(1.f / d->temperature * 1.44269504f)) return WCC_ERR_SHAPE;
   if (d->K > WCC_MAX_TEACHER) return WCC_ERR_UNSUPPORTED;
   return WCC_OK;
 }

@@ -39,3 +39,13 @@ def test_workspaces_are_whole_blocks(t):
                      (wcc.adapter_workspace_bytes, wcc.make_adapter_desc(rows, 1000, width, 0, 0, t))]
             for call, d in descs:
                 assert call(d) >= 0 and call(d) % 256 == 0
+
+
+def test_temperatures_whose_factor_overflows_are_refused():
+    """log2(e) / temperature is what a logit's difference is multiplied by: infinite, it made the largest logit's 0 NaN."""
+    for tau in (1e-45, 2.9e-39, 3e-39, 3.5e-39, 4.2e-39):
+        with pytest.raises(wcc.WccError) as e:
+            wcc.distill_workspace_bytes(wcc.make_distill_desc(5, 100, 3, wcc.F32, temperature=tau))
+        assert e.value.status == 2
+    for tau in (4.3e-39, 1e-38, 1.0, 3e38):
+        assert wcc.distill_workspace_bytes(wcc.make_distill_desc(5, 100, 3, wcc.F32, temperature=tau)) >= 0
