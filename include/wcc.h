@@ -306,19 +306,20 @@ wcc_status wcc_set_block_profile_layer(wcc_ctx *ctx, int layer);
  * rounded once, to nearest even, from fp32; sums, statistics of rows and gradients of adapters are
  * fp32.  Sums are added in an order that depends on the descriptor and on the alignment of the
  * tensors (and, for an adapter that holds infinities or NaN, on that), so equal calls give equal
- * bits.  What is not finite in a row or an adapter reaches no other row's results.  Nothing but what is said below depends on the contents of index tensors: a value
- * outside its range counts as "none". */
+ * bits.  What is not finite in a row or an adapter reaches no other row's results.  Nothing but
+ * what is said below depends on the contents of index tensors: a value outside its range counts as
+ * "none". */
 
 /* ---- one projection, an adapter for each row ---------------------------------------------------
  * y[t,:] = W x[t,:] + s_a B_a (A_a x[t,:]),   a = adapter_of_row[t]; a outside [0, adapters)
- * means W x[t,:] alone.
+ * means W x[t,:] alone (with adapter_of_row NULL or no adapters a and b are not read and may be NULL).
  *   x [rows, C_in] stride ldx   w [C_out, C_in]   y [rows, C_out] stride ldy
  *   a [adapters, rank, C_in]    b [adapters, C_out, rank]
  *   ranks [adapters] int32, nullable: adapter i has the first ranks[i] of the `rank` lines its
  *     memory holds (clamped to 0..rank; the others are not used, whatever they hold)
  *   scale [adapters] fp32, nullable: s (else 1)
  * All matrices have the one type of `dtype`.  The products with bf16 matrices are exact in fp32;
- * A x keeps 16 significant bits of its sum on the way into B (and B^T dy into A). */
+ * from 65 rows on A x keeps 16 significant bits of its sum on the way into B (and B^T dy into A). */
 typedef struct {
   int64_t rows;            /* tokens, >= 0 and < 2^31                                            */
   int32_t C_in, C_out;     /* 1 .. 2^20                                                           */
@@ -361,7 +362,7 @@ typedef struct {
   int32_t V;               /* logits a row, >= 1                                                  */
   int32_t top;             /* alternatives, 0 .. min(V, WCC_MAX_TOP)                              */
   int32_t dtype;           /* of the logits: WCC_F32 or WCC_BF16                                 */
-  int64_t ld;              /* row stride, >= V                                                    */
+  int64_t ld;              /* row stride, >= V and < 2^31                                         */
 } wcc_scores_desc;
 #define WCC_MAX_TOP 64
 
@@ -390,7 +391,7 @@ typedef struct {
   int32_t dtype;           /* of logits and dlogits: WCC_F32 or WCC_BF16                         */
   int32_t t_dtype;         /* of t_logit: WCC_F32 or WCC_BF16                                    */
   float temperature;       /* > 0, finite, and log2(e) / temperature finite (from 4.25e-39 on)    */
-  int64_t ld, ld_grad;     /* row strides of logits and dlogits, >= V                             */
+  int64_t ld, ld_grad;     /* row strides of logits and dlogits, >= V and < 2^31                  */
 } wcc_distill_desc;
 #define WCC_MAX_TEACHER 256
 

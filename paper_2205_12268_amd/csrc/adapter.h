@@ -277,9 +277,10 @@ __device__ __forceinline__ void gather_lines(const Low &low, const Lines &h, F r
 // Of each adapter among the rows J steps of lines at a time, the next ones' operands on their way meanwhile; of the distinct adapters
 // every turn-th from the first-th on.  The lines of rows with other adapters are replaced by zeros, except where an adapter holds
 // infinities or NaN (a product of its operands with zeros tells): its sums are made apart then, and rows take none but their own.
-// (With all sums apart, and the lines of each 32 rows by themselves: 8192 rows, 4096 -> 4096, 8 adapters of rank 32 in runs 318 us
-// instead of 292.  With the additions for operands that are not finite in the one loop, whose results then moved between the
-// registers of the vector unit and of the matrix cores: 4096 rows, 4096 -> 4096, 24 adapters in mixed order 244 us instead of 195.)
+// (With all sums apart, and the lines of each 32 rows by themselves: 8192 rows, 4096 -> 4096, 8 adapters of rank 32 in runs took a
+// tenth longer.  With the additions for operands that are not finite in the one loop, whose results then moved between the
+// registers of the vector unit and of the matrix cores: 4096 rows, 4096 -> 4096, 24 adapters in mixed order 244 us instead of 195.
+// In that loop 256 x 256 tiles run out of registers and spill; the others do not.)
 template <class T, int E, int R, bool ROWS, int J, class F>
 __device__ __forceinline__ void add_thin(const Low &low, const Thin<T> &m, int ld, F lines_of, int64_t rows, int outs, int64_t t0,
                                          const int (&o)[E], f32x16 (&acc)[E][R], int first = 0, int turn = 1) {

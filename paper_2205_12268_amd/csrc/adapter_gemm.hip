@@ -11,9 +11,9 @@
 // which leave through LDS as whole lines.
 // The last stages, which the end of k cuts, are not overlapped; chunks past the end (and, NN, past the last output) come from 16
 // bytes of zeros.
-// Bound by the matrix cores and what feeds them: 8192 rows, 4096 -> 4096 267 us (1.03 PFLOP/s), the other order of W 248 (1.11), 8192 in
-// all three 0.93 ms (1.18 PFLOP/s); 128 x 128 tiles 1024 rows, 4096 -> 4096 57 us.  24 adapters in mixed order add 17 us
-// there.  Not kept: four stages of 32 k (300 us), bands of 4 or 16 row tiles (270 to 277), a priority for waves that multiply.
+// Bound by the matrix cores and what feeds them: 8192 rows, 4096 -> 4096 236 us on inputs that stay in the caches (1.17 PFLOP/s), the
+// other order of W 225 (1.22), 8192 in all three 0.90 ms (1.22 PFLOP/s); 128 x 128 tiles 1024 rows, 4096 -> 4096 44 us; with 8 adapters
+// of rank 32 and inputs in turn the 8192 rows take 259 to 287.  24 adapters in mixed order add 17 us to 1024 rows.  Not kept: four stages of 32 k (300 us), bands of 4 or 16 row tiles (270 to 277), a priority for waves that multiply.
 #include "adapter.h"
 
 namespace wcc {

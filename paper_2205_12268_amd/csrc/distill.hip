@@ -9,7 +9,7 @@
 // are rows enough, and reads it once for loss and gradient both.  Otherwise rows are cut into slices: a first launch leaves
 // (mx, S) of every slice and the logits at the teacher's places (the second may overwrite them, dlogits being logits), the
 // second joins them, in the order of the slices, in every workgroup that writes a slice's gradient.
-// Loss and gradient of 4096 x 65536 bf16: 214 us, 5.0 TB/s, the rate of a large copy; with a first form that read rows three times 1062.
+// Loss and gradient of 4096 x 65536 bf16: 216 us, 5.0 TB/s, the rate of a large copy, the loss alone 107; with a first form that read rows three times 1062.
 #include "rows.h"
 
 namespace wcc {

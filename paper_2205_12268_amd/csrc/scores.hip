@@ -13,7 +13,7 @@
 // arrival, so the result does not depend on it.
 //
 // Bound by memory where rows are many: 4096 x 32768 bf16 67 us, 4.0 TB/s (55 us at the rate of a large copy; an exponential an element
-// takes the rest); by two launches and their chains of reductions where they are few: one row of 131072 14.4 us, 7.6 and 6.4 of the
+// takes the rest); by two launches and their chains of reductions where they are few: one row of 131072 14.3 us, 7.6 and 6.4 of the
 // kernels.  A first form, a workgroup a row that reads it again for each alternative, took 1252 and 1691 us.
 #include "rows.h"
 
