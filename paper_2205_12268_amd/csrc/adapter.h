@@ -354,7 +354,7 @@ __device__ __forceinline__ void add_thin(const Low &low, const Thin<T> &m, int l
   };
   pass(first);
   int a = -2, lines = 0, j0 = 0;  // (none yet: the first round only loads)
-  bool some_apart = false;
+  bool apart = false, some_apart = false;
   while (a != -1) {
     int next = a, next_lines = lines, next_j = j0 + J * KS;
     if (next_j >= lines) {
@@ -370,7 +370,7 @@ __device__ __forceinline__ void add_thin(const Low &low, const Thin<T> &m, int l
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       if (a < 0) break;
-      const bool mine = id[r] == a;
+      const bool mine = id[r] == a && !apart;  // (a line may be infinite, and its product with the zeros NaN)
       const T *h = lines_of(r);
 #pragma unroll
       for (int s = 0; s < J; ++s)
@@ -383,7 +383,8 @@ __device__ __forceinline__ void add_thin(const Low &low, const Thin<T> &m, int l
     for (int s = 0; s < J; ++s)
 #pragma unroll
       for (int e = 0; e < E; ++e) mf[s][e] = cut_k<T>(nf[s][e], j0 + s * KS + half * VE, lines);
-    if (checked(mf)) {
+    apart = checked(mf);
+    if (apart) {
       some_apart = true;
 #pragma unroll
       for (int s = 0; s < J; ++s)

@@ -96,3 +96,21 @@ def test_lines(ctx, size, bad):
     want = adapter_backward(*v)
     assert bool(torch.isinf(want["db"][0][1]).any())
     same(backward(ctx, *v)["db"], want["db"], 0, ci + rows, False)
+
+
+@pytest.mark.parametrize("bad", [math.inf, -math.inf])
+@pytest.mark.parametrize("size", SIZES, ids=lambda s: "-".join(map(str, s)))
+def test_lines_beside_an_infinite_adapter(ctx, size, bad):
+    """Infinite lines of an adapter that holds an infinity itself: outputs whose elements of B are finite have an infinity, not NaN."""
+    t, rows, ci, co, n, _ = size
+    v = list(inputs(rows, ci, co, n, 1, t, 15, ranks=False))
+    at = rows // 3
+    v[2][at] = 1
+    v[0] = v[0].clone()
+    v[0][at, ci // 2] = bad
+    v[1] = torch.where(v[1] == 0, 1.0, v[1].float().abs()).to(v[1].dtype) * (1 if float(v[3][1, 0, ci // 2]) > 0 else -1)  # W x of the sign of A x
+    v[4] = torch.where(v[4] == 0, 1.0, v[4].float().abs()).to(v[4].dtype)  # and B h
+    v[4][1, co // 2, 0] = math.inf
+    want = adapter_forward(*v[:7])
+    assert bool(torch.isinf(want[0][at]).all())
+    same(forward(ctx, *v[:7]), want, ci, ci + 1, t == "bf16")
