@@ -75,7 +75,7 @@ typedef enum {
   WCC_ERR_UNSUPPORTED = 6, /* valid request this build has no kernel for                  */
   WCC_ERR_HIP = 7,         /* the HIP runtime reported an error                           */
   WCC_ERR_ALIGN = 8        /* a tensor pointer is not 16-byte aligned (the operators on rows
-                              of tokens at the end of this file: not to its elements)     */
+                              at the end of this file: not to what they say)              */
 } wcc_status;
 
 typedef enum { WCC_F32 = 0, WCC_BF16 = 1, WCC_I8 = 2, WCC_I4 = 3 } wcc_dtype;
@@ -413,6 +413,115 @@ wcc_status wcc_distill_forward(wcc_ctx *ctx, const wcc_distill_desc *desc, const
 wcc_status wcc_distill_backward(wcc_ctx *ctx, const wcc_distill_desc *desc, const void *logits,
                                 const int32_t *t_idx, const void *t_logit, const float *stats,
                                 const float *weight /*nullable*/, void *dlogits, void *stream);
+
+/* ==== a block on rows ========================================================================
+ * What a network's blocks do on rows of tokens (or of pixels, channels last), forward and for
+ * training: rows kept in 8 bits until the backward pass, group norm with an activation, and a
+ * gated feed-forward block.  The conventions are those of the head, above. */
+
+/* ---- rows in 8 bits ----------------------------------------------------------------------------
+ * WCC_KEPT_BLOCK neighbouring values of a row share a step 2^e; a value is kept as the nearest
+ * multiple of it (ties to the even one), an int8 code in -127..127.  With m the block's largest
+ * magnitude e = floor(log2 m) - 6, one more if m / 2^e would round to 128, and at least -126: a
+ * value is off by half a step at most, and exact once it has been kept (code * 2^e is a bf16
+ * number).  Exceptions: magnitudes of 127.5 * 2^121 and above are kept as 127 * 2^121; a block that
+ * holds an infinity or NaN stands for NaN throughout.
+ *   x [rows, width] stride ld
+ *   codes [rows, P] int8, P = width rounded up to whole blocks, 0 behind the last value; 16-byte
+ *     aligned
+ *   steps [rows, P / WCC_KEPT_BLOCK] uint8: e + 127, 255 for a block that stands for NaN */
+#define WCC_KEPT_BLOCK 32
+typedef struct {
+  int64_t rows;            /* >= 0 and < 2^31                                                     */
+  int32_t width;           /* 1 .. 2^20                                                           */
+  int32_t dtype;           /* of x: WCC_F32 or WCC_BF16                                          */
+  int64_t ld;              /* row stride of x, >= width and < 2^31                                */
+} wcc_rows_desc;
+
+wcc_status wcc_rows_keep(wcc_ctx *ctx, const wcc_rows_desc *desc, const void *x, int8_t *codes,
+                         uint8_t *steps, void *stream);
+
+/* The values that codes and steps stand for. */
+wcc_status wcc_rows_restore(wcc_ctx *ctx, const wcc_rows_desc *desc, const int8_t *codes,
+                            const uint8_t *steps, void *x, void *stream);
+
+/* Activations: act(z) = z, max(z, 0), z / (1 + exp(-z)), z Phi(z) with the normal distribution Phi.
+ * The slope of WCC_ACT_RELU at 0 is 0.  Results at infinite z are unspecified. */
+typedef enum { WCC_ACT_NONE = 0, WCC_ACT_RELU = 1, WCC_ACT_SILU = 2, WCC_ACT_GELU = 3 } wcc_act;
+
+/* ---- group norm with an activation -------------------------------------------------------------
+ * Over the pixels of a sample that are there and the C / groups channels of a group,
+ *   mean, var = mean of (x - mean)^2, rstd = 1 / sqrt(var + eps)
+ *   y = act(gamma[c] (x - mean) rstd + beta[c])
+ * x and y hold samples * pixels rows of C channels.  counts [samples] int32 (nullable: all): of sample
+ * i the first counts[i] pixels are there (clamped to 0..pixels); the rows behind them are not read,
+ * and in outputs stay as they were.  A sample without pixels has mean 0 and var 0. */
+typedef struct {
+  int32_t samples;         /* >= 0; samples * pixels < 2^31, samples * groups <= 2^23             */
+  int64_t pixels;          /* of a sample, >= 1                                                   */
+  int32_t C, groups;       /* 1 .. 2^20; groups divides C                                         */
+  int32_t act;             /* wcc_act                                                             */
+  int32_t dtype;           /* of x, y and their gradients: WCC_F32 or WCC_BF16                   */
+  float eps;               /* > 0, finite                                                         */
+  int64_t ldx, ldy;        /* row strides of x and dx, of y and dy, >= C and < 2^31               */
+} wcc_group_norm_desc;
+
+/* Workspace of the two calls below for this descriptor (a multiple of 256). */
+wcc_status wcc_group_norm_workspace_bytes(const wcc_group_norm_desc *desc, size_t *bytes);
+
+/* stats [samples, groups, 2] receives mean and rstd.  codes and steps (both or neither): x as
+ * wcc_rows_keep keeps it, in the same pass.  y may be x if ldy = ldx. */
+wcc_status wcc_group_norm_forward(wcc_ctx *ctx, const wcc_group_norm_desc *desc, const void *x,
+                                  const float *gamma /*nullable: 1*/, const float *beta /*nullable: 0*/,
+                                  const int32_t *counts /*nullable*/, void *y, float *stats /*nullable*/,
+                                  int8_t *codes /*nullable*/, uint8_t *steps /*nullable*/, void *stream);
+
+/* The gradients for a gradient dy of y, from x or, with x NULL, from the values that codes and steps
+ * stand for, and from the stats of the forward call.  With xh = (x - mean) rstd, z = gamma xh + beta,
+ * dz = dy act'(z), and the means taken over a group as above:
+ *   dx = rstd (gamma dz - mean(gamma dz) - xh mean(gamma dz xh))
+ *   dgamma = sum dz xh, dbeta = sum dz over all samples and pixels   (fp32, written whole)
+ * dx may be dy if ldx = ldy. */
+wcc_status wcc_group_norm_backward(wcc_ctx *ctx, const wcc_group_norm_desc *desc,
+                                   const void *x /*nullable*/, const int8_t *codes, const uint8_t *steps,
+                                   const float *gamma, const float *beta, const int32_t *counts,
+                                   const float *stats, const void *dy, void *dx /*nullable*/,
+                                   float *dgamma /*nullable*/, float *dbeta /*nullable*/, void *stream);
+
+/* ---- the gated feed-forward block --------------------------------------------------------------
+ * Of each row, with g = w_gate x and u = w_up x:   y = act(g) u
+ *   x [rows, C_in] stride ldx   w_gate, w_up [C_out, C_in]   y [rows, C_out] stride ldy
+ * All matrices have the one type of `dtype`; products are summed in fp32. */
+typedef struct {
+  int64_t rows;            /* tokens, >= 0 and < 2^31                                            */
+  int32_t C_in, C_out;     /* 1 .. 2^20                                                           */
+  int32_t act;             /* wcc_act                                                             */
+  int32_t dtype;           /* WCC_F32 or WCC_BF16                                                */
+  int32_t train;           /* 0: the workspace holds the forward call alone; else both            */
+  int64_t ldx, ldy;        /* row strides of x and dx, of y and dy: < 2^31                        */
+} wcc_gated_desc;
+
+/* Workspace of the calls below for this descriptor (a multiple of 256).  With more than 2^23 tiles of
+ * 128 rows by 64 channels: WCC_ERR_UNSUPPORTED. */
+wcc_status wcc_gated_workspace_bytes(const wcc_gated_desc *desc, size_t *bytes);
+
+/* codes and steps (both or neither) receive g and u as wcc_rows_keep keeps rows of C_out values, from
+ * their fp32 sums: g's codes [rows, P], then u's; steps alike.  y overlaps no input. */
+wcc_status wcc_gated_forward(wcc_ctx *ctx, const wcc_gated_desc *desc, const void *x,
+                             const void *w_gate, const void *w_up, void *y, int8_t *codes /*nullable*/,
+                             uint8_t *steps /*nullable*/, void *stream);
+
+/* The gradients for a gradient dy of y (each in the type of x, nullable; dw_* written whole):
+ *   dg = dy u act'(g), du = dy act(g)
+ *   dx = w_gate^T dg + w_up^T du      dw_gate = sum_t dg x^T      dw_up = sum_t du x^T
+ * x is x or, with x NULL, the values that x_codes and x_steps stand for; g and u are those that codes
+ * and steps stand for, or made again with codes NULL.  bf16: dg and du are rounded to bf16 on their
+ * way into the products.  x (or its codes) may be NULL if codes are given and dw_gate and dw_up are
+ * NULL, the weights if codes are given and dx is NULL.  Outputs overlap no input. */
+wcc_status wcc_gated_backward(wcc_ctx *ctx, const wcc_gated_desc *desc, const void *x,
+                              const int8_t *x_codes, const uint8_t *x_steps, const void *w_gate,
+                              const void *w_up, const int8_t *codes, const uint8_t *steps,
+                              const void *dy, void *dx, void *dw_gate, void *dw_up, void *stream);
 
 #ifdef __cplusplus
 }

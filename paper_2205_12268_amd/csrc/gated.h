@@ -1,0 +1,115 @@
+// The gated feed-forward block: what its translation units share.
+//
+// With g = Wg x and u = Wu x of a row:  y = act(g) u,  dg = dy u act'(g),  du = dy act(g),
+//   dx = Wg^T dg + Wu^T du,  dWg = sum_t dg x^T,  dWu = sum_t du x^T.
+// dg and du of all rows are held in the workspace, [rows][2][room of C_out] in the type of x: rounded to bf16 once, which the products
+// they go into need anyway.
+#pragma once
+
+#include "block.h"
+#include "tiles.h"
+
+namespace wcc {
+
+constexpr int kRoom = 64;  // lines of d are a multiple of this long, zeros behind C_out
+inline int64_t room_of(int64_t width) { return (width + kRoom - 1) / kRoom * kRoom; }
+
+// Where a pair of projections goes.
+template <class T>
+struct Gate {
+  int64_t rows;
+  int outs;
+  // forward
+  T *y;
+  int64_t ldy;
+  int8_t *codes;   // nullable: [2][rows][blocks * 32]
+  uint8_t *steps;  // [2][rows][blocks]
+  // backward
+  const T *dy;     // stride ldy
+  T *d;            // [rows][2][room]
+  int64_t room;
+};
+
+// 4 neighbouring outputs from o on (o a multiple of 4) of row t.  Forward: step bytes of the blocks they lie in, where codes are kept.
+// What lies behind the last output is 0 in codes and in d.
+template <class T, int ACT, bool BACK>
+__device__ __forceinline__ void finish(const Gate<T> &p, int64_t t, int o, float (&g)[4], float (&u)[4], uint32_t gb, uint32_t ub) {
+  const int left = p.outs - o;
+  T *out = BACK ? nullptr : p.y + t * p.ldy + o;
+  if constexpr (!BACK) {
+    if (p.codes) {
+      const int64_t blocks = (p.outs + kKept - 1) / kKept, at = t * blocks * kKept + o, up = p.rows * blocks * kKept;
+      if (o < blocks * kKept) {
+        *reinterpret_cast<uint32_t *>(p.codes + at) = gb == 255 ? 0 : codes_of(g[0], g[1], g[2], g[3], per_step(gb));
+        *reinterpret_cast<uint32_t *>(p.codes + up + at) = ub == 255 ? 0 : codes_of(u[0], u[1], u[2], u[3], per_step(ub));
+        if (o % kKept == 0) {
+          p.steps[t * blocks + o / kKept] = (uint8_t)gb;
+          p.steps[p.rows * blocks + t * blocks + o / kKept] = (uint8_t)ub;
+        }
+      }
+    }
+    float f[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float v, s;
+      act_of<T, ACT>(g[j], v, s);
+      f[j] = v * u[j];
+    }
+    if (left >= 4) {
+      if constexpr (sizeof(T) == 4) {
+        *reinterpret_cast<f32x4_any *>(out) = f32x4_any{f[0], f[1], f[2], f[3]};
+      } else {
+        typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+        *reinterpret_cast<u32x2_any *>(out) = u32x2_any{(uint32_t)narrow<bf16_t>(f[0]) | (uint32_t)narrow<bf16_t>(f[1]) << 16,
+                                                        (uint32_t)narrow<bf16_t>(f[2]) | (uint32_t)narrow<bf16_t>(f[3]) << 16};
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 3; ++j)
+        if (j < left) out[j] = narrow<T>(f[j]);
+    }
+  } else {
+    const T *top = p.dy + t * p.ldy + o;
+    T dg[4], du[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float v, s;
+      act_of<T, ACT>(g[j], v, s);
+      const float dy = j < left ? widen(top[j]) : 0.f;
+      dg[j] = narrow<T>(j < left ? dy * u[j] * s : 0.f), du[j] = narrow<T>(j < left ? dy * v : 0.f);
+    }
+    T *at = p.d + t * 2 * p.room + o;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) at[j] = dg[j], at[p.room + j] = du[j];
+  }
+}
+
+// A line of an operand is at p + line * s (k contiguous) or p + line (lines contiguous, k s apart).
+template <class T>
+struct Side {
+  const T *p;
+  int64_t s;
+  int64_t lines;
+};
+// result[row of a][line of b] = sum over phases and k of a(row, k) b(line, k)
+template <class T>
+struct Product {
+  Side<T> a[2], b[2];
+  int phases;
+  int64_t k;     // of each phase
+  T *out[2];     // per batch: with two batches a[i], b[i] give out[i]
+  int64_t ld;
+  int batches;
+};
+
+// fp32 sums of ranges of k that the calls below leave in the workspace, in bytes
+size_t tile_gate_parts(int64_t rows, int64_t outs, int64_t k);
+size_t tile_product_parts(int64_t rows, int64_t lines, int64_t k, int batches);
+
+template <class T>
+hipError_t tile_gate(const Gate<T> &p, int act, bool back, const Side<T> &x, const T *w_gate, const T *w_up, int64_t k, float *part,
+                     hipStream_t s);
+template <class T, bool AT>
+hipError_t tile_product(const Product<T> &p, float *part, hipStream_t s);
+
+}  // namespace wcc

@@ -17,6 +17,8 @@ LIB_PATH = os.path.join(_HERE, "csrc", "libwcc.so")
 F32, BF16, I8, I4 = 0, 1, 2, 3
 STATIC_SCRATCH_BYTES = 64 << 20  # WCC_STATIC_SCRATCH_BYTES of wcc.h
 NORM_L1, NORM_L2 = 0, 1
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU = 0, 1, 2, 3
+KEPT_BLOCK = 32  # WCC_KEPT_BLOCK of wcc.h
 STAGES = ("haar_fwd", "norm_select", "gather", "pointwise", "scatter_ihaar", "event_pair",
           "depthwise")
 
@@ -27,7 +29,10 @@ EXPORTS = ("wcc_create", "wcc_destroy", "wcc_workspace_bytes", "wcc_set_workspac
            "wcc_set_block_profile_layer", "wcc_block_is_chained",
            "wcc_adapter_workspace_bytes", "wcc_adapter_forward", "wcc_adapter_backward",
            "wcc_scores_workspace_bytes", "wcc_token_scores",
-           "wcc_distill_workspace_bytes", "wcc_distill_forward", "wcc_distill_backward")
+           "wcc_distill_workspace_bytes", "wcc_distill_forward", "wcc_distill_backward",
+           "wcc_rows_keep", "wcc_rows_restore",
+           "wcc_group_norm_workspace_bytes", "wcc_group_norm_forward", "wcc_group_norm_backward",
+           "wcc_gated_workspace_bytes", "wcc_gated_forward", "wcc_gated_backward")
 
 
 class Desc(C.Structure):
@@ -61,6 +66,23 @@ class DistillDesc(C.Structure):
     """Mirror of ``wcc_distill_desc``."""
     _fields_ = [("rows", C.c_int64), ("V", C.c_int32), ("K", C.c_int32), ("dtype", C.c_int32), ("t_dtype", C.c_int32),
                 ("temperature", C.c_float), ("ld", C.c_int64), ("ld_grad", C.c_int64)]
+
+
+class RowsDesc(C.Structure):
+    """Mirror of ``wcc_rows_desc``."""
+    _fields_ = [("rows", C.c_int64), ("width", C.c_int32), ("dtype", C.c_int32), ("ld", C.c_int64)]
+
+
+class GroupNormDesc(C.Structure):
+    """Mirror of ``wcc_group_norm_desc``."""
+    _fields_ = [("samples", C.c_int32), ("pixels", C.c_int64), ("C", C.c_int32), ("groups", C.c_int32), ("act", C.c_int32),
+                ("dtype", C.c_int32), ("eps", C.c_float), ("ldx", C.c_int64), ("ldy", C.c_int64)]
+
+
+class GatedDesc(C.Structure):
+    """Mirror of ``wcc_gated_desc``."""
+    _fields_ = [("rows", C.c_int64), ("C_in", C.c_int32), ("C_out", C.c_int32), ("act", C.c_int32), ("dtype", C.c_int32),
+                ("train", C.c_int32), ("ldx", C.c_int64), ("ldy", C.c_int64)]
 
 
 class WccError(RuntimeError):
@@ -114,6 +136,14 @@ def lib():
         L.wcc_distill_workspace_bytes.argtypes = [C.POINTER(DistillDesc), sz]
         L.wcc_distill_forward.argtypes = [vp, C.POINTER(DistillDesc)] + [vp] * 8
         L.wcc_distill_backward.argtypes = [vp, C.POINTER(DistillDesc)] + [vp] * 7
+        for call in ("wcc_rows_keep", "wcc_rows_restore"):
+            getattr(L, call).argtypes = [vp, C.POINTER(RowsDesc)] + [vp] * 4
+        L.wcc_group_norm_workspace_bytes.argtypes = [C.POINTER(GroupNormDesc), sz]
+        L.wcc_group_norm_forward.argtypes = [vp, C.POINTER(GroupNormDesc)] + [vp] * 9
+        L.wcc_group_norm_backward.argtypes = [vp, C.POINTER(GroupNormDesc)] + [vp] * 12
+        L.wcc_gated_workspace_bytes.argtypes = [C.POINTER(GatedDesc), sz]
+        L.wcc_gated_forward.argtypes = [vp, C.POINTER(GatedDesc)] + [vp] * 7
+        L.wcc_gated_backward.argtypes = [vp, C.POINTER(GatedDesc)] + [vp] * 12
         for name in EXPORTS:
             if name not in ("wcc_k", "wcc_status_string"):
                 getattr(L, name).restype = C.c_int
@@ -179,9 +209,27 @@ def make_distill_desc(rows, V, K, dtype, t_dtype=F32, temperature=1.0, ld=None, 
     return DistillDesc(rows, V, K, dtype, t_dtype, temperature, V if ld is None else ld, V if ld_grad is None else ld_grad)
 
 
+def make_rows_desc(rows, width, dtype, ld=None) -> RowsDesc:
+    return RowsDesc(rows, width, dtype, width if ld is None else ld)
+
+
+def make_group_norm_desc(samples, pixels, Cc, groups, dtype, act=ACT_NONE, eps=1e-5, ldx=None, ldy=None) -> GroupNormDesc:
+    return GroupNormDesc(samples, pixels, Cc, groups, act, dtype, eps, Cc if ldx is None else ldx, Cc if ldy is None else ldy)
+
+
+def make_gated_desc(rows, C_in, C_out, dtype, act=ACT_SILU, train=False, ldx=None, ldy=None) -> GatedDesc:
+    return GatedDesc(rows, C_in, C_out, act, dtype, int(bool(train)), C_in if ldx is None else ldx, C_out if ldy is None else ldy)
+
+
+def kept_room(width: int) -> int:
+    """Codes of a row of `width` values: whole blocks."""
+    return -(-width // KEPT_BLOCK) * KEPT_BLOCK
+
+
 def _workspace_of(desc) -> int:
     call = {BlockDesc: "wcc_block_workspace_bytes", AdapterDesc: "wcc_adapter_workspace_bytes",
-            ScoresDesc: "wcc_scores_workspace_bytes", DistillDesc: "wcc_distill_workspace_bytes"}.get(type(desc), "wcc_workspace_bytes")
+            ScoresDesc: "wcc_scores_workspace_bytes", DistillDesc: "wcc_distill_workspace_bytes",
+            GroupNormDesc: "wcc_group_norm_workspace_bytes", GatedDesc: "wcc_gated_workspace_bytes"}.get(type(desc), "wcc_workspace_bytes")
     out = C.c_size_t(0)
     _check(getattr(lib(), call)(C.byref(desc), C.byref(out)), call)
     return int(out.value)
@@ -196,6 +244,14 @@ def scores_workspace_bytes(desc: ScoresDesc) -> int:
 
 
 def distill_workspace_bytes(desc: DistillDesc) -> int:
+    return _workspace_of(desc)
+
+
+def group_norm_workspace_bytes(desc: GroupNormDesc) -> int:
+    return _workspace_of(desc)
+
+
+def gated_workspace_bytes(desc: GatedDesc) -> int:
     return _workspace_of(desc)
 
 
@@ -225,6 +281,12 @@ def _whole(t, shape, dtype):
         return None
     assert t.is_cuda and t.is_contiguous() and t.dtype == dtype and tuple(t.shape) == shape, "not the descriptor's tensor"
     return t.data_ptr()
+
+
+def _kept(codes, steps, lead, width):
+    """Addresses of rows in 8 bits: codes [*lead, whole blocks of width], steps [*lead, blocks]."""
+    room = kept_room(width)
+    return _whole(codes, (*lead, room), torch.int8), _whole(steps, (*lead, room // KEPT_BLOCK), torch.uint8)
 
 
 def _stream():
@@ -365,3 +427,44 @@ class Context:
             self._h, C.byref(d), _rows(logits, d.rows, d.V, d.ld, d.dtype), _whole(t_idx, (d.rows, d.K), torch.int32),
             _whole(t_logit, (d.rows, d.K), _TORCH[d.t_dtype]), _whole(stats, (d.rows, 2), f), _whole(weight, (d.rows,), f),
             _rows(dlogits, d.rows, d.V, d.ld_grad, d.dtype), _stream()), "wcc_distill_backward")
+
+    # ---- a block on rows ----
+    def wcc_rows_keep(self, desc, x, codes, steps):
+        d = desc
+        _check(lib().wcc_rows_keep(self._h, C.byref(d), _rows(x, d.rows, d.width, d.ld, d.dtype), *_kept(codes, steps, (d.rows,), d.width),
+                                   _stream()), "wcc_rows_keep")
+
+    def wcc_rows_restore(self, desc, codes, steps, x):
+        d = desc
+        _check(lib().wcc_rows_restore(self._h, C.byref(d), *_kept(codes, steps, (d.rows,), d.width),
+                                      _rows(x, d.rows, d.width, d.ld, d.dtype), _stream()), "wcc_rows_restore")
+
+    def wcc_group_norm_forward(self, desc, x, gamma, beta, counts, y, stats=None, codes=None, steps=None):
+        d, f, rows = desc, torch.float32, desc.samples * desc.pixels
+        _check(lib().wcc_group_norm_forward(
+            self._h, C.byref(d), _rows(x, rows, d.C, d.ldx, d.dtype), _whole(gamma, (d.C,), f), _whole(beta, (d.C,), f),
+            _whole(counts, (d.samples,), torch.int32), _rows(y, rows, d.C, d.ldy, d.dtype), _whole(stats, (d.samples, d.groups, 2), f),
+            *_kept(codes, steps, (rows,), d.C), _stream()), "wcc_group_norm_forward")
+
+    def wcc_group_norm_backward(self, desc, x, codes, steps, gamma, beta, counts, stats, dy, dx=None, dgamma=None, dbeta=None):
+        d, f, rows = desc, torch.float32, desc.samples * desc.pixels
+        _check(lib().wcc_group_norm_backward(
+            self._h, C.byref(d), _rows(x, rows, d.C, d.ldx, d.dtype), *_kept(codes, steps, (rows,), d.C), _whole(gamma, (d.C,), f),
+            _whole(beta, (d.C,), f), _whole(counts, (d.samples,), torch.int32), _whole(stats, (d.samples, d.groups, 2), f),
+            _rows(dy, rows, d.C, d.ldy, d.dtype), _rows(dx, rows, d.C, d.ldx, d.dtype), _whole(dgamma, (d.C,), f),
+            _whole(dbeta, (d.C,), f), _stream()), "wcc_group_norm_backward")
+
+    def wcc_gated_forward(self, desc, x, w_gate, w_up, y, codes=None, steps=None):
+        d, t = desc, _TORCH[desc.dtype]
+        _check(lib().wcc_gated_forward(
+            self._h, C.byref(d), _rows(x, d.rows, d.C_in, d.ldx, d.dtype), _whole(w_gate, (d.C_out, d.C_in), t),
+            _whole(w_up, (d.C_out, d.C_in), t), _rows(y, d.rows, d.C_out, d.ldy, d.dtype), *_kept(codes, steps, (2, d.rows), d.C_out),
+            _stream()), "wcc_gated_forward")
+
+    def wcc_gated_backward(self, desc, x, x_codes, x_steps, w_gate, w_up, codes, steps, dy, dx=None, dw_gate=None, dw_up=None):
+        d, t = desc, _TORCH[desc.dtype]
+        _check(lib().wcc_gated_backward(
+            self._h, C.byref(d), _rows(x, d.rows, d.C_in, d.ldx, d.dtype), *_kept(x_codes, x_steps, (d.rows,), d.C_in),
+            _whole(w_gate, (d.C_out, d.C_in), t), _whole(w_up, (d.C_out, d.C_in), t), *_kept(codes, steps, (2, d.rows), d.C_out),
+            _rows(dy, d.rows, d.C_out, d.ldy, d.dtype), _rows(dx, d.rows, d.C_in, d.ldx, d.dtype),
+            _whole(dw_gate, (d.C_out, d.C_in), t), _whole(dw_up, (d.C_out, d.C_in), t), _stream()), "wcc_gated_backward")
