@@ -107,9 +107,20 @@ size_t tile_gate_parts(int64_t rows, int64_t outs, int64_t k);
 size_t tile_product_parts(int64_t rows, int64_t lines, int64_t k, int batches);
 
 template <class T>
-hipError_t tile_gate(const Gate<T> &p, int act, bool back, const Side<T> &x, const T *w_gate, const T *w_up, int64_t k, float *part,
-                     hipStream_t s);
+hipError_t tile_gate(const Gate<T> &p, int act, bool back, const Side<T> &x, const T *w_gate, const T *w_up, int64_t ldw, int64_t k,
+                     float *part, hipStream_t s);
 template <class T, bool AT>
 hipError_t tile_product(const Product<T> &p, float *part, hipStream_t s);
+
+// bf16, many rows (gated_gemm.hip).  Operands whose k or lines are contiguous and 16 bytes a load: pointers and strides are multiples.
+bool gemm_takes(const void *p, int64_t ld, int64_t width);
+hipError_t gemm_gate(const Gate<bf16_t> &p, int act, bool back, const Side<bf16_t> &x, const bf16_t *w_gate, const bf16_t *w_up, int64_t ldw,
+                     int64_t k, hipStream_t s);
+size_t gemm_dx_parts(int64_t rows, int64_t C_in, int64_t room);
+size_t gemm_dw_parts(int64_t rows, int64_t C_in, int64_t C_out);
+hipError_t gemm_dx(const bf16_t *d, int64_t room, int64_t rows, const bf16_t *w_gate, const bf16_t *w_up, int64_t ldw, int64_t C_in, int64_t C_out,
+                   bf16_t *dx, int64_t ld, float *part, hipStream_t s);
+hipError_t gemm_dw(const bf16_t *d, int64_t room, int64_t rows, const bf16_t *x, int64_t ldx, int64_t width, int64_t C_in, int64_t C_out,
+                   bf16_t *dw_gate, bf16_t *dw_up, float *part, hipStream_t s);
 
 }  // namespace wcc

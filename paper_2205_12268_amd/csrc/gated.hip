@@ -42,36 +42,128 @@ __global__ __launch_bounds__(256) void zeros_kernel(uint16_t *p, int64_t n) {
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = 0;
 }
 
+// Matrices of bf16 copied to rows of a stride that 16-byte loads take, zeros behind their width.  Three at most in one launch.
+struct Copy {
+  const bf16_t *from;
+  bf16_t *to;
+  int64_t ld, rows;
+};
+struct Copies {
+  Copy c[3];
+  int width;
+  int64_t room;
+};
+__global__ __launch_bounds__(256) void copy_kernel(Copies a) {
+  const Copy c = a.c[blockIdx.y];
+  const int64_t per_row = a.room / 8;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < c.rows * per_row; i += (int64_t)gridDim.x * 256) {
+    const int64_t t = i / per_row, e = (i - t * per_row) * 8;
+    *reinterpret_cast<u32x4 *>(c.to + t * a.room + e) = load_part<bf16_t>(c.from + t * c.ld + e, (int)(a.width - e));
+  }
+}
+
 size_t up(size_t v) { return (v + 255) / 256 * 256; }
 
+// Which kernels a call takes, and what the workspace holds: dg and du; x where it comes as codes or has to be copied; the weights where
+// they have to be copied; sums of ranges of k.
 struct Plan {
-  size_t d, x, part, bytes;  // of the backward pass: dg and du; x where it is kept in codes; sums of ranges of k
-  int64_t room, ldx;
+  bool gemm, copy_x, copy_w;
+  size_t d, x, w, part, bytes;
+  int64_t room, ldx, k;  // of d's halves; of rows and weights that were copied; C_in in whole chunks of 16 bytes
 };
 
+// Tiles fed straight from memory from 2^28 products on; rows or weights that 16-byte loads do not take are copied for it from 2^30 on.
 Plan plan_of(const wcc_gated_desc &g, bool backward) {
   Plan p = {};
   const size_t size = g.dtype == WCC_F32 ? 4 : 2;
-  p.room = room_of(g.C_out), p.ldx = room_of(g.C_in);
-  size_t parts = tile_gate_parts(g.rows, g.C_out, g.C_in);
+  const double products = 2.0 * g.rows * g.C_in * g.C_out;
+  p.room = room_of(g.C_out), p.ldx = room_of(g.C_in), p.k = (g.C_in + 7) / 8 * 8;
+  p.copy_w = g.C_in % 8 != 0, p.copy_x = p.copy_w || g.ldx % 8 != 0;
+  p.gemm = g.dtype == WCC_BF16 && g.rows > 64 && g.ldx < 1 << 21 && products >= (p.copy_x ? 1 << 30 : 1 << 28);
+  if (!p.gemm) p.copy_x = p.copy_w = false;
+  size_t parts = p.gemm ? 0 : tile_gate_parts(g.rows, g.C_out, g.C_in), at = 0;
+  if (backward) at += up((size_t)g.rows * 2 * p.room * size);
+  p.x = at;
+  if (backward || p.copy_x) at += up((size_t)g.rows * p.ldx * size);
+  p.w = at;
+  if (p.copy_w) at += 2 * up((size_t)g.C_out * p.ldx * size);
+  p.part = at;
   if (backward) {
-    p.x = up((size_t)g.rows * 2 * p.room * size);
-    p.part = p.x + up((size_t)g.rows * p.ldx * size);
-    parts = std::max({parts, tile_product_parts(g.rows, g.C_in, g.C_out, 1), tile_product_parts(g.C_out, g.C_in, g.rows, 2)});
+    if (p.gemm) parts = std::max({parts, gemm_dx_parts(g.rows, g.C_in, p.room), gemm_dw_parts(g.rows, g.C_in, g.C_out)});
+    // (tensors at odd addresses take the other tiles)
+    parts = std::max({parts, tile_gate_parts(g.rows, g.C_out, g.C_in), tile_product_parts(g.rows, g.C_in, g.C_out, 1), tile_product_parts(g.C_out, g.C_in, g.rows, 2)});
+  } else {
+    parts = std::max(parts, tile_gate_parts(g.rows, g.C_out, g.C_in));
   }
   p.bytes = p.part + up(parts);
   return p;
 }
 
+// The operands of a call as its products take them.
+template <class T>
+struct Operands {
+  bool gemm;
+  Side<T> x;
+  const T *wg, *wu;
+  int64_t ldw;
+};
+template <class T>
+hipError_t prepare(const wcc_gated_desc &d, const Plan &p, const GatedArgs &g, bool x_used, bool w_used, Operands<T> &o, hipStream_t s) {
+  o.wg = static_cast<const T *>(g.w_gate), o.wu = static_cast<const T *>(g.w_up), o.ldw = d.C_in;
+  o.x = Side<T>{static_cast<const T *>(g.x), d.ldx, d.rows};
+  o.gemm = p.gemm;
+  hipError_t e = hipSuccess;
+  if (x_used && !g.x) {  // (whole blocks: zeros behind the width)
+    wcc_rows_desc r = {};
+    r.rows = d.rows, r.width = (int32_t)(kept_blocks(d.C_in) * kKept), r.dtype = d.dtype, r.ld = p.ldx;
+    KeepArgs k = {};
+    k.back = g.ws + p.x, k.codes = const_cast<int8_t *>(g.x_codes), k.steps = const_cast<uint8_t *>(g.x_steps);
+    if ((e = launch_restore(r, k, s)) != hipSuccess) return e;
+    o.x = Side<T>{static_cast<const T *>(k.back), p.ldx, d.rows};
+  }
+  if constexpr (sizeof(T) == 2) {
+    Copies c = {};
+    int n = 0;
+    c.width = d.C_in, c.room = p.ldx;
+    if (x_used && g.x && p.copy_x) {
+      T *to = reinterpret_cast<T *>(g.ws + p.x);
+      c.c[n++] = Copy{o.x.p, to, d.ldx, d.rows};
+      o.x = Side<T>{to, p.ldx, d.rows};
+    }
+    if (w_used && p.copy_w) {
+      T *to = reinterpret_cast<T *>(g.ws + p.w), *next = reinterpret_cast<T *>(g.ws + p.w + up((size_t)d.C_out * p.ldx * sizeof(T)));
+      c.c[n++] = Copy{o.wg, to, d.C_in, d.C_out}, c.c[n++] = Copy{o.wu, next, d.C_in, d.C_out};
+      o.wg = to, o.wu = next, o.ldw = p.ldx;
+    }
+    if (n > 0) {
+      const int64_t most = std::max<int64_t>(d.rows, d.C_out) * (p.ldx / 8);
+      copy_kernel<<<dim3((unsigned)std::min<int64_t>((most + 255) / 256, 2048), n), 256, 0, s>>>(c);
+      e = hipGetLastError();
+    }
+    if (x_used) o.gemm = o.gemm && gemm_takes(o.x.p, o.x.s, p.k);
+    if (w_used) o.gemm = o.gemm && gemm_takes(o.wg, o.ldw, p.k) && gemm_takes(o.wu, o.ldw, p.k);
+  }
+  return e;
+}
+
+template <class T>
+hipError_t gate_of(const wcc_gated_desc &d, const Plan &p, const Gate<T> &gate, bool back, const Operands<T> &o, float *part, hipStream_t s) {
+  if constexpr (sizeof(T) == 2) {
+    if (o.gemm) return gemm_gate(gate, d.act, back, o.x, o.wg, o.wu, o.ldw, p.k, s);
+  }
+  return tile_gate<T>(gate, d.act, back, o.x, o.wg, o.wu, o.ldw, d.C_in, part, s);
+}
+
 template <class T>
 hipError_t forward(const wcc_gated_desc &d, const GatedArgs &g, hipStream_t s) {
   const Plan p = plan_of(d, false);
+  Operands<T> o;
+  hipError_t e = prepare<T>(d, p, g, true, true, o, s);
+  if (e != hipSuccess) return e;
   Gate<T> gate = {};
   gate.rows = d.rows, gate.outs = d.C_out, gate.y = static_cast<T *>(g.y), gate.ldy = d.ldy, gate.codes = g.codes, gate.steps = g.steps;
   gate.room = p.room;
-  const Side<T> x{static_cast<const T *>(g.x), d.ldx, d.rows};
-  return tile_gate<T>(gate, d.act, false, x, static_cast<const T *>(g.w_gate), static_cast<const T *>(g.w_up), d.C_in,
-                      reinterpret_cast<float *>(g.ws + p.part), s);
+  return gate_of<T>(d, p, gate, false, o, reinterpret_cast<float *>(g.ws + p.part), s);
 }
 
 template <class T, int ACT>
@@ -83,23 +175,17 @@ void kept_slopes(const Gate<T> &gate, hipStream_t s) {
 template <class T>
 hipError_t backward(const wcc_gated_desc &d, const GatedArgs &g, hipStream_t s) {
   const Plan p = plan_of(d, true);
-  const T *wg = static_cast<const T *>(g.w_gate), *wu = static_cast<const T *>(g.w_up);
   float *part = reinterpret_cast<float *>(g.ws + p.part);
-  Side<T> x{static_cast<const T *>(g.x), d.ldx, d.rows};
-  hipError_t e = hipSuccess;
-  const bool dw = g.dw_gate || g.dw_up;
-  if (!g.x && (dw || !g.codes)) {
-    wcc_rows_desc r = {};
-    r.rows = d.rows, r.width = d.C_in, r.dtype = d.dtype, r.ld = p.ldx;
-    KeepArgs k = {};
-    k.back = g.ws + p.x, k.codes = const_cast<int8_t *>(g.x_codes), k.steps = const_cast<uint8_t *>(g.x_steps);
-    if ((e = launch_restore(r, k, s)) != hipSuccess) return e;
-    x = Side<T>{static_cast<const T *>(k.back), p.ldx, d.rows};
-  }
+  const bool dw = g.dw_gate || g.dw_up, again = !g.codes;
+  Operands<T> o;
+  hipError_t e = prepare<T>(d, p, g, dw || again, g.dx || again, o, s);
+  if (e != hipSuccess) return e;
   Gate<T> gate = {};
   gate.rows = d.rows, gate.outs = d.C_out, gate.ldy = d.ldy, gate.codes = g.codes, gate.steps = g.steps;
   gate.dy = static_cast<const T *>(g.dy), gate.d = reinterpret_cast<T *>(g.ws + p.d), gate.room = p.room;
-  if (g.codes) {
+  if (again) {
+    e = gate_of<T>(d, p, gate, true, o, part, s);
+  } else {
     switch (d.act) {
       case WCC_ACT_RELU: kept_slopes<T, WCC_ACT_RELU>(gate, s); break;
       case WCC_ACT_SILU: kept_slopes<T, WCC_ACT_SILU>(gate, s); break;
@@ -107,16 +193,22 @@ hipError_t backward(const wcc_gated_desc &d, const GatedArgs &g, hipStream_t s) 
       default: kept_slopes<T, WCC_ACT_NONE>(gate, s);
     }
     e = hipGetLastError();
-  } else {
-    e = tile_gate<T>(gate, d.act, true, x, wg, wu, d.C_in, part, s);
   }
   if (e != hipSuccess) return e;
   const T *dg = gate.d, *du = gate.d + p.room;
+  if constexpr (sizeof(T) == 2) {
+    if (o.gemm) {
+      if (g.dx && (e = gemm_dx(dg, p.room, d.rows, o.wg, o.wu, o.ldw, d.C_in, d.C_out, static_cast<T *>(g.dx), d.ldx, part, s)) != hipSuccess)
+        return e;
+      return dw ? gemm_dw(dg, p.room, d.rows, o.x.p, o.x.s, p.k, d.C_in, d.C_out, static_cast<T *>(g.dw_gate), static_cast<T *>(g.dw_up), part, s)
+                : hipSuccess;
+    }
+  }
   if (g.dx) {
     Product<T> m = {};
     m.phases = 2, m.batches = 1, m.k = d.C_out, m.ld = d.ldx, m.out[0] = static_cast<T *>(g.dx);
     m.a[0] = Side<T>{dg, 2 * p.room, d.rows}, m.a[1] = Side<T>{du, 2 * p.room, d.rows};
-    m.b[0] = Side<T>{wg, d.C_in, d.C_in}, m.b[1] = Side<T>{wu, d.C_in, d.C_in};
+    m.b[0] = Side<T>{o.wg, o.ldw, d.C_in}, m.b[1] = Side<T>{o.wu, o.ldw, d.C_in};
     if ((e = tile_product<T, false>(m, part, s)) != hipSuccess) return e;
   }
   if (dw) {
@@ -126,7 +218,7 @@ hipError_t backward(const wcc_gated_desc &d, const GatedArgs &g, hipStream_t s) 
     if (g.dw_gate) m.a[n] = Side<T>{dg, 2 * p.room, d.C_out}, m.out[n++] = static_cast<T *>(g.dw_gate);
     if (g.dw_up) m.a[n] = Side<T>{du, 2 * p.room, d.C_out}, m.out[n++] = static_cast<T *>(g.dw_up);
     m.batches = n;
-    m.b[0] = m.b[1] = Side<T>{x.p, x.s, d.C_in};
+    m.b[0] = m.b[1] = Side<T>{o.x.p, o.x.s, d.C_in};
     if ((e = tile_product<T, true>(m, part, s)) != hipSuccess) return e;
   }
   return hipSuccess;

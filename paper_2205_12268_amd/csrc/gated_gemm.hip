@@ -1,0 +1,582 @@
+// The products of the gated block for many rows of bf16: the matrix cores fed from LDS, which loads go to straight from memory.
+//
+// A workgroup of four waves has BT x BO results and two stages of 64 k in LDS; loads (16 bytes a lane) go there without passing
+// registers.  A wave's operands of a whole stage fit its registers beside the results, so a stage's half of LDS is free after a quarter
+// of its products: from there on the loads of the stage after the next go out, one between every few products.  Two barriers a stage:
+// LDS is read; the next stage is there.
+// LDS has no padding (such a load writes 1 KiB in a row), so the 16-byte chunks of a line are exchanged by a key of the line, at the load
+// by choosing which chunk of memory a lane asks for: the lines that a read takes at once are on different banks.  Operands come
+// either with k contiguous, or with their lines contiguous (the weights for dx; both for the weights' gradients): LDS holds lines of k then
+// and the reads transpose 4 x 16 blocks.
+// Loads go through buffer descriptors that end where the operand does: what lies behind the last line or the last k is 0 without a
+// branch, and the stages past the last are loads of nothing.
+#include "gated.h"
+
+namespace wcc {
+namespace {
+
+constexpr uint32_t kNowhere = 0x80000000u;  // beyond any descriptor here
+
+using Rsrc = __amdgpu_buffer_rsrc_t;
+__device__ __forceinline__ Rsrc buffer(const char *p, int64_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(p), 0, (int)(uint32_t)max(bytes, (int64_t)0), 0x00020000);
+}
+__device__ __forceinline__ void buffer_to_lds(Rsrc r, uint32_t off, unsigned char *to) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)to, 16, off, 0, 0, 0);
+}
+
+// An operand in memory as a tile sees it.
+//   along:  line l at p + l * ld, k contiguous; `lines` of them there, `k` long
+//   across: k at p + k * ld, lines contiguous; `lines` of them there
+// In bytes but for the counts.  Two halves: along, lines in turns of 32 from p[0] and p[1] (the two weights); across, k from `turn` on in
+// p[1], from its first line on (dx: the two weights again).
+struct Operand {
+  const char *p[2];
+  int64_t ld;
+  int64_t lines, k;
+  int64_t turn;
+};
+
+template <int B, bool ACROSS, bool TURNS>
+struct Feed {
+  static constexpr int Bytes = B * kLine, L = Bytes / 4096;   // of a stage; loads of a wave
+  static constexpr int C = B / 8, R = 64 / C;                 // across: chunks of a line of k, lines of a load
+  static constexpr int PerLoad = ACROSS ? R : 8;
+  uint32_t off[2], at[2];  // the lane's places in loads of even and odd number; at: this stage's (along)
+  int chunk[2];
+  uint32_t step;
+  Rsrc r[2];
+
+  __device__ __forceinline__ void aim(const Operand &o) {
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    step = (uint32_t)(PerLoad * o.ld);
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      if constexpr (ACROSS) {
+        const int row = b * R + lane / C;
+        chunk[b] = 0;
+        off[b] = (uint32_t)((wv * L * R + lane / C) * o.ld + ((lane % C) ^ ((row & 3) * 4)) * 16);
+      } else {
+        const int row = b * 8 + lane / 8;
+        chunk[b] = (lane % 8) ^ chunk_key(row);
+        // (in turns of 32 lines a wave's loads are at the lines of both halves that its 64 lie in, or of the one that its 32 lie in)
+        const int first = TURNS ? (B == 256 ? wv * 32 : (wv >> 1) * 32) : wv * L * 8;
+        off[b] = (uint32_t)((first + lane / 8) * o.ld + chunk[b] * 16);
+      }
+    }
+    if constexpr (!ACROSS) {
+      const int64_t bytes = o.lines > 0 ? (min(o.lines, (int64_t)B) - 1) * o.ld + o.k * 2 : 0;
+      r[0] = buffer(o.p[0], bytes);
+      if constexpr (TURNS) {
+        r[1] = buffer(o.p[1], bytes);
+        if (B == 128 && (wv & 1)) r[0] = r[1];
+      }
+    }
+  }
+  // before the loads of a stage
+  __device__ __forceinline__ void turn_to(const Operand &o, int64_t stage) {
+    int64_t k = stage * kK;
+    if constexpr (ACROSS) {
+      const char *p = o.p[0];
+      if constexpr (TURNS) {
+        if (k >= o.turn) p = o.p[1], k -= o.turn;
+      }
+      const int64_t n = min(o.k - k, (int64_t)kK);
+      const bool some = n > 0 && o.lines > 0;
+      r[0] = buffer(some ? p + k * o.ld : p, some ? (n - 1) * o.ld + min(o.lines, (int64_t)B) * 2 : 0);
+    } else {
+      const int64_t left = o.k - k;
+#pragma unroll
+      for (int b = 0; b < 2; ++b) at[b] = chunk[b] * 8 < left ? off[b] + (uint32_t)(k * 2) : kNowhere;
+    }
+  }
+  template <int i>
+  __device__ __forceinline__ void load(unsigned char *to) const {
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    unsigned char *place = to + (wv * L + i) * 1024;
+    if constexpr (ACROSS) {
+      buffer_to_lds(r[0], off[i & 1] + i * step, place);
+    } else {
+      // (turns: the second half of a wave's loads is at the other weight's lines)
+      constexpr int n = TURNS && B == 256 ? i % (L / 2) : i, which = TURNS && B == 256 ? i / (L / 2) : 0;
+      buffer_to_lds(r[which], at[i & 1] + n * step, place);
+    }
+  }
+};
+
+// The barrier by itself (a fence would wait for all loads); the clobbers keep the reads of LDS on their sides of it.
+__device__ __forceinline__ void bare_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+// all but the last n loads of every wave have arrived
+template <int n>
+__device__ __forceinline__ void arrived() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(n) : "memory");
+  bare_barrier();
+}
+
+// The first operand of the matrix cores is W (outputs), the second X (rows): a lane has one row's results, four neighbouring outputs at a
+// time.
+template <int BT, int BO, bool XA, bool WA, bool XTURNS, bool WTURNS>
+struct Gemm {
+  static constexpr int WT = 2, WO = 2, ET = BT / WT / 32, EO = BO / WO / 32;
+  using X = Feed<BT, XA, XTURNS>;
+  using W = Feed<BO, WA, WTURNS>;
+  static constexpr int XL = X::L, WL = W::L, L = XL + WL;
+  struct Operands {
+    u32x4 x[ET], w[EO];
+  };
+  X x;
+  W w;
+
+  template <int from, int to>
+  __device__ __forceinline__ void load(unsigned char *xs, unsigned char *ws) const {
+    if constexpr (from < to) {
+      if constexpr (from < XL) x.template load<from>(xs);
+      else w.template load<from - XL>(ws);
+      load<from + 1, to>(xs, ws);
+    }
+  }
+  // 32 lines from `line` on, 16 k from k on, of lines of k that are B lines wide
+  template <int B>
+  __device__ static __forceinline__ u32x4 across(const unsigned char *s, int line, int k) {
+    const int lane = threadIdx.x & 63, g = lane >> 4, q = lane & 15;
+    const int n = line + (g & 1) * 16 + (q & 3) * 4, kk = k + (g >> 1) * 8 + (q >> 2);
+    u32x4 v;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int row = kk + h * 4;
+      const uint2 u = turned(s + row * (B * 2) + (((n >> 3) ^ ((row & 3) * 4)) << 4) + (n & 7) * 2);
+      v[2 * h] = u.x, v[2 * h + 1] = u.y;
+    }
+    return v;
+  }
+  __device__ static __forceinline__ void fetch(const unsigned char *xs, const unsigned char *ws, int step, Operands &f) {
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, ln = lane & 31, half = lane >> 5;
+    const int tw = (wv / WO) * (ET * 32), ow = (wv % WO) * (EO * 32);
+#pragma unroll
+    for (int e = 0; e < EO; ++e) f.w[e] = WA ? across<BO>(ws, ow + e * 32, step * 16) : chunk_of(ws, ow + e * 32 + ln, step * 2 + half);
+#pragma unroll
+    for (int r = 0; r < ET; ++r) f.x[r] = XA ? across<BT>(xs, tw + r * 32, step * 16) : chunk_of(xs, tw + r * 32 + ln, step * 2 + half);
+  }
+  __device__ static __forceinline__ void multiply(const Operands &f, f32x16 (&acc)[EO][ET]) {
+#pragma unroll
+    for (int e = 0; e < EO; ++e)
+#pragma unroll
+      for (int r = 0; r < ET; ++r) acc[e][r] = mma<bf16_t>(f.w[e], f.x[r], acc[e][r]);
+  }
+  // The order of a step: its reads of LDS two at a time between the first products (the rest of which hide the last one's way),
+  // its loads between the others, as far apart as they get: a load takes 16 cycles on its way out, a product 32.
+  template <int reads, int loads>
+  __device__ static __forceinline__ void spread() {
+    constexpr int M = ET * EO, N = (reads + 1) / 2;
+    if constexpr (M < 16) {  // (two workgroups a compute unit hide each other's)
+      __builtin_amdgcn_sched_barrier(0);
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      if (i < M) __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    }
+    constexpr int each = loads > 0 && M > N ? (M - N) / loads : 0;
+#pragma unroll
+    for (int i = 0; i < loads; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+      if (each > 0) __builtin_amdgcn_sched_group_barrier(0x008, each, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, M, 0);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  // The stage in (xs, ws), whose first two steps' operands are on their way to f; the next one is in (xn, wn), and `later` is loaded
+  // where this one was.
+  __device__ __forceinline__ void stage(const Operand &xo, const Operand &wo, int64_t later, unsigned char *xs, unsigned char *ws,
+                                        const unsigned char *xn, const unsigned char *wn, Operands (&f)[4], f32x16 (&acc)[EO][ET]) {
+    constexpr int Reads = ET * (XA ? 2 : 1) + EO * (WA ? 2 : 1), L1 = (L + 2) / 3, L2 = 2 * L1;
+    x.turn_to(xo, later), w.turn_to(wo, later);
+    fetch(xs, ws, 2, f[2]);
+    fetch(xs, ws, 3, f[3]);
+    multiply(f[0], acc);
+    spread<2 * Reads, 0>();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    bare_barrier();
+    load<0, L1>(xs, ws);
+    multiply(f[1], acc);
+    spread<0, L1>();
+    load<L1, L2>(xs, ws);
+    multiply(f[2], acc);
+    spread<0, L2 - L1>();
+    arrived<L2>();
+    fetch(xn, wn, 0, f[0]);
+    fetch(xn, wn, 1, f[1]);
+    load<L2, L>(xs, ws);
+    multiply(f[3], acc);
+    spread<2 * Reads, L - L2>();
+  }
+  // acc += the products over stages s0 .. s1
+  __device__ __forceinline__ void run(const Operand &xo, const Operand &wo, int64_t s0, int64_t s1, unsigned char *xs0, unsigned char *ws0,
+                                      unsigned char *xs1, unsigned char *ws1, f32x16 (&acc)[EO][ET]) {
+    const int64_t none = (int64_t)1 << 40;  // (a stage of nothing)
+    auto at = [&](int64_t s) { return s < s1 ? s : none; };
+    x.aim(xo), w.aim(wo);
+    Operands f[4];
+    x.turn_to(xo, s0), w.turn_to(wo, s0);
+    load<0, L>(xs0, ws0);
+    x.turn_to(xo, at(s0 + 1)), w.turn_to(wo, at(s0 + 1));
+    load<0, L>(xs1, ws1);
+    arrived<L>();
+    fetch(xs0, ws0, 0, f[0]);
+    fetch(xs0, ws0, 1, f[1]);
+    int64_t s = s0;
+    for (; s + 1 < s1; s += 2) {
+      stage(xo, wo, at(s + 2), xs0, ws0, xs1, ws1, f, acc);
+      stage(xo, wo, at(s + 3), xs1, ws1, xs0, ws0, f, acc);
+    }
+    if (s < s1) stage(xo, wo, none, xs0, ws0, xs1, ws1, f, acc);
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // nothing is on its way to LDS from here on
+    bare_barrier();
+  }
+};
+
+__device__ __forceinline__ uint2 narrow4(float a, float b, float c, float d) {
+  return uint2{(uint32_t)narrow<bf16_t>(a) | (uint32_t)narrow<bf16_t>(b) << 16, (uint32_t)narrow<bf16_t>(c) | (uint32_t)narrow<bf16_t>(d) << 16};
+}
+
+// 32 rows of `Row` bytes that a wave has written to LDS in 8-byte pieces, exchanged by a key of the row (even, so that pairs of them stay
+// together): 16 bytes a lane, f(row, byte in the row, the 16 bytes).  (A wave reads what it wrote itself: LDS is in order.)
+template <int Row>
+__device__ __forceinline__ int twist(int row) { return row % (Row / 16) * 2; }
+template <int Row>
+__device__ __forceinline__ void put(unsigned char *lds, int row, int piece, const uint2 &v) {
+  *reinterpret_cast<uint2 *>(lds + row * Row + ((piece ^ twist<Row>(row)) << 3)) = v;
+}
+template <int Row, class F>
+__device__ __forceinline__ void leave(const unsigned char *lds, F f) {
+  constexpr int Lanes = Row / 16, Rows = 64 / Lanes;
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int r0 = 0; r0 < 32; r0 += Rows) {
+    const int row = r0 + lane / Lanes, c = lane % Lanes;
+    f(row, c * 16, *reinterpret_cast<const u32x4 *>(lds + row * Row + (((2 * c) ^ twist<Row>(row)) << 3)));
+  }
+}
+
+// ---- the two projections -------------------------------------------------------------------------------------
+template <int B, int ACT, bool BACK>
+__global__ __launch_bounds__(256, B == 128 ? 2 : 1) void gate_gemm_kernel(Gate<bf16_t> p, Operand x, Operand w, int64_t tiles_t, int tiles_o) {
+  using G = Gemm<B, B, false, false, false, true>;
+  constexpr int ET = G::ET, EO = G::EO, Pairs = EO / 2, Row = Pairs * 64;
+  __shared__ __align__(1024) unsigned char xs0[G::X::Bytes], ws0[G::W::Bytes], xs1[G::X::Bytes], ws1[G::W::Bytes];
+  int64_t tt;
+  int to;
+  tile_of(in_runs(blockIdx.x, tiles_t * tiles_o), tiles_t, tiles_o, tt, to);
+  const int64_t t0 = tt * B;
+  const int o0 = to * (B / 2);
+  x.p[0] += t0 * x.ld, x.lines -= t0;
+  w.p[0] += o0 * w.ld, w.p[1] += o0 * w.ld, w.lines -= o0;
+  w.lines = min(w.lines, (int64_t)(B / 2));
+  f32x16 acc[EO][ET] = {};
+  G g;
+  g.run(x, w, 0, (x.k + kK - 1) / kK, xs0, ws0, xs1, ws1, acc);
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, ln = lane & 31, half = lane >> 5;
+  const int64_t tw = t0 + (wv / G::WO) * (ET * 32);
+  const int ow = o0 + (wv % G::WO) * (Pairs * 32);
+  unsigned char *own = wv == 0 ? xs0 : wv == 1 ? ws0 : wv == 2 ? xs1 : ws1;
+  const int64_t blocks = (p.outs + kKept - 1) / kKept;
+#pragma unroll
+  for (int r = 0; r < ET; ++r) {
+    const int64_t t = tw + r * 32 + ln;
+    unsigned char *second = own + 32 * Row;
+#pragma unroll
+    for (int j = 0; j < Pairs; ++j) {
+      const f32x16 &ga = acc[2 * j][r], &ua = acc[2 * j + 1][r];  // (lines behind the last are 0)
+      if constexpr (BACK) {
+        const int o = ow + j * 32;
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          const int at = o + result_line(i, half);
+          float dg[4], du[4];
+          uint2 top = {0, 0};
+          if (t < p.rows && at < p.outs) {
+            const bf16_t *q = p.dy + t * p.ldy + at;
+            typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+            if (at + 4 <= p.outs) {
+              const u32x2_any v = *reinterpret_cast<const u32x2_any *>(q);
+              top = uint2{v.x, v.y};
+            } else {
+              top.x = q[0];
+              if (at + 1 < p.outs) top.x |= (uint32_t)q[1] << 16;
+              if (at + 2 < p.outs) top.y = q[2];
+            }
+          }
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            float v, s;
+            act_of<bf16_t, ACT>(ga[i + k], v, s);
+            const uint32_t word = k < 2 ? top.x : top.y;
+            const float dy = __uint_as_float(k & 1 ? word & 0xffff0000u : word << 16);
+            dg[k] = dy * ua[i + k] * s, du[k] = dy * v;
+            if (at + k >= p.outs) dg[k] = du[k] = 0.f;  // (what lies behind is 0)
+          }
+          put<Row>(own, ln, j * 8 + (i >> 1) + half, narrow4(dg[0], dg[1], dg[2], dg[3]));
+          put<Row>(second, ln, j * 8 + (i >> 1) + half, narrow4(du[0], du[1], du[2], du[3]));
+        }
+      } else {
+        if (p.codes) {
+          uint32_t m[2] = {0, 0};
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            m[0] = max(m[0], __float_as_uint(ga[i]) & 0x7fffffffu);
+            m[1] = max(m[1], __float_as_uint(ua[i]) & 0x7fffffffu);
+          }
+          const int64_t block = ow / kKept + j;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t b = step_of(max(m[h], (uint32_t)__shfl_xor((int)m[h], 32, 64)));
+            const float per = per_step(b);
+            const f32x16 &v = h ? ua : ga;
+            if (half == h && t < p.rows && block < blocks) p.steps[((int64_t)h * p.rows + t) * blocks + block] = (uint8_t)b;
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+              const uint32_t c = b == 255 ? 0 : codes_of(v[i], v[i + 1], v[i + 2], v[i + 3], per);
+              *reinterpret_cast<uint32_t *>(second + (h * Pairs + j) * 1024 + ln * 32 + result_line(i, half)) = c;
+            }
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          float f[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            float v, s;
+            act_of<bf16_t, ACT>(ga[i + k], v, s);
+            f[k] = v * ua[i + k];
+          }
+          put<Row>(own, ln, j * 8 + (i >> 1) + half, narrow4(f[0], f[1], f[2], f[3]));
+        }
+      }
+    }
+    if constexpr (BACK) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        leave<Row>(h ? second : own, [&](int row, int b, const u32x4 &v) {
+          const int o = ow + b / 2;
+          if (tw + r * 32 + row < p.rows && o < p.room)
+            *reinterpret_cast<u32x4 *>(p.d + ((tw + r * 32 + row) * 2 + h) * p.room + o) = v;
+        });
+    } else {
+      leave<Row>(own, [&](int row, int b, const u32x4 &v) {
+        const int o = ow + b / 2;
+        if (tw + r * 32 + row < p.rows && o < p.outs) store_part<bf16_t>(p.y + (tw + r * 32 + row) * p.ldy + o, p.outs - o, v);
+      });
+      if (p.codes) {  // blocks of 32 rows of 32 bytes: 16 bytes a lane
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int j = 0; j < Pairs; ++j) {
+            const int row = lane / 2, b = lane % 2 * 16;
+            const int64_t t2 = tw + r * 32 + row, block = ow / kKept + j;
+            const u32x4 v = *reinterpret_cast<const u32x4 *>(second + (h * Pairs + j) * 1024 + row * 32 + b);
+            if (t2 < p.rows && block < blocks) *reinterpret_cast<u32x4 *>(p.codes + (((int64_t)h * p.rows + t2) * blocks + block) * kKept + b) = v;
+          }
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
+// ---- dx and the weights' gradients -----------------------------------------------------------------------------
+struct Result {
+  bf16_t *out[2];  // rows from `turn` on go to out[1], from its first on
+  int64_t ld, rows, outs, turn;
+  float *part;     // PARTS: [splits][turns * rows][outs]
+};
+
+template <int BT, int BO, bool XA, bool PARTS>
+__global__ __launch_bounds__(256, BT == 128 && BO == 128 ? 2 : 1) void product_gemm_kernel(Result p, Operand x, Operand w, int64_t tiles_t,
+                                                                                       int tiles_o, int splits, int64_t chunk,
+                                                                                       int64_t stages) {
+  using G = Gemm<BT, BO, XA, true, false, !XA>;
+  constexpr int ET = G::ET, EO = G::EO, Row = EO * 64;
+  __shared__ __align__(1024) unsigned char xs0[G::X::Bytes], ws0[G::W::Bytes], xs1[G::X::Bytes], ws1[G::W::Bytes];
+  const int64_t tiles = tiles_t * tiles_o, block = in_runs(blockIdx.x, tiles * splits), split = block / tiles;
+  int64_t tt;
+  int to;
+  tile_of(block % tiles, tiles_t, tiles_o, tt, to);
+  // rows of the second half begin with a tile of their own
+  const int64_t tiles_half = (p.rows + BT - 1) / BT, second = tt >= tiles_half ? 1 : 0;
+  const int64_t t0 = (tt - second * tiles_half) * BT;
+  const int64_t o0 = (int64_t)to * BO;
+  if constexpr (XA) x.p[0] += (second * p.turn + t0) * 2;
+  else x.p[0] += t0 * x.ld;
+  x.lines -= t0;
+  w.p[0] += o0 * 2, w.p[1] += o0 * 2, w.lines -= o0;
+  f32x16 acc[EO][ET] = {};
+  G g;
+  g.run(x, w, split * chunk, min(stages, (split + 1) * chunk), xs0, ws0, xs1, ws1, acc);
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, ln = lane & 31, half = lane >> 5;
+  const int64_t tw = t0 + (wv / G::WO) * (ET * 32), ow = o0 + (wv % G::WO) * (EO * 32);
+  unsigned char *own = wv == 0 ? xs0 : wv == 1 ? ws0 : wv == 2 ? xs1 : ws1;
+#pragma unroll
+  for (int r = 0; r < ET; ++r) {
+    if constexpr (PARTS) {
+      const int64_t t = tw + r * 32 + ln, halves = p.out[1] ? 2 : 1;
+      if (t < p.rows) {
+        float *q = p.part + ((split * halves + second) * p.rows + t) * p.outs;
+#pragma unroll
+        for (int e = 0; e < EO; ++e)
+#pragma unroll
+          for (int i = 0; i < 16; i += 4) {
+            const int64_t o = ow + e * 32 + result_line(i, half);
+            if (o + 4 <= p.outs) {
+              *reinterpret_cast<f32x4_any *>(q + o) = f32x4_any{acc[e][r][i], acc[e][r][i + 1], acc[e][r][i + 2], acc[e][r][i + 3]};
+            } else {
+#pragma unroll
+              for (int k = 0; k < 3; ++k)
+                if (o + k < p.outs) q[o + k] = acc[e][r][i + k];
+            }
+          }
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < EO; ++e)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+          put<Row>(own, ln, e * 8 + (i >> 1) + half, narrow4(acc[e][r][i], acc[e][r][i + 1], acc[e][r][i + 2], acc[e][r][i + 3]));
+      leave<Row>(own, [&](int row, int b, const u32x4 &v) {
+        const int64_t o = ow + b / 2, t = tw + r * 32 + row;
+        if (t < p.rows && o < p.outs) store_part<bf16_t>(p.out[second] + t * p.ld + o, (int)min(p.outs - o, (int64_t)8), v);
+      });
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
+__global__ __launch_bounds__(256) void product_gemm_join_kernel(Result p, int splits) {
+  const int64_t all = p.rows * p.outs, halves = p.out[1] ? 2 : 1;
+  const int h = blockIdx.y;
+  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < all; i += (int64_t)gridDim.x * 1024) {
+    f32x4_any v = {};
+    const int n = (int)min(all - i, (int64_t)4);
+    for (int s = 0; s < splits; ++s) {
+      const float *q = p.part + (s * halves + h) * all + i;
+      if (n == 4) {
+        v += *reinterpret_cast<const f32x4_any *>(q);
+      } else {
+        for (int j = 0; j < n; ++j) v[j] += q[j];
+      }
+    }
+    for (int j = 0; j < n; ++j) p.out[h][(i + j) / p.outs * p.ld + (i + j) % p.outs] = narrow<bf16_t>(v[j]);
+  }
+}
+
+bool on_16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+int64_t tiles(int64_t n, int64_t size) { return (n + size - 1) / size; }
+
+template <class F>
+hipError_t by_act(int act, F f) {
+  switch (act) {
+    case WCC_ACT_RELU: return f(std::integral_constant<int, WCC_ACT_RELU>());
+    case WCC_ACT_SILU: return f(std::integral_constant<int, WCC_ACT_SILU>());
+    case WCC_ACT_GELU: return f(std::integral_constant<int, WCC_ACT_GELU>());
+    default: return f(std::integral_constant<int, WCC_ACT_NONE>());
+  }
+}
+
+struct ProductPlan {
+  int bt, bo, splits;
+  int64_t stages, chunk;
+};
+// rows: of one half
+ProductPlan plan_of(int64_t rows, int64_t outs, int64_t k, int halves) {
+  ProductPlan p;
+  p.stages = tiles(k, kK);
+  const bool large = halves * tiles(rows, 256) * tiles(outs, 256) >= 200;
+  p.bt = p.bo = large ? 256 : 128;
+  const int64_t n = halves * tiles(rows, p.bt) * tiles(outs, p.bo), slots = large ? 256 : 512;
+  const int64_t want = std::min<int64_t>({std::max<int64_t>(slots / n, 1), std::max<int64_t>(p.stages / 4, 1), 16});
+  p.chunk = tiles(p.stages, want);
+  p.splits = (int)tiles(p.stages, p.chunk);
+  return p;
+}
+
+template <int BT, int BO, bool XA>
+void launch_product(const Result &r, const Operand &x, const Operand &w, const ProductPlan &p, int halves, hipStream_t s) {
+  const int64_t tiles_t = halves * tiles(r.rows, BT);
+  const int tiles_o = (int)tiles(r.outs, BO);
+  const unsigned blocks = (unsigned)(tiles_t * tiles_o * p.splits);
+  if (p.splits > 1) {
+    product_gemm_kernel<BT, BO, XA, true><<<blocks, 256, 0, s>>>(r, x, w, tiles_t, tiles_o, p.splits, p.chunk, p.stages);
+    product_gemm_join_kernel<<<dim3((unsigned)std::min<int64_t>(tiles(r.rows * r.outs, 1024), 4096), halves), 256, 0, s>>>(r, p.splits);
+  } else {
+    product_gemm_kernel<BT, BO, XA, false><<<blocks, 256, 0, s>>>(r, x, w, tiles_t, tiles_o, 1, p.stages, p.stages);
+  }
+}
+
+template <bool XA>
+hipError_t product(const Result &r, const Operand &x, const Operand &w, int64_t k, int halves, hipStream_t s) {
+  const ProductPlan p = plan_of(r.rows, r.outs, k, halves);
+  if (p.bt == 256) launch_product<256, 256, XA>(r, x, w, p, halves, s);
+  else launch_product<128, 128, XA>(r, x, w, p, halves, s);
+  return hipGetLastError();
+}
+
+size_t parts_of(int64_t rows, int64_t outs, int64_t k, int halves) {
+  const ProductPlan p = plan_of(rows, outs, k, halves);
+  return p.splits > 1 ? (size_t)p.splits * halves * rows * outs * sizeof(float) : 0;
+}
+
+}  // namespace
+
+// 16-byte loads, tiles within a descriptor
+bool gemm_takes(const void *p, int64_t ld, int64_t width) { return on_16(p) && ld % 8 == 0 && ld < 1 << 21 && width % 8 == 0; }
+
+hipError_t gemm_gate(const Gate<bf16_t> &p, int act, bool back, const Side<bf16_t> &x, const bf16_t *w_gate, const bf16_t *w_up, int64_t ldw,
+                     int64_t k, hipStream_t s) {
+  Operand xo = {}, wo = {};
+  xo.p[0] = reinterpret_cast<const char *>(x.p), xo.ld = x.s * 2, xo.lines = x.lines, xo.k = k;
+  wo.p[0] = reinterpret_cast<const char *>(w_gate), wo.p[1] = reinterpret_cast<const char *>(w_up), wo.ld = ldw * 2, wo.lines = p.outs, wo.k = k;
+  return by_act(act, [&](auto a) {
+    constexpr int ACT = decltype(a)::value;
+    auto go = [&](auto size, auto b) {
+      constexpr int B = decltype(size)::value;
+      const int64_t tiles_t = tiles(p.rows, B);
+      const int tiles_o = (int)tiles(p.outs, B / 2);
+      gate_gemm_kernel<B, ACT, decltype(b)::value><<<(unsigned)(tiles_t * tiles_o), 256, 0, s>>>(p, xo, wo, tiles_t, tiles_o);
+    };
+    const bool large = tiles(p.rows, 256) * tiles(p.outs, 128) >= 200;
+    using L = std::integral_constant<int, 256>;
+    using S = std::integral_constant<int, 128>;
+    if (large) back ? go(L(), std::true_type()) : go(L(), std::false_type());
+    else back ? go(S(), std::true_type()) : go(S(), std::false_type());
+    return hipGetLastError();
+  });
+}
+
+size_t gemm_dx_parts(int64_t rows, int64_t C_in, int64_t room) { return parts_of(rows, C_in, 2 * room, 1); }
+size_t gemm_dw_parts(int64_t rows, int64_t C_in, int64_t C_out) { return parts_of(C_out, C_in, rows, 2); }
+
+hipError_t gemm_dx(const bf16_t *d, int64_t room, int64_t rows, const bf16_t *w_gate, const bf16_t *w_up, int64_t ldw, int64_t C_in, int64_t C_out,
+                   bf16_t *dx, int64_t ld, float *part, hipStream_t s) {
+  Operand x = {}, w = {};
+  x.p[0] = reinterpret_cast<const char *>(d), x.ld = 4 * room, x.lines = rows, x.k = 2 * room;
+  w.p[0] = reinterpret_cast<const char *>(w_gate), w.p[1] = reinterpret_cast<const char *>(w_up);
+  w.ld = ldw * 2, w.lines = ldw, w.k = C_out, w.turn = room;
+  const Result r{{dx, nullptr}, ld, rows, C_in, 0, part};
+  return product<false>(r, x, w, 2 * room, 1, s);
+}
+
+hipError_t gemm_dw(const bf16_t *d, int64_t room, int64_t rows, const bf16_t *x, int64_t ldx, int64_t width, int64_t C_in, int64_t C_out,
+                   bf16_t *dw_gate, bf16_t *dw_up, float *part, hipStream_t s) {
+  Operand a = {}, b = {};
+  a.p[0] = reinterpret_cast<const char *>(d), a.ld = 4 * room, a.lines = room, a.k = rows;
+  b.p[0] = reinterpret_cast<const char *>(x), b.ld = ldx * 2, b.lines = width, b.k = rows;
+  const int halves = dw_gate && dw_up ? 2 : 1;
+  if (!dw_gate) a.p[0] += room * 2;
+  const Result r{{dw_gate ? dw_gate : dw_up, halves == 2 ? dw_up : nullptr}, C_in, C_out, C_in, room, part};
+  return product<true>(r, a, b, rows, halves, s);
+}
+
+}  // namespace wcc

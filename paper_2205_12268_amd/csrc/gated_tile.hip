@@ -108,7 +108,7 @@ struct Grid {
 // ---- the two projections -------------------------------------------------------------------------------------
 template <class T, int ACT, bool BACK, bool PARTS>
 __global__ __launch_bounds__(256, 2) void gate_tile_kernel(Gate<T> p, Side<T> x, const T *__restrict__ w_gate, const T *__restrict__ w_up,
-                                                           int64_t k, Grid n, float *__restrict__ part) {
+                                                           int64_t ldw, int64_t k, Grid n, float *__restrict__ part) {
   __shared__ __align__(16) unsigned char lds[2][2 * kTile * kRowBytes];
   const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, ln = lane & 31, half = lane >> 5, wm = wv >> 1, wn = wv & 1;
   const int64_t at = in_runs(blockIdx.x, n.tiles * n.splits), split = at / n.tiles;
@@ -121,7 +121,7 @@ __global__ __launch_bounds__(256, 2) void gate_tile_kernel(Gate<T> p, Side<T> x,
   a.aim([&](int i, bool &there) { there = true; return x.p + min(t0 + i, x.lines - 1) * x.s; }, 1);
   b.aim([&](int i, bool &there) {
     there = true;
-    return (i < kTile / 2 ? w_gate : w_up) + (int64_t)min(o0 + i % (kTile / 2), p.outs - 1) * k;
+    return (i < kTile / 2 ? w_gate : w_up) + (int64_t)min(o0 + i % (kTile / 2), p.outs - 1) * ldw;
   }, 1);
   f32x16 acc[2][2] = {};
   multiply<T>(a, b, split * n.chunk, min(k, (split + 1) * n.chunk), wm, [&](int e) { return e * (kTile / 2) + wn * 32; }, lds, acc);
@@ -282,21 +282,21 @@ size_t tile_product_parts(int64_t rows, int64_t lines, int64_t k, int batches) {
 }
 
 template <class T>
-hipError_t tile_gate(const Gate<T> &p, int act, bool back, const Side<T> &x, const T *w_gate, const T *w_up, int64_t k, float *part,
-                     hipStream_t s) {
+hipError_t tile_gate(const Gate<T> &p, int act, bool back, const Side<T> &x, const T *w_gate, const T *w_up, int64_t ldw, int64_t k,
+                     float *part, hipStream_t s) {
   const Grid n = grid_of(p.rows, p.outs, kTile / 2, k, 1);
   const unsigned blocks = (unsigned)(n.tiles * n.splits);
   return by_act(act, [&](auto a) {
     constexpr int ACT = decltype(a)::value;
     if (n.splits > 1) {
-      gate_tile_kernel<T, WCC_ACT_NONE, false, true><<<blocks, 256, 0, s>>>(p, x, w_gate, w_up, k, n, part);
+      gate_tile_kernel<T, WCC_ACT_NONE, false, true><<<blocks, 256, 0, s>>>(p, x, w_gate, w_up, ldw, k, n, part);
       const unsigned join = (unsigned)tiles(p.rows * (p.room / 4), 256);
       if (back) gate_join_kernel<T, ACT, true><<<join, 256, 0, s>>>(p, n.splits, part);
       else gate_join_kernel<T, ACT, false><<<join, 256, 0, s>>>(p, n.splits, part);
     } else if (back) {
-      gate_tile_kernel<T, ACT, true, false><<<blocks, 256, 0, s>>>(p, x, w_gate, w_up, k, n, part);
+      gate_tile_kernel<T, ACT, true, false><<<blocks, 256, 0, s>>>(p, x, w_gate, w_up, ldw, k, n, part);
     } else {
-      gate_tile_kernel<T, ACT, false, false><<<blocks, 256, 0, s>>>(p, x, w_gate, w_up, k, n, part);
+      gate_tile_kernel<T, ACT, false, false><<<blocks, 256, 0, s>>>(p, x, w_gate, w_up, ldw, k, n, part);
     }
     return hipGetLastError();
   });
@@ -316,9 +316,10 @@ hipError_t tile_product(const Product<T> &p, float *part, hipStream_t s) {
   return hipGetLastError();
 }
 
-template hipError_t tile_gate<float>(const Gate<float> &, int, bool, const Side<float> &, const float *, const float *, int64_t, float *, hipStream_t);
-template hipError_t tile_gate<bf16_t>(const Gate<bf16_t> &, int, bool, const Side<bf16_t> &, const bf16_t *, const bf16_t *, int64_t, float *,
-                                      hipStream_t);
+template hipError_t tile_gate<float>(const Gate<float> &, int, bool, const Side<float> &, const float *, const float *, int64_t, int64_t,
+                                     float *, hipStream_t);
+template hipError_t tile_gate<bf16_t>(const Gate<bf16_t> &, int, bool, const Side<bf16_t> &, const bf16_t *, const bf16_t *, int64_t,
+                                      int64_t, float *, hipStream_t);
 template hipError_t tile_product<float, false>(const Product<float> &, float *, hipStream_t);
 template hipError_t tile_product<float, true>(const Product<float> &, float *, hipStream_t);
 template hipError_t tile_product<bf16_t, false>(const Product<bf16_t> &, float *, hipStream_t);
