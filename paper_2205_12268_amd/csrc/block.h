@@ -107,18 +107,25 @@ __device__ __forceinline__ void act_of(float z, float &v, float &s) {
     const float e = exp_neg<T>(z), d = 1.f + e, p = sizeof(T) == 2 ? rcp_fast(d) : 1.f / d;
     v = z * p, s = p * fmaf(z, 1.f - p, 1.f);
   } else {
-    float below, bell;  // Phi(z), and exp(-z^2 / 2)
+    // Phi(-|z|) = exp(-z^2 / 2) q(t) with t = 1 / (1 + c |z|), q a polynomial; the slope needs the exponential too.  bf16: q from formula
+    // 7.1.26 of Abramowitz and Stegun for erf, off by 1.5e-7.  fp32: q fitted to scaled erfc on (0, 1], largest |z| times the error made
+    // smallest, 8e-11; evaluated in fp32 Phi is off by 2.2e-7 at most.  (erfcf and expf by themselves: 1156 x 960 values three times
+    // 13.3 us for the gradient's first pass.)
+    const float bell = exp2_fast(z * z * (-0.5f * kLog2e));
+    float q;
     if constexpr (sizeof(T) == 2) {
-      // erf by formula 7.1.26 of Abramowitz and Stegun, off by 1.5e-7; it needs the exponential that the slope needs too
-      bell = exp2_fast(z * z * (-0.5f * kLog2e));
       const float t = rcp_fast(fmaf(fabsf(z), 0.3275911f * 0.70710678f, 1.f));
-      const float poly = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
-      const float tail = 0.5f * poly * bell;
-      below = z > 0.f ? 1.f - tail : tail;
+      q = 0.5f * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
     } else {
-      below = 0.5f * erfcf(z * -0.70710678118654752f);
-      bell = expf(-0.5f * z * z);
+      constexpr float c[8] = {0.10840163007532476f, 0.12539058690897514f, 0.020029725850715104f, 0.3222110849783336f, -0.35860964023713915f,
+                              0.4851653549820245f, -0.24534892171368822f, 0.04276017923424634f};
+      const float t = rcp_fast(fmaf(fabsf(z), 0.275f, 1.f));
+      q = c[7];
+#pragma unroll
+      for (int i = 6; i >= 0; --i) q = fmaf(q, t, c[i]);
+      q *= t;
     }
+    const float tail = q * bell, below = z > 0.f ? 1.f - tail : tail;
     v = z * below, s = fmaf(z * 0.39894228040143268f, bell, below);
   }
 }

@@ -9,8 +9,9 @@
 // sums of x and x^2 are fp64: products of fp32 values are exact there, so that a mean far above the spread costs nothing that a
 // shift would have to bring back.
 //
-// Three launches: sums of chunks of pixels by channel; a small one that joins them; a second pass that goes backwards over the chunks,
-// so that it begins with what the caches hold.  Bound by memory: the second pass reads again what the first has read.
+// Maps that one workgroup's registers hold (a sample, some of its groups) take one launch.  Larger ones take three: sums of chunks of
+// pixels by channel; a small one that joins them; a second pass that goes backwards over the chunks, so that it begins with what
+// the caches hold; where the chunks are few, the second pass joins them and there are two.  Bound by memory: the second pass reads again what the first has read.
 #include "block.h"
 
 namespace wcc {
@@ -33,6 +34,16 @@ struct Sums {
 
 __device__ __forceinline__ int64_t pixels_of(const int32_t *counts, int64_t pixels, int sample) {
   return counts ? min((int64_t)max(counts[sample], 0), pixels) : pixels;
+}
+
+// mean and rstd from the sums of values and of their squares, by 1 / their number.  The reciprocal root is the hardware's, two steps of
+// Newton's behind it.
+__device__ __forceinline__ float2 stat_of(const double2 &s, double per, float eps) {
+  const double mean = s.x * per, rest = s.y * per - mean * mean, v = (rest < 0.0 ? 0.0 : rest) + (double)eps;  // (NaN stays)
+  double r = __builtin_amdgcn_rsq(v);
+  r = r * fma(-0.5 * v * r, r, 1.5);
+  r = r * fma(-0.5 * v * r, r, 1.5);
+  return float2{(float)mean, (float)r};
 }
 
 // The input of the backward pass: x itself, or what it is kept as.
@@ -73,8 +84,8 @@ template <int VE>
 struct Place {
   int sample, chunk, rows, col, ty, c0;
   int64_t begin, end;  // the thread's first pixel, the chunk's end
-  __device__ __forceinline__ Place(int64_t b, const Shape &d, const Sums &s, const int32_t *counts, int lanes) {
-    sample = (int)(b / s.chunks), chunk = (int)(b % s.chunks);
+  __device__ __forceinline__ Place(int b, const Shape &d, const Sums &s, const int32_t *counts, int lanes) {
+    sample = b / s.chunks, chunk = b % s.chunks;
     rows = 256 / lanes;
     col = threadIdx.x % lanes, ty = threadIdx.x / lanes;
     c0 = (blockIdx.y * lanes + col) * VE;
@@ -94,19 +105,49 @@ __device__ __forceinline__ void affine(const float *gamma, const float *beta, in
   }
 }
 
+// Pairs of sums of NT threads' VE channels in LDS, one channel's after the other (a thread's own side by side would all be on one bank).
+template <int NT, int VE>
+struct Room {
+  double2 v[VE][NT + 1];
+  __device__ __forceinline__ void put(const double (&a)[VE], const double (&b)[VE]) {
+#pragma unroll
+    for (int j = 0; j < VE; ++j) v[j][threadIdx.x] = double2{a[j], b[j]};
+  }
+  // channel c of the threads from `first` on
+  __device__ __forceinline__ double2 at(int first, int c) const { return v[c % VE][first + c / VE]; }
+};
+
 // the threads' sums by channel added up over the pixels' threads, to the chunk's place in `part`
 template <int VE>
 __device__ __forceinline__ void leave_sums(const Shape &d, const Sums &s, const Place<VE> &at, int lanes, const double (&a)[VE],
-                                           const double (&b)[VE], double2 *room) {
-#pragma unroll
-  for (int j = 0; j < VE; ++j) room[threadIdx.x * VE + j] = double2{a[j], b[j]};
+                                           const double (&b)[VE], Room<256, VE> &room) {
+  room.put(a, b);
   __syncthreads();
   const int width = lanes * VE, first = blockIdx.y * width;
   double2 *out = s.part + ((int64_t)at.sample * s.chunks + at.chunk) * d.C + first;
   for (int c = threadIdx.x; c < min(width, d.C - first); c += 256) {
-    double2 v = room[c];
-    for (int r = 1; r < at.rows; ++r) v.x += room[r * width + c].x, v.y += room[r * width + c].y;
+    double2 v = {0.0, 0.0};
+    for (int r = 0; r < at.rows; ++r) {
+      const double2 q = room.at(r * lanes, c);
+      v.x += q.x, v.y += q.y;
+    }
     out[c] = v;
+  }
+}
+
+// A pair of sums for each group from `entries` pairs each, entry(g, i), a power of two of threads for each group; to all[g].
+template <int NT, class F>
+__device__ __forceinline__ void by_group(int groups, int entries, double2 *all, F entry) {
+  int lg = 0;
+  while (lg < 6 && groups << (lg + 1) <= NT) ++lg;
+  for (int g = threadIdx.x >> lg; g < groups; g += NT >> lg) {
+    double2 v = {0.0, 0.0};
+    for (int i = threadIdx.x & ((1 << lg) - 1); i < entries; i += 1 << lg) {
+      const double2 q = entry(g, i);
+      v.x += q.x, v.y += q.y;
+    }
+    for (int off = 1 << lg >> 1; off > 0; off >>= 1) v.x += __shfl_xor(v.x, off, 64), v.y += __shfl_xor(v.y, off, 64);
+    if ((threadIdx.x & ((1 << lg) - 1)) == 0) all[g] = v;
   }
 }
 
@@ -115,7 +156,7 @@ template <class T>
 __global__ __launch_bounds__(256) void norm_sums_kernel(const T *__restrict__ x, const int32_t *__restrict__ counts, Shape d, Sums s,
                                                         int lanes) {
   constexpr int VE = VecOf<T>::N;
-  __shared__ double2 room[256 * VE];
+  __shared__ Room<256, VE> room;
   const Place<VE> at(blockIdx.x, d, s, counts, lanes);
   double sum[VE] = {}, sq[VE] = {};
   if (at.ty < at.rows && at.c0 < d.C) {
@@ -136,32 +177,37 @@ __global__ __launch_bounds__(256) void norm_sums_kernel(const T *__restrict__ x,
   leave_sums<VE>(d, s, at, lanes, sum, sq, room);
 }
 
-// ---- the chunks joined: a workgroup for each group of a sample -------------------------------------------------
-// `lanes` channels side by side, the other threads over the chunks.  BACK: chan is left too, and m1, m2 beside the statistics.
+// ---- the chunks joined -----------------------------------------------------------------------------------------
+// A workgroup for each group of a sample: a power of two (`lanes`, 64 at most) of channels side by side, the other threads over the
+// chunks.  BACK: m1 and m2 beside the statistics, and chan is left.
 template <bool BACK>
 __global__ __launch_bounds__(256) void norm_join_kernel(const int32_t *__restrict__ counts, Shape d, Sums s, const float *__restrict__ gamma,
                                                         float *__restrict__ stats, int lanes) {
-  __shared__ double2 room[256];
-  const int group = blockIdx.x % d.groups, sample = blockIdx.x / d.groups, rows = 256 / lanes, tid = threadIdx.x;
-  const int col = tid % lanes, ty = tid / lanes;
+  __shared__ double2 room[4][64];
+  const int group = blockIdx.x % d.groups, sample = blockIdx.x / d.groups, tid = threadIdx.x, lane = tid & 63;
+  const int rows = 256 / lanes, col = tid % lanes, ty = tid / lanes;
   const int64_t n = pixels_of(counts, d.pixels, sample);
   const int chunks = (int)min((int64_t)s.chunks, (n + s.chunk - 1) / s.chunk);
+  const double per = 1.0 / (double)max(n * d.per, (int64_t)1);
   double2 all = {0.0, 0.0};
   for (int c0 = 0; c0 < d.per; c0 += lanes) {
-    double2 a = {0.0, 0.0};
     const int c = c0 + col;
-    if (ty < rows && c < d.per) {
+    double2 a = {0.0, 0.0};
+    if (c < d.per) {
       const double2 *p = s.part + (int64_t)sample * s.chunks * d.C + group * d.per + c;
-#pragma unroll 4
+#pragma unroll 8
       for (int k = ty; k < chunks; k += rows) {
         const double2 v = p[(int64_t)k * d.C];
         a.x += v.x, a.y += v.y;
       }
     }
-    room[tid] = a;
+    for (int off = lanes; off < 64; off <<= 1) a.x += __shfl_xor(a.x, off, 64), a.y += __shfl_xor(a.y, off, 64);
+    if (lane < lanes) room[tid >> 6][lane] = a;
     __syncthreads();
     if (tid < lanes && c < d.per) {
-      for (int r = 1; r < rows; ++r) a.x += room[r * lanes + col].x, a.y += room[r * lanes + col].y;
+      a = {0.0, 0.0};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) a.x += room[w][lane].x, a.y += room[w][lane].y;
       if constexpr (BACK) {
         s.chan[(int64_t)sample * d.C + group * d.per + c] = a;
         const double w = gamma ? gamma[group * d.per + c] : 1.f;
@@ -171,39 +217,81 @@ __global__ __launch_bounds__(256) void norm_join_kernel(const int32_t *__restric
     }
     __syncthreads();
   }
-  room[tid] = all;  // (0 beyond `lanes`)
-  __syncthreads();
-  for (int h = 128; h > 0; h >>= 1) {
-    if (tid < h) room[tid].x += room[tid + h].x, room[tid].y += room[tid + h].y;
-    __syncthreads();
-  }
+  if (tid >= 64) return;
+  for (int off = lanes >> 1; off > 0; off >>= 1) all.x += __shfl_xor(all.x, off, 64), all.y += __shfl_xor(all.y, off, 64);
   if (tid != 0) return;
-  const double size = (double)max(n * d.per, (int64_t)1);
   const int64_t at = blockIdx.x;
   if constexpr (BACK) {
-    s.group[at] = float4{stats[2 * at], stats[2 * at + 1], (float)(room[0].x / size), (float)(room[0].y / size)};
+    s.group[at] = float4{stats[2 * at], stats[2 * at + 1], (float)(all.x * per), (float)(all.y * per)};
   } else {
-    const double mean = room[0].x / size, left = room[0].y / size - mean * mean, var = left < 0.0 ? 0.0 : left;  // (NaN stays)
-    const float rstd = (float)(1.0 / sqrt(var + (double)d.eps));
-    s.group[at] = float4{(float)mean, rstd, 0.f, 0.f};
-    if (stats) stats[2 * at] = (float)mean, stats[2 * at + 1] = rstd;
+    const float2 q = stat_of(all, per, d.eps);
+    s.group[at] = float4{q.x, q.y, 0.f, 0.f};
+    if (stats) stats[2 * at] = q.x, stats[2 * at + 1] = q.y;
   }
 }
 
+// The same by every workgroup of the second pass for its sample, where the chunks are few and the channels kShort at most: groups'
+// values to `group` in LDS.  The sample's first workgroup leaves the statistics.
+constexpr int kShort = 512;
+struct ShortRoom {
+  double2 chan[kShort], all[kShort];
+  float4 group[kShort];
+};
+template <bool BACK>
+__device__ __forceinline__ void join_short(int sample, bool first, int64_t n, const Shape &d, const Sums &s, const float *gamma, float *stats,
+                                           ShortRoom &room) {
+  const int chunks = (int)min((int64_t)s.chunks, (n + s.chunk - 1) / s.chunk);
+  const double per = 1.0 / (double)max(n * d.per, (int64_t)1);
+  const int parts = max(256 / d.C, 1);
+  for (int i = threadIdx.x; i < parts * d.C; i += 256) {
+    const int c = i % d.C;
+    const double2 *p = s.part + (int64_t)sample * s.chunks * d.C + c;
+    double2 a = {0.0, 0.0};
+#pragma unroll 8
+    for (int k = i / d.C; k < chunks; k += parts) {
+      const double2 v = p[(int64_t)k * d.C];
+      a.x += v.x, a.y += v.y;
+    }
+    const double w = BACK && gamma ? gamma[c] : 1.f;
+    room.chan[i] = double2{a.x * w, a.y * w};
+  }
+  __syncthreads();
+  by_group<256>(d.groups, parts * d.per, room.all, [&](int g, int i) { return room.chan[i / d.per * d.C + g * d.per + i % d.per]; });
+  __syncthreads();
+  for (int g = threadIdx.x; g < d.groups; g += 256) {
+    const int64_t at = (int64_t)sample * d.groups + g;
+    if constexpr (BACK) {
+      room.group[g] = float4{stats[2 * at], stats[2 * at + 1], (float)(room.all[g].x * per), (float)(room.all[g].y * per)};
+    } else {
+      const float2 q = stat_of(room.all[g], per, d.eps);
+      room.group[g] = float4{q.x, q.y, 0.f, 0.f};
+      if (stats && first) stats[2 * at] = q.x, stats[2 * at + 1] = q.y;
+    }
+  }
+  __syncthreads();
+}
+
 // ---- forward: the second pass ------------------------------------------------------------------------------
-template <class T, int ACT, bool KEEP>
+template <class T, int ACT, bool KEEP, bool SHORT>
 __global__ __launch_bounds__(256) void norm_apply_kernel(const T *x, const float *__restrict__ gamma, const float *__restrict__ beta,
                                                          const int32_t *__restrict__ counts, Shape d, Sums s, int lanes, T *y,
-                                                         int8_t *__restrict__ codes, uint8_t *__restrict__ steps) {
+                                                         float *__restrict__ stats, int8_t *__restrict__ codes,
+                                                         uint8_t *__restrict__ steps) {
   constexpr int VE = VecOf<T>::N;
+  __shared__ std::conditional_t<SHORT, ShortRoom, char> room;
   const Place<VE> at(gridDim.x - 1 - blockIdx.x, d, s, counts, lanes);
   const int c0 = at.c0, blocks = (d.C + kKept - 1) / kKept;
+  if constexpr (SHORT)
+    join_short<false>(at.sample, at.chunk == 0 && blockIdx.y == 0, pixels_of(counts, d.pixels, at.sample), d, s, nullptr, stats, room);
   if (at.ty >= at.rows || c0 >= (KEEP ? blocks * kKept : d.C)) return;
   float g[VE], b[VE], mean[VE];
   affine<VE>(gamma, beta, c0, d.C, g, b);
 #pragma unroll
   for (int j = 0; j < VE; ++j) {
-    const float4 q = s.group[(int64_t)at.sample * d.groups + min(c0 + j, d.C - 1) / d.per];
+    const int group = min(c0 + j, d.C - 1) / d.per;
+    float4 q;
+    if constexpr (SHORT) q = room.group[group];
+    else q = s.group[(int64_t)at.sample * d.groups + group];
     mean[j] = q.x, g[j] *= q.y;
   }
   const int64_t row0 = (int64_t)at.sample * d.pixels;
@@ -238,7 +326,7 @@ __global__ __launch_bounds__(256) void norm_grad_sums_kernel(Input<T, KEPT> in, 
                                                              const float *__restrict__ beta, const float *__restrict__ stats,
                                                              const int32_t *__restrict__ counts, Shape d, Sums s, int lanes) {
   constexpr int VE = VecOf<T>::N;
-  __shared__ double2 room[256 * VE];
+  __shared__ Room<256, VE> room;
   const Place<VE> at(blockIdx.x, d, s, counts, lanes);
   const int c0 = at.c0;
   double sum[VE] = {}, dot[VE] = {};
@@ -282,19 +370,51 @@ __global__ __launch_bounds__(256) void norm_grad_sums_kernel(Input<T, KEPT> in, 
 }
 
 // ---- backward: the second pass -----------------------------------------------------------------------------
-template <class T, int ACT, bool KEPT>
+// dgamma and dbeta of a channel, over the samples (and SHORT, their chunks) in their order
+template <bool SHORT>
+__device__ __forceinline__ void affine_grad(int c, const Shape &d, const Sums &s, float *dgamma, float *dbeta) {
+  if (c >= d.C) return;
+  const double2 *p = (SHORT ? s.part : s.chan) + c;
+  const int n = d.samples * (SHORT ? s.chunks : 1);
+  double2 a = {0.0, 0.0};
+#pragma unroll 8
+  for (int i = 0; i < n; ++i) {
+    const double2 v = p[(int64_t)i * d.C];
+    a.x += v.x, a.y += v.y;
+  }
+  if (dbeta) dbeta[c] = (float)a.x;
+  if (dgamma) dgamma[c] = (float)a.y;
+}
+template <bool SHORT>
+__global__ __launch_bounds__(256) void norm_affine_grad_kernel(Shape d, Sums s, float *__restrict__ dgamma, float *__restrict__ dbeta) {
+  affine_grad<SHORT>(blockIdx.x * 256 + threadIdx.x, d, s, dgamma, dbeta);
+}
+
+// (workgroups past `tiles` do dgamma and dbeta)
+template <class T, int ACT, bool KEPT, bool SHORT>
 __global__ __launch_bounds__(256) void norm_grad_apply_kernel(Input<T, KEPT> in, const T *dy, const float *__restrict__ gamma,
                                                               const float *__restrict__ beta, const int32_t *__restrict__ counts, Shape d,
-                                                              Sums s, int lanes, T *dx) {
+                                                              Sums s, int lanes, int tiles, T *dx, float *__restrict__ stats,
+                                                              float *__restrict__ dgamma, float *__restrict__ dbeta) {
   constexpr int VE = VecOf<T>::N;
-  const Place<VE> at(gridDim.x - 1 - blockIdx.x, d, s, counts, lanes);
+  __shared__ std::conditional_t<SHORT, ShortRoom, char> room;
+  if ((int)blockIdx.x >= tiles) {
+    if (blockIdx.y == 0) affine_grad<SHORT>((blockIdx.x - tiles) * 256 + threadIdx.x, d, s, dgamma, dbeta);
+    return;
+  }
+  const Place<VE> at(tiles - 1 - blockIdx.x, d, s, counts, lanes);
   const int c0 = at.c0;
+  if constexpr (SHORT) join_short<true>(at.sample, false, pixels_of(counts, d.pixels, at.sample), d, s, gamma, stats, room);
   if (at.ty >= at.rows || c0 >= d.C) return;
   float g[VE], b[VE];
   float4 q[VE];
   affine<VE>(gamma, beta, c0, d.C, g, b);
 #pragma unroll
-  for (int j = 0; j < VE; ++j) q[j] = s.group[(int64_t)at.sample * d.groups + min(c0 + j, d.C - 1) / d.per];
+  for (int j = 0; j < VE; ++j) {
+    const int group = min(c0 + j, d.C - 1) / d.per;
+    if constexpr (SHORT) q[j] = room.group[group];
+    else q[j] = s.group[(int64_t)at.sample * d.groups + group];
+  }
   const int64_t row0 = (int64_t)at.sample * d.pixels;
   for (int64_t t = at.begin; t < at.end; t += 4 * at.rows) {
     u32x4 w[4];
@@ -322,28 +442,239 @@ __global__ __launch_bounds__(256) void norm_grad_apply_kernel(Input<T, KEPT> in,
   }
 }
 
-// dgamma and dbeta: a thread for each channel, over the samples in their order
-__global__ __launch_bounds__(256) void norm_affine_grad_kernel(const double2 *__restrict__ chan, int samples, int C, float *__restrict__ dgamma,
-                                                               float *__restrict__ dbeta) {
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= C) return;
-  double2 a = {0.0, 0.0};
-#pragma unroll 4
-  for (int i = 0; i < samples; ++i) {
-    const double2 v = chan[(int64_t)i * C + c];
-    a.x += v.x, a.y += v.y;
+// ---- maps that a workgroup's registers hold: one launch --------------------------------------------------------
+// A workgroup has a sample's pixels of `take` neighbouring groups; `lanes` threads side by side hold vectors of their channels (from the
+// first group's on, at any element), kHeld vectors a thread at most.
+constexpr int kThreads = 512, kHeld = 8, kWidest = 512;  // kWidest: channels of a workgroup
+
+template <class T>
+struct HeldPlace {
+  static constexpr int VE = VecOf<T>::N;
+  int sample, first, groups, width, lanes, rows, col, ty, c0, left;  // first: group; c0: channel; left: channels of the workgroup from it on
+  int64_t n, row0;
+  __device__ __forceinline__ HeldPlace(const Shape &d, const int32_t *counts, int take, int lanes_) : lanes(lanes_) {
+    const int tiles = (d.groups + take - 1) / take;
+    sample = blockIdx.x / tiles, first = blockIdx.x % tiles * take;
+    groups = min(take, d.groups - first), width = groups * d.per;
+    rows = kThreads / lanes;
+    col = threadIdx.x % lanes, ty = threadIdx.x / lanes;
+    c0 = first * d.per + col * VE, left = ty < rows ? width - col * VE : 0;
+    n = pixels_of(counts, d.pixels, sample);
+    row0 = (int64_t)sample * d.pixels;
   }
-  if (dbeta) dbeta[c] = (float)a.x;
-  if (dgamma) dgamma[c] = (float)a.y;
+  __device__ __forceinline__ bool there(int i) const { return left > 0 && ty + (int64_t)i * rows < n; }
+  __device__ __forceinline__ int64_t row(int i) const { return row0 + ty + (int64_t)i * rows; }
+};
+
+// The threads' pairs of sums by channel joined: the sum of each channel goes to f, the groups' to `all`; w(c): what a channel counts in
+// its group.  Columns first, in as many parts as there are threads, then the groups.
+template <class T, class F, class W>
+__device__ __forceinline__ void join_held(const HeldPlace<T> &at, int per, const double (&a)[VecOf<T>::N], const double (&b)[VecOf<T>::N],
+                                          Room<kThreads, VecOf<T>::N> &room, double2 *col_room, double2 *all, F f, W w) {
+  const int tid = threadIdx.x;
+  room.put(a, b);
+  __syncthreads();
+  const int parts = max(kThreads / at.width, 1);
+  for (int i = tid; i < parts * at.width; i += kThreads) {
+    const int c = i % at.width;
+    double2 v = {0.0, 0.0};
+#pragma unroll 4
+    for (int r = i / at.width; r < at.rows; r += parts) {
+      const double2 q = room.at(r * at.lanes, c);
+      v.x += q.x, v.y += q.y;
+    }
+    col_room[i] = v;
+  }
+  __syncthreads();
+  for (int c = tid; c < at.width; c += kThreads) {
+    double2 v = col_room[c];
+    for (int p = 1; p < parts; ++p) v.x += col_room[p * at.width + c].x, v.y += col_room[p * at.width + c].y;
+    f(c, v);
+  }
+  by_group<kThreads>(at.groups, parts * per, all, [&](int g, int i) {
+    const int c = g * per + i % per;
+    const double2 q = col_room[i / per * at.width + c];
+    const double weight = w(c);
+    return double2{q.x * weight, q.y * weight};
+  });
+  __syncthreads();
+}
+
+template <class T, int ACT, bool KEEP>
+__global__ __launch_bounds__(kThreads) void norm_held_kernel(const T *x, const float *__restrict__ gamma, const float *__restrict__ beta,
+                                                             const int32_t *__restrict__ counts, Shape d, int take, int lanes, T *y,
+                                                             float *__restrict__ stats, int8_t *__restrict__ codes,
+                                                             uint8_t *__restrict__ steps) {
+  constexpr int VE = VecOf<T>::N;
+  __shared__ Room<kThreads, VE> room;
+  __shared__ double2 col_room[kWidest], all[kWidest];
+  const HeldPlace<T> at(d, counts, take, lanes);
+  u32x4 v[kHeld];
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) v[i] = at.there(i) ? load_part<T>(x + at.row(i) * d.ldx + at.c0, at.left) : u32x4{};
+  float g[VE], b[VE], mean[VE];
+  affine<VE>(gamma, beta, at.c0, d.C, g, b);
+  const double per = 1.0 / (double)max(at.n * d.per, (int64_t)1);
+  double sum[VE] = {}, sq[VE] = {};
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i)
+#pragma unroll
+    for (int j = 0; j < VE; ++j) {
+      const double f = elem<T>(v[i], j);
+      sum[j] += f, sq[j] = fma(f, f, sq[j]);
+    }
+  join_held<T>(at, d.per, sum, sq, room, col_room, all, [](int, double2) {}, [](int) { return 1.0; });
+  float2 *stat_room = reinterpret_cast<float2 *>(col_room);  // (read by nobody any more)
+  for (int g = threadIdx.x; g < at.groups; g += kThreads) {
+    const float2 q = stat_of(all[g], per, d.eps);
+    stat_room[g] = q;
+    if (stats) {
+      float *p = stats + 2 * ((int64_t)at.sample * d.groups + at.first + g);
+      p[0] = q.x, p[1] = q.y;
+    }
+  }
+  __syncthreads();
+  const int blocks = (d.C + kKept - 1) / kKept;
+  const bool mine = KEEP ? at.ty < at.rows && at.c0 < blocks * kKept : at.left > 0;
+  if (!mine) return;
+#pragma unroll
+  for (int j = 0; j < VE; ++j) {
+    const float2 q = stat_room[min(at.col * VE + j, at.width - 1) / d.per];
+    mean[j] = q.x, g[j] *= q.y;
+  }
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    if (at.ty + (int64_t)i * at.rows >= at.n) break;
+    const int64_t row = at.row(i);
+    if constexpr (KEEP) {  // (the lanes of a block have the same pixels)
+      const uint32_t step = step_of(top_of_block<T>(v[i]));
+      store_codes<T>(codes + row * blocks * kKept + at.c0, v[i], per_step(step));
+      if (at.c0 % kKept == 0) steps[row * blocks + at.c0 / kKept] = (uint8_t)step;
+    }
+    float f[VE];
+#pragma unroll
+    for (int j = 0; j < VE; ++j) {
+      float slope;
+      act_of<T, ACT>(fmaf(elem<T>(v[i], j) - mean[j], g[j], b[j]), f[j], slope);
+    }
+    store_part<T>(y + row * d.ldy + at.c0, at.left, pack<T>(f));
+  }
+}
+
+template <class T, int ACT, bool KEPT>
+__global__ __launch_bounds__(kThreads) void norm_grad_held_kernel(Input<T, KEPT> in, const T *dy, const float *__restrict__ gamma,
+                                                                  const float *__restrict__ beta, const float *__restrict__ stats,
+                                                                  const int32_t *__restrict__ counts, Shape d, double2 *__restrict__ chan,
+                                                                  int take, int lanes, T *dx, float *__restrict__ dgamma,
+                                                                  float *__restrict__ dbeta) {
+  constexpr int VE = VecOf<T>::N;
+  __shared__ Room<kThreads, VE> room;
+  __shared__ double2 col_room[kWidest], all[kWidest];
+  const HeldPlace<T> at(d, counts, take, lanes);
+  typename Input<T, KEPT>::Raw v[kHeld];
+  u32x4 w[kHeld];
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    v[i] = {}, w[i] = u32x4{};
+    if (at.there(i)) v[i] = in.load(at.row(i), at.c0, at.left), w[i] = load_part<T>(dy + at.row(i) * d.ldy + at.c0, at.left);
+  }
+  float g[VE], b[VE], mean[VE], rstd[VE];
+  affine<VE>(gamma, beta, at.c0, d.C, g, b);
+#pragma unroll
+  for (int j = 0; j < VE; ++j) {
+    const int64_t q = 2 * ((int64_t)at.sample * d.groups + at.first + min(at.col * VE + j, at.width - 1) / d.per);
+    mean[j] = stats[q], rstd[j] = stats[q + 1];
+  }
+  const double per = 1.0 / (double)max(at.n * d.per, (int64_t)1);
+  double sum[VE] = {}, dot[VE] = {};
+#pragma unroll
+  for (int i0 = 0; i0 < kHeld; i0 += 4) {
+    float s4[VE] = {}, d4[VE] = {};  // (four at a time in fp32)
+#pragma unroll
+    for (int i = i0; i < i0 + 4; ++i) {
+      if (!at.there(i)) break;
+      const float step = in.step(v[i]);
+#pragma unroll
+      for (int j = 0; j < VE; ++j) {
+        const float xh = (in.at(v[i], j, step) - mean[j]) * rstd[j];
+        float value, slope;
+        act_of<T, ACT>(fmaf(xh, g[j], b[j]), value, slope);
+        const float dz = elem<T>(w[i], j) * slope;
+        s4[j] += dz, d4[j] = fmaf(dz, xh, d4[j]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < VE; ++j) sum[j] += s4[j], dot[j] += d4[j];
+  }
+  const int first = at.first * d.per;
+  join_held<T>(
+      at, d.per, sum, dot, room, col_room, all,
+      [&](int c, double2 s) {
+        if (d.samples > 1) {
+          chan[(int64_t)at.sample * d.C + first + c] = s;
+        } else {
+          if (dbeta) dbeta[first + c] = (float)s.x;
+          if (dgamma) dgamma[first + c] = (float)s.y;
+        }
+      },
+      [&](int c) { return gamma ? (double)gamma[first + c] : 1.0; });
+  if (!dx || at.left <= 0) return;
+  float m1[VE], m2[VE];
+#pragma unroll
+  for (int j = 0; j < VE; ++j) {
+    const double2 q = all[min(at.col * VE + j, at.width - 1) / d.per];
+    m1[j] = (float)(q.x * per), m2[j] = (float)(q.y * per);
+  }
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    if (!at.there(i)) break;
+    const float step = in.step(v[i]);
+    float f[VE];
+#pragma unroll
+    for (int j = 0; j < VE; ++j) {
+      const float xh = (in.at(v[i], j, step) - mean[j]) * rstd[j];
+      float value, slope;
+      act_of<T, ACT>(fmaf(xh, g[j], b[j]), value, slope);
+      f[j] = rstd[j] * ((elem<T>(w[i], j) * slope) * g[j] - m1[j] - xh * m2[j]);
+    }
+    store_part<T>(dx + at.row(i) * d.ldx + at.c0, at.left, pack<T>(f));
+  }
 }
 
 // ---- host ---------------------------------------------------------------------------------------------------
 struct Plan {
+  int take, take_kept;  // groups of a workgroup whose registers hold them, 0: none does; with codes
   int lanes, cols;  // threads side by side, workgroups side by side
   int chunks;
   int64_t chunk;
+  bool few;  // the second pass joins the chunks by itself
   size_t part, group, chan, bytes;
 };
+
+int held_lanes(const wcc_group_norm_desc &d, int take, int VE);
+
+// Groups of a workgroup whose registers hold their sample, 0 if none does.  As many as read 128 bytes of a pixel, a line of memory, where
+// that leaves 512 workgroups, else 64 or 16 bytes: a small map is bound by what a compute unit computes (one map of 256 pixels and 96
+// channels in one workgroup 9.8 us).  With codes, whole blocks of channels.
+int held_of(const wcc_group_norm_desc &d, int VE, bool kept) {
+  const int per = d.C / d.groups, size = 16 / VE;
+  auto fits = [&](int take) {
+    const int64_t width = (int64_t)take * per;
+    if (kept && width % kKept != 0 && take < d.groups) return false;
+    const int lanes = held_lanes(d, take, VE);
+    return lanes <= kThreads && (d.pixels + kThreads / lanes - 1) / (kThreads / lanes) <= kHeld;
+  };
+  int best = 0;
+  for (const int least : {16, 64, 128}) {
+    for (int take = 1; take <= d.groups && (int64_t)take * per <= kWidest; ++take) {
+      if (!fits(take) || ((int64_t)take * per * size < least && take < d.groups)) continue;
+      best = take;
+      break;
+    }
+    if (best && (int64_t)d.samples * ((d.groups + best - 1) / best) <= 512) break;
+  }
+  return best;
+}
 
 size_t up(size_t v) { return (v + 255) / 256 * 256; }
 
@@ -351,20 +682,26 @@ Plan plan_of(const wcc_group_norm_desc &d) {
   const int VE = d.dtype == WCC_F32 ? 4 : 8;
   const int64_t vectors = kept_blocks(d.C) * (kKept / VE);  // (whole blocks: what keeps x needs all lanes of each)
   Plan p;
-  p.lanes = (int)std::min<int64_t>(vectors, 256);
+  p.take = held_of(d, VE, false), p.take_kept = held_of(d, VE, true);
+  p.lanes = (int)std::min<int64_t>(vectors, 64);  // (1 KiB a pixel; with all of a wide map's a workgroup had one pixel at a time, and many chunks)
   p.cols = (int)((vectors + p.lanes - 1) / p.lanes);
   const int rows = 256 / p.lanes;
-  // chunks: as many as give every compute unit eight workgroups, of four pixels a thread at least
-  const int64_t most = std::max<int64_t>((d.pixels + 4 * rows - 1) / (4 * rows), 1);
+  // chunks: as many as give every compute unit eight workgroups, of eight pixels a thread at least
+  const int64_t most = std::max<int64_t>((d.pixels + 8 * rows - 1) / (8 * rows), 1);
   const int64_t want = std::max<int64_t>(2048 / std::max<int64_t>((int64_t)d.samples * p.cols, 1), 1);
   const int64_t n = std::min(most, want);
   p.chunk = std::max<int64_t>((d.pixels + n - 1) / n, 1);
   p.chunks = (int)std::max<int64_t>((d.pixels + p.chunk - 1) / p.chunk, 1);
+  p.few = d.C <= kShort && p.chunks * d.C <= 4096;
   p.part = 0;
   p.group = up((size_t)d.samples * p.chunks * d.C * sizeof(double2));
   p.chan = p.group + up((size_t)d.samples * d.groups * sizeof(float4));
   p.bytes = p.chan + up((size_t)d.samples * d.C * sizeof(double2));
   return p;
+}
+
+int held_lanes(const wcc_group_norm_desc &d, int take, int VE) {
+  return (int)(kept_blocks((int64_t)take * (d.C / d.groups)) * (kKept / VE));
 }
 
 Sums sums_of(const Plan &p, char *ws) {
@@ -374,7 +711,11 @@ Sums sums_of(const Plan &p, char *ws) {
 Shape shape_of(const wcc_group_norm_desc &d) {
   return Shape{d.pixels, d.ldx, d.ldy, d.samples, d.C, d.groups, d.C / d.groups, d.eps};
 }
-int join_lanes(const wcc_group_norm_desc &d) { return std::min(d.C / d.groups, 256); }
+int join_lanes(const wcc_group_norm_desc &d) {
+  int n = 1;
+  while (n < 64 && n < d.C / d.groups) n *= 2;
+  return n;
+}
 
 template <class F>
 void by_act(int act, F f) {
@@ -393,12 +734,31 @@ hipError_t forward(const wcc_group_norm_desc &d, const NormArgs &g, hipStream_t 
   const Shape sh = shape_of(d);
   const T *x = static_cast<const T *>(g.x);
   T *y = static_cast<T *>(g.y);
+  if (const int take = g.codes ? p.take_kept : p.take) {
+    const unsigned n = (unsigned)(d.samples * ((d.groups + take - 1) / take));
+    const int lanes = held_lanes(d, take, VecOf<T>::N);
+    by_act(d.act, [&](auto act) {
+      if (g.codes)
+        norm_held_kernel<T, act(), true>
+            <<<n, kThreads, 0, st>>>(x, g.gamma, g.beta, g.counts, sh, take, lanes, y, g.stats, g.codes, g.steps);
+      else
+        norm_held_kernel<T, act(), false>
+            <<<n, kThreads, 0, st>>>(x, g.gamma, g.beta, g.counts, sh, take, lanes, y, g.stats, nullptr, nullptr);
+    });
+    return hipGetLastError();
+  }
   const dim3 grid((unsigned)(p.chunks * d.samples), p.cols);
   norm_sums_kernel<T><<<grid, 256, 0, st>>>(x, g.counts, sh, s, p.lanes);
-  norm_join_kernel<false><<<(unsigned)(d.groups * d.samples), 256, 0, st>>>(g.counts, sh, s, nullptr, g.stats, join_lanes(d));
+  if (!p.few) norm_join_kernel<false><<<(unsigned)(d.groups * d.samples), 256, 0, st>>>(g.counts, sh, s, nullptr, g.stats, join_lanes(d));
   by_act(d.act, [&](auto act) {
-    if (g.codes) norm_apply_kernel<T, act(), true><<<grid, 256, 0, st>>>(x, g.gamma, g.beta, g.counts, sh, s, p.lanes, y, g.codes, g.steps);
-    else norm_apply_kernel<T, act(), false><<<grid, 256, 0, st>>>(x, g.gamma, g.beta, g.counts, sh, s, p.lanes, y, nullptr, nullptr);
+    auto go = [&](auto keep, auto few) {
+      norm_apply_kernel<T, act(), keep(), few()>
+          <<<grid, 256, 0, st>>>(x, g.gamma, g.beta, g.counts, sh, s, p.lanes, y, g.stats, g.codes, g.steps);
+    };
+    const std::true_type yes;
+    const std::false_type no;
+    if (p.few) g.codes ? go(yes, yes) : go(no, yes);
+    else g.codes ? go(yes, no) : go(no, no);
   });
   return hipGetLastError();
 }
@@ -411,16 +771,38 @@ hipError_t backward(const wcc_group_norm_desc &d, const NormArgs &g, hipStream_t
   const Input<T, KEPT> in{static_cast<const T *>(g.x), d.ldx, g.codes, g.steps, (int)kept_blocks(d.C)};
   const T *dy = static_cast<const T *>(g.dy);
   const dim3 grid((unsigned)(p.chunks * d.samples), p.cols);
-  if (d.samples > 0)
+  const bool wide = g.dgamma || g.dbeta;
+  const int take = KEPT ? p.take_kept : p.take;
+  if (take && d.samples > 0) {
+    const unsigned n = (unsigned)(d.samples * ((d.groups + take - 1) / take));
+    const int lanes = held_lanes(d, take, VecOf<T>::N);
+    by_act(d.act, [&](auto act) {
+      norm_grad_held_kernel<T, act(), KEPT><<<n, kThreads, 0, st>>>(in, dy, g.gamma, g.beta, g.stats, g.counts, sh, s.chan, take, lanes,
+                                                                   static_cast<T *>(g.dx), g.dgamma, g.dbeta);
+    });
+    if (d.samples == 1) return hipGetLastError();
+  } else if (d.samples > 0) {
+    const int n = p.chunks * d.samples, more = wide ? (d.C + 255) / 256 : 0;
     by_act(d.act, [&](auto act) {
       norm_grad_sums_kernel<T, act(), KEPT><<<grid, 256, 0, st>>>(in, dy, g.gamma, g.beta, g.stats, g.counts, sh, s, p.lanes);
-      norm_join_kernel<true><<<(unsigned)(d.groups * d.samples), 256, 0, st>>>(g.counts, sh, s, g.gamma, g.stats, join_lanes(d));
-      if (g.dx)
-        norm_grad_apply_kernel<T, act(), KEPT>
-            <<<grid, 256, 0, st>>>(in, dy, g.gamma, g.beta, g.counts, sh, s, p.lanes, static_cast<T *>(g.dx));
+      if (!p.few) norm_join_kernel<true><<<(unsigned)(d.groups * d.samples), 256, 0, st>>>(g.counts, sh, s, g.gamma, g.stats, join_lanes(d));
+      if (!g.dx) return;
+      const dim3 both((unsigned)(n + more), p.cols);
+      T *dx = static_cast<T *>(g.dx);
+      if (p.few)
+        norm_grad_apply_kernel<T, act(), KEPT, true>
+            <<<both, 256, 0, st>>>(in, dy, g.gamma, g.beta, g.counts, sh, s, p.lanes, n, dx, g.stats, g.dgamma, g.dbeta);
+      else
+        norm_grad_apply_kernel<T, act(), KEPT, false>
+            <<<both, 256, 0, st>>>(in, dy, g.gamma, g.beta, g.counts, sh, s, p.lanes, n, dx, g.stats, g.dgamma, g.dbeta);
     });
-  if (g.dgamma || g.dbeta)
-    norm_affine_grad_kernel<<<(unsigned)((d.C + 255) / 256), 256, 0, st>>>(s.chan, d.samples, d.C, g.dgamma, g.dbeta);
+    if (g.dx) return hipGetLastError();
+  }
+  if (wide) {
+    const unsigned n = (unsigned)((d.C + 255) / 256);
+    if (p.few && !take) norm_affine_grad_kernel<true><<<n, 256, 0, st>>>(sh, s, g.dgamma, g.dbeta);
+    else norm_affine_grad_kernel<false><<<n, 256, 0, st>>>(sh, s, g.dgamma, g.dbeta);
+  }
   return hipGetLastError();
 }
 

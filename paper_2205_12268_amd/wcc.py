@@ -289,8 +289,14 @@ def _kept(codes, steps, lead, width):
     return _whole(codes, (*lead, room), torch.int8), _whole(steps, (*lead, room // KEPT_BLOCK), torch.uint8)
 
 
+# (the current stream's handle without an object around it, which costs 2.5 us a call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream():
-    return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    if _raw_stream is None:
+        return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(torch.cuda.current_device())
 
 
 class Context:

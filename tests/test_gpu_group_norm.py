@@ -291,3 +291,26 @@ def test_no_samples(ctx):
     dgamma, dbeta = torch.ones(8, device="cuda"), torch.ones(8, device="cuda")
     ctx.wcc_group_norm_backward(d, None, None, None, None, None, None, None, None, None, dgamma, dbeta)
     assert not bool(dgamma.any()) and not bool(dbeta.any()) and CODE["f32"] == wcc.F32
+
+
+HELD = [  # samples, pixels, C, groups: what a workgroup's registers hold, and what is just too large for them
+    (2, 4096, 8, 1), (2, 4097, 8, 1), (1, 1024, 32, 4), (1, 1025, 32, 4), (3, 128, 256, 32), (1, 64, 512, 1), (1, 64, 520, 1), (300, 4, 128, 32),
+    (2, 2000, 64, 64), (7, 9, 480, 5), (1, 2048, 24, 2), (1, 8192, 4, 4),
+]
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("size", HELD, ids=lambda s: "x".join(map(str, s)))
+def test_what_registers_hold(ctx, t, size):
+    samples, pixels, C, groups = size
+    counts = [pixels, 0, pixels // 2] if samples == 3 else None
+    x, gamma, beta, counts, dy = inputs(samples, pixels, C, t, sum(size), 0, 0, counts)
+    got = forward(ctx, x, samples, groups, "silu", gamma, beta, counts)
+    mask = there(counts, samples, pixels)
+    want = group_norm(x, samples, groups, gamma, beta, counts, EPS, "silu", dy)
+    rows_near(got["y"], want["y"], mask, t == "bf16", "y")
+    near(got["stats"], want["stats"], False, "stats")
+    grads = backward(ctx, x, None, samples, groups, "silu", gamma, beta, counts, got["stats"], dy)
+    rows_near(grads["dx"], want["dx"], mask, t == "bf16", "dx")
+    for k in ("dgamma", "dbeta"):
+        near(grads[k], want[k], False, k)
