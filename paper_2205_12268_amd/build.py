@@ -14,7 +14,7 @@ LIB = os.path.join(CSRC, "libwcc.so")
 PROBE_LIB = os.path.join(CSRC, "libwcc_probe.so")
 SOURCES = ["haar_fwd.hip", "haar_keep.hip", "haar_inv.hip", "layer_tail.hip", "select.hip", "select_two.hip", "gather.hip", "pointwise.hip",
            "depthwise.hip", "haar_chain.hip", "scores.hip", "distill.hip", "adapter.hip", "adapter_tile.hip", "adapter_gemm.hip", "head_api.hip",
-           "rows_keep.hip", "group_norm.hip", "gated.hip", "gated_tile.hip", "gated_gemm.hip", "block_api.hip", "wcc_api.hip"]
+           "rows_keep.hip", "group_norm.hip", "gated.hip", "gated_tile.hip", "gated_gemm.hip", "gated_thin.hip", "block_api.hip", "wcc_api.hip"]
 PROBE_SOURCES = ["stream_probe.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-I" + INCLUDE,
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

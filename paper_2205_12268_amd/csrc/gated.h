@@ -102,9 +102,9 @@ struct Product {
   int batches;
 };
 
-// fp32 sums of ranges of k that the calls below leave in the workspace, in bytes
-size_t tile_gate_parts(int64_t rows, int64_t outs, int64_t k);
-size_t tile_product_parts(int64_t rows, int64_t lines, int64_t k, int batches);
+// fp32 sums of ranges of k that the calls below leave in the workspace, in bytes; size: of an element
+size_t tile_gate_parts(int64_t rows, int64_t outs, int64_t k, int size);
+size_t tile_product_parts(int64_t rows, int64_t lines, int64_t k, int batches, int size);
 
 template <class T>
 hipError_t tile_gate(const Gate<T> &p, int act, bool back, const Side<T> &x, const T *w_gate, const T *w_up, int64_t ldw, int64_t k,
@@ -115,6 +115,9 @@ hipError_t tile_product(const Product<T> &p, float *part, hipStream_t s);
 // bf16, many rows (gated_gemm.hip).  Operands whose k or lines are contiguous and 16 bytes a load: pointers and strides are multiples.
 bool gemm_takes(const void *p, int64_t ld, int64_t width);
 hipError_t gemm_gate(const Gate<bf16_t> &p, int act, bool back, const Side<bf16_t> &x, const bf16_t *w_gate, const bf16_t *w_up, int64_t ldw,
+                     int64_t k, hipStream_t s);
+// the same for few rows (gated_thin.hip)
+hipError_t thin_gate(const Gate<bf16_t> &p, int act, bool back, const Side<bf16_t> &x, const bf16_t *w_gate, const bf16_t *w_up, int64_t ldw,
                      int64_t k, hipStream_t s);
 size_t gemm_dx_parts(int64_t rows, int64_t C_in, int64_t room);
 size_t gemm_dw_parts(int64_t rows, int64_t C_in, int64_t C_out);

@@ -72,16 +72,18 @@ struct Plan {
   int64_t room, ldx, k;  // of d's halves; of rows and weights that were copied; C_in in whole chunks of 16 bytes
 };
 
+constexpr int kThin = 64;  // rows of few
+
 // Tiles fed straight from memory from 2^28 products on; rows or weights that 16-byte loads do not take are copied for it from 2^30 on.
 Plan plan_of(const wcc_gated_desc &g, bool backward) {
   Plan p = {};
-  const size_t size = g.dtype == WCC_F32 ? 4 : 2;
+  const int size = g.dtype == WCC_F32 ? 4 : 2;
   const double products = 2.0 * g.rows * g.C_in * g.C_out;
   p.room = room_of(g.C_out), p.ldx = room_of(g.C_in), p.k = (g.C_in + 7) / 8 * 8;
   p.copy_w = g.C_in % 8 != 0, p.copy_x = p.copy_w || g.ldx % 8 != 0;
-  p.gemm = g.dtype == WCC_BF16 && g.rows > 64 && g.ldx < 1 << 21 && products >= (p.copy_x ? 1 << 30 : 1 << 28);
+  p.gemm = g.dtype == WCC_BF16 && g.rows > kThin && g.ldx < 1 << 21 && products >= (p.copy_x ? 1 << 30 : 1 << 28);
   if (!p.gemm) p.copy_x = p.copy_w = false;
-  size_t parts = p.gemm ? 0 : tile_gate_parts(g.rows, g.C_out, g.C_in), at = 0;
+  size_t parts = tile_gate_parts(g.rows, g.C_out, g.C_in, size), at = 0;  // (tensors at odd addresses take these tiles)
   if (backward) at += up((size_t)g.rows * 2 * p.room * size);
   p.x = at;
   if (backward || p.copy_x) at += up((size_t)g.rows * p.ldx * size);
@@ -90,10 +92,7 @@ Plan plan_of(const wcc_gated_desc &g, bool backward) {
   p.part = at;
   if (backward) {
     if (p.gemm) parts = std::max({parts, gemm_dx_parts(g.rows, g.C_in, p.room), gemm_dw_parts(g.rows, g.C_in, g.C_out)});
-    // (tensors at odd addresses take the other tiles)
-    parts = std::max({parts, tile_gate_parts(g.rows, g.C_out, g.C_in), tile_product_parts(g.rows, g.C_in, g.C_out, 1), tile_product_parts(g.C_out, g.C_in, g.rows, 2)});
-  } else {
-    parts = std::max(parts, tile_gate_parts(g.rows, g.C_out, g.C_in));
+    parts = std::max({parts, tile_product_parts(g.rows, g.C_in, g.C_out, 1, size), tile_product_parts(g.C_out, g.C_in, g.rows, 2, size)});
   }
   p.bytes = p.part + up(parts);
   return p;
@@ -149,6 +148,8 @@ hipError_t prepare(const wcc_gated_desc &d, const Plan &p, const GatedArgs &g, b
 template <class T>
 hipError_t gate_of(const wcc_gated_desc &d, const Plan &p, const Gate<T> &gate, bool back, const Operands<T> &o, float *part, hipStream_t s) {
   if constexpr (sizeof(T) == 2) {
+    if (d.rows <= kThin && d.C_in % 8 == 0 && gemm_takes(o.x.p, o.x.s, p.k) && gemm_takes(o.wg, o.ldw, p.k) && gemm_takes(o.wu, o.ldw, p.k))
+      return thin_gate(gate, d.act, back, o.x, o.wg, o.wu, o.ldw, p.k, s);
     if (o.gemm) return gemm_gate(gate, d.act, back, o.x, o.wg, o.wu, o.ldw, p.k, s);
   }
   return tile_gate<T>(gate, d.act, back, o.x, o.wg, o.wu, o.ldw, d.C_in, part, s);
