@@ -70,17 +70,25 @@ __device__ __forceinline__ void finish(const Gate<T> &p, int64_t t, int o, float
     }
   } else {
     const T *top = p.dy + t * p.ldy + o;
+    T dy[4] = {};
+    if (left >= 4) {
+      __builtin_memcpy(dy, top, sizeof dy);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 3; ++j)
+        if (j < left) dy[j] = top[j];
+    }
     T dg[4], du[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       float v, s;
       act_of<T, ACT>(g[j], v, s);
-      const float dy = j < left ? widen(top[j]) : 0.f;
-      dg[j] = narrow<T>(j < left ? dy * u[j] * s : 0.f), du[j] = narrow<T>(j < left ? dy * v : 0.f);
+      const float d = widen(dy[j]);
+      dg[j] = narrow<T>(j < left ? d * u[j] * s : 0.f), du[j] = narrow<T>(j < left ? d * v : 0.f);
     }
-    T *at = p.d + t * 2 * p.room + o;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) at[j] = dg[j], at[p.room + j] = du[j];
+    T *at = p.d + t * 2 * p.room + o;  // (o and the room are multiples of 4)
+    __builtin_memcpy(__builtin_assume_aligned(at, 4 * sizeof(T)), dg, sizeof dg);
+    __builtin_memcpy(__builtin_assume_aligned(at + p.room, 4 * sizeof(T)), du, sizeof du);
   }
 }
 
@@ -112,18 +120,21 @@ hipError_t tile_gate(const Gate<T> &p, int act, bool back, const Side<T> &x, con
 template <class T, bool AT>
 hipError_t tile_product(const Product<T> &p, float *part, hipStream_t s);
 
-// bf16, many rows (gated_gemm.hip).  Operands whose k or lines are contiguous and 16 bytes a load: pointers and strides are multiples.
-bool gemm_takes(const void *p, int64_t ld, int64_t width);
-hipError_t gemm_gate(const Gate<bf16_t> &p, int act, bool back, const Side<bf16_t> &x, const bf16_t *w_gate, const bf16_t *w_up, int64_t ldw,
-                     int64_t k, hipStream_t s);
-// the same for few rows (gated_thin.hip)
+// Many rows (gated_gemm.hip).  Operands whose k or lines are contiguous and 16 bytes a load: pointers and strides are multiples.
+bool gemm_takes(const void *p, int64_t ld, int64_t width, int size);
+template <class T>
+hipError_t gemm_gate(const Gate<T> &p, int act, bool back, const Side<T> &x, const T *w_gate, const T *w_up, int64_t ldw, int64_t k, hipStream_t s);
+size_t gemm_dx_parts(int64_t rows, int64_t C_in, int64_t room, int size);
+size_t gemm_dw_parts(int64_t rows, int64_t C_in, int64_t C_out, int size);
+template <class T>
+hipError_t gemm_dx(const T *d, int64_t room, int64_t rows, const T *w_gate, const T *w_up, int64_t ldw, int64_t C_in, int64_t C_out, T *dx,
+                   int64_t ld, float *part, hipStream_t s);
+template <class T>
+hipError_t gemm_dw(const T *d, int64_t room, int64_t rows, const T *x, int64_t ldx, int64_t width, int64_t C_in, int64_t C_out, T *dw_gate,
+                   T *dw_up, float *part, hipStream_t s);
+
+// The two projections for few rows of bf16 (gated_thin.hip), operands as above.
 hipError_t thin_gate(const Gate<bf16_t> &p, int act, bool back, const Side<bf16_t> &x, const bf16_t *w_gate, const bf16_t *w_up, int64_t ldw,
                      int64_t k, hipStream_t s);
-size_t gemm_dx_parts(int64_t rows, int64_t C_in, int64_t room);
-size_t gemm_dw_parts(int64_t rows, int64_t C_in, int64_t C_out);
-hipError_t gemm_dx(const bf16_t *d, int64_t room, int64_t rows, const bf16_t *w_gate, const bf16_t *w_up, int64_t ldw, int64_t C_in, int64_t C_out,
-                   bf16_t *dx, int64_t ld, float *part, hipStream_t s);
-hipError_t gemm_dw(const bf16_t *d, int64_t room, int64_t rows, const bf16_t *x, int64_t ldx, int64_t width, int64_t C_in, int64_t C_out,
-                   bf16_t *dw_gate, bf16_t *dw_up, float *part, hipStream_t s);
 
 }  // namespace wcc

@@ -74,14 +74,17 @@ struct Plan {
 
 constexpr int kThin = 64;  // rows of few
 
-// Tiles fed straight from memory from 2^28 products on; rows or weights that 16-byte loads do not take are copied for it from 2^30 on.
+// Tiles fed straight from memory from 2^28 products on (fp32: 2^25); bf16 rows or weights that 16-byte loads do not take are copied for it
+// from 2^30 on, fp32 ones go by way of registers.
 Plan plan_of(const wcc_gated_desc &g, bool backward) {
   Plan p = {};
   const int size = g.dtype == WCC_F32 ? 4 : 2;
   const double products = 2.0 * g.rows * g.C_in * g.C_out;
   p.room = room_of(g.C_out), p.ldx = room_of(g.C_in), p.k = (g.C_in + 7) / 8 * 8;
-  p.copy_w = g.C_in % 8 != 0, p.copy_x = p.copy_w || g.ldx % 8 != 0;
-  p.gemm = g.dtype == WCC_BF16 && g.rows > kThin && g.ldx < 1 << 21 && products >= (p.copy_x ? 1 << 30 : 1 << 28);
+  const int each = 16 / size;
+  p.copy_w = g.C_in % each != 0, p.copy_x = p.copy_w || g.ldx % each != 0;
+  p.gemm = g.rows > kThin && (size == 2 ? products >= (p.copy_x ? 1 << 30 : 1 << 28) : !p.copy_w && products >= 1 << 25);
+  if (size == 4) p.copy_x = p.copy_w = false, p.k = g.C_in;
   if (!p.gemm) p.copy_x = p.copy_w = false;
   size_t parts = tile_gate_parts(g.rows, g.C_out, g.C_in, size), at = 0;  // (tensors at odd addresses take these tiles)
   if (backward) at += up((size_t)g.rows * 2 * p.room * size);
@@ -91,7 +94,7 @@ Plan plan_of(const wcc_gated_desc &g, bool backward) {
   if (p.copy_w) at += 2 * up((size_t)g.C_out * p.ldx * size);
   p.part = at;
   if (backward) {
-    if (p.gemm) parts = std::max({parts, gemm_dx_parts(g.rows, g.C_in, p.room), gemm_dw_parts(g.rows, g.C_in, g.C_out)});
+    if (p.gemm) parts = std::max({parts, gemm_dx_parts(g.rows, g.C_in, p.room, size), gemm_dw_parts(g.rows, g.C_in, g.C_out, size)});
     parts = std::max({parts, tile_product_parts(g.rows, g.C_in, g.C_out, 1, size), tile_product_parts(g.C_out, g.C_in, g.rows, 2, size)});
   }
   p.bytes = p.part + up(parts);
@@ -101,7 +104,7 @@ Plan plan_of(const wcc_gated_desc &g, bool backward) {
 // The operands of a call as its products take them.
 template <class T>
 struct Operands {
-  bool gemm;
+  bool takes, gemm;  // 16-byte loads; tiles fed straight from memory
   Side<T> x;
   const T *wg, *wu;
   int64_t ldw;
@@ -110,7 +113,7 @@ template <class T>
 hipError_t prepare(const wcc_gated_desc &d, const Plan &p, const GatedArgs &g, bool x_used, bool w_used, Operands<T> &o, hipStream_t s) {
   o.wg = static_cast<const T *>(g.w_gate), o.wu = static_cast<const T *>(g.w_up), o.ldw = d.C_in;
   o.x = Side<T>{static_cast<const T *>(g.x), d.ldx, d.rows};
-  o.gemm = p.gemm;
+  o.takes = true;
   hipError_t e = hipSuccess;
   if (x_used && !g.x) {  // (whole blocks: zeros behind the width)
     wcc_rows_desc r = {};
@@ -139,19 +142,19 @@ hipError_t prepare(const wcc_gated_desc &d, const Plan &p, const GatedArgs &g, b
       copy_kernel<<<dim3((unsigned)std::min<int64_t>((most + 255) / 256, 2048), n), 256, 0, s>>>(c);
       e = hipGetLastError();
     }
-    if (x_used) o.gemm = o.gemm && gemm_takes(o.x.p, o.x.s, p.k);
-    if (w_used) o.gemm = o.gemm && gemm_takes(o.wg, o.ldw, p.k) && gemm_takes(o.wu, o.ldw, p.k);
   }
+  if (x_used) o.takes = gemm_takes(o.x.p, o.x.s, p.k, sizeof(T));
+  if (w_used) o.takes = o.takes && gemm_takes(o.wg, o.ldw, p.k, sizeof(T)) && gemm_takes(o.wu, o.ldw, p.k, sizeof(T));
+  o.gemm = p.gemm && o.takes;
   return e;
 }
 
 template <class T>
 hipError_t gate_of(const wcc_gated_desc &d, const Plan &p, const Gate<T> &gate, bool back, const Operands<T> &o, float *part, hipStream_t s) {
   if constexpr (sizeof(T) == 2) {
-    if (d.rows <= kThin && d.C_in % 8 == 0 && gemm_takes(o.x.p, o.x.s, p.k) && gemm_takes(o.wg, o.ldw, p.k) && gemm_takes(o.wu, o.ldw, p.k))
-      return thin_gate(gate, d.act, back, o.x, o.wg, o.wu, o.ldw, p.k, s);
-    if (o.gemm) return gemm_gate(gate, d.act, back, o.x, o.wg, o.wu, o.ldw, p.k, s);
+    if (d.rows <= kThin && o.takes) return thin_gate(gate, d.act, back, o.x, o.wg, o.wu, o.ldw, p.k, s);
   }
+  if (o.gemm) return gemm_gate<T>(gate, d.act, back, o.x, o.wg, o.wu, o.ldw, p.k, s);
   return tile_gate<T>(gate, d.act, back, o.x, o.wg, o.wu, o.ldw, d.C_in, part, s);
 }
 
@@ -197,13 +200,11 @@ hipError_t backward(const wcc_gated_desc &d, const GatedArgs &g, hipStream_t s) 
   }
   if (e != hipSuccess) return e;
   const T *dg = gate.d, *du = gate.d + p.room;
-  if constexpr (sizeof(T) == 2) {
-    if (o.gemm) {
-      if (g.dx && (e = gemm_dx(dg, p.room, d.rows, o.wg, o.wu, o.ldw, d.C_in, d.C_out, static_cast<T *>(g.dx), d.ldx, part, s)) != hipSuccess)
-        return e;
-      return dw ? gemm_dw(dg, p.room, d.rows, o.x.p, o.x.s, p.k, d.C_in, d.C_out, static_cast<T *>(g.dw_gate), static_cast<T *>(g.dw_up), part, s)
-                : hipSuccess;
-    }
+  if (o.gemm) {
+    if (g.dx && (e = gemm_dx<T>(dg, p.room, d.rows, o.wg, o.wu, o.ldw, d.C_in, d.C_out, static_cast<T *>(g.dx), d.ldx, part, s)) != hipSuccess)
+      return e;
+    return dw ? gemm_dw<T>(dg, p.room, d.rows, o.x.p, o.x.s, p.k, d.C_in, d.C_out, static_cast<T *>(g.dw_gate), static_cast<T *>(g.dw_up), part, s)
+              : hipSuccess;
   }
   if (g.dx) {
     Product<T> m = {};

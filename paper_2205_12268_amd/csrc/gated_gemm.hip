@@ -10,6 +10,8 @@
 // and the reads transpose 4 x 16 blocks.
 // Loads go through buffer descriptors that end where the operand does: what lies behind the last line or the last k is 0 without a
 // branch, and the stages past the last are loads of nothing.
+#include <algorithm>
+
 #include "gated.h"
 
 namespace wcc {
@@ -37,11 +39,13 @@ struct Operand {
   int64_t turn;
 };
 
-template <int B, bool ACROSS, bool TURNS>
+template <class T, int B, bool ACROSS, bool TURNS>
 struct Feed {
-  static constexpr int Bytes = B * kLine, L = Bytes / 4096;   // of a stage; loads of a wave
-  static constexpr int C = B / 8, R = 64 / C;                 // across: chunks of a line of k, lines of a load
+  static constexpr int Size = sizeof(T), VE = 16 / Size, KS = kLine / Size;  // KS: k of a stage
+  static constexpr int Bytes = B * kLine, L = Bytes / 4096;                  // of a stage; loads of a wave
+  static constexpr int C = B / VE, R = 64 / C;                               // across: chunks of a line of k, lines of a load
   static constexpr int PerLoad = ACROSS ? R : 8;
+  static_assert(!ACROSS || Size == 4 || C >= 16, "keys of lines reach chunk 15");
   uint32_t off[2], at[2];  // the lane's places in loads of even and odd number; at: this stage's (along)
   int chunk[2];
   uint32_t step;
@@ -55,17 +59,17 @@ struct Feed {
       if constexpr (ACROSS) {
         const int row = b * R + lane / C;
         chunk[b] = 0;
-        off[b] = (uint32_t)((wv * L * R + lane / C) * o.ld + ((lane % C) ^ ((row & 3) * 4)) * 16);
+        off[b] = (uint32_t)((wv * L * R + lane / C) * o.ld + ((lane % C) ^ (Size == 2 ? (row & 3) * 4 : 0)) * 16);
       } else {
         const int row = b * 8 + lane / 8;
         chunk[b] = (lane % 8) ^ chunk_key(row);
         // (in turns of 32 lines a wave's loads are at the lines of both halves that its 64 lie in, or of the one that its 32 lie in)
-        const int first = TURNS ? (B == 256 ? wv * 32 : (wv >> 1) * 32) : wv * L * 8;
+        const int first = TURNS ? (B == 256 ? wv * 32 : (wv >> 1) * 32) : wv * L * 8;  // (TURNS: B is 128 or 256)
         off[b] = (uint32_t)((first + lane / 8) * o.ld + chunk[b] * 16);
       }
     }
     if constexpr (!ACROSS) {
-      const int64_t bytes = o.lines > 0 ? (min(o.lines, (int64_t)B) - 1) * o.ld + o.k * 2 : 0;
+      const int64_t bytes = o.lines > 0 ? (min(o.lines, (int64_t)B) - 1) * o.ld + o.k * Size : 0;
       r[0] = buffer(o.p[0], bytes);
       if constexpr (TURNS) {
         r[1] = buffer(o.p[1], bytes);
@@ -75,19 +79,19 @@ struct Feed {
   }
   // before the loads of a stage
   __device__ __forceinline__ void turn_to(const Operand &o, int64_t stage) {
-    int64_t k = stage * kK;
+    int64_t k = stage * KS;
     if constexpr (ACROSS) {
       const char *p = o.p[0];
       if constexpr (TURNS) {
         if (k >= o.turn) p = o.p[1], k -= o.turn;
       }
-      const int64_t n = min(o.k - k, (int64_t)kK);
+      const int64_t n = min(o.k - k, (int64_t)KS);
       const bool some = n > 0 && o.lines > 0;
-      r[0] = buffer(some ? p + k * o.ld : p, some ? (n - 1) * o.ld + min(o.lines, (int64_t)B) * 2 : 0);
+      r[0] = buffer(some ? p + k * o.ld : p, some ? (n - 1) * o.ld + min(o.lines, (int64_t)B) * Size : 0);
     } else {
       const int64_t left = o.k - k;
 #pragma unroll
-      for (int b = 0; b < 2; ++b) at[b] = chunk[b] * 8 < left ? off[b] + (uint32_t)(k * 2) : kNowhere;
+      for (int b = 0; b < 2; ++b) at[b] = chunk[b] * VE < left ? off[b] + (uint32_t)(k * Size) : kNowhere;
     }
   }
   template <int i>
@@ -119,11 +123,11 @@ __device__ __forceinline__ void arrived() {
 
 // The first operand of the matrix cores is W (outputs), the second X (rows): a lane has one row's results, four neighbouring outputs at a
 // time.
-template <int BT, int BO, bool XA, bool WA, bool XTURNS, bool WTURNS>
+template <class T, int BT, int BO, bool XA, bool WA, bool XTURNS, bool WTURNS>
 struct Gemm {
   static constexpr int WT = 2, WO = 2, ET = BT / WT / 32, EO = BO / WO / 32;
-  using X = Feed<BT, XA, XTURNS>;
-  using W = Feed<BO, WA, WTURNS>;
+  using X = Feed<T, BT, XA, XTURNS>;
+  using W = Feed<T, BO, WA, WTURNS>;
   static constexpr int XL = X::L, WL = W::L, L = XL + WL;
   struct Operands {
     u32x4 x[ET], w[EO];
@@ -139,17 +143,24 @@ struct Gemm {
       load<from + 1, to>(xs, ws);
     }
   }
-  // 32 lines from `line` on, 16 k from k on, of lines of k that are B lines wide
+  // 32 lines from `line` on, the k of a step, of lines of k that are B lines wide
   template <int B>
-  __device__ static __forceinline__ u32x4 across(const unsigned char *s, int line, int k) {
-    const int lane = threadIdx.x & 63, g = lane >> 4, q = lane & 15;
-    const int n = line + (g & 1) * 16 + (q & 3) * 4, kk = k + (g >> 1) * 8 + (q >> 2);
+  __device__ static __forceinline__ u32x4 across(const unsigned char *s, int line, int step) {
+    const int lane = threadIdx.x & 63;
     u32x4 v;
+    if constexpr (sizeof(T) == 4) {
+      const unsigned char *at = s + (step * 8 + (lane >> 5) * 4) * (B * 4) + (line + (lane & 31)) * 4;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int row = kk + h * 4;
-      const uint2 u = turned(s + row * (B * 2) + (((n >> 3) ^ ((row & 3) * 4)) << 4) + (n & 7) * 2);
-      v[2 * h] = u.x, v[2 * h + 1] = u.y;
+      for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const uint32_t *>(at + i * (B * 4));
+    } else {
+      const int g = lane >> 4, q = lane & 15;
+      const int n = line + (g & 1) * 16 + (q & 3) * 4, kk = step * 16 + (g >> 1) * 8 + (q >> 2);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int row = kk + h * 4;
+        const uint2 u = turned(s + row * (B * 2) + (((n >> 3) ^ ((row & 3) * 4)) << 4) + (n & 7) * 2);
+        v[2 * h] = u.x, v[2 * h + 1] = u.y;
+      }
     }
     return v;
   }
@@ -157,22 +168,22 @@ struct Gemm {
     const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, ln = lane & 31, half = lane >> 5;
     const int tw = (wv / WO) * (ET * 32), ow = (wv % WO) * (EO * 32);
 #pragma unroll
-    for (int e = 0; e < EO; ++e) f.w[e] = WA ? across<BO>(ws, ow + e * 32, step * 16) : chunk_of(ws, ow + e * 32 + ln, step * 2 + half);
+    for (int e = 0; e < EO; ++e) f.w[e] = WA ? across<BO>(ws, ow + e * 32, step) : chunk_of(ws, ow + e * 32 + ln, step * 2 + half);
 #pragma unroll
-    for (int r = 0; r < ET; ++r) f.x[r] = XA ? across<BT>(xs, tw + r * 32, step * 16) : chunk_of(xs, tw + r * 32 + ln, step * 2 + half);
+    for (int r = 0; r < ET; ++r) f.x[r] = XA ? across<BT>(xs, tw + r * 32, step) : chunk_of(xs, tw + r * 32 + ln, step * 2 + half);
   }
   __device__ static __forceinline__ void multiply(const Operands &f, f32x16 (&acc)[EO][ET]) {
 #pragma unroll
     for (int e = 0; e < EO; ++e)
 #pragma unroll
-      for (int r = 0; r < ET; ++r) acc[e][r] = mma<bf16_t>(f.w[e], f.x[r], acc[e][r]);
+      for (int r = 0; r < ET; ++r) acc[e][r] = mma<T>(f.w[e], f.x[r], acc[e][r]);
   }
   // The order of a step: its reads of LDS two at a time between the first products (the rest of which hide the last one's way),
   // its loads between the others, as far apart as they get: a load takes 16 cycles on its way out, a product 32.
   template <int reads, int loads>
   __device__ static __forceinline__ void spread() {
     constexpr int M = ET * EO, N = (reads + 1) / 2;
-    if constexpr (M < 16) {  // (two workgroups a compute unit hide each other's)
+    if constexpr (M < 16 || sizeof(T) == 4) {  // (two workgroups a compute unit hide each other's)
       __builtin_amdgcn_sched_barrier(0);
       return;
     }
@@ -264,27 +275,55 @@ __device__ __forceinline__ void leave(const unsigned char *lds, F f) {
 }
 
 // ---- the two projections -------------------------------------------------------------------------------------
-template <int B, int ACT, bool BACK>
-__global__ __launch_bounds__(256, B == 128 ? 2 : 1) void gate_gemm_kernel(Gate<bf16_t> p, Operand x, Operand w, int64_t tiles_t, int tiles_o) {
-  using G = Gemm<B, B, false, false, false, true>;
+template <class T, int BT, int BO, int ACT, bool BACK>
+__global__ __launch_bounds__(256, BO == 128 ? 2 : 1) void gate_gemm_kernel(Gate<T> p, Operand x, Operand w, int64_t tiles_t, int tiles_o) {
+  using G = Gemm<T, BT, BO, false, false, false, true>;
   constexpr int ET = G::ET, EO = G::EO, Pairs = EO / 2, Row = Pairs * 64;
   __shared__ __align__(1024) unsigned char xs0[G::X::Bytes], ws0[G::W::Bytes], xs1[G::X::Bytes], ws1[G::W::Bytes];
   int64_t tt;
   int to;
   tile_of(in_runs(blockIdx.x, tiles_t * tiles_o), tiles_t, tiles_o, tt, to);
-  const int64_t t0 = tt * B;
-  const int o0 = to * (B / 2);
+  const int64_t t0 = tt * BT;
+  const int o0 = to * (BO / 2);
   x.p[0] += t0 * x.ld, x.lines -= t0;
   w.p[0] += o0 * w.ld, w.p[1] += o0 * w.ld, w.lines -= o0;
-  w.lines = min(w.lines, (int64_t)(B / 2));
+  w.lines = min(w.lines, (int64_t)(BO / 2));
   f32x16 acc[EO][ET] = {};
   G g;
-  g.run(x, w, 0, (x.k + kK - 1) / kK, xs0, ws0, xs1, ws1, acc);
+  g.run(x, w, 0, (x.k + G::X::KS - 1) / G::X::KS, xs0, ws0, xs1, ws1, acc);
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, ln = lane & 31, half = lane >> 5;
   const int64_t tw = t0 + (wv / G::WO) * (ET * 32);
   const int ow = o0 + (wv % G::WO) * (Pairs * 32);
-  unsigned char *own = wv == 0 ? xs0 : wv == 1 ? ws0 : wv == 2 ? xs1 : ws1;
+  unsigned char *own = wv == 0 ? xs0 : wv == 1 ? ws0 : wv == 2 ? xs1 : ws1;  // (8 KiB each at least)
   const int64_t blocks = (p.outs + kKept - 1) / kKept;
+  if constexpr (sizeof(T) == 4) {  // (bound by the matrix cores: straight to memory)
+#pragma unroll
+    for (int r = 0; r < ET; ++r)
+#pragma unroll
+      for (int j = 0; j < Pairs; ++j) {
+        const f32x16 &ga = acc[2 * j][r], &ua = acc[2 * j + 1][r];  // (lines behind the last are 0)
+        uint32_t m[2] = {0, 0};
+        if (!BACK && p.codes) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            m[0] = max(m[0], __float_as_uint(ga[i]) & 0x7fffffffu);
+            m[1] = max(m[1], __float_as_uint(ua[i]) & 0x7fffffffu);
+          }
+#pragma unroll
+          for (int h = 0; h < 2; ++h) m[h] = step_of(max(m[h], (uint32_t)__shfl_xor((int)m[h], 32, 64)));
+        }
+        const int64_t t = tw + r * 32 + ln;
+        if (t < p.rows) {
+#pragma unroll
+          for (int i = 0; i < 16; i += 4) {
+            float gv[4] = {ga[i], ga[i + 1], ga[i + 2], ga[i + 3]}, uv[4] = {ua[i], ua[i + 1], ua[i + 2], ua[i + 3]};
+            const int o = ow + j * 32 + result_line(i, half);
+            if (o < p.room) finish<T, ACT, BACK>(p, t, o, gv, uv, m[0], m[1]);
+          }
+        }
+      }
+    return;
+  } else {
 #pragma unroll
   for (int r = 0; r < ET; ++r) {
     const int64_t t = tw + r * 32 + ln;
@@ -385,20 +424,22 @@ __global__ __launch_bounds__(256, B == 128 ? 2 : 1) void gate_gemm_kernel(Gate<b
     }
     __builtin_amdgcn_sched_barrier(0);
   }
+  }
 }
 
 // ---- dx and the weights' gradients -----------------------------------------------------------------------------
+template <class T>
 struct Result {
-  bf16_t *out[2];  // rows from `turn` on go to out[1], from its first on
+  T *out[2];  // rows from `turn` on go to out[1], from its first on
   int64_t ld, rows, outs, turn;
   float *part;     // PARTS: [splits][turns * rows][outs]
 };
 
-template <int BT, int BO, bool XA, bool PARTS>
-__global__ __launch_bounds__(256, BT == 128 && BO == 128 ? 2 : 1) void product_gemm_kernel(Result p, Operand x, Operand w, int64_t tiles_t,
+template <class T, int BT, int BO, bool XA, bool PARTS>
+__global__ __launch_bounds__(256, BO == 128 && BT <= 128 ? 2 : 1) void product_gemm_kernel(Result<T> p, Operand x, Operand w, int64_t tiles_t,
                                                                                        int tiles_o, int splits, int64_t chunk,
                                                                                        int64_t stages) {
-  using G = Gemm<BT, BO, XA, true, false, !XA>;
+  using G = Gemm<T, BT, BO, XA, true, false, !XA>;
   constexpr int ET = G::ET, EO = G::EO, Row = EO * 64;
   __shared__ __align__(1024) unsigned char xs0[G::X::Bytes], ws0[G::W::Bytes], xs1[G::X::Bytes], ws1[G::W::Bytes];
   const int64_t tiles = tiles_t * tiles_o, block = in_runs(blockIdx.x, tiles * splits), split = block / tiles;
@@ -409,10 +450,10 @@ __global__ __launch_bounds__(256, BT == 128 && BO == 128 ? 2 : 1) void product_g
   const int64_t tiles_half = (p.rows + BT - 1) / BT, second = tt >= tiles_half ? 1 : 0;
   const int64_t t0 = (tt - second * tiles_half) * BT;
   const int64_t o0 = (int64_t)to * BO;
-  if constexpr (XA) x.p[0] += (second * p.turn + t0) * 2;
+  if constexpr (XA) x.p[0] += (second * p.turn + t0) * (int64_t)sizeof(T);
   else x.p[0] += t0 * x.ld;
   x.lines -= t0;
-  w.p[0] += o0 * 2, w.p[1] += o0 * 2, w.lines -= o0;
+  w.p[0] += o0 * sizeof(T), w.p[1] += o0 * sizeof(T), w.lines -= o0;
   f32x16 acc[EO][ET] = {};
   G g;
   g.run(x, w, split * chunk, min(stages, (split + 1) * chunk), xs0, ws0, xs1, ws1, acc);
@@ -421,10 +462,12 @@ __global__ __launch_bounds__(256, BT == 128 && BO == 128 ? 2 : 1) void product_g
   unsigned char *own = wv == 0 ? xs0 : wv == 1 ? ws0 : wv == 2 ? xs1 : ws1;
 #pragma unroll
   for (int r = 0; r < ET; ++r) {
-    if constexpr (PARTS) {
+    if constexpr (PARTS || sizeof(T) == 4) {
       const int64_t t = tw + r * 32 + ln, halves = p.out[1] ? 2 : 1;
       if (t < p.rows) {
-        float *q = p.part + ((split * halves + second) * p.rows + t) * p.outs;
+        float *q;
+        if constexpr (PARTS) q = p.part + ((split * halves + second) * p.rows + t) * p.outs;
+        else q = reinterpret_cast<float *>(p.out[second]) + t * p.ld;
 #pragma unroll
         for (int e = 0; e < EO; ++e)
 #pragma unroll
@@ -454,7 +497,8 @@ __global__ __launch_bounds__(256, BT == 128 && BO == 128 ? 2 : 1) void product_g
   }
 }
 
-__global__ __launch_bounds__(256) void product_gemm_join_kernel(Result p, int splits) {
+template <class T>
+__global__ __launch_bounds__(256) void product_gemm_join_kernel(Result<T> p, int splits) {
   const int64_t all = p.rows * p.outs, halves = p.out[1] ? 2 : 1;
   const int h = blockIdx.y;
   for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < all; i += (int64_t)gridDim.x * 1024) {
@@ -468,7 +512,7 @@ __global__ __launch_bounds__(256) void product_gemm_join_kernel(Result p, int sp
         for (int j = 0; j < n; ++j) v[j] += q[j];
       }
     }
-    for (int j = 0; j < n; ++j) p.out[h][(i + j) / p.outs * p.ld + (i + j) % p.outs] = narrow<bf16_t>(v[j]);
+    for (int j = 0; j < n; ++j) p.out[h][(i + j) / p.outs * p.ld + (i + j) % p.outs] = narrow<T>(v[j]);
   }
 }
 
@@ -490,11 +534,12 @@ struct ProductPlan {
   int64_t stages, chunk;
 };
 // rows: of one half
-ProductPlan plan_of(int64_t rows, int64_t outs, int64_t k, int halves) {
+ProductPlan plan_of(int64_t rows, int64_t outs, int64_t k, int halves, int size) {
   ProductPlan p;
-  p.stages = tiles(k, kK);
-  const bool large = halves * tiles(rows, 256) * tiles(outs, 256) >= 200;
+  p.stages = tiles(k, kLine / size);
+  const bool large = size == 2 && halves * tiles(rows, 256) * tiles(outs, 256) >= 200;
   p.bt = p.bo = large ? 256 : 128;
+  if (size == 4 && halves * tiles(rows, 128) * tiles(outs, 128) < 256) p.bt = 64;
   const int64_t n = halves * tiles(rows, p.bt) * tiles(outs, p.bo), slots = large ? 256 : 512;
   const int64_t want = std::min<int64_t>({std::max<int64_t>(slots / n, 1), std::max<int64_t>(p.stages / 4, 1), 16});
   p.chunk = tiles(p.stages, want);
@@ -502,81 +547,111 @@ ProductPlan plan_of(int64_t rows, int64_t outs, int64_t k, int halves) {
   return p;
 }
 
-template <int BT, int BO, bool XA>
-void launch_product(const Result &r, const Operand &x, const Operand &w, const ProductPlan &p, int halves, hipStream_t s) {
+template <class T, int BT, int BO, bool XA>
+void launch_product(const Result<T> &r, const Operand &x, const Operand &w, const ProductPlan &p, int halves, hipStream_t s) {
   const int64_t tiles_t = halves * tiles(r.rows, BT);
   const int tiles_o = (int)tiles(r.outs, BO);
   const unsigned blocks = (unsigned)(tiles_t * tiles_o * p.splits);
   if (p.splits > 1) {
-    product_gemm_kernel<BT, BO, XA, true><<<blocks, 256, 0, s>>>(r, x, w, tiles_t, tiles_o, p.splits, p.chunk, p.stages);
-    product_gemm_join_kernel<<<dim3((unsigned)std::min<int64_t>(tiles(r.rows * r.outs, 1024), 4096), halves), 256, 0, s>>>(r, p.splits);
+    product_gemm_kernel<T, BT, BO, XA, true><<<blocks, 256, 0, s>>>(r, x, w, tiles_t, tiles_o, p.splits, p.chunk, p.stages);
+    product_gemm_join_kernel<T><<<dim3((unsigned)std::min<int64_t>(tiles(r.rows * r.outs, 1024), 4096), halves), 256, 0, s>>>(r, p.splits);
   } else {
-    product_gemm_kernel<BT, BO, XA, false><<<blocks, 256, 0, s>>>(r, x, w, tiles_t, tiles_o, 1, p.stages, p.stages);
+    product_gemm_kernel<T, BT, BO, XA, false><<<blocks, 256, 0, s>>>(r, x, w, tiles_t, tiles_o, 1, p.stages, p.stages);
   }
 }
 
-template <bool XA>
-hipError_t product(const Result &r, const Operand &x, const Operand &w, int64_t k, int halves, hipStream_t s) {
-  const ProductPlan p = plan_of(r.rows, r.outs, k, halves);
-  if (p.bt == 256) launch_product<256, 256, XA>(r, x, w, p, halves, s);
-  else launch_product<128, 128, XA>(r, x, w, p, halves, s);
+template <class T, bool XA>
+hipError_t product(const Result<T> &r, const Operand &x, const Operand &w, int64_t k, int halves, hipStream_t s) {
+  const ProductPlan p = plan_of(r.rows, r.outs, k, XA ? 2 : 1, sizeof(T));  // (the same for one of the weights' gradients as for both)
+  if constexpr (sizeof(T) == 2) {
+    if (p.bt == 256) launch_product<T, 256, 256, XA>(r, x, w, p, halves, s);
+    else launch_product<T, 128, 128, XA>(r, x, w, p, halves, s);
+  } else {
+    if (p.bt == 64) launch_product<T, 64, 128, XA>(r, x, w, p, halves, s);
+    else launch_product<T, 128, 128, XA>(r, x, w, p, halves, s);
+  }
   return hipGetLastError();
 }
 
-size_t parts_of(int64_t rows, int64_t outs, int64_t k, int halves) {
-  const ProductPlan p = plan_of(rows, outs, k, halves);
+size_t parts_of(int64_t rows, int64_t outs, int64_t k, int halves, int size) {
+  const ProductPlan p = plan_of(rows, outs, k, halves, size);
   return p.splits > 1 ? (size_t)p.splits * halves * rows * outs * sizeof(float) : 0;
 }
 
 }  // namespace
 
 // 16-byte loads, tiles within a descriptor
-bool gemm_takes(const void *p, int64_t ld, int64_t width) { return on_16(p) && ld % 8 == 0 && ld < 1 << 21 && width % 8 == 0; }
+bool gemm_takes(const void *p, int64_t ld, int64_t width, int size) {
+  const int each = 16 / size;
+  return on_16(p) && ld % each == 0 && ld * size < 1 << 22 && width % each == 0;
+}
 
-hipError_t gemm_gate(const Gate<bf16_t> &p, int act, bool back, const Side<bf16_t> &x, const bf16_t *w_gate, const bf16_t *w_up, int64_t ldw,
-                     int64_t k, hipStream_t s) {
+template <class T>
+hipError_t gemm_gate(const Gate<T> &p, int act, bool back, const Side<T> &x, const T *w_gate, const T *w_up, int64_t ldw, int64_t k, hipStream_t s) {
   Operand xo = {}, wo = {};
-  xo.p[0] = reinterpret_cast<const char *>(x.p), xo.ld = x.s * 2, xo.lines = x.lines, xo.k = k;
-  wo.p[0] = reinterpret_cast<const char *>(w_gate), wo.p[1] = reinterpret_cast<const char *>(w_up), wo.ld = ldw * 2, wo.lines = p.outs, wo.k = k;
+  xo.p[0] = reinterpret_cast<const char *>(x.p), xo.ld = x.s * sizeof(T), xo.lines = x.lines, xo.k = k;
+  wo.p[0] = reinterpret_cast<const char *>(w_gate), wo.p[1] = reinterpret_cast<const char *>(w_up), wo.ld = ldw * sizeof(T);
+  wo.lines = p.outs, wo.k = k;
   return by_act(act, [&](auto a) {
     constexpr int ACT = decltype(a)::value;
-    auto go = [&](auto size, auto b) {
-      constexpr int B = decltype(size)::value;
-      const int64_t tiles_t = tiles(p.rows, B);
-      const int tiles_o = (int)tiles(p.outs, B / 2);
-      gate_gemm_kernel<B, ACT, decltype(b)::value><<<(unsigned)(tiles_t * tiles_o), 256, 0, s>>>(p, xo, wo, tiles_t, tiles_o);
+    auto go = [&](auto bt, auto bo) {
+      constexpr int BT = decltype(bt)::value, BO = decltype(bo)::value;
+      const int64_t tiles_t = tiles(p.rows, BT);
+      const int tiles_o = (int)tiles(p.outs, BO / 2);
+      const unsigned n = (unsigned)(tiles_t * tiles_o);
+      if (back) gate_gemm_kernel<T, BT, BO, ACT, true><<<n, 256, 0, s>>>(p, xo, wo, tiles_t, tiles_o);
+      else gate_gemm_kernel<T, BT, BO, ACT, false><<<n, 256, 0, s>>>(p, xo, wo, tiles_t, tiles_o);
     };
-    const bool large = tiles(p.rows, 256) * tiles(p.outs, 128) >= 200;
-    using L = std::integral_constant<int, 256>;
-    using S = std::integral_constant<int, 128>;
-    if (large) back ? go(L(), std::true_type()) : go(L(), std::false_type());
-    else back ? go(S(), std::true_type()) : go(S(), std::false_type());
+    const std::integral_constant<int, 256> L;
+    const std::integral_constant<int, 128> M;
+    const std::integral_constant<int, 64> S;
+    bool large = false;
+    if constexpr (sizeof(T) == 2) {
+      large = tiles(p.rows, 256) * tiles(p.outs, 128) >= 200;
+      if (large) go(L, L);
+    }
+    if (!large) {
+      if (sizeof(T) == 4 && tiles(p.rows, 128) * tiles(p.outs, 64) < 256) go(S, M);  // (bf16, 777 rows 1000 -> 1537: 15.4 us, 13.4 without)
+      else go(M, M);
+    }
     return hipGetLastError();
   });
 }
 
-size_t gemm_dx_parts(int64_t rows, int64_t C_in, int64_t room) { return parts_of(rows, C_in, 2 * room, 1); }
-size_t gemm_dw_parts(int64_t rows, int64_t C_in, int64_t C_out) { return parts_of(C_out, C_in, rows, 2); }
+size_t gemm_dx_parts(int64_t rows, int64_t C_in, int64_t room, int size) { return parts_of(rows, C_in, 2 * room, 1, size); }
+size_t gemm_dw_parts(int64_t rows, int64_t C_in, int64_t C_out, int size) {
+  return parts_of(C_out, C_in, rows, 2, size);
+}
 
-hipError_t gemm_dx(const bf16_t *d, int64_t room, int64_t rows, const bf16_t *w_gate, const bf16_t *w_up, int64_t ldw, int64_t C_in, int64_t C_out,
-                   bf16_t *dx, int64_t ld, float *part, hipStream_t s) {
+template <class T>
+hipError_t gemm_dx(const T *d, int64_t room, int64_t rows, const T *w_gate, const T *w_up, int64_t ldw, int64_t C_in, int64_t C_out, T *dx,
+                   int64_t ld, float *part, hipStream_t s) {
   Operand x = {}, w = {};
-  x.p[0] = reinterpret_cast<const char *>(d), x.ld = 4 * room, x.lines = rows, x.k = 2 * room;
+  x.p[0] = reinterpret_cast<const char *>(d), x.ld = 2 * room * sizeof(T), x.lines = rows, x.k = 2 * room;
   w.p[0] = reinterpret_cast<const char *>(w_gate), w.p[1] = reinterpret_cast<const char *>(w_up);
-  w.ld = ldw * 2, w.lines = ldw, w.k = C_out, w.turn = room;
-  const Result r{{dx, nullptr}, ld, rows, C_in, 0, part};
-  return product<false>(r, x, w, 2 * room, 1, s);
+  w.ld = ldw * sizeof(T), w.lines = ldw, w.k = C_out, w.turn = room;
+  const Result<T> r{{dx, nullptr}, ld, rows, C_in, 0, part};
+  return product<T, false>(r, x, w, 2 * room, 1, s);
 }
 
-hipError_t gemm_dw(const bf16_t *d, int64_t room, int64_t rows, const bf16_t *x, int64_t ldx, int64_t width, int64_t C_in, int64_t C_out,
-                   bf16_t *dw_gate, bf16_t *dw_up, float *part, hipStream_t s) {
+template <class T>
+hipError_t gemm_dw(const T *d, int64_t room, int64_t rows, const T *x, int64_t ldx, int64_t width, int64_t C_in, int64_t C_out, T *dw_gate,
+                   T *dw_up, float *part, hipStream_t s) {
   Operand a = {}, b = {};
-  a.p[0] = reinterpret_cast<const char *>(d), a.ld = 4 * room, a.lines = room, a.k = rows;
-  b.p[0] = reinterpret_cast<const char *>(x), b.ld = ldx * 2, b.lines = width, b.k = rows;
+  a.p[0] = reinterpret_cast<const char *>(d), a.ld = 2 * room * sizeof(T), a.lines = room, a.k = rows;
+  b.p[0] = reinterpret_cast<const char *>(x), b.ld = ldx * sizeof(T), b.lines = width, b.k = rows;
   const int halves = dw_gate && dw_up ? 2 : 1;
-  if (!dw_gate) a.p[0] += room * 2;
-  const Result r{{dw_gate ? dw_gate : dw_up, halves == 2 ? dw_up : nullptr}, C_in, C_out, C_in, room, part};
-  return product<true>(r, a, b, rows, halves, s);
+  if (!dw_gate) a.p[0] += room * sizeof(T);
+  const Result<T> r{{dw_gate ? dw_gate : dw_up, halves == 2 ? dw_up : nullptr}, C_in, C_out, C_in, room, part};
+  return product<T, true>(r, a, b, rows, halves, s);
 }
+
+#define WCC_GEMM(T)                                                                                                                          \
+  template hipError_t gemm_gate<T>(const Gate<T> &, int, bool, const Side<T> &, const T *, const T *, int64_t, int64_t, hipStream_t);        \
+  template hipError_t gemm_dx<T>(const T *, int64_t, int64_t, const T *, const T *, int64_t, int64_t, int64_t, T *, int64_t, float *, hipStream_t); \
+  template hipError_t gemm_dw<T>(const T *, int64_t, int64_t, const T *, int64_t, int64_t, int64_t, int64_t, T *, T *, float *, hipStream_t);
+WCC_GEMM(float)
+WCC_GEMM(bf16_t)
+#undef WCC_GEMM
 
 }  // namespace wcc

@@ -318,7 +318,7 @@ hipError_t tile_gate(const Gate<T> &p, int act, bool back, const Side<T> &x, con
 template <class T, bool AT>
 hipError_t tile_product(const Product<T> &p, float *part, hipStream_t s) {
   const int64_t rows = p.a[0].lines, lines = p.b[0].lines;
-  const Grid n = grid_of(rows, lines, kTile, p.k, p.batches, sizeof(T));
+  const Grid n = grid_of(rows, lines, kTile, p.k, AT ? 2 : 1, sizeof(T));  // (the same for one of the weights' gradients as for both)
   const dim3 blocks((unsigned)(n.tiles * n.splits), p.batches);
   auto go = [&](auto size) {
     constexpr int ET = decltype(size)::value;
