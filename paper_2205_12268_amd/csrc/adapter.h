@@ -29,21 +29,7 @@ struct Thin {
   int sj, sc;
 };
 
-// ---- fp32 values of k for one line, as operands ---------------------------------------------------------------
-// bf16 operands carry 8 bits each: P of them take P * 8 bits of the values, the rest of each going to the next.
-__device__ __forceinline__ float left_of(float v, uint32_t part) {  // (nothing of an infinity, or it would be NaN)
-  return (part & 0x7f80) == 0x7f80 ? 0.f : v - __uint_as_float(part << 16);
-}
-// bf16 operands with 0 in the place of infinities and NaN: what meets parts past the first, which are 0 where the first has all of a
-// value, so that an infinity by a value is not made NaN by its parts
-__device__ __forceinline__ u32x4 finite_of(u32x4 v) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if ((v[i] & 0x7f80u) == 0x7f80u) v[i] &= 0xffff0000u;
-    if ((v[i] & 0x7f800000u) == 0x7f800000u) v[i] &= 0xffffu;
-  }
-  return v;
-}
+// ---- fp32 values of k for one line, as operands, in P parts ----------------------------------------------------
 template <class T, int P>
 __device__ __forceinline__ void split_to(const float *v, u32x4 (&f)[P]) {
   if constexpr (sizeof(T) == 4) {

@@ -3,7 +3,9 @@
 // With g = Wg x and u = Wu x of a row:  y = act(g) u,  dg = dy u act'(g),  du = dy act(g),
 //   dx = Wg^T dg + Wu^T du,  dWg = sum_t dg x^T,  dWu = sum_t du x^T.
 // dg and du of all rows are held in the workspace, [rows][2][room of C_out] in the type of x: rounded to bf16 once, which the products
-// they go into need anyway.
+// they go into need anyway.  That rounding is of the size of the results' own.  Where dg and du are few values its share in a result
+// may be well above the average's, so there they are held in two parts of bf16, [rows][2 parts][2][room], 16 bits, and the products take
+// the second parts too (with 0 for weights and rows that are not finite: 0 of a second part by infinity is NaN).
 #pragma once
 
 #include "block.h"
@@ -26,9 +28,12 @@ struct Gate {
   uint8_t *steps;  // [2][rows][blocks]
   // backward
   const T *dy;     // stride ldy
-  T *d;            // [rows][2][room]
+  T *d;            // [rows][parts][2][room]
   int64_t room;
+  int parts;
 };
+// values of dg or du that are held in two parts
+constexpr int64_t kFew = 1 << 17;
 
 // 4 neighbouring outputs from o on (o a multiple of 4) of row t.  Forward: step bytes of the blocks they lie in, where codes are kept.
 // What lies behind the last output is 0 in codes and in d.
@@ -86,9 +91,23 @@ __device__ __forceinline__ void finish(const Gate<T> &p, int64_t t, int o, float
       const float d = widen(dy[j]);
       dg[j] = narrow<T>(j < left ? d * u[j] * s : 0.f), du[j] = narrow<T>(j < left ? d * v : 0.f);
     }
-    T *at = p.d + t * 2 * p.room + o;  // (o and the room are multiples of 4)
+    T *at = p.d + t * p.parts * 2 * p.room + o;  // (o and the room are multiples of 4)
     __builtin_memcpy(__builtin_assume_aligned(at, 4 * sizeof(T)), dg, sizeof dg);
     __builtin_memcpy(__builtin_assume_aligned(at + p.room, 4 * sizeof(T)), du, sizeof du);
+    if constexpr (sizeof(T) == 2) {
+      if (p.parts == 2) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float v, s;
+          act_of<T, ACT>(g[j], v, s);
+          const float d = widen(dy[j]);
+          dg[j] = narrow<T>(left_of(j < left ? d * u[j] * s : 0.f, dg[j])), du[j] = narrow<T>(left_of(j < left ? d * v : 0.f, du[j]));
+        }
+        at += 2 * p.room;
+        __builtin_memcpy(__builtin_assume_aligned(at, 4 * sizeof(T)), dg, sizeof dg);
+        __builtin_memcpy(__builtin_assume_aligned(at + p.room, 4 * sizeof(T)), du, sizeof du);
+      }
+    }
   }
 }
 
@@ -102,10 +121,10 @@ struct Side {
 // result[row of a][line of b] = sum over phases and k of a(row, k) b(line, k)
 template <class T>
 struct Product {
-  Side<T> a[2], b[2];
-  int phases;
-  int64_t k;     // of each phase
-  T *out[2];     // per batch: with two batches a[i], b[i] give out[i]
+  Side<T> a[4], b[4];  // of phase f and batch i at f * batches + i
+  int phases, second;  // from `second` on phases are of second parts
+  int64_t k;           // of each phase
+  T *out[2];           // of each batch
   int64_t ld;
   int batches;
 };
@@ -124,13 +143,13 @@ hipError_t tile_product(const Product<T> &p, float *part, hipStream_t s);
 bool gemm_takes(const void *p, int64_t ld, int64_t width, int size);
 template <class T>
 hipError_t gemm_gate(const Gate<T> &p, int act, bool back, const Side<T> &x, const T *w_gate, const T *w_up, int64_t ldw, int64_t k, hipStream_t s);
-size_t gemm_dx_parts(int64_t rows, int64_t C_in, int64_t room, int size);
-size_t gemm_dw_parts(int64_t rows, int64_t C_in, int64_t C_out, int size);
+size_t gemm_dx_parts(int64_t rows, int64_t C_in, int64_t room, int parts, int size);
+size_t gemm_dw_parts(int64_t rows, int64_t C_in, int64_t C_out, int parts, int size);
 template <class T>
-hipError_t gemm_dx(const T *d, int64_t room, int64_t rows, const T *w_gate, const T *w_up, int64_t ldw, int64_t C_in, int64_t C_out, T *dx,
+hipError_t gemm_dx(const T *d, int64_t room, int parts, int64_t rows, const T *w_gate, const T *w_up, int64_t ldw, int64_t C_in, int64_t C_out, T *dx,
                    int64_t ld, float *part, hipStream_t s);
 template <class T>
-hipError_t gemm_dw(const T *d, int64_t room, int64_t rows, const T *x, int64_t ldx, int64_t width, int64_t C_in, int64_t C_out, T *dw_gate,
+hipError_t gemm_dw(const T *d, int64_t room, int parts, int64_t rows, const T *x, int64_t ldx, int64_t width, int64_t C_in, int64_t C_out, T *dw_gate,
                    T *dw_up, float *part, hipStream_t s);
 
 // The two projections for few rows of bf16 (gated_thin.hip), operands as above.

@@ -31,9 +31,17 @@ __global__ __launch_bounds__(256) void kept_slopes_kernel(Gate<T> p) {
         }
       }
     }
-    T *d = p.d + t * 2 * p.room + o;
+    T *d = p.d + t * p.parts * 2 * p.room + o;
     *reinterpret_cast<u32x4 *>(d) = pack<T>(dg);
     *reinterpret_cast<u32x4 *>(d + p.room) = pack<T>(du);
+    if constexpr (sizeof(T) == 2) {
+      if (p.parts == 2) {
+#pragma unroll
+        for (int j = 0; j < VE; ++j) dg[j] = left_of(dg[j], narrow<T>(dg[j])), du[j] = left_of(du[j], narrow<T>(du[j]));
+        *reinterpret_cast<u32x4 *>(d + 2 * p.room) = pack<T>(dg);
+        *reinterpret_cast<u32x4 *>(d + 3 * p.room) = pack<T>(du);
+      }
+    }
   }
 }
 
@@ -67,7 +75,9 @@ size_t up(size_t v) { return (v + 255) / 256 * 256; }
 // Which kernels a call takes, and what the workspace holds: dg and du; x where it comes as codes or has to be copied; the weights where
 // they have to be copied; sums of ranges of k.
 struct Plan {
-  bool gemm, copy_x, copy_w;
+  bool gemm, copy_x, copy_w;  // tiles fed straight from memory
+  bool back;                  // the same for the products of the backward pass
+  int parts;                  // of dg and du
   size_t d, x, w, part, bytes;
   int64_t room, ldx, k;  // of d's halves; of rows and weights that were copied; C_in in whole chunks of 16 bytes
 };
@@ -85,16 +95,19 @@ Plan plan_of(const wcc_gated_desc &g, bool backward) {
   p.copy_w = g.C_in % each != 0, p.copy_x = p.copy_w || g.ldx % each != 0;
   p.gemm = g.rows > kThin && (size == 2 ? products >= (p.copy_x ? 1 << 30 : 1 << 28) : !p.copy_w && products >= 1 << 25);
   if (size == 4) p.copy_x = p.copy_w = false, p.k = g.C_in;
+  p.parts = size == 2 && g.rows * (int64_t)g.C_out < kFew ? 2 : 1;
+  // (few rows, whose products are bound by the weights and their gradients: any that 16-byte loads take)
+  p.back = p.gemm || (size == 2 && g.rows <= kThin && g.C_in % each == 0 && products >= 1 << 20);
   if (!p.gemm) p.copy_x = p.copy_w = false;
   size_t parts = tile_gate_parts(g.rows, g.C_out, g.C_in, size), at = 0;  // (tensors at odd addresses take these tiles)
-  if (backward) at += up((size_t)g.rows * 2 * p.room * size);
+  if (backward) at += up((size_t)g.rows * p.parts * 2 * p.room * size);
   p.x = at;
   if (backward || p.copy_x) at += up((size_t)g.rows * p.ldx * size);
   p.w = at;
   if (p.copy_w) at += 2 * up((size_t)g.C_out * p.ldx * size);
   p.part = at;
   if (backward) {
-    if (p.gemm) parts = std::max({parts, gemm_dx_parts(g.rows, g.C_in, p.room, size), gemm_dw_parts(g.rows, g.C_in, g.C_out, size)});
+    if (p.back) parts = std::max({parts, gemm_dx_parts(g.rows, g.C_in, p.room, p.parts, size), gemm_dw_parts(g.rows, g.C_in, g.C_out, p.parts, size)});
     parts = std::max({parts, tile_product_parts(g.rows, g.C_in, g.C_out, 1, size), tile_product_parts(g.C_out, g.C_in, g.rows, 2, size)});
   }
   p.bytes = p.part + up(parts);
@@ -104,7 +117,7 @@ Plan plan_of(const wcc_gated_desc &g, bool backward) {
 // The operands of a call as its products take them.
 template <class T>
 struct Operands {
-  bool takes, gemm;  // 16-byte loads; tiles fed straight from memory
+  bool takes;  // 16-byte loads
   Side<T> x;
   const T *wg, *wu;
   int64_t ldw;
@@ -145,7 +158,6 @@ hipError_t prepare(const wcc_gated_desc &d, const Plan &p, const GatedArgs &g, b
   }
   if (x_used) o.takes = gemm_takes(o.x.p, o.x.s, p.k, sizeof(T));
   if (w_used) o.takes = o.takes && gemm_takes(o.wg, o.ldw, p.k, sizeof(T)) && gemm_takes(o.wu, o.ldw, p.k, sizeof(T));
-  o.gemm = p.gemm && o.takes;
   return e;
 }
 
@@ -154,7 +166,7 @@ hipError_t gate_of(const wcc_gated_desc &d, const Plan &p, const Gate<T> &gate, 
   if constexpr (sizeof(T) == 2) {
     if (d.rows <= kThin && o.takes) return thin_gate(gate, d.act, back, o.x, o.wg, o.wu, o.ldw, p.k, s);
   }
-  if (o.gemm) return gemm_gate<T>(gate, d.act, back, o.x, o.wg, o.wu, o.ldw, p.k, s);
+  if (p.gemm && o.takes && !(back && p.parts == 2)) return gemm_gate<T>(gate, d.act, back, o.x, o.wg, o.wu, o.ldw, p.k, s);
   return tile_gate<T>(gate, d.act, back, o.x, o.wg, o.wu, o.ldw, d.C_in, part, s);
 }
 
@@ -166,7 +178,7 @@ hipError_t forward(const wcc_gated_desc &d, const GatedArgs &g, hipStream_t s) {
   if (e != hipSuccess) return e;
   Gate<T> gate = {};
   gate.rows = d.rows, gate.outs = d.C_out, gate.y = static_cast<T *>(g.y), gate.ldy = d.ldy, gate.codes = g.codes, gate.steps = g.steps;
-  gate.room = p.room;
+  gate.room = p.room, gate.parts = p.parts;
   return gate_of<T>(d, p, gate, false, o, reinterpret_cast<float *>(g.ws + p.part), s);
 }
 
@@ -186,7 +198,7 @@ hipError_t backward(const wcc_gated_desc &d, const GatedArgs &g, hipStream_t s) 
   if (e != hipSuccess) return e;
   Gate<T> gate = {};
   gate.rows = d.rows, gate.outs = d.C_out, gate.ldy = d.ldy, gate.codes = g.codes, gate.steps = g.steps;
-  gate.dy = static_cast<const T *>(g.dy), gate.d = reinterpret_cast<T *>(g.ws + p.d), gate.room = p.room;
+  gate.dy = static_cast<const T *>(g.dy), gate.d = reinterpret_cast<T *>(g.ws + p.d), gate.room = p.room, gate.parts = p.parts;
   if (again) {
     e = gate_of<T>(d, p, gate, true, o, part, s);
   } else {
@@ -200,27 +212,33 @@ hipError_t backward(const wcc_gated_desc &d, const GatedArgs &g, hipStream_t s) 
   }
   if (e != hipSuccess) return e;
   const T *dg = gate.d, *du = gate.d + p.room;
-  if (o.gemm) {
-    if (g.dx && (e = gemm_dx<T>(dg, p.room, d.rows, o.wg, o.wu, o.ldw, d.C_in, d.C_out, static_cast<T *>(g.dx), d.ldx, part, s)) != hipSuccess)
+  if (p.back && o.takes) {
+    if (g.dx && (e = gemm_dx<T>(dg, p.room, p.parts, d.rows, o.wg, o.wu, o.ldw, d.C_in, d.C_out, static_cast<T *>(g.dx), d.ldx, part, s)) != hipSuccess)
       return e;
-    return dw ? gemm_dw<T>(dg, p.room, d.rows, o.x.p, o.x.s, p.k, d.C_in, d.C_out, static_cast<T *>(g.dw_gate), static_cast<T *>(g.dw_up), part, s)
+    return dw ? gemm_dw<T>(dg, p.room, p.parts, d.rows, o.x.p, o.x.s, p.k, d.C_in, d.C_out, static_cast<T *>(g.dw_gate),
+                           static_cast<T *>(g.dw_up), part, s)
               : hipSuccess;
   }
+  const int64_t ldd = p.parts * 2 * p.room, next = 2 * p.room;
   if (g.dx) {
     Product<T> m = {};
-    m.phases = 2, m.batches = 1, m.k = d.C_out, m.ld = d.ldx, m.out[0] = static_cast<T *>(g.dx);
-    m.a[0] = Side<T>{dg, 2 * p.room, d.rows}, m.a[1] = Side<T>{du, 2 * p.room, d.rows};
-    m.b[0] = Side<T>{o.wg, o.ldw, d.C_in}, m.b[1] = Side<T>{o.wu, o.ldw, d.C_in};
+    m.phases = 2 * p.parts, m.second = 2, m.batches = 1, m.k = d.C_out, m.ld = d.ldx, m.out[0] = static_cast<T *>(g.dx);
+    for (int i = 0; i < p.parts; ++i) {
+      m.a[2 * i] = Side<T>{dg + i * next, ldd, d.rows}, m.a[2 * i + 1] = Side<T>{du + i * next, ldd, d.rows};
+      m.b[2 * i] = Side<T>{o.wg, o.ldw, d.C_in}, m.b[2 * i + 1] = Side<T>{o.wu, o.ldw, d.C_in};
+    }
     if ((e = tile_product<T, false>(m, part, s)) != hipSuccess) return e;
   }
   if (dw) {
     Product<T> m = {};
-    m.phases = 1, m.k = d.rows, m.ld = d.C_in;
-    int n = 0;
-    if (g.dw_gate) m.a[n] = Side<T>{dg, 2 * p.room, d.C_out}, m.out[n++] = static_cast<T *>(g.dw_gate);
-    if (g.dw_up) m.a[n] = Side<T>{du, 2 * p.room, d.C_out}, m.out[n++] = static_cast<T *>(g.dw_up);
-    m.batches = n;
-    m.b[0] = m.b[1] = Side<T>{o.x.p, o.x.s, d.C_in};
+    m.phases = p.parts, m.second = 1, m.k = d.rows, m.ld = d.C_in;
+    if (g.dw_gate) m.out[m.batches++] = static_cast<T *>(g.dw_gate);
+    if (g.dw_up) m.out[m.batches++] = static_cast<T *>(g.dw_up);
+    for (int i = 0; i < p.parts; ++i) {
+      int n = i * m.batches;
+      if (g.dw_gate) m.a[n] = Side<T>{dg + i * next, ldd, d.C_out}, m.b[n++] = Side<T>{o.x.p, o.x.s, d.C_in};
+      if (g.dw_up) m.a[n] = Side<T>{du + i * next, ldd, d.C_out}, m.b[n] = Side<T>{o.x.p, o.x.s, d.C_in};
+    }
     if ((e = tile_product<T, true>(m, part, s)) != hipSuccess) return e;
   }
   return hipSuccess;

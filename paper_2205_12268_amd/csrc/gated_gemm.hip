@@ -31,12 +31,12 @@ __device__ __forceinline__ void buffer_to_lds(Rsrc r, uint32_t off, unsigned cha
 //   along:  line l at p + l * ld, k contiguous; `lines` of them there, `k` long
 //   across: k at p + k * ld, lines contiguous; `lines` of them there
 // In bytes but for the counts.  Two halves: along, lines in turns of 32 from p[0] and p[1] (the two weights); across, k from `turn` on in
-// p[1], from its first line on (dx: the two weights again).
+// p[1], from its first line on (dx: the two weights again), and from `again` on the same once more (second parts).
 struct Operand {
   const char *p[2];
   int64_t ld;
   int64_t lines, k;
-  int64_t turn;
+  int64_t turn, again;
 };
 
 template <class T, int B, bool ACROSS, bool TURNS>
@@ -83,6 +83,7 @@ struct Feed {
     if constexpr (ACROSS) {
       const char *p = o.p[0];
       if constexpr (TURNS) {
+        if (k >= o.again) k -= o.again;
         if (k >= o.turn) p = o.p[1], k -= o.turn;
       }
       const int64_t n = min(o.k - k, (int64_t)KS);
@@ -123,7 +124,8 @@ __device__ __forceinline__ void arrived() {
 
 // The first operand of the matrix cores is W (outputs), the second X (rows): a lane has one row's results, four neighbouring outputs at a
 // time.
-template <class T, int BT, int BO, bool XA, bool WA, bool XTURNS, bool WTURNS>
+// TWO: from stage `second` on X is of second parts, by what is finite in W.
+template <class T, int BT, int BO, bool XA, bool WA, bool XTURNS, bool WTURNS, bool TWO>
 struct Gemm {
   static constexpr int WT = 2, WO = 2, ET = BT / WT / 32, EO = BO / WO / 32;
   using X = Feed<T, BT, XA, XTURNS>;
@@ -134,6 +136,7 @@ struct Gemm {
   };
   X x;
   W w;
+  int64_t second;
 
   template <int from, int to>
   __device__ __forceinline__ void load(unsigned char *xs, unsigned char *ws) const {
@@ -164,13 +167,19 @@ struct Gemm {
     }
     return v;
   }
-  __device__ static __forceinline__ void fetch(const unsigned char *xs, const unsigned char *ws, int step, Operands &f) {
+  __device__ __forceinline__ void fetch(const unsigned char *xs, const unsigned char *ws, int step, int64_t stage, Operands &f) const {
     const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, ln = lane & 31, half = lane >> 5;
     const int tw = (wv / WO) * (ET * 32), ow = (wv % WO) * (EO * 32);
 #pragma unroll
     for (int e = 0; e < EO; ++e) f.w[e] = WA ? across<BO>(ws, ow + e * 32, step) : chunk_of(ws, ow + e * 32 + ln, step * 2 + half);
 #pragma unroll
     for (int r = 0; r < ET; ++r) f.x[r] = XA ? across<BT>(xs, tw + r * 32, step) : chunk_of(xs, tw + r * 32 + ln, step * 2 + half);
+    if constexpr (TWO) {
+      if (stage >= second) {
+#pragma unroll
+        for (int e = 0; e < EO; ++e) f.w[e] = finite_of(f.w[e]);
+      }
+    }
   }
   __device__ static __forceinline__ void multiply(const Operands &f, f32x16 (&acc)[EO][ET]) {
 #pragma unroll
@@ -203,12 +212,12 @@ struct Gemm {
   }
   // The stage in (xs, ws), whose first two steps' operands are on their way to f; the next one is in (xn, wn), and `later` is loaded
   // where this one was.
-  __device__ __forceinline__ void stage(const Operand &xo, const Operand &wo, int64_t later, unsigned char *xs, unsigned char *ws,
+  __device__ __forceinline__ void stage(const Operand &xo, const Operand &wo, int64_t now, int64_t later, unsigned char *xs, unsigned char *ws,
                                         const unsigned char *xn, const unsigned char *wn, Operands (&f)[4], f32x16 (&acc)[EO][ET]) {
     constexpr int Reads = ET * (XA ? 2 : 1) + EO * (WA ? 2 : 1), L1 = (L + 2) / 3, L2 = 2 * L1;
     x.turn_to(xo, later), w.turn_to(wo, later);
-    fetch(xs, ws, 2, f[2]);
-    fetch(xs, ws, 3, f[3]);
+    fetch(xs, ws, 2, now, f[2]);
+    fetch(xs, ws, 3, now, f[3]);
     multiply(f[0], acc);
     spread<2 * Reads, 0>();
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -220,8 +229,8 @@ struct Gemm {
     multiply(f[2], acc);
     spread<0, L2 - L1>();
     arrived<L2>();
-    fetch(xn, wn, 0, f[0]);
-    fetch(xn, wn, 1, f[1]);
+    fetch(xn, wn, 0, now + 1, f[0]);
+    fetch(xn, wn, 1, now + 1, f[1]);
     load<L2, L>(xs, ws);
     multiply(f[3], acc);
     spread<2 * Reads, L - L2>();
@@ -238,14 +247,14 @@ struct Gemm {
     x.turn_to(xo, at(s0 + 1)), w.turn_to(wo, at(s0 + 1));
     load<0, L>(xs1, ws1);
     arrived<L>();
-    fetch(xs0, ws0, 0, f[0]);
-    fetch(xs0, ws0, 1, f[1]);
+    fetch(xs0, ws0, 0, s0, f[0]);
+    fetch(xs0, ws0, 1, s0, f[1]);
     int64_t s = s0;
     for (; s + 1 < s1; s += 2) {
-      stage(xo, wo, at(s + 2), xs0, ws0, xs1, ws1, f, acc);
-      stage(xo, wo, at(s + 3), xs1, ws1, xs0, ws0, f, acc);
+      stage(xo, wo, s, at(s + 2), xs0, ws0, xs1, ws1, f, acc);
+      stage(xo, wo, s + 1, at(s + 3), xs1, ws1, xs0, ws0, f, acc);
     }
-    if (s < s1) stage(xo, wo, none, xs0, ws0, xs1, ws1, f, acc);
+    if (s < s1) stage(xo, wo, s, none, xs0, ws0, xs1, ws1, f, acc);
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // nothing is on its way to LDS from here on
     bare_barrier();
   }
@@ -277,7 +286,7 @@ __device__ __forceinline__ void leave(const unsigned char *lds, F f) {
 // ---- the two projections -------------------------------------------------------------------------------------
 template <class T, int BT, int BO, int ACT, bool BACK>
 __global__ __launch_bounds__(256, BO == 128 ? 2 : 1) void gate_gemm_kernel(Gate<T> p, Operand x, Operand w, int64_t tiles_t, int tiles_o) {
-  using G = Gemm<T, BT, BO, false, false, false, true>;
+  using G = Gemm<T, BT, BO, false, false, false, true, false>;
   constexpr int ET = G::ET, EO = G::EO, Pairs = EO / 2, Row = Pairs * 64;
   __shared__ __align__(1024) unsigned char xs0[G::X::Bytes], ws0[G::W::Bytes], xs1[G::X::Bytes], ws1[G::W::Bytes];
   int64_t tt;
@@ -435,11 +444,11 @@ struct Result {
   float *part;     // PARTS: [splits][turns * rows][outs]
 };
 
-template <class T, int BT, int BO, bool XA, bool PARTS>
+template <class T, int BT, int BO, bool XA, bool PARTS, bool TWO>
 __global__ __launch_bounds__(256, BO == 128 && BT <= 128 ? 2 : 1) void product_gemm_kernel(Result<T> p, Operand x, Operand w, int64_t tiles_t,
                                                                                        int tiles_o, int splits, int64_t chunk,
-                                                                                       int64_t stages) {
-  using G = Gemm<T, BT, BO, XA, true, false, !XA>;
+                                                                                       int64_t stages, int64_t from) {
+  using G = Gemm<T, BT, BO, XA, true, XA && TWO, !XA || TWO, TWO>;
   constexpr int ET = G::ET, EO = G::EO, Row = EO * 64;
   __shared__ __align__(1024) unsigned char xs0[G::X::Bytes], ws0[G::W::Bytes], xs1[G::X::Bytes], ws1[G::W::Bytes];
   const int64_t tiles = tiles_t * tiles_o, block = in_runs(blockIdx.x, tiles * splits), split = block / tiles;
@@ -450,12 +459,13 @@ __global__ __launch_bounds__(256, BO == 128 && BT <= 128 ? 2 : 1) void product_g
   const int64_t tiles_half = (p.rows + BT - 1) / BT, second = tt >= tiles_half ? 1 : 0;
   const int64_t t0 = (tt - second * tiles_half) * BT;
   const int64_t o0 = (int64_t)to * BO;
-  if constexpr (XA) x.p[0] += (second * p.turn + t0) * (int64_t)sizeof(T);
+  if constexpr (XA) x.p[0] += (second * p.turn + t0) * (int64_t)sizeof(T), x.p[1] += (second * p.turn + t0) * (int64_t)sizeof(T);
   else x.p[0] += t0 * x.ld;
   x.lines -= t0;
   w.p[0] += o0 * sizeof(T), w.p[1] += o0 * sizeof(T), w.lines -= o0;
   f32x16 acc[EO][ET] = {};
   G g;
+  g.second = from;
   g.run(x, w, split * chunk, min(stages, (split + 1) * chunk), xs0, ws0, xs1, ws1, acc);
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, ln = lane & 31, half = lane >> 5;
   const int64_t tw = t0 + (wv / G::WO) * (ET * 32), ow = o0 + (wv % G::WO) * (EO * 32);
@@ -547,28 +557,35 @@ ProductPlan plan_of(int64_t rows, int64_t outs, int64_t k, int halves, int size)
   return p;
 }
 
-template <class T, int BT, int BO, bool XA>
-void launch_product(const Result<T> &r, const Operand &x, const Operand &w, const ProductPlan &p, int halves, hipStream_t s) {
+template <class T, int BT, int BO, bool XA, bool TWO>
+void launch_product(const Result<T> &r, const Operand &x, const Operand &w, const ProductPlan &p, int halves, int64_t from, hipStream_t s) {
   const int64_t tiles_t = halves * tiles(r.rows, BT);
   const int tiles_o = (int)tiles(r.outs, BO);
   const unsigned blocks = (unsigned)(tiles_t * tiles_o * p.splits);
   if (p.splits > 1) {
-    product_gemm_kernel<T, BT, BO, XA, true><<<blocks, 256, 0, s>>>(r, x, w, tiles_t, tiles_o, p.splits, p.chunk, p.stages);
+    product_gemm_kernel<T, BT, BO, XA, true, TWO><<<blocks, 256, 0, s>>>(r, x, w, tiles_t, tiles_o, p.splits, p.chunk, p.stages, from);
     product_gemm_join_kernel<T><<<dim3((unsigned)std::min<int64_t>(tiles(r.rows * r.outs, 1024), 4096), halves), 256, 0, s>>>(r, p.splits);
   } else {
-    product_gemm_kernel<T, BT, BO, XA, false><<<blocks, 256, 0, s>>>(r, x, w, tiles_t, tiles_o, 1, p.stages, p.stages);
+    product_gemm_kernel<T, BT, BO, XA, false, TWO><<<blocks, 256, 0, s>>>(r, x, w, tiles_t, tiles_o, 1, p.stages, p.stages, from);
   }
 }
 
+// k: of all parts; from: the stage that second parts begin with
 template <class T, bool XA>
-hipError_t product(const Result<T> &r, const Operand &x, const Operand &w, int64_t k, int halves, hipStream_t s) {
+hipError_t product(const Result<T> &r, const Operand &x, const Operand &w, int64_t k, int parts, int halves, int64_t from, hipStream_t s) {
   const ProductPlan p = plan_of(r.rows, r.outs, k, XA ? 2 : 1, sizeof(T));  // (the same for one of the weights' gradients as for both)
   if constexpr (sizeof(T) == 2) {
-    if (p.bt == 256) launch_product<T, 256, 256, XA>(r, x, w, p, halves, s);
-    else launch_product<T, 128, 128, XA>(r, x, w, p, halves, s);
+    if (parts == 2) {
+      if (p.bt == 256) launch_product<T, 256, 256, XA, true>(r, x, w, p, halves, from, s);
+      else launch_product<T, 128, 128, XA, true>(r, x, w, p, halves, from, s);
+    } else if (p.bt == 256) {
+      launch_product<T, 256, 256, XA, false>(r, x, w, p, halves, 0, s);
+    } else {
+      launch_product<T, 128, 128, XA, false>(r, x, w, p, halves, 0, s);
+    }
   } else {
-    if (p.bt == 64) launch_product<T, 64, 128, XA>(r, x, w, p, halves, s);
-    else launch_product<T, 128, 128, XA>(r, x, w, p, halves, s);
+    if (p.bt == 64) launch_product<T, 64, 128, XA, false>(r, x, w, p, halves, 0, s);
+    else launch_product<T, 128, 128, XA, false>(r, x, w, p, halves, 0, s);
   }
   return hipGetLastError();
 }
@@ -618,38 +635,46 @@ hipError_t gemm_gate(const Gate<T> &p, int act, bool back, const Side<T> &x, con
   });
 }
 
-size_t gemm_dx_parts(int64_t rows, int64_t C_in, int64_t room, int size) { return parts_of(rows, C_in, 2 * room, 1, size); }
-size_t gemm_dw_parts(int64_t rows, int64_t C_in, int64_t C_out, int size) {
-  return parts_of(C_out, C_in, rows, 2, size);
+// k of the weights' gradients: rows, of each part in whole stages
+int64_t rows_of_parts(int64_t rows, int parts, int size) {
+  const int each = kLine / size;
+  return parts == 2 ? (rows + each - 1) / each * each * 2 : rows;
+}
+size_t gemm_dx_parts(int64_t rows, int64_t C_in, int64_t room, int parts, int size) { return parts_of(rows, C_in, parts * 2 * room, 1, size); }
+size_t gemm_dw_parts(int64_t rows, int64_t C_in, int64_t C_out, int parts, int size) {
+  return parts_of(C_out, C_in, rows_of_parts(rows, parts, size), 2, size);
 }
 
 template <class T>
-hipError_t gemm_dx(const T *d, int64_t room, int64_t rows, const T *w_gate, const T *w_up, int64_t ldw, int64_t C_in, int64_t C_out, T *dx,
-                   int64_t ld, float *part, hipStream_t s) {
+hipError_t gemm_dx(const T *d, int64_t room, int parts, int64_t rows, const T *w_gate, const T *w_up, int64_t ldw, int64_t C_in, int64_t C_out,
+                   T *dx, int64_t ld, float *part, hipStream_t s) {
   Operand x = {}, w = {};
-  x.p[0] = reinterpret_cast<const char *>(d), x.ld = 2 * room * sizeof(T), x.lines = rows, x.k = 2 * room;
+  x.p[0] = reinterpret_cast<const char *>(d), x.ld = parts * 2 * room * sizeof(T), x.lines = rows, x.k = parts * 2 * room;
   w.p[0] = reinterpret_cast<const char *>(w_gate), w.p[1] = reinterpret_cast<const char *>(w_up);
-  w.ld = ldw * sizeof(T), w.lines = ldw, w.k = C_out, w.turn = room;
+  w.ld = ldw * sizeof(T), w.lines = ldw, w.k = C_out, w.turn = room, w.again = 2 * room;
   const Result<T> r{{dx, nullptr}, ld, rows, C_in, 0, part};
-  return product<T, false>(r, x, w, 2 * room, 1, s);
+  return product<T, false>(r, x, w, x.k, parts, 1, 2 * room * (int64_t)sizeof(T) / kLine, s);
 }
 
 template <class T>
-hipError_t gemm_dw(const T *d, int64_t room, int64_t rows, const T *x, int64_t ldx, int64_t width, int64_t C_in, int64_t C_out, T *dw_gate,
-                   T *dw_up, float *part, hipStream_t s) {
+hipError_t gemm_dw(const T *d, int64_t room, int parts, int64_t rows, const T *x, int64_t ldx, int64_t width, int64_t C_in, int64_t C_out,
+                   T *dw_gate, T *dw_up, float *part, hipStream_t s) {
   Operand a = {}, b = {};
-  a.p[0] = reinterpret_cast<const char *>(d), a.ld = 2 * room * sizeof(T), a.lines = room, a.k = rows;
-  b.p[0] = reinterpret_cast<const char *>(x), b.ld = ldx * sizeof(T), b.lines = width, b.k = rows;
+  const int64_t k = rows_of_parts(rows, parts, sizeof(T)), never = (int64_t)1 << 60;
+  a.p[0] = reinterpret_cast<const char *>(d), a.p[1] = reinterpret_cast<const char *>(d + 2 * room);
+  a.ld = parts * 2 * room * sizeof(T), a.lines = room, a.k = rows, a.turn = k / parts, a.again = never;
+  b.p[0] = b.p[1] = reinterpret_cast<const char *>(x), b.ld = ldx * sizeof(T), b.lines = width, b.k = rows, b.turn = k / parts, b.again = never;
   const int halves = dw_gate && dw_up ? 2 : 1;
-  if (!dw_gate) a.p[0] += room * sizeof(T);
+  if (!dw_gate) a.p[0] += room * sizeof(T), a.p[1] += room * sizeof(T);
   const Result<T> r{{dw_gate ? dw_gate : dw_up, halves == 2 ? dw_up : nullptr}, C_in, C_out, C_in, room, part};
-  return product<T, true>(r, a, b, rows, halves, s);
+  return product<T, true>(r, a, b, k, parts, halves, k / parts * (int64_t)sizeof(T) / kLine, s);
 }
 
 #define WCC_GEMM(T)                                                                                                                          \
   template hipError_t gemm_gate<T>(const Gate<T> &, int, bool, const Side<T> &, const T *, const T *, int64_t, int64_t, hipStream_t);        \
-  template hipError_t gemm_dx<T>(const T *, int64_t, int64_t, const T *, const T *, int64_t, int64_t, int64_t, T *, int64_t, float *, hipStream_t); \
-  template hipError_t gemm_dw<T>(const T *, int64_t, int64_t, const T *, int64_t, int64_t, int64_t, int64_t, T *, T *, float *, hipStream_t);
+  template hipError_t gemm_dx<T>(const T *, int64_t, int, int64_t, const T *, const T *, int64_t, int64_t, int64_t, T *, int64_t, float *,   \
+                                 hipStream_t);                                                                                               \
+  template hipError_t gemm_dw<T>(const T *, int64_t, int, int64_t, const T *, int64_t, int64_t, int64_t, int64_t, T *, T *, float *, hipStream_t);
 WCC_GEMM(float)
 WCC_GEMM(bf16_t)
 #undef WCC_GEMM

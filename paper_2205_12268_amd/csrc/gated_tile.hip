@@ -67,9 +67,9 @@ struct Loader {
   }
 };
 
-// acc[e][r] += the products over k0 .. k1; wave (wm, wn) has rows (wm * ET + r) * 32 and lines first(e) of the second operand
+// acc[e][r] += the products over k0 .. k1 (second: of a's second part, by what is finite in b); wave (wm, wn) has rows (wm * ET + r) * 32 and lines first(e) of the second operand
 template <class T, bool AT, bool BT, int ET, class F>
-__device__ __forceinline__ void multiply(const Loader<T, AT, 64 * ET> &a, const Loader<T, BT, kTile> &b, int64_t k0, int64_t k1, int wm, F first,
+__device__ __forceinline__ void multiply(const Loader<T, AT, 64 * ET> &a, const Loader<T, BT, kTile> &b, int64_t k0, int64_t k1, int wm, F first, bool second,
                                          unsigned char (&lds)[2][(64 * ET + kTile) * kRowBytes], f32x16 (&acc)[2][ET]) {
   constexpr int KB = kStage / (int)sizeof(T), Rows = 64 * ET;
   const int lane = threadIdx.x & 63, ln = lane & 31, half = lane >> 5;
@@ -89,8 +89,12 @@ __device__ __forceinline__ void multiply(const Loader<T, AT, 64 * ET> &a, const 
       for (int r = 0; r < ET; ++r)
         af[r] = *reinterpret_cast<const u32x4 *>(lds[buf] + ((wm * ET + r) * 32 + ln) * kRowBytes + ks * 32 + half * 16);
 #pragma unroll
-      for (int e = 0; e < 2; ++e)
+      for (int e = 0; e < 2; ++e) {
         bf[e] = *reinterpret_cast<const u32x4 *>(lds[buf] + (Rows + first(e) + ln) * kRowBytes + ks * 32 + half * 16);
+        if constexpr (sizeof(T) == 2) {
+          if (second) bf[e] = finite_of(bf[e]);
+        }
+      }
 #pragma unroll
       for (int r = 0; r < ET; ++r)
 #pragma unroll
@@ -128,7 +132,7 @@ __global__ __launch_bounds__(256, 2) void gate_tile_kernel(Gate<T> p, Side<T> x,
     return (i < kTile / 2 ? w_gate : w_up) + (int64_t)min(o0 + i % (kTile / 2), p.outs - 1) * ldw;
   }, 1);
   f32x16 acc[2][ET] = {};
-  multiply<T, false, false, ET>(a, b, split * n.chunk, min(k, (split + 1) * n.chunk), wm, [&](int e) { return e * (kTile / 2) + wn * 32; }, lds, acc);
+  multiply<T, false, false, ET>(a, b, split * n.chunk, min(k, (split + 1) * n.chunk), wm, [&](int e) { return e * (kTile / 2) + wn * 32; }, false, lds, acc);
 #pragma unroll
   for (int r = 0; r < ET; ++r) {
     const int64_t t = t0 + (wm * ET + r) * 32 + ln;
@@ -211,7 +215,7 @@ __global__ __launch_bounds__(256, 2) void product_tile_kernel(Product<T> p, Grid
   const int64_t r0 = tt * (64 * ET), o0 = (int64_t)to * kTile, rows = p.a[0].lines, lines = p.b[0].lines;
   f32x16 acc[2][ET] = {};
   for (int f = 0; f < p.phases; ++f) {
-    const Side<T> sa = p.a[f + batch], sb = p.b[f + batch];
+    const Side<T> sa = p.a[f * p.batches + batch], sb = p.b[f * p.batches + batch];
     Loader<T, AT, 64 * ET> a;
     Loader<T, true, kTile> b;
     a.aim([&](int i, bool &there) {
@@ -222,7 +226,7 @@ __global__ __launch_bounds__(256, 2) void product_tile_kernel(Product<T> p, Grid
       there = o0 + i < lines;
       return sb.p + min(o0 + i, lines - 1);
     }, sb.s);
-    multiply<T, AT, true, ET>(a, b, split * n.chunk, min(p.k, (split + 1) * n.chunk), wm, [&](int e) { return wn * 64 + e * 32; }, lds, acc);
+    multiply<T, AT, true, ET>(a, b, split * n.chunk, min(p.k, (split + 1) * n.chunk), wm, [&](int e) { return wn * 64 + e * 32; }, f >= p.second, lds, acc);
   }
 #pragma unroll
   for (int r = 0; r < ET; ++r) {

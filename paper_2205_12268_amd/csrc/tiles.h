@@ -102,6 +102,21 @@ __device__ __forceinline__ void load_k_pair(const T *p, int64_t sk, int left, bo
   }
 }
 
+// ---- fp32 values as operands of bf16 ---------------------------------------------------------------------------
+// bf16 operands carry 8 bits each: P of them take P * 8 bits of the values, the rest of each going to the next.
+__device__ __forceinline__ float left_of(float v, uint32_t part) {  // (nothing of an infinity, or it would be NaN)
+  return (part & 0x7f80) == 0x7f80 ? 0.f : v - __uint_as_float(part << 16);
+}
+// bf16 operands with 0 in the place of infinities and NaN: what meets parts past the first, which are 0 where the first has all of a
+// value, so that an infinity by a value is not made NaN by its parts
+__device__ __forceinline__ u32x4 finite_of(u32x4 v) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if ((v[i] & 0x7f80u) == 0x7f80u) v[i] &= 0xffff0000u;
+    if ((v[i] & 0x7f800000u) == 0x7f800000u) v[i] &= 0xffffu;
+  }
+  return v;
+}
 // An order of workgroups that leaves each of the eight XCDs (they go to them in turn) a run of neighbours, and of tiles within it in
 // blocks of up to eight row tiles, so that what neighbours share is in their L2.
 __device__ __forceinline__ int64_t in_runs(int64_t b, int64_t n) {

@@ -144,7 +144,8 @@ def gated_forward(x, w_gate, w_up, name):
 
 
 def gated_backward(x, w_gate, w_up, name, dy, narrow, kept_gu=None):
-    """{"dx", "dw_gate", "dw_up"}: (result, bound); narrow: dg and du are rounded to bf16; kept_gu: values of g and u."""
+    """{"dx", "dw_gate", "dw_up"}: (result, bound); narrow: dg and du are rounded to bf16, twice (16 bits) where they are fewer than 2^17
+    values each; kept_gu: values of g and u."""
     (g, eg), (u, eu) = (projected(x, w) for w in (w_gate, w_up)) if kept_gu is None else ((v.double().cpu(), 0 * v.double().cpu()) for v in kept_gu)
     x, dy, wg, wu = (v.double().cpu() for v in (x, dy, w_gate, w_up))
     value, slope = act(g, name)
@@ -152,13 +153,14 @@ def gated_backward(x, w_gate, w_up, name, dy, narrow, kept_gu=None):
     dg, du = dy * u * slope, dy * value
     edg = dy.abs() * (eu * (slope.abs() + es) + u.abs() * es) + 2 * U * dg.abs()
     edu = dy.abs() * ev + U * du.abs()
-    if narrow:
-        edg, edu = edg + NARROW * 1.001 * (dg.abs() + edg), edu + NARROW * 1.001 * (du.abs() + edu)
     rows, n = dy.shape
+    if narrow:
+        off = 1.001 * (NARROW ** 2 if rows * n < 1 << 17 else NARROW)
+        edg, edu = edg + off * (dg.abs() + edg), edu + off * (du.abs() + edu)
     sums = lambda k, mag: (k + 64) * U * mag * 1.01  # noqa: E731
-    return {"dx": (dg @ wg + du @ wu, edg @ wg.abs() + edu @ wu.abs() + sums(2 * n, dg.abs() @ wg.abs() + du.abs() @ wu.abs())),
-            "dw_gate": (dg.t() @ x, edg.t() @ x.abs() + sums(rows, dg.abs().t() @ x.abs())),
-            "dw_up": (du.t() @ x, edu.t() @ x.abs() + sums(rows, du.abs().t() @ x.abs()))}
+    return {"dx": (dg @ wg + du @ wu, edg @ wg.abs() + edu @ wu.abs() + sums(4 * n, dg.abs() @ wg.abs() + du.abs() @ wu.abs())),
+            "dw_gate": (dg.t() @ x, edg.t() @ x.abs() + sums(2 * rows, dg.abs().t() @ x.abs())),
+            "dw_up": (du.t() @ x, edu.t() @ x.abs() + sums(2 * rows, du.abs().t() @ x.abs()))}
 
 
 def near(got, want, narrow, what=""):

@@ -176,6 +176,35 @@ def test_what_is_not_finite_stays_in_its_row(ctx, t, rows):
     assert bool(torch.isnan(again["dx"][bad]).all()) and bool(torch.isfinite(again["dx"][fine.cuda()]).all())
 
 
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [(5, 104, 72), (40, 1000, 88), (300, 72, 96), (1500, 64, 200), (700, 1032, 600)], ids=str)
+def test_infinite_weights_stay_infinities(ctx, t, size):
+    """A weight's infinity, or a row's, by a gradient that is not 0 is an infinity of its sign, whatever the gradient is held as."""
+    rows, ci, co = size
+    x, wg, wu, dy = inputs(rows, ci, co, t, 11)
+    _, codes, steps = forward(ctx, x, wg, wu, "silu")
+    clean = backward(ctx, x, None, wg, wu, "silu", dy, (codes, steps))
+    wu[3, 5] = math.inf
+    got = backward(ctx, x, None, wg, wu, "silu", dy, (codes, steps))
+    g = codes[0].double()[:, 3] * torch.exp2(steps[0].double()[:, 0] - 127)
+    du = dy[:, 3].double() * g * torch.sigmoid(g)
+    assert torch.equal(got["dx"][:, 5][du > 0], torch.full_like(dy[:, 0], math.inf)[du > 0])
+    assert torch.equal(got["dx"][:, 5][du < 0], torch.full_like(dy[:, 0], -math.inf)[du < 0])
+    others = torch.arange(ci).cuda() != 5
+    assert torch.equal(got["dx"][:, others], clean["dx"][:, others])
+    x[1, 7] = -math.inf
+    got = backward(ctx, x, None, wg, wu, "silu", dy, (codes, steps))
+    u = codes[1].double()[1, :co] * torch.exp2(steps[1].double()[1] - 127).repeat_interleave(32)[:co]
+    g = codes[0].double()[1, :co] * torch.exp2(steps[0].double()[1] - 127).repeat_interleave(32)[:co]
+    p = torch.sigmoid(g)
+    du, dg = dy[1].double() * g * p, dy[1].double() * u * p * (1 + g * (1 - p))
+    for k, v in (("dw_up", du), ("dw_gate", dg)):
+        sure = v.abs() > 1e-30
+        assert torch.equal(got[k][:, 7].double()[sure], (-math.inf * v.sign())[sure]), k
+        others = torch.arange(ci).cuda() != 7
+        assert torch.equal(got[k][:, others], clean[k][:, others])
+
+
 def test_gradients_against_differences(ctx):
     """sum(y r) along random ways, fp32, steps of 2^-7: second-order terms are 2^-14 times a third derivative below 100, rounding
     2^-24 of a sum of about 300 over 2^-6."""
