@@ -136,21 +136,36 @@ size_t tile_product_parts(int64_t rows, int64_t lines, int64_t k, int batches, i
 template <class T>
 hipError_t tile_gate(const Gate<T> &p, int act, bool back, const Side<T> &x, const T *w_gate, const T *w_up, int64_t ldw, int64_t k,
                      float *part, hipStream_t s);
+// the sums of `splits` ranges of k, [splits][rows][2][room], joined
+template <class T>
+hipError_t join_gate(const Gate<T> &p, int act, bool back, int splits, const float *part, hipStream_t s);
 template <class T, bool AT>
 hipError_t tile_product(const Product<T> &p, float *part, hipStream_t s);
 
 // Many rows (gated_gemm.hip).  Operands whose k or lines are contiguous and 16 bytes a load: pointers and strides are multiples.
 bool gemm_takes(const void *p, int64_t ld, int64_t width, int size);
+size_t gemm_gate_parts(int64_t rows, int64_t outs, int64_t k, int size);
 template <class T>
-hipError_t gemm_gate(const Gate<T> &p, int act, bool back, const Side<T> &x, const T *w_gate, const T *w_up, int64_t ldw, int64_t k, hipStream_t s);
-size_t gemm_dx_parts(int64_t rows, int64_t C_in, int64_t room, int parts, int size);
-size_t gemm_dw_parts(int64_t rows, int64_t C_in, int64_t C_out, int parts, int size);
+hipError_t gemm_gate(const Gate<T> &p, int act, bool back, const Side<T> &x, const T *w_gate, const T *w_up, int64_t ldw, int64_t k, float *part,
+                     hipStream_t s);
+// dx and the weights' gradients from dg and du, all in one launch, and one that joins ranges of k.
 template <class T>
-hipError_t gemm_dx(const T *d, int64_t room, int parts, int64_t rows, const T *w_gate, const T *w_up, int64_t ldw, int64_t C_in, int64_t C_out, T *dx,
-                   int64_t ld, float *part, hipStream_t s);
+struct Backward {
+  const T *d;
+  int64_t room, rows;
+  int parts;
+  const T *w_gate, *w_up;
+  int64_t ldw;
+  const T *x;
+  int64_t ldx, width;
+  int64_t C_in, C_out;
+  T *dx;  // nullable, as the two below
+  int64_t ld;
+  T *dw_gate, *dw_up;
+};
+size_t gemm_back_parts(int64_t rows, int64_t C_in, int64_t C_out, int parts, int size);
 template <class T>
-hipError_t gemm_dw(const T *d, int64_t room, int parts, int64_t rows, const T *x, int64_t ldx, int64_t width, int64_t C_in, int64_t C_out, T *dw_gate,
-                   T *dw_up, float *part, hipStream_t s);
+hipError_t gemm_back(const Backward<T> &b, float *part, hipStream_t s);
 
 // The two projections for few rows of bf16 (gated_thin.hip), operands as above.
 hipError_t thin_gate(const Gate<bf16_t> &p, int act, bool back, const Side<bf16_t> &x, const bf16_t *w_gate, const bf16_t *w_up, int64_t ldw,

@@ -84,7 +84,7 @@ struct Plan {
 
 constexpr int kThin = 64;  // rows of few
 
-// Tiles fed straight from memory from 2^28 products on (fp32: 2^25); bf16 rows or weights that 16-byte loads do not take are copied for it
+// Tiles fed straight from memory from 2^28 products on (fp32: 2^22); bf16 rows or weights that 16-byte loads do not take are copied for it
 // from 2^30 on, fp32 ones go by way of registers.
 Plan plan_of(const wcc_gated_desc &g, bool backward) {
   Plan p = {};
@@ -93,13 +93,14 @@ Plan plan_of(const wcc_gated_desc &g, bool backward) {
   p.room = room_of(g.C_out), p.ldx = room_of(g.C_in), p.k = (g.C_in + 7) / 8 * 8;
   const int each = 16 / size;
   p.copy_w = g.C_in % each != 0, p.copy_x = p.copy_w || g.ldx % each != 0;
-  p.gemm = g.rows > kThin && (size == 2 ? products >= (p.copy_x ? 1 << 30 : 1 << 28) : !p.copy_w && products >= 1 << 25);
+  p.gemm = size == 2 ? g.rows > kThin && products >= (p.copy_x ? 1 << 30 : 1 << 28) : !p.copy_x && products >= 1 << 22;
   if (size == 4) p.copy_x = p.copy_w = false, p.k = g.C_in;
   p.parts = size == 2 && g.rows * (int64_t)g.C_out < kFew ? 2 : 1;
   // (few rows, whose products are bound by the weights and their gradients: any that 16-byte loads take)
   p.back = p.gemm || (size == 2 && g.rows <= kThin && g.C_in % each == 0 && products >= 1 << 20);
   if (!p.gemm) p.copy_x = p.copy_w = false;
   size_t parts = tile_gate_parts(g.rows, g.C_out, g.C_in, size), at = 0;  // (tensors at odd addresses take these tiles)
+  if (p.gemm) parts = std::max(parts, gemm_gate_parts(g.rows, g.C_out, p.k, size));
   if (backward) at += up((size_t)g.rows * p.parts * 2 * p.room * size);
   p.x = at;
   if (backward || p.copy_x) at += up((size_t)g.rows * p.ldx * size);
@@ -107,7 +108,7 @@ Plan plan_of(const wcc_gated_desc &g, bool backward) {
   if (p.copy_w) at += 2 * up((size_t)g.C_out * p.ldx * size);
   p.part = at;
   if (backward) {
-    if (p.back) parts = std::max({parts, gemm_dx_parts(g.rows, g.C_in, p.room, p.parts, size), gemm_dw_parts(g.rows, g.C_in, g.C_out, p.parts, size)});
+    if (p.back) parts = std::max(parts, gemm_back_parts(g.rows, g.C_in, g.C_out, p.parts, size));
     parts = std::max({parts, tile_product_parts(g.rows, g.C_in, g.C_out, 1, size), tile_product_parts(g.C_out, g.C_in, g.rows, 2, size)});
   }
   p.bytes = p.part + up(parts);
@@ -166,7 +167,7 @@ hipError_t gate_of(const wcc_gated_desc &d, const Plan &p, const Gate<T> &gate, 
   if constexpr (sizeof(T) == 2) {
     if (d.rows <= kThin && o.takes) return thin_gate(gate, d.act, back, o.x, o.wg, o.wu, o.ldw, p.k, s);
   }
-  if (p.gemm && o.takes && !(back && p.parts == 2)) return gemm_gate<T>(gate, d.act, back, o.x, o.wg, o.wu, o.ldw, p.k, s);
+  if (p.gemm && o.takes && !(back && p.parts == 2)) return gemm_gate<T>(gate, d.act, back, o.x, o.wg, o.wu, o.ldw, p.k, part, s);
   return tile_gate<T>(gate, d.act, back, o.x, o.wg, o.wu, o.ldw, d.C_in, part, s);
 }
 
@@ -213,11 +214,9 @@ hipError_t backward(const wcc_gated_desc &d, const GatedArgs &g, hipStream_t s) 
   if (e != hipSuccess) return e;
   const T *dg = gate.d, *du = gate.d + p.room;
   if (p.back && o.takes) {
-    if (g.dx && (e = gemm_dx<T>(dg, p.room, p.parts, d.rows, o.wg, o.wu, o.ldw, d.C_in, d.C_out, static_cast<T *>(g.dx), d.ldx, part, s)) != hipSuccess)
-      return e;
-    return dw ? gemm_dw<T>(dg, p.room, p.parts, d.rows, o.x.p, o.x.s, p.k, d.C_in, d.C_out, static_cast<T *>(g.dw_gate),
-                           static_cast<T *>(g.dw_up), part, s)
-              : hipSuccess;
+    const Backward<T> b{dg, p.room, d.rows, p.parts, o.wg, o.wu, o.ldw, o.x.p, o.x.s, p.k, d.C_in, d.C_out, static_cast<T *>(g.dx), d.ldx,
+                        static_cast<T *>(g.dw_gate), static_cast<T *>(g.dw_up)};
+    return gemm_back<T>(b, part, s);
   }
   const int64_t ldd = p.parts * 2 * p.room, next = 2 * p.room;
   if (g.dx) {

@@ -284,14 +284,17 @@ __device__ __forceinline__ void leave(const unsigned char *lds, F f) {
 }
 
 // ---- the two projections -------------------------------------------------------------------------------------
-template <class T, int BT, int BO, int ACT, bool BACK>
-__global__ __launch_bounds__(256, BO == 128 ? 2 : 1) void gate_gemm_kernel(Gate<T> p, Operand x, Operand w, int64_t tiles_t, int tiles_o) {
+// PARTS: a range of k, whose sums go to part [splits][rows][2][room].
+template <class T, int BT, int BO, int ACT, bool BACK, bool PARTS>
+__global__ __launch_bounds__(256, BO == 128 ? 2 : 1) void gate_gemm_kernel(Gate<T> p, Operand x, Operand w, int64_t tiles_t, int tiles_o,
+                                                                         int64_t chunk, float *__restrict__ part) {
   using G = Gemm<T, BT, BO, false, false, false, true, false>;
   constexpr int ET = G::ET, EO = G::EO, Pairs = EO / 2, Row = Pairs * 64;
   __shared__ __align__(1024) unsigned char xs0[G::X::Bytes], ws0[G::W::Bytes], xs1[G::X::Bytes], ws1[G::W::Bytes];
+  const int64_t tiles = tiles_t * tiles_o, at = in_runs(blockIdx.x, gridDim.x), split = PARTS ? at / tiles : 0;
   int64_t tt;
   int to;
-  tile_of(in_runs(blockIdx.x, tiles_t * tiles_o), tiles_t, tiles_o, tt, to);
+  tile_of(at - split * tiles, tiles_t, tiles_o, tt, to);
   const int64_t t0 = tt * BT;
   const int o0 = to * (BO / 2);
   x.p[0] += t0 * x.ld, x.lines -= t0;
@@ -299,13 +302,29 @@ __global__ __launch_bounds__(256, BO == 128 ? 2 : 1) void gate_gemm_kernel(Gate<
   w.lines = min(w.lines, (int64_t)(BO / 2));
   f32x16 acc[EO][ET] = {};
   G g;
-  g.run(x, w, 0, (x.k + G::X::KS - 1) / G::X::KS, xs0, ws0, xs1, ws1, acc);
+  const int64_t stages = (x.k + G::X::KS - 1) / G::X::KS;
+  g.run(x, w, split * chunk, PARTS ? min(stages, (split + 1) * chunk) : stages, xs0, ws0, xs1, ws1, acc);
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, ln = lane & 31, half = lane >> 5;
   const int64_t tw = t0 + (wv / G::WO) * (ET * 32);
   const int ow = o0 + (wv % G::WO) * (Pairs * 32);
   unsigned char *own = wv == 0 ? xs0 : wv == 1 ? ws0 : wv == 2 ? xs1 : ws1;  // (8 KiB each at least)
   const int64_t blocks = (p.outs + kKept - 1) / kKept;
-  if constexpr (sizeof(T) == 4) {  // (bound by the matrix cores: straight to memory)
+  if constexpr (PARTS) {
+#pragma unroll
+    for (int r = 0; r < ET; ++r) {
+      const int64_t t = tw + r * 32 + ln;
+      if (t >= p.rows) continue;
+#pragma unroll
+      for (int e = 0; e < EO; ++e)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          const int o = ow + (e >> 1) * 32 + result_line(i, half);
+          float *q = part + ((split * p.rows + t) * 2 + (e & 1)) * p.room + o;
+          if (o < p.room) *reinterpret_cast<f32x4_any *>(q) = f32x4_any{acc[e][r][i], acc[e][r][i + 1], acc[e][r][i + 2], acc[e][r][i + 3]};
+        }
+    }
+    return;
+  } else if constexpr (sizeof(T) == 4) {  // (bound by the matrix cores: straight to memory)
 #pragma unroll
     for (int r = 0; r < ET; ++r)
 #pragma unroll
@@ -444,17 +463,27 @@ struct Result {
   float *part;     // PARTS: [splits][turns * rows][outs]
 };
 
-template <class T, int BT, int BO, bool XA, bool PARTS, bool TWO>
-__global__ __launch_bounds__(256, BO == 128 && BT <= 128 ? 2 : 1) void product_gemm_kernel(Result<T> p, Operand x, Operand w, int64_t tiles_t,
-                                                                                       int tiles_o, int splits, int64_t chunk,
-                                                                                       int64_t stages, int64_t from) {
+template <class T>
+struct Job {
+  Result<T> r;
+  Operand x, w;
+  int64_t tiles_t;
+  int tiles_o, splits;
+  int64_t chunk, stages, from;  // from: the stage that second parts begin with
+  int64_t blocks;               // 0: none
+};
+
+template <class T, int BT, int BO, bool XA, bool TWO>
+__device__ __forceinline__ void product_tile(const Job<T> &job, int64_t block, unsigned char *xs0, unsigned char *ws0, unsigned char *xs1,
+                                             unsigned char *ws1) {
   using G = Gemm<T, BT, BO, XA, true, XA && TWO, !XA || TWO, TWO>;
   constexpr int ET = G::ET, EO = G::EO, Row = EO * 64;
-  __shared__ __align__(1024) unsigned char xs0[G::X::Bytes], ws0[G::W::Bytes], xs1[G::X::Bytes], ws1[G::W::Bytes];
-  const int64_t tiles = tiles_t * tiles_o, block = in_runs(blockIdx.x, tiles * splits), split = block / tiles;
+  const Result<T> &p = job.r;
+  Operand x = job.x, w = job.w;
+  const int64_t tiles = job.tiles_t * job.tiles_o, split = block / tiles;
   int64_t tt;
   int to;
-  tile_of(block % tiles, tiles_t, tiles_o, tt, to);
+  tile_of(block % tiles, job.tiles_t, job.tiles_o, tt, to);
   // rows of the second half begin with a tile of their own
   const int64_t tiles_half = (p.rows + BT - 1) / BT, second = tt >= tiles_half ? 1 : 0;
   const int64_t t0 = (tt - second * tiles_half) * BT;
@@ -465,18 +494,18 @@ __global__ __launch_bounds__(256, BO == 128 && BT <= 128 ? 2 : 1) void product_g
   w.p[0] += o0 * sizeof(T), w.p[1] += o0 * sizeof(T), w.lines -= o0;
   f32x16 acc[EO][ET] = {};
   G g;
-  g.second = from;
-  g.run(x, w, split * chunk, min(stages, (split + 1) * chunk), xs0, ws0, xs1, ws1, acc);
+  g.second = job.from;
+  g.run(x, w, split * job.chunk, min(job.stages, (split + 1) * job.chunk), xs0, ws0, xs1, ws1, acc);
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, ln = lane & 31, half = lane >> 5;
   const int64_t tw = t0 + (wv / G::WO) * (ET * 32), ow = o0 + (wv % G::WO) * (EO * 32);
   unsigned char *own = wv == 0 ? xs0 : wv == 1 ? ws0 : wv == 2 ? xs1 : ws1;
 #pragma unroll
   for (int r = 0; r < ET; ++r) {
-    if constexpr (PARTS || sizeof(T) == 4) {
+    if (sizeof(T) == 4 || job.splits > 1) {
       const int64_t t = tw + r * 32 + ln, halves = p.out[1] ? 2 : 1;
       if (t < p.rows) {
         float *q;
-        if constexpr (PARTS) q = p.part + ((split * halves + second) * p.rows + t) * p.outs;
+        if (job.splits > 1) q = p.part + ((split * halves + second) * p.rows + t) * p.outs;
         else q = reinterpret_cast<float *>(p.out[second]) + t * p.ld;
 #pragma unroll
         for (int e = 0; e < EO; ++e)
@@ -492,7 +521,7 @@ __global__ __launch_bounds__(256, BO == 128 && BT <= 128 ? 2 : 1) void product_g
             }
           }
       }
-    } else {
+    } else if constexpr (sizeof(T) == 2) {
 #pragma unroll
       for (int e = 0; e < EO; ++e)
 #pragma unroll
@@ -507,22 +536,37 @@ __global__ __launch_bounds__(256, BO == 128 && BT <= 128 ? 2 : 1) void product_g
   }
 }
 
+// dx's tiles, the longer ones, before the weights'
+template <class T, int BT, int BO, bool TWO>
+__global__ __launch_bounds__(256, BO == 128 && BT <= 128 ? 2 : 1) void product_gemm_kernel(Job<T> dx, Job<T> dw) {
+  __shared__ __align__(1024) unsigned char xs0[BT * kLine], ws0[BO * kLine], xs1[BT * kLine], ws1[BO * kLine];
+  const int64_t b = blockIdx.x;
+  if (b < dx.blocks) product_tile<T, BT, BO, false, TWO>(dx, in_runs(b, dx.blocks), xs0, ws0, xs1, ws1);
+  else product_tile<T, BT, BO, true, TWO>(dw, in_runs(b - dx.blocks, dw.blocks), xs0, ws0, xs1, ws1);
+}
+
+// Sums of ranges of k joined in their order: dx, then the one or two of the weights.
 template <class T>
-__global__ __launch_bounds__(256) void product_gemm_join_kernel(Result<T> p, int splits) {
+__global__ __launch_bounds__(256) void product_gemm_join_kernel(Job<T> dx, Job<T> dw, int first) {
+  const int which = first + blockIdx.y, h = which > 0 ? which - 1 : 0;
+  const Job<T> &job = which == 0 ? dx : dw;
+  const Result<T> &p = job.r;
   const int64_t all = p.rows * p.outs, halves = p.out[1] ? 2 : 1;
-  const int h = blockIdx.y;
   for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < all; i += (int64_t)gridDim.x * 1024) {
     f32x4_any v = {};
     const int n = (int)min(all - i, (int64_t)4);
-    for (int s = 0; s < splits; ++s) {
-      const float *q = p.part + (s * halves + h) * all + i;
-      if (n == 4) {
-        v += *reinterpret_cast<const f32x4_any *>(q);
-      } else {
-        for (int j = 0; j < n; ++j) v[j] += q[j];
-      }
+    if (n == 4) {
+#pragma unroll 4
+      for (int s = 0; s < job.splits; ++s) v += *reinterpret_cast<const f32x4_any *>(p.part + (s * halves + h) * all + i);
+    } else {
+      for (int s = 0; s < job.splits; ++s)
+        for (int j = 0; j < n; ++j) v[j] += p.part[(s * halves + h) * all + i + j];
     }
-    for (int j = 0; j < n; ++j) p.out[h][(i + j) / p.outs * p.ld + (i + j) % p.outs] = narrow<T>(v[j]);
+    int64_t row = i / p.outs, o = i - row * p.outs;
+    for (int j = 0; j < n; ++j) {
+      p.out[h][row * p.ld + o] = narrow<T>(v[j]);
+      if (++o == p.outs) o = 0, ++row;
+    }
   }
 }
 
@@ -539,60 +583,58 @@ hipError_t by_act(int act, F f) {
   }
 }
 
+// How the products of a backward pass are cut.  dx: rows x C_in over 2 room; the weights' gradients, both: 2 C_out x C_in over the rows.
+// Each workgroup has about as many stages as there are for every place (256, or 512 of the smaller tiles), four at least.
 struct ProductPlan {
-  int bt, bo, splits;
-  int64_t stages, chunk;
+  int bt, bo;
+  struct Part {
+    int64_t stages, chunk;
+    int splits;
+    size_t bytes;
+  } dx, dw;
 };
-// rows: of one half
-ProductPlan plan_of(int64_t rows, int64_t outs, int64_t k, int halves, int size) {
-  ProductPlan p;
-  p.stages = tiles(k, kLine / size);
-  const bool large = size == 2 && halves * tiles(rows, 256) * tiles(outs, 256) >= 200;
-  p.bt = p.bo = large ? 256 : 128;
-  if (size == 4 && halves * tiles(rows, 128) * tiles(outs, 128) < 256) p.bt = 64;
-  const int64_t n = halves * tiles(rows, p.bt) * tiles(outs, p.bo), slots = large ? 256 : 512;
-  const int64_t want = std::min<int64_t>({std::max<int64_t>(slots / n, 1), std::max<int64_t>(p.stages / 4, 1), 16});
-  p.chunk = tiles(p.stages, want);
-  p.splits = (int)tiles(p.stages, p.chunk);
+ProductPlan plan_of(int64_t rows, int64_t C_in, int64_t C_out, int64_t room, int parts, int size) {
+  ProductPlan p = {};
+  const int each = kLine / size;
+  p.dx.stages = parts * 2 * room / each, p.dw.stages = parts * tiles(rows, each);
+  auto tiles_of = [&](int64_t bt, int64_t bo, int64_t &dx, int64_t &dw) {
+    dx = tiles(rows, bt) * tiles(C_in, bo), dw = 2 * tiles(C_out, bt) * tiles(C_in, bo);
+    return dx + dw;
+  };
+  int64_t dx, dw;
+  p.bt = p.bo = 128;
+  if (size == 2 && tiles_of(256, 256, dx, dw) >= 200) p.bt = p.bo = 256;
+  if (size == 4 && tiles_of(128, 128, dx, dw) < 384) p.bt = 64;
+  tiles_of(p.bt, p.bo, dx, dw);
+  const int64_t slots = p.bt == 256 ? 256 : 512, mean = std::max<int64_t>((dx * p.dx.stages + dw * p.dw.stages) / slots, 4);
+  for (ProductPlan::Part *q : {&p.dx, &p.dw}) {
+    const int64_t want = std::min<int64_t>(std::max<int64_t>((q->stages + mean / 2) / mean, 1), 32);
+    q->chunk = tiles(q->stages, want);
+    q->splits = (int)tiles(q->stages, q->chunk);
+  }
+  p.dx.bytes = p.dx.splits > 1 ? (size_t)p.dx.splits * rows * C_in * sizeof(float) : 0;
+  p.dx.bytes = (p.dx.bytes + 255) / 256 * 256;
+  p.dw.bytes = p.dw.splits > 1 ? (size_t)p.dw.splits * 2 * C_out * C_in * sizeof(float) : 0;
   return p;
 }
 
-template <class T, int BT, int BO, bool XA, bool TWO>
-void launch_product(const Result<T> &r, const Operand &x, const Operand &w, const ProductPlan &p, int halves, int64_t from, hipStream_t s) {
-  const int64_t tiles_t = halves * tiles(r.rows, BT);
-  const int tiles_o = (int)tiles(r.outs, BO);
-  const unsigned blocks = (unsigned)(tiles_t * tiles_o * p.splits);
-  if (p.splits > 1) {
-    product_gemm_kernel<T, BT, BO, XA, true, TWO><<<blocks, 256, 0, s>>>(r, x, w, tiles_t, tiles_o, p.splits, p.chunk, p.stages, from);
-    product_gemm_join_kernel<T><<<dim3((unsigned)std::min<int64_t>(tiles(r.rows * r.outs, 1024), 4096), halves), 256, 0, s>>>(r, p.splits);
-  } else {
-    product_gemm_kernel<T, BT, BO, XA, false, TWO><<<blocks, 256, 0, s>>>(r, x, w, tiles_t, tiles_o, 1, p.stages, p.stages, from);
-  }
-}
-
-// k: of all parts; from: the stage that second parts begin with
-template <class T, bool XA>
-hipError_t product(const Result<T> &r, const Operand &x, const Operand &w, int64_t k, int parts, int halves, int64_t from, hipStream_t s) {
-  const ProductPlan p = plan_of(r.rows, r.outs, k, XA ? 2 : 1, sizeof(T));  // (the same for one of the weights' gradients as for both)
-  if constexpr (sizeof(T) == 2) {
-    if (parts == 2) {
-      if (p.bt == 256) launch_product<T, 256, 256, XA, true>(r, x, w, p, halves, from, s);
-      else launch_product<T, 128, 128, XA, true>(r, x, w, p, halves, from, s);
-    } else if (p.bt == 256) {
-      launch_product<T, 256, 256, XA, false>(r, x, w, p, halves, 0, s);
-    } else {
-      launch_product<T, 128, 128, XA, false>(r, x, w, p, halves, 0, s);
-    }
-  } else {
-    if (p.bt == 64) launch_product<T, 64, 128, XA, false>(r, x, w, p, halves, 0, s);
-    else launch_product<T, 128, 128, XA, false>(r, x, w, p, halves, 0, s);
-  }
-  return hipGetLastError();
-}
-
-size_t parts_of(int64_t rows, int64_t outs, int64_t k, int halves, int size) {
-  const ProductPlan p = plan_of(rows, outs, k, halves, size);
-  return p.splits > 1 ? (size_t)p.splits * halves * rows * outs * sizeof(float) : 0;
+// The two projections: tiles of 256 x 128 outputs of both where three quarters of the compute units have one, else of 128 x 64 (fp32, few:
+// of 64 x 64); few and long ones in ranges of eight stages and more.
+struct GatePlan {
+  int bt, bo, splits;
+  int64_t stages, chunk;
+};
+GatePlan gate_plan(int64_t rows, int64_t outs, int64_t k, int size) {
+  GatePlan p = {};
+  p.stages = tiles(k, kLine / size);
+  p.bt = p.bo = 128;
+  if (size == 2 && tiles(rows, 256) * tiles(outs, 128) >= 200) p.bt = p.bo = 256;
+  if (size == 4 && tiles(rows, 128) * tiles(outs, 64) < 256) p.bt = 64;
+  const int64_t n = tiles(rows, p.bt) * tiles(outs, p.bo / 2);
+  const int64_t want = n < 128 ? std::max<int64_t>(std::min<int64_t>({384 / n, p.stages / 8, 16}), 1) : 1;
+  p.chunk = tiles(p.stages, want);
+  p.splits = (int)tiles(p.stages, p.chunk);
+  return p;
 }
 
 }  // namespace
@@ -604,77 +646,106 @@ bool gemm_takes(const void *p, int64_t ld, int64_t width, int size) {
 }
 
 template <class T>
-hipError_t gemm_gate(const Gate<T> &p, int act, bool back, const Side<T> &x, const T *w_gate, const T *w_up, int64_t ldw, int64_t k, hipStream_t s) {
+hipError_t gemm_gate(const Gate<T> &p, int act, bool back, const Side<T> &x, const T *w_gate, const T *w_up, int64_t ldw, int64_t k,
+                     float *part, hipStream_t s) {
+  const GatePlan plan = gate_plan(p.rows, p.outs, k, sizeof(T));
   Operand xo = {}, wo = {};
   xo.p[0] = reinterpret_cast<const char *>(x.p), xo.ld = x.s * sizeof(T), xo.lines = x.lines, xo.k = k;
   wo.p[0] = reinterpret_cast<const char *>(w_gate), wo.p[1] = reinterpret_cast<const char *>(w_up), wo.ld = ldw * sizeof(T);
   wo.lines = p.outs, wo.k = k;
-  return by_act(act, [&](auto a) {
+  return by_act(plan.splits > 1 ? (int)WCC_ACT_NONE : act, [&](auto a) {  // (ranges: sums as they are)
     constexpr int ACT = decltype(a)::value;
     auto go = [&](auto bt, auto bo) {
       constexpr int BT = decltype(bt)::value, BO = decltype(bo)::value;
       const int64_t tiles_t = tiles(p.rows, BT);
       const int tiles_o = (int)tiles(p.outs, BO / 2);
-      const unsigned n = (unsigned)(tiles_t * tiles_o);
-      if (back) gate_gemm_kernel<T, BT, BO, ACT, true><<<n, 256, 0, s>>>(p, xo, wo, tiles_t, tiles_o);
-      else gate_gemm_kernel<T, BT, BO, ACT, false><<<n, 256, 0, s>>>(p, xo, wo, tiles_t, tiles_o);
+      const unsigned n = (unsigned)(tiles_t * tiles_o * plan.splits);
+      if (plan.splits > 1) {
+        if constexpr (BO == 128 && ACT == WCC_ACT_NONE) gate_gemm_kernel<T, BT, BO, ACT, false, true><<<n, 256, 0, s>>>(p, xo, wo, tiles_t, tiles_o, plan.chunk, part);
+      } else if (back) {
+        gate_gemm_kernel<T, BT, BO, ACT, true, false><<<n, 256, 0, s>>>(p, xo, wo, tiles_t, tiles_o, 0, nullptr);
+      } else {
+        gate_gemm_kernel<T, BT, BO, ACT, false, false><<<n, 256, 0, s>>>(p, xo, wo, tiles_t, tiles_o, 0, nullptr);
+      }
     };
     const std::integral_constant<int, 256> L;
     const std::integral_constant<int, 128> M;
     const std::integral_constant<int, 64> S;
-    bool large = false;
     if constexpr (sizeof(T) == 2) {
-      large = tiles(p.rows, 256) * tiles(p.outs, 128) >= 200;
-      if (large) go(L, L);
-    }
-    if (!large) {
-      if (sizeof(T) == 4 && tiles(p.rows, 128) * tiles(p.outs, 64) < 256) go(S, M);  // (bf16, 777 rows 1000 -> 1537: 15.4 us, 13.4 without)
+      if (plan.bt == 256) go(L, L);
+      else go(M, M);
+    } else {
+      if (plan.bt == 64) go(S, M);
       else go(M, M);
     }
-    return hipGetLastError();
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess || plan.splits == 1 ? e : join_gate<T>(p, act, back, plan.splits, part, s);
   });
 }
 
-// k of the weights' gradients: rows, of each part in whole stages
-int64_t rows_of_parts(int64_t rows, int parts, int size) {
-  const int each = kLine / size;
-  return parts == 2 ? (rows + each - 1) / each * each * 2 : rows;
+size_t gemm_gate_parts(int64_t rows, int64_t outs, int64_t k, int size) {
+  const GatePlan p = gate_plan(rows, outs, k, size);
+  return p.splits > 1 ? (size_t)p.splits * rows * 2 * room_of(outs) * sizeof(float) : 0;
 }
-size_t gemm_dx_parts(int64_t rows, int64_t C_in, int64_t room, int parts, int size) { return parts_of(rows, C_in, parts * 2 * room, 1, size); }
-size_t gemm_dw_parts(int64_t rows, int64_t C_in, int64_t C_out, int parts, int size) {
-  return parts_of(C_out, C_in, rows_of_parts(rows, parts, size), 2, size);
-}
-
-template <class T>
-hipError_t gemm_dx(const T *d, int64_t room, int parts, int64_t rows, const T *w_gate, const T *w_up, int64_t ldw, int64_t C_in, int64_t C_out,
-                   T *dx, int64_t ld, float *part, hipStream_t s) {
-  Operand x = {}, w = {};
-  x.p[0] = reinterpret_cast<const char *>(d), x.ld = parts * 2 * room * sizeof(T), x.lines = rows, x.k = parts * 2 * room;
-  w.p[0] = reinterpret_cast<const char *>(w_gate), w.p[1] = reinterpret_cast<const char *>(w_up);
-  w.ld = ldw * sizeof(T), w.lines = ldw, w.k = C_out, w.turn = room, w.again = 2 * room;
-  const Result<T> r{{dx, nullptr}, ld, rows, C_in, 0, part};
-  return product<T, false>(r, x, w, x.k, parts, 1, 2 * room * (int64_t)sizeof(T) / kLine, s);
+size_t gemm_back_parts(int64_t rows, int64_t C_in, int64_t C_out, int parts, int size) {
+  const ProductPlan p = plan_of(rows, C_in, C_out, room_of(C_out), parts, size);
+  return p.dx.bytes + p.dw.bytes;
 }
 
 template <class T>
-hipError_t gemm_dw(const T *d, int64_t room, int parts, int64_t rows, const T *x, int64_t ldx, int64_t width, int64_t C_in, int64_t C_out,
-                   T *dw_gate, T *dw_up, float *part, hipStream_t s) {
-  Operand a = {}, b = {};
-  const int64_t k = rows_of_parts(rows, parts, sizeof(T)), never = (int64_t)1 << 60;
-  a.p[0] = reinterpret_cast<const char *>(d), a.p[1] = reinterpret_cast<const char *>(d + 2 * room);
-  a.ld = parts * 2 * room * sizeof(T), a.lines = room, a.k = rows, a.turn = k / parts, a.again = never;
-  b.p[0] = b.p[1] = reinterpret_cast<const char *>(x), b.ld = ldx * sizeof(T), b.lines = width, b.k = rows, b.turn = k / parts, b.again = never;
-  const int halves = dw_gate && dw_up ? 2 : 1;
-  if (!dw_gate) a.p[0] += room * sizeof(T), a.p[1] += room * sizeof(T);
-  const Result<T> r{{dw_gate ? dw_gate : dw_up, halves == 2 ? dw_up : nullptr}, C_in, C_out, C_in, room, part};
-  return product<T, true>(r, a, b, k, parts, halves, k / parts * (int64_t)sizeof(T) / kLine, s);
+hipError_t gemm_back(const Backward<T> &b, float *part, hipStream_t s) {
+  const int64_t size = sizeof(T), never = (int64_t)1 << 60;
+  const ProductPlan p = plan_of(b.rows, b.C_in, b.C_out, b.room, b.parts, sizeof(T));  // (whichever gradients are asked for)
+  Job<T> dx = {}, dw = {};
+  if (b.dx) {
+    Operand &x = dx.x, &w = dx.w;
+    x.p[0] = reinterpret_cast<const char *>(b.d), x.ld = b.parts * 2 * b.room * size, x.lines = b.rows, x.k = b.parts * 2 * b.room;
+    w.p[0] = reinterpret_cast<const char *>(b.w_gate), w.p[1] = reinterpret_cast<const char *>(b.w_up);
+    w.ld = b.ldw * size, w.lines = b.ldw, w.k = b.C_out, w.turn = b.room, w.again = 2 * b.room;
+    dx.r = Result<T>{{b.dx, nullptr}, b.ld, b.rows, b.C_in, 0, part};
+    dx.from = 2 * b.room * size / kLine;
+    dx.tiles_t = tiles(b.rows, p.bt), dx.tiles_o = (int)tiles(b.C_in, p.bo);
+    dx.splits = p.dx.splits, dx.chunk = p.dx.chunk, dx.stages = p.dx.stages;
+    dx.blocks = dx.tiles_t * dx.tiles_o * dx.splits;
+  }
+  if (b.dw_gate || b.dw_up) {
+    Operand &x = dw.x, &w = dw.w;
+    const int halves = b.dw_gate && b.dw_up ? 2 : 1;
+    const T *d = b.dw_gate ? b.d : b.d + b.room;
+    const int64_t turn = p.dw.stages / b.parts * (kLine / size);  // rows of a part, in whole stages
+    x.p[0] = reinterpret_cast<const char *>(d), x.p[1] = reinterpret_cast<const char *>(d + 2 * b.room);
+    x.ld = b.parts * 2 * b.room * size, x.lines = b.room, x.k = b.rows, x.turn = turn, x.again = never;
+    w.p[0] = w.p[1] = reinterpret_cast<const char *>(b.x), w.ld = b.ldx * size, w.lines = b.width, w.k = b.rows, w.turn = turn, w.again = never;
+    dw.r = Result<T>{{b.dw_gate ? b.dw_gate : b.dw_up, halves == 2 ? b.dw_up : nullptr}, b.C_in, b.C_out, b.C_in, b.room,
+                     part + p.dx.bytes / sizeof(float)};
+    dw.from = p.dw.stages / b.parts;
+    dw.tiles_t = halves * tiles(b.C_out, p.bt), dw.tiles_o = (int)tiles(b.C_in, p.bo);
+    dw.splits = p.dw.splits, dw.chunk = p.dw.chunk, dw.stages = p.dw.stages;
+    dw.blocks = dw.tiles_t * dw.tiles_o * dw.splits;
+  }
+  const unsigned n = (unsigned)(dx.blocks + dw.blocks);
+  if (n == 0) return hipSuccess;
+  if constexpr (sizeof(T) == 2) {
+    if (p.bt == 256 && b.parts == 2) product_gemm_kernel<T, 256, 256, true><<<n, 256, 0, s>>>(dx, dw);
+    else if (p.bt == 256) product_gemm_kernel<T, 256, 256, false><<<n, 256, 0, s>>>(dx, dw);
+    else if (b.parts == 2) product_gemm_kernel<T, 128, 128, true><<<n, 256, 0, s>>>(dx, dw);
+    else product_gemm_kernel<T, 128, 128, false><<<n, 256, 0, s>>>(dx, dw);
+  } else {
+    if (p.bt == 64) product_gemm_kernel<T, 64, 128, false><<<n, 256, 0, s>>>(dx, dw);
+    else product_gemm_kernel<T, 128, 128, false><<<n, 256, 0, s>>>(dx, dw);
+  }
+  const bool join_dx = dx.splits > 1, join_dw = dw.splits > 1;
+  if (join_dx || join_dw) {
+    const int64_t most = std::max(join_dx ? dx.r.rows * dx.r.outs : 0, join_dw ? dw.r.rows * dw.r.outs : 0);
+    const int first = join_dx ? 0 : 1, count = (join_dx ? 1 : 0) + (join_dw ? dw.r.out[1] ? 2 : 1 : 0);
+    product_gemm_join_kernel<T><<<dim3((unsigned)std::min<int64_t>(tiles(most, 1024), 4096), count), 256, 0, s>>>(dx, dw, first);
+  }
+  return hipGetLastError();
 }
 
 #define WCC_GEMM(T)                                                                                                                          \
-  template hipError_t gemm_gate<T>(const Gate<T> &, int, bool, const Side<T> &, const T *, const T *, int64_t, int64_t, hipStream_t);        \
-  template hipError_t gemm_dx<T>(const T *, int64_t, int, int64_t, const T *, const T *, int64_t, int64_t, int64_t, T *, int64_t, float *,   \
-                                 hipStream_t);                                                                                               \
-  template hipError_t gemm_dw<T>(const T *, int64_t, int, int64_t, const T *, int64_t, int64_t, int64_t, int64_t, T *, T *, float *, hipStream_t);
+  template hipError_t gemm_gate<T>(const Gate<T> &, int, bool, const Side<T> &, const T *, const T *, int64_t, int64_t, float *, hipStream_t); \
+  template hipError_t gemm_back<T>(const Backward<T> &, float *, hipStream_t);
 WCC_GEMM(float)
 WCC_GEMM(bf16_t)
 #undef WCC_GEMM

@@ -294,6 +294,19 @@ size_t tile_product_parts(int64_t rows, int64_t lines, int64_t k, int batches, i
 }
 
 template <class T>
+hipError_t join_gate(const Gate<T> &p, int act, bool back, int splits, const float *part, hipStream_t s) {
+  const unsigned n = (unsigned)tiles(p.rows * (p.room / 4), 256);
+  return by_act(act, [&](auto a) {
+    constexpr int ACT = decltype(a)::value;
+    if (back) gate_join_kernel<T, ACT, true><<<n, 256, 0, s>>>(p, splits, part);
+    else gate_join_kernel<T, ACT, false><<<n, 256, 0, s>>>(p, splits, part);
+    return hipGetLastError();
+  });
+}
+template hipError_t join_gate<float>(const Gate<float> &, int, bool, int, const float *, hipStream_t);
+template hipError_t join_gate<bf16_t>(const Gate<bf16_t> &, int, bool, int, const float *, hipStream_t);
+
+template <class T>
 hipError_t tile_gate(const Gate<T> &p, int act, bool back, const Side<T> &x, const T *w_gate, const T *w_up, int64_t ldw, int64_t k,
                      float *part, hipStream_t s) {
   const Grid n = grid_of(p.rows, p.outs, kTile / 2, k, 1, sizeof(T));
@@ -304,9 +317,6 @@ hipError_t tile_gate(const Gate<T> &p, int act, bool back, const Side<T> &x, con
       constexpr int ET = decltype(size)::value;
       if (n.splits > 1) {
         gate_tile_kernel<T, ET, WCC_ACT_NONE, false, true><<<blocks, 256, 0, s>>>(p, x, w_gate, w_up, ldw, k, n, part);
-        const unsigned join = (unsigned)tiles(p.rows * (p.room / 4), 256);
-        if (back) gate_join_kernel<T, ACT, true><<<join, 256, 0, s>>>(p, n.splits, part);
-        else gate_join_kernel<T, ACT, false><<<join, 256, 0, s>>>(p, n.splits, part);
       } else if (back) {
         gate_tile_kernel<T, ET, ACT, true, false><<<blocks, 256, 0, s>>>(p, x, w_gate, w_up, ldw, k, n, part);
       } else {
@@ -315,7 +325,8 @@ hipError_t tile_gate(const Gate<T> &p, int act, bool back, const Side<T> &x, con
     };
     if (n.et == 1) go(std::integral_constant<int, 1>());
     else go(std::integral_constant<int, 2>());
-    return hipGetLastError();
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess || n.splits == 1 ? e : join_gate<T>(p, act, back, n.splits, part, s);
   });
 }
 
