@@ -131,19 +131,29 @@ __device__ __forceinline__ void act_of(float z, float &v, float &s) {
 }
 
 // ---- rows by vectors -----------------------------------------------------------------------------------
-// 16 bytes of a row of which `left` elements are there, the rest 0
+// 16 bytes of a row of which `left` elements are there, the rest 0; cut ones in pieces of 8, 4 and 2 bytes
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32x1_any __attribute__((aligned(2)));
 template <class T>
 __device__ __forceinline__ u32x4 load_part(const T *p, int left) {
   constexpr int VE = VecOf<T>::N;
   if (left >= VE) return *reinterpret_cast<const u32x4_any *>(p);
   u32x4 v = {};
-#pragma unroll
-  for (int j = 0; j < VE - 1; ++j)
-    if (j < left) {
-      const uint32_t b = bits_of(p[j]);
-      if constexpr (sizeof(T) == 4) v[j] = b;
-      else v[j >> 1] |= b << (16 * (j & 1));
-    }
+  if (left <= 0) return v;
+  const char *at = reinterpret_cast<const char *>(p);
+  const int bytes = left * (int)sizeof(T);
+  uint32_t four = 0, two = 0;
+  if (bytes & 8) {
+    const u32x2_any q = *reinterpret_cast<const u32x2_any *>(at);
+    v[0] = q[0], v[1] = q[1];
+  }
+  if (bytes & 4) four = *reinterpret_cast<const u32x1_any *>(at + (bytes & 8));
+  if constexpr (sizeof(T) == 2) {
+    if (bytes & 2) two = *reinterpret_cast<const uint16_t *>(at + (bytes & 12));
+  }
+  const uint32_t next = bytes & 4 ? four : two, last = bytes & 4 ? two : 0;
+  if (bytes & 8) v[2] = next, v[3] = last;
+  else v[0] = next, v[1] = last;
   return v;
 }
 template <class T>
@@ -153,12 +163,15 @@ __device__ __forceinline__ void store_part(T *p, int left, const u32x4 &v) {
     *reinterpret_cast<u32x4_any *>(p) = v;
     return;
   }
-#pragma unroll
-  for (int j = 0; j < VE - 1; ++j)
-    if (j < left) {
-      if constexpr (sizeof(T) == 4) p[j] = __uint_as_float(v[j]);
-      else p[j] = (bf16_t)(v[j >> 1] >> (16 * (j & 1)));
-    }
+  if (left <= 0) return;
+  char *at = reinterpret_cast<char *>(p);
+  const int bytes = left * (int)sizeof(T);
+  if (bytes & 8) *reinterpret_cast<u32x2_any *>(at) = u32x2_any{v[0], v[1]};
+  const uint32_t next = bytes & 8 ? v[2] : v[0], last = bytes & 8 ? v[3] : v[1];
+  if (bytes & 4) *reinterpret_cast<u32x1_any *>(at + (bytes & 8)) = next;
+  if constexpr (sizeof(T) == 2) {
+    if (bytes & 2) *reinterpret_cast<uint16_t *>(at + (bytes & 12)) = (uint16_t)(bytes & 4 ? last : next);
+  }
 }
 // the largest magnitude of a vector, as bits
 template <class T>

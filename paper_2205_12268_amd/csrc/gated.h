@@ -64,8 +64,7 @@ __device__ __forceinline__ void finish(const Gate<T> &p, int64_t t, int o, float
       if constexpr (sizeof(T) == 4) {
         *reinterpret_cast<f32x4_any *>(out) = f32x4_any{f[0], f[1], f[2], f[3]};
       } else {
-        typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
-        *reinterpret_cast<u32x2_any *>(out) = u32x2_any{(uint32_t)narrow<bf16_t>(f[0]) | (uint32_t)narrow<bf16_t>(f[1]) << 16,
+          *reinterpret_cast<u32x2_any *>(out) = u32x2_any{(uint32_t)narrow<bf16_t>(f[0]) | (uint32_t)narrow<bf16_t>(f[1]) << 16,
                                                         (uint32_t)narrow<bf16_t>(f[2]) | (uint32_t)narrow<bf16_t>(f[3]) << 16};
       }
     } else {

@@ -84,8 +84,8 @@ struct Plan {
 
 constexpr int kThin = 64;  // rows of few
 
-// Tiles fed straight from memory from 2^28 products on (fp32: 2^22); bf16 rows or weights that 16-byte loads do not take are copied for it
-// from 2^30 on, fp32 ones go by way of registers.
+// Tiles fed straight from memory from 2^25 products on (fp32: any); bf16 rows or weights that 16-byte loads do not take are copied for it
+// from 2^27 on, fp32 ones go by way of registers.
 Plan plan_of(const wcc_gated_desc &g, bool backward) {
   Plan p = {};
   const int size = g.dtype == WCC_F32 ? 4 : 2;
@@ -93,7 +93,7 @@ Plan plan_of(const wcc_gated_desc &g, bool backward) {
   p.room = room_of(g.C_out), p.ldx = room_of(g.C_in), p.k = (g.C_in + 7) / 8 * 8;
   const int each = 16 / size;
   p.copy_w = g.C_in % each != 0, p.copy_x = p.copy_w || g.ldx % each != 0;
-  p.gemm = size == 2 ? g.rows > kThin && products >= (p.copy_x ? 1 << 30 : 1 << 28) : !p.copy_x && products >= 1 << 22;
+  p.gemm = size == 2 ? g.rows > kThin && products >= (p.copy_x ? 1 << 27 : 1 << 25) : !p.copy_x;
   if (size == 4) p.copy_x = p.copy_w = false, p.k = g.C_in;
   p.parts = size == 2 && g.rows * (int64_t)g.C_out < kFew ? 2 : 1;
   // (few rows, whose products are bound by the weights and their gradients: any that 16-byte loads take)

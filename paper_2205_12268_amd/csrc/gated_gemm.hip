@@ -368,8 +368,7 @@ __global__ __launch_bounds__(256, BO == 128 ? 2 : 1) void gate_gemm_kernel(Gate<
           uint2 top = {0, 0};
           if (t < p.rows && at < p.outs) {
             const bf16_t *q = p.dy + t * p.ldy + at;
-            typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
-            if (at + 4 <= p.outs) {
+                  if (at + 4 <= p.outs) {
               const u32x2_any v = *reinterpret_cast<const u32x2_any *>(q);
               top = uint2{v.x, v.y};
             } else {
@@ -584,7 +583,7 @@ hipError_t by_act(int act, F f) {
 }
 
 // How the products of a backward pass are cut.  dx: rows x C_in over 2 room; the weights' gradients, both: 2 C_out x C_in over the rows.
-// Each workgroup has about as many stages as there are for every place (256, or 512 of the smaller tiles), four at least.
+// Each workgroup has about as many stages as there are for every place (256, or 512 of the smaller tiles).
 struct ProductPlan {
   int bt, bo;
   struct Part {
@@ -603,22 +602,34 @@ ProductPlan plan_of(int64_t rows, int64_t C_in, int64_t C_out, int64_t room, int
   };
   int64_t dx, dw;
   p.bt = p.bo = 128;
-  if (size == 2 && tiles_of(256, 256, dx, dw) >= 200) p.bt = p.bo = 256;
+  // (the larger ones where three quarters of the compute units have one, and four fifths of them lie within the results)
+  if (size == 2 && tiles_of(256, 256, dx, dw) >= 200 && 5 * C_in * (rows + 2 * C_out) >= 4 * 65536 * (dx + dw)) p.bt = p.bo = 256;
   if (size == 4 && tiles_of(128, 128, dx, dw) < 384) p.bt = 64;
   tiles_of(p.bt, p.bo, dx, dw);
-  const int64_t slots = p.bt == 256 ? 256 : 512, mean = std::max<int64_t>((dx * p.dx.stages + dw * p.dw.stages) / slots, 4);
-  for (ProductPlan::Part *q : {&p.dx, &p.dw}) {
-    const int64_t want = std::min<int64_t>(std::max<int64_t>((q->stages + mean / 2) / mean, 1), 32);
-    q->chunk = tiles(q->stages, want);
-    q->splits = (int)tiles(q->stages, q->chunk);
+  // Ranges for the shortest time by a rough count: a workgroup takes its stages and as much as four for its beginning and end; more of them
+  // than there are places wait.
+  const int64_t slots = p.bt == 256 ? 256 : 512, mean = std::max<int64_t>(tiles(dx * p.dx.stages + dw * p.dw.stages, slots), 4);
+  int64_t best = 0;
+  for (int i = 0; i < 16; ++i) {
+    const int64_t has = mean + i * mean / 8;
+    auto cut = [&](int64_t stages) { return std::min<int64_t>(std::max<int64_t>((stages + has / 2) / has, 1), 64); };
+    const int64_t n = cut(p.dx.stages), m = cut(p.dw.stages), blocks = dx * n + dw * m;
+    const int64_t a = tiles(p.dx.stages, n) + 4, b = tiles(p.dw.stages, m) + 4;
+    const int64_t time = blocks <= slots ? std::max(a, b) : std::max(std::max(a, b), (dx * n * a + dw * m * b) / slots + std::min(a, b));
+    if (best == 0 || time < best) {
+      best = time;
+      p.dx.chunk = tiles(p.dx.stages, n), p.dw.chunk = tiles(p.dw.stages, m);
+    }
   }
+  p.dx.splits = (int)tiles(p.dx.stages, p.dx.chunk), p.dw.splits = (int)tiles(p.dw.stages, p.dw.chunk);
   p.dx.bytes = p.dx.splits > 1 ? (size_t)p.dx.splits * rows * C_in * sizeof(float) : 0;
   p.dx.bytes = (p.dx.bytes + 255) / 256 * 256;
   p.dw.bytes = p.dw.splits > 1 ? (size_t)p.dw.splits * 2 * C_out * C_in * sizeof(float) : 0;
   return p;
 }
 
-// The two projections: tiles of 256 x 128 outputs of both where three quarters of the compute units have one, else of 128 x 64 (fp32, few:
+// The two projections: tiles of 256 x 128 outputs of both where three quarters of the compute units have one and
+// their end is not most of the work, else of 128 x 64 (fp32, few:
 // of 64 x 64); few and long ones in ranges of eight stages and more.
 struct GatePlan {
   int bt, bo, splits;
@@ -628,7 +639,7 @@ GatePlan gate_plan(int64_t rows, int64_t outs, int64_t k, int size) {
   GatePlan p = {};
   p.stages = tiles(k, kLine / size);
   p.bt = p.bo = 128;
-  if (size == 2 && tiles(rows, 256) * tiles(outs, 128) >= 200) p.bt = p.bo = 256;
+  if (size == 2 && p.stages >= 12 && tiles(rows, 256) * tiles(outs, 128) >= 200) p.bt = p.bo = 256;
   if (size == 4 && tiles(rows, 128) * tiles(outs, 64) < 256) p.bt = 64;
   const int64_t n = tiles(rows, p.bt) * tiles(outs, p.bo / 2);
   const int64_t want = n < 128 ? std::max<int64_t>(std::min<int64_t>({384 / n, p.stages / 8, 16}), 1) : 1;

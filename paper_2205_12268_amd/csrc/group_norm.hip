@@ -46,6 +46,58 @@ __device__ __forceinline__ float2 stat_of(const double2 &s, double per, float ep
   return float2{(float)mean, (float)r};
 }
 
+// The groups of neighbouring channels from c on, by one division.
+struct GroupOf {
+  int g, r, per;
+  __device__ __forceinline__ GroupOf(int c, int per_) : g(c / per_), r(c - g * per_), per(per_) {}
+  __device__ __forceinline__ int next() {  // of this channel; on to the next one
+    const int now = g;
+    if (++r == per) r = 0, ++g;
+    return now;
+  }
+};
+
+// A thread's vector of channels in a row: `left` of them from c0 on, the rest 0.  Loads have no branch between them, or they would wait for each
+// other (7 us for one small map): all are whole, in the row's last vector from where it ends backwards, and are moved and cut where they are
+// used.  Rows narrower than a vector are read in pieces.
+template <class T>
+struct Columns {
+  static constexpr int VE = VecOf<T>::N;
+  int off, back, left;
+  uint32_t mask[4];
+  bool cut, narrow;  // (the same for all threads)
+  __device__ __forceinline__ Columns(int c0, int left_, int C, bool cut_) : left(max(left_, 0)), cut(cut_), narrow(C < VE) {
+    off = narrow ? (left > 0 ? c0 : 0) : min(c0, C - VE);
+    back = left > 0 ? c0 - off : 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(T) == 4) mask[i] = i < left ? ~0u : 0u;
+      else mask[i] = 2 * i + 1 < left ? ~0u : 2 * i < left ? 0xffffu : 0u;
+    }
+  }
+  // row(i): the row of vector i, which is there
+  template <int N, class F>
+  __device__ __forceinline__ void load(u32x4 (&v)[N], F row) const {
+    if (!narrow) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = *reinterpret_cast<const u32x4_any *>(row(i) + off);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = load_part<T>(row(i) + off, left);
+    }
+  }
+  __device__ __forceinline__ u32x4 fix(u32x4 v) const {
+    if (!cut || narrow) return v;
+    const int words = sizeof(T) == 4 ? back : back >> 1;
+    if (words & 2) v = u32x4{v[2], v[3], 0, 0};
+    if (words & 1) v = u32x4{v[1], v[2], v[3], 0};
+    if constexpr (sizeof(T) == 2) {
+      if (back & 1) v = u32x4{v[0] >> 16 | v[1] << 16, v[1] >> 16 | v[2] << 16, v[2] >> 16 | v[3] << 16, v[3] >> 16};
+    }
+    return u32x4{v[0] & mask[0], v[1] & mask[1], v[2] & mask[2], v[3] & mask[3]};
+  }
+};
+
 // The input of the backward pass: x itself, or what it is kept as.
 template <class T, bool KEPT>
 struct Input {
@@ -59,21 +111,33 @@ struct Input {
     uint2 c;
     uint32_t step;
   };
-  __device__ __forceinline__ Raw load(int64_t row, int e, int left) const {
-    Raw r = {};
+  // vectors of rows row(i), which are there
+  template <int N, class F>
+  __device__ __forceinline__ void load(Raw (&r)[N], const Columns<T> &cols, int c0, F row) const {
     if constexpr (KEPT) {
-      const int8_t *p = codes + row * blocks * kKept + e;
-      if constexpr (sizeof(T) == 4) r.c.x = *reinterpret_cast<const uint32_t *>(p);
-      else r.c = *reinterpret_cast<const uint2 *>(p);
-      r.step = steps[row * blocks + e / kKept];
+      const int e = min(c0, blocks * kKept - VecOf<T>::N);  // (threads past the row's end)
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int8_t *p = codes + row(i) * blocks * kKept + e;
+        if constexpr (sizeof(T) == 4) r[i].c.x = *reinterpret_cast<const uint32_t *>(p);
+        else r[i].c = *reinterpret_cast<const uint2 *>(p);
+        r[i].step = steps[row(i) * blocks + e / kKept];
+      }
     } else {
-      r.v = load_part<T>(x + row * ld + e, left);
+      u32x4 v[N];
+      cols.load(v, [&](int i) { return x + row(i) * ld; });
+#pragma unroll
+      for (int i = 0; i < N; ++i) r[i].v = v[i];
     }
+  }
+  __device__ __forceinline__ static Raw fix(Raw r, const Columns<T> &cols) {
+    if constexpr (!KEPT) r.v = cols.fix(r.v);
     return r;
   }
-  __device__ __forceinline__ static float at(const Raw &r, int j, float step) {
-    if constexpr (KEPT) return kept_value(j < 4 ? r.c.x : r.c.y, j & 3, step);
-    else return elem<T>(r.v, j);
+  // element j without the mean
+  __device__ __forceinline__ static float at(const Raw &r, int j, float step, float mean) {
+    if constexpr (KEPT) return fmaf((float)(int8_t)((j < 4 ? r.c.x : r.c.y) >> (8 * (j & 3))), step, -mean);
+    else return elem<T>(r.v, j) - mean;
   }
   __device__ __forceinline__ static float step(const Raw &r) { return KEPT ? step_value(r.step) : 0.f; }
 };
@@ -160,18 +224,21 @@ __global__ __launch_bounds__(256) void norm_sums_kernel(const T *__restrict__ x,
   const Place<VE> at(blockIdx.x, d, s, counts, lanes);
   double sum[VE] = {}, sq[VE] = {};
   if (at.ty < at.rows && at.c0 < d.C) {
-    const T *p = x + (int64_t)at.sample * d.pixels * d.ldx + at.c0;
+    const T *p = x + (int64_t)at.sample * d.pixels * d.ldx;
+    const Columns<T> cols(at.c0, d.C - at.c0, d.C, d.C % VE != 0);
     for (int64_t t = at.begin; t < at.end; t += 4 * at.rows) {
       u32x4 v[4];
+      cols.load(v, [&](int u) { return p + min(t + u * at.rows, at.end - 1) * d.ldx; });
 #pragma unroll
-      for (int u = 0; u < 4; ++u) v[u] = t + u * at.rows < at.end ? load_part<T>(p + (t + u * at.rows) * d.ldx, d.C - at.c0) : u32x4{};
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
+      for (int u = 0; u < 4; ++u) {
+        if (t + u * at.rows >= at.end) break;
+        v[u] = cols.fix(v[u]);
 #pragma unroll
         for (int j = 0; j < VE; ++j) {
           const double f = elem<T>(v[u], j);
           sum[j] += f, sq[j] = fma(f, f, sq[j]);
         }
+      }
     }
   }
   leave_sums<VE>(d, s, at, lanes, sum, sq, room);
@@ -286,24 +353,25 @@ __global__ __launch_bounds__(256) void norm_apply_kernel(const T *x, const float
   if (at.ty >= at.rows || c0 >= (KEEP ? blocks * kKept : d.C)) return;
   float g[VE], b[VE], mean[VE];
   affine<VE>(gamma, beta, c0, d.C, g, b);
+  GroupOf of(c0, d.per);
 #pragma unroll
   for (int j = 0; j < VE; ++j) {
-    const int group = min(c0 + j, d.C - 1) / d.per;
+    const int group = min(of.next(), d.groups - 1);
     float4 q;
     if constexpr (SHORT) q = room.group[group];
     else q = s.group[(int64_t)at.sample * d.groups + group];
     mean[j] = q.x, g[j] *= q.y;
   }
   const int64_t row0 = (int64_t)at.sample * d.pixels;
+  const Columns<T> cols(c0, d.C - c0, d.C, d.C % (KEEP ? kKept : VE) != 0);
   for (int64_t t = at.begin; t < at.end; t += 4 * at.rows) {
     u32x4 v[4];
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-      v[u] = t + u * at.rows < at.end ? load_part<T>(x + (row0 + t + u * at.rows) * d.ldx + c0, d.C - c0) : u32x4{};
+    cols.load(v, [&](int u) { return x + (row0 + min(t + u * at.rows, at.end - 1)) * d.ldx; });
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int64_t row = row0 + t + u * at.rows;
       if (t + u * at.rows >= at.end) break;
+      v[u] = cols.fix(v[u]);
       if constexpr (KEEP) {  // (the lanes of a block have the same pixels)
         const uint32_t step = step_of(top_of_block<T>(v[u]));
         store_codes<T>(codes + row * blocks * kKept + c0, v[u], per_step(step));
@@ -333,38 +401,40 @@ __global__ __launch_bounds__(256) void norm_grad_sums_kernel(Input<T, KEPT> in, 
   if (at.ty < at.rows && c0 < d.C) {
     float g[VE], b[VE], mean[VE], rstd[VE];
     affine<VE>(gamma, beta, c0, d.C, g, b);
+    GroupOf of(c0, d.per);
 #pragma unroll
     for (int j = 0; j < VE; ++j) {
-      const int64_t q = 2 * ((int64_t)at.sample * d.groups + min(c0 + j, d.C - 1) / d.per);
-      mean[j] = stats[q], rstd[j] = stats[q + 1];
+      const int64_t q = 2 * ((int64_t)at.sample * d.groups + min(of.next(), d.groups - 1));
+      mean[j] = stats[q], rstd[j] = stats[q + 1], g[j] *= rstd[j];
     }
     const int64_t row0 = (int64_t)at.sample * d.pixels;
+    const Columns<T> cols(c0, d.C - c0, d.C, d.C % VE != 0);
     for (int64_t t = at.begin; t < at.end; t += 4 * at.rows) {
       u32x4 w[4];
       typename Input<T, KEPT>::Raw v[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int64_t row = row0 + (t + u * at.rows < at.end ? t + u * at.rows : t);
-        v[u] = in.load(row, c0, d.C - c0);
-        w[u] = load_part<T>(dy + row * d.ldy + c0, d.C - c0);
-      }
+      auto row = [&](int u) { return row0 + min(t + u * at.rows, at.end - 1); };
+      in.load(v, cols, c0, row);
+      cols.load(w, [&](int u) { return dy + row(u) * d.ldy; });
       float s4[VE] = {}, d4[VE] = {};  // (four at a time in fp32)
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         if (t + u * at.rows >= at.end) break;
+        v[u] = in.fix(v[u], cols), w[u] = cols.fix(w[u]);
         const float step = in.step(v[u]);
 #pragma unroll
         for (int j = 0; j < VE; ++j) {
-          const float xh = (in.at(v[u], j, step) - mean[j]) * rstd[j];
+          const float x = in.at(v[u], j, step, mean[j]);
           float value, slope;
-          act_of<T, ACT>(fmaf(xh, g[j], b[j]), value, slope);
+          act_of<T, ACT>(fmaf(x, g[j], b[j]), value, slope);
           const float dz = elem<T>(w[u], j) * slope;
-          s4[j] += dz, d4[j] = fmaf(dz, xh, d4[j]);
+          s4[j] += dz, d4[j] = fmaf(dz, x, d4[j]);
         }
       }
 #pragma unroll
       for (int j = 0; j < VE; ++j) sum[j] += s4[j], dot[j] += d4[j];
     }
+#pragma unroll
+    for (int j = 0; j < VE; ++j) dot[j] *= rstd[j];
   }
   leave_sums<VE>(d, s, at, lanes, sum, dot, room);
 }
@@ -409,33 +479,34 @@ __global__ __launch_bounds__(256) void norm_grad_apply_kernel(Input<T, KEPT> in,
   float g[VE], b[VE];
   float4 q[VE];
   affine<VE>(gamma, beta, c0, d.C, g, b);
+  GroupOf of(c0, d.per);
 #pragma unroll
   for (int j = 0; j < VE; ++j) {
-    const int group = min(c0 + j, d.C - 1) / d.per;
+    const int group = min(of.next(), d.groups - 1);
     if constexpr (SHORT) q[j] = room.group[group];
     else q[j] = s.group[(int64_t)at.sample * d.groups + group];
+    g[j] *= q[j].y, q[j].z *= q[j].y, q[j].w *= q[j].y * q[j].y;  // dx = gamma rstd dz - rstd m1 - (x - mean) rstd^2 m2
   }
   const int64_t row0 = (int64_t)at.sample * d.pixels;
+  const Columns<T> cols(c0, d.C - c0, d.C, d.C % VE != 0);
   for (int64_t t = at.begin; t < at.end; t += 4 * at.rows) {
     u32x4 w[4];
     typename Input<T, KEPT>::Raw v[4];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int64_t row = row0 + (t + u * at.rows < at.end ? t + u * at.rows : t);
-      v[u] = in.load(row, c0, d.C - c0);
-      w[u] = load_part<T>(dy + row * d.ldy + c0, d.C - c0);
-    }
+    auto row = [&](int u) { return row0 + min(t + u * at.rows, at.end - 1); };
+    in.load(v, cols, c0, row);
+    cols.load(w, [&](int u) { return dy + row(u) * d.ldy; });
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       if (t + u * at.rows >= at.end) break;
+      v[u] = in.fix(v[u], cols), w[u] = cols.fix(w[u]);
       const float step = in.step(v[u]);
       float f[VE];
 #pragma unroll
       for (int j = 0; j < VE; ++j) {
-        const float xh = (in.at(v[u], j, step) - q[j].x) * q[j].y;
+        const float x = in.at(v[u], j, step, q[j].x);
         float value, slope;
-        act_of<T, ACT>(fmaf(xh, g[j], b[j]), value, slope);
-        f[j] = q[j].y * ((elem<T>(w[u], j) * slope) * g[j] - q[j].z - xh * q[j].w);
+        act_of<T, ACT>(fmaf(x, g[j], b[j]), value, slope);
+        f[j] = fmaf(elem<T>(w[u], j) * slope, g[j], -fmaf(x, q[j].w, q[j].z));
       }
       store_part<T>(dx + (row0 + t + u * at.rows) * d.ldx + c0, d.C - c0, pack<T>(f));
     }
@@ -444,10 +515,10 @@ __global__ __launch_bounds__(256) void norm_grad_apply_kernel(Input<T, KEPT> in,
 
 // ---- maps that a workgroup's registers hold: one launch --------------------------------------------------------
 // A workgroup has a sample's pixels of `take` neighbouring groups; `lanes` threads side by side hold vectors of their channels (from the
-// first group's on, at any element), kHeld vectors a thread at most.
-constexpr int kThreads = 512, kHeld = 8, kWidest = 512;  // kWidest: channels of a workgroup
+// first group's on, at any element), kHeld vectors a thread at most.  NT: its threads, and the channels it has at most.
+constexpr int kHeld = 8;  // (or 2, where they suffice: a quarter of the instructions to fetch)
 
-template <class T>
+template <class T, int NT>
 struct HeldPlace {
   static constexpr int VE = VecOf<T>::N;
   int sample, first, groups, width, lanes, rows, col, ty, c0, left;  // first: group; c0: channel; left: channels of the workgroup from it on
@@ -456,7 +527,7 @@ struct HeldPlace {
     const int tiles = (d.groups + take - 1) / take;
     sample = blockIdx.x / tiles, first = blockIdx.x % tiles * take;
     groups = min(take, d.groups - first), width = groups * d.per;
-    rows = kThreads / lanes;
+    rows = NT / lanes;
     col = threadIdx.x % lanes, ty = threadIdx.x / lanes;
     c0 = first * d.per + col * VE, left = ty < rows ? width - col * VE : 0;
     n = pixels_of(counts, d.pixels, sample);
@@ -464,21 +535,23 @@ struct HeldPlace {
   }
   __device__ __forceinline__ bool there(int i) const { return left > 0 && ty + (int64_t)i * rows < n; }
   __device__ __forceinline__ int64_t row(int i) const { return row0 + ty + (int64_t)i * rows; }
+  __device__ __forceinline__ int64_t some_row(int i) const { return row0 + min(ty + (int64_t)i * rows, n - 1); }  // (one that is there)
+  __device__ __forceinline__ Columns<T> columns(const Shape &d) const { return Columns<T>(c0, left, d.C, width % (lanes * VE) != 0 || NT % lanes != 0); }
 };
 
 // The threads' pairs of sums by channel joined: the sum of each channel goes to f, the groups' to `all`; w(c): what a channel counts in
 // its group.  Columns first, in as many parts as there are threads, then the groups.
-template <class T, class F, class W>
-__device__ __forceinline__ void join_held(const HeldPlace<T> &at, int per, const double (&a)[VecOf<T>::N], const double (&b)[VecOf<T>::N],
-                                          Room<kThreads, VecOf<T>::N> &room, double2 *col_room, double2 *all, F f, W w) {
+template <class T, int NT, class F, class W>
+__device__ __forceinline__ void join_held(const HeldPlace<T, NT> &at, int per, const double (&a)[VecOf<T>::N], const double (&b)[VecOf<T>::N],
+                                          Room<NT, VecOf<T>::N> &room, double2 *col_room, double2 *all, F f, W w) {
   const int tid = threadIdx.x;
   room.put(a, b);
   __syncthreads();
-  const int parts = max(kThreads / at.width, 1);
-  for (int i = tid; i < parts * at.width; i += kThreads) {
+  const int parts = max(min(NT / at.width, at.rows / 8), 1);  // (of eight rows and more: one thread adds up the parts of a channel)
+  for (int i = tid; i < parts * at.width; i += NT) {
     const int c = i % at.width;
     double2 v = {0.0, 0.0};
-#pragma unroll 4
+#pragma unroll 8
     for (int r = i / at.width; r < at.rows; r += parts) {
       const double2 q = room.at(r * at.lanes, c);
       v.x += q.x, v.y += q.y;
@@ -486,12 +559,13 @@ __device__ __forceinline__ void join_held(const HeldPlace<T> &at, int per, const
     col_room[i] = v;
   }
   __syncthreads();
-  for (int c = tid; c < at.width; c += kThreads) {
+  for (int c = tid; c < at.width; c += NT) {
     double2 v = col_room[c];
+#pragma unroll 4
     for (int p = 1; p < parts; ++p) v.x += col_room[p * at.width + c].x, v.y += col_room[p * at.width + c].y;
     f(c, v);
   }
-  by_group<kThreads>(at.groups, parts * per, all, [&](int g, int i) {
+  by_group<NT>(at.groups, parts * per, all, [&](int g, int i) {
     const int c = g * per + i % per;
     const double2 q = col_room[i / per * at.width + c];
     const double weight = w(c);
@@ -500,32 +574,34 @@ __device__ __forceinline__ void join_held(const HeldPlace<T> &at, int per, const
   __syncthreads();
 }
 
-template <class T, int ACT, bool KEEP>
-__global__ __launch_bounds__(kThreads) void norm_held_kernel(const T *x, const float *__restrict__ gamma, const float *__restrict__ beta,
+template <class T, int NT, int HELD, int ACT, bool KEEP>
+__global__ __launch_bounds__(NT) void norm_held_kernel(const T *x, const float *__restrict__ gamma, const float *__restrict__ beta,
                                                              const int32_t *__restrict__ counts, Shape d, int take, int lanes, T *y,
                                                              float *__restrict__ stats, int8_t *__restrict__ codes,
                                                              uint8_t *__restrict__ steps) {
   constexpr int VE = VecOf<T>::N;
-  __shared__ Room<kThreads, VE> room;
-  __shared__ double2 col_room[kWidest], all[kWidest];
-  const HeldPlace<T> at(d, counts, take, lanes);
-  u32x4 v[kHeld];
+  __shared__ Room<NT, VE> room;
+  __shared__ double2 col_room[NT], all[NT];
+  const HeldPlace<T, NT> at(d, counts, take, lanes);
+  u32x4 v[HELD];
+  const Columns<T> cols = at.columns(d);
+  if (at.n > 0) cols.load(v, [&](int i) { return x + at.some_row(i) * d.ldx; });
 #pragma unroll
-  for (int i = 0; i < kHeld; ++i) v[i] = at.there(i) ? load_part<T>(x + at.row(i) * d.ldx + at.c0, at.left) : u32x4{};
+  for (int i = 0; i < HELD; ++i) v[i] = at.there(i) ? cols.fix(v[i]) : u32x4{};
   float g[VE], b[VE], mean[VE];
   affine<VE>(gamma, beta, at.c0, d.C, g, b);
   const double per = 1.0 / (double)max(at.n * d.per, (int64_t)1);
   double sum[VE] = {}, sq[VE] = {};
 #pragma unroll
-  for (int i = 0; i < kHeld; ++i)
+  for (int i = 0; i < HELD; ++i)
 #pragma unroll
     for (int j = 0; j < VE; ++j) {
       const double f = elem<T>(v[i], j);
       sum[j] += f, sq[j] = fma(f, f, sq[j]);
     }
-  join_held<T>(at, d.per, sum, sq, room, col_room, all, [](int, double2) {}, [](int) { return 1.0; });
+  join_held<T, NT>(at, d.per, sum, sq, room, col_room, all, [](int, double2) {}, [](int) { return 1.0; });
   float2 *stat_room = reinterpret_cast<float2 *>(col_room);  // (read by nobody any more)
-  for (int g = threadIdx.x; g < at.groups; g += kThreads) {
+  for (int g = threadIdx.x; g < at.groups; g += NT) {
     const float2 q = stat_of(all[g], per, d.eps);
     stat_room[g] = q;
     if (stats) {
@@ -537,13 +613,14 @@ __global__ __launch_bounds__(kThreads) void norm_held_kernel(const T *x, const f
   const int blocks = (d.C + kKept - 1) / kKept;
   const bool mine = KEEP ? at.ty < at.rows && at.c0 < blocks * kKept : at.left > 0;
   if (!mine) return;
+  GroupOf of(at.col * VE, d.per);
 #pragma unroll
   for (int j = 0; j < VE; ++j) {
-    const float2 q = stat_room[min(at.col * VE + j, at.width - 1) / d.per];
+    const float2 q = stat_room[min(of.next(), at.groups - 1)];
     mean[j] = q.x, g[j] *= q.y;
   }
 #pragma unroll
-  for (int i = 0; i < kHeld; ++i) {
+  for (int i = 0; i < HELD; ++i) {
     if (at.ty + (int64_t)i * at.rows >= at.n) break;
     const int64_t row = at.row(i);
     if constexpr (KEEP) {  // (the lanes of a block have the same pixels)
@@ -561,53 +638,59 @@ __global__ __launch_bounds__(kThreads) void norm_held_kernel(const T *x, const f
   }
 }
 
-template <class T, int ACT, bool KEPT>
-__global__ __launch_bounds__(kThreads) void norm_grad_held_kernel(Input<T, KEPT> in, const T *dy, const float *__restrict__ gamma,
+template <class T, int NT, int HELD, int ACT, bool KEPT>
+__global__ __launch_bounds__(NT) void norm_grad_held_kernel(Input<T, KEPT> in, const T *dy, const float *__restrict__ gamma,
                                                                   const float *__restrict__ beta, const float *__restrict__ stats,
                                                                   const int32_t *__restrict__ counts, Shape d, double2 *__restrict__ chan,
                                                                   int take, int lanes, T *dx, float *__restrict__ dgamma,
                                                                   float *__restrict__ dbeta) {
   constexpr int VE = VecOf<T>::N;
-  __shared__ Room<kThreads, VE> room;
-  __shared__ double2 col_room[kWidest], all[kWidest];
-  const HeldPlace<T> at(d, counts, take, lanes);
-  typename Input<T, KEPT>::Raw v[kHeld];
-  u32x4 w[kHeld];
+  __shared__ Room<NT, VE> room;
+  __shared__ double2 col_room[NT], all[NT];
+  const HeldPlace<T, NT> at(d, counts, take, lanes);
+  typename Input<T, KEPT>::Raw v[HELD];
+  u32x4 w[HELD];
+  const Columns<T> cols = at.columns(d);
+  if (at.n > 0) {
+    auto row = [&](int i) { return at.some_row(i); };
+    in.load(v, cols, at.c0, row);
+    cols.load(w, [&](int i) { return dy + row(i) * d.ldy; });
 #pragma unroll
-  for (int i = 0; i < kHeld; ++i) {
-    v[i] = {}, w[i] = u32x4{};
-    if (at.there(i)) v[i] = in.load(at.row(i), at.c0, at.left), w[i] = load_part<T>(dy + at.row(i) * d.ldy + at.c0, at.left);
+    for (int i = 0; i < HELD; ++i) v[i] = in.fix(v[i], cols), w[i] = cols.fix(w[i]);
   }
   float g[VE], b[VE], mean[VE], rstd[VE];
   affine<VE>(gamma, beta, at.c0, d.C, g, b);
+  GroupOf of(at.col * VE, d.per), of_sums = of;
 #pragma unroll
   for (int j = 0; j < VE; ++j) {
-    const int64_t q = 2 * ((int64_t)at.sample * d.groups + at.first + min(at.col * VE + j, at.width - 1) / d.per);
-    mean[j] = stats[q], rstd[j] = stats[q + 1];
+    const int64_t q = 2 * ((int64_t)at.sample * d.groups + at.first + min(of.next(), at.groups - 1));
+    mean[j] = stats[q], rstd[j] = stats[q + 1], g[j] *= rstd[j];
   }
   const double per = 1.0 / (double)max(at.n * d.per, (int64_t)1);
   double sum[VE] = {}, dot[VE] = {};
 #pragma unroll
-  for (int i0 = 0; i0 < kHeld; i0 += 4) {
+  for (int i0 = 0; i0 < HELD; i0 += 4) {
     float s4[VE] = {}, d4[VE] = {};  // (four at a time in fp32)
 #pragma unroll
-    for (int i = i0; i < i0 + 4; ++i) {
+    for (int i = i0; i < min(i0 + 4, HELD); ++i) {
       if (!at.there(i)) break;
       const float step = in.step(v[i]);
 #pragma unroll
       for (int j = 0; j < VE; ++j) {
-        const float xh = (in.at(v[i], j, step) - mean[j]) * rstd[j];
+        const float x = in.at(v[i], j, step, mean[j]);
         float value, slope;
-        act_of<T, ACT>(fmaf(xh, g[j], b[j]), value, slope);
+        act_of<T, ACT>(fmaf(x, g[j], b[j]), value, slope);
         const float dz = elem<T>(w[i], j) * slope;
-        s4[j] += dz, d4[j] = fmaf(dz, xh, d4[j]);
+        s4[j] += dz, d4[j] = fmaf(dz, x, d4[j]);
       }
     }
 #pragma unroll
     for (int j = 0; j < VE; ++j) sum[j] += s4[j], dot[j] += d4[j];
   }
+#pragma unroll
+  for (int j = 0; j < VE; ++j) dot[j] *= rstd[j];
   const int first = at.first * d.per;
-  join_held<T>(
+  join_held<T, NT>(
       at, d.per, sum, dot, room, col_room, all,
       [&](int c, double2 s) {
         if (d.samples > 1) {
@@ -622,28 +705,32 @@ __global__ __launch_bounds__(kThreads) void norm_grad_held_kernel(Input<T, KEPT>
   float m1[VE], m2[VE];
 #pragma unroll
   for (int j = 0; j < VE; ++j) {
-    const double2 q = all[min(at.col * VE + j, at.width - 1) / d.per];
-    m1[j] = (float)(q.x * per), m2[j] = (float)(q.y * per);
+    const double2 q = all[min(of_sums.next(), at.groups - 1)];
+    m1[j] = rstd[j] * (float)(q.x * per), m2[j] = rstd[j] * rstd[j] * (float)(q.y * per);
   }
 #pragma unroll
-  for (int i = 0; i < kHeld; ++i) {
+  for (int i = 0; i < HELD; ++i) {
     if (!at.there(i)) break;
     const float step = in.step(v[i]);
     float f[VE];
 #pragma unroll
     for (int j = 0; j < VE; ++j) {
-      const float xh = (in.at(v[i], j, step) - mean[j]) * rstd[j];
+      const float x = in.at(v[i], j, step, mean[j]);
       float value, slope;
-      act_of<T, ACT>(fmaf(xh, g[j], b[j]), value, slope);
-      f[j] = rstd[j] * ((elem<T>(w[i], j) * slope) * g[j] - m1[j] - xh * m2[j]);
+      act_of<T, ACT>(fmaf(x, g[j], b[j]), value, slope);
+      f[j] = fmaf(elem<T>(w[i], j) * slope, g[j], -fmaf(x, m2[j], m1[j]));
     }
     store_part<T>(dx + at.row(i) * d.ldx + at.c0, at.left, pack<T>(f));
   }
 }
 
 // ---- host ---------------------------------------------------------------------------------------------------
+// Groups of a workgroup whose registers hold their sample, and its threads.
+struct Held {
+  int take, threads, held;  // take 0: no workgroup's registers do; held: vectors of a thread, at most
+};
 struct Plan {
-  int take, take_kept;  // groups of a workgroup whose registers hold them, 0: none does; with codes
+  Held held, held_kept;  // with codes
   int lanes, cols;  // threads side by side, workgroups side by side
   int chunks;
   int64_t chunk;
@@ -651,27 +738,32 @@ struct Plan {
   size_t part, group, chan, bytes;
 };
 
-int held_lanes(const wcc_group_norm_desc &d, int take, int VE);
+int held_lanes(const wcc_group_norm_desc &d, int take, int VE, bool kept);
 
-// Groups of a workgroup whose registers hold their sample, 0 if none does.  As many as read 128 bytes of a pixel, a line of memory, where
-// that leaves 512 workgroups, else 64 or 16 bytes: a small map is bound by what a compute unit computes (one map of 256 pixels and 96
-// channels in one workgroup 9.8 us).  With codes, whole blocks of channels.
-int held_of(const wcc_group_norm_desc &d, int VE, bool kept) {
+// Groups of a workgroup whose registers hold their sample (take), and its threads, 256 where they suffice: three workgroups a compute unit.
+// As many groups as read 128 bytes of a pixel, a line of memory, where that leaves 512 workgroups, else 64 or 16 bytes: a small map is bound
+// by what a compute unit computes (one map of 256 pixels and 96 channels in one workgroup 9.8 us).  With codes, whole blocks of channels.
+Held held_of(const wcc_group_norm_desc &d, int VE, bool kept) {
   const int per = d.C / d.groups, size = 16 / VE;
-  auto fits = [&](int take) {
-    const int64_t width = (int64_t)take * per;
-    if (kept && width % kKept != 0 && take < d.groups) return false;
-    const int lanes = held_lanes(d, take, VE);
-    return lanes <= kThreads && (d.pixels + kThreads / lanes - 1) / (kThreads / lanes) <= kHeld;
-  };
-  int best = 0;
+  Held best = {0, 0, 0};
+  if (d.pixels > kHeld * 512) return best;
+  int whole = 1;  // groups whose channels are whole blocks
+  if (kept)
+    while ((int64_t)whole * per % kKept != 0) whole *= 2;
   for (const int least : {16, 64, 128}) {
-    for (int take = 1; take <= d.groups && (int64_t)take * per <= kWidest; ++take) {
-      if (!fits(take) || ((int64_t)take * per * size < least && take < d.groups)) continue;
-      best = take;
+    int take = std::max((least + per * size - 1) / (per * size), 1);
+    take = std::min((take + whole - 1) / whole * whole, d.groups);
+    const int64_t width = (int64_t)take * per;
+    if (width > 512) break;
+    const int lanes = held_lanes(d, take, VE, kept);
+    for (const int threads : {256, 512}) {
+      if (width > threads || lanes > threads) continue;
+      const int64_t most = (d.pixels + threads / lanes - 1) / (threads / lanes);
+      if (most > kHeld) continue;
+      best = Held{take, threads, most <= 2 ? 2 : kHeld};
       break;
     }
-    if (best && (int64_t)d.samples * ((d.groups + best - 1) / best) <= 512) break;
+    if (best.take && (int64_t)d.samples * ((d.groups + best.take - 1) / best.take) <= 512) break;
   }
   return best;
 }
@@ -682,17 +774,20 @@ Plan plan_of(const wcc_group_norm_desc &d) {
   const int VE = d.dtype == WCC_F32 ? 4 : 8;
   const int64_t vectors = kept_blocks(d.C) * (kKept / VE);  // (whole blocks: what keeps x needs all lanes of each)
   Plan p;
-  p.take = held_of(d, VE, false), p.take_kept = held_of(d, VE, true);
+  p.held = held_of(d, VE, false), p.held_kept = held_of(d, VE, true);
   p.lanes = (int)std::min<int64_t>(vectors, 64);  // (1 KiB a pixel; with all of a wide map's a workgroup had one pixel at a time, and many chunks)
   p.cols = (int)((vectors + p.lanes - 1) / p.lanes);
   const int rows = 256 / p.lanes;
-  // chunks: as many as give every compute unit eight workgroups, of eight pixels a thread at least
-  const int64_t most = std::max<int64_t>((d.pixels + 8 * rows - 1) / (8 * rows), 1);
-  const int64_t want = std::max<int64_t>(2048 / std::max<int64_t>((int64_t)d.samples * p.cols, 1), 1);
-  const int64_t n = std::min(most, want);
+  // Chunks: as many as give every compute unit eight workgroups, of eight pixels a thread at least; four where there are few, as long as the
+  // second pass can join them by itself: up to 2048 pairs of sums, two workgroups a compute unit.
+  const int64_t fours = std::max<int64_t>((d.pixels + 4 * rows - 1) / (4 * rows), 1), eights = (fours + 1) / 2;
+  const int64_t each = std::max<int64_t>((int64_t)d.samples * p.cols, 1), want = std::max<int64_t>(2048 / each, 1);
+  const int64_t joined = d.C <= kShort ? std::min<int64_t>(2048 / d.C, 512 / each) : 0;
+  int64_t n = std::min(eights, want);
+  if (n < joined) n = std::min({fours, want, joined});
   p.chunk = std::max<int64_t>((d.pixels + n - 1) / n, 1);
   p.chunks = (int)std::max<int64_t>((d.pixels + p.chunk - 1) / p.chunk, 1);
-  p.few = d.C <= kShort && p.chunks * d.C <= 4096;
+  p.few = p.chunks <= joined;
   p.part = 0;
   p.group = up((size_t)d.samples * p.chunks * d.C * sizeof(double2));
   p.chan = p.group + up((size_t)d.samples * d.groups * sizeof(float4));
@@ -700,8 +795,9 @@ Plan plan_of(const wcc_group_norm_desc &d) {
   return p;
 }
 
-int held_lanes(const wcc_group_norm_desc &d, int take, int VE) {
-  return (int)(kept_blocks((int64_t)take * (d.C / d.groups)) * (kKept / VE));
+int held_lanes(const wcc_group_norm_desc &d, int take, int VE, bool kept) {
+  const int64_t width = (int64_t)take * (d.C / d.groups);
+  return (int)(kept ? kept_blocks(width) * (kKept / VE) : (width + VE - 1) / VE);
 }
 
 Sums sums_of(const Plan &p, char *ws) {
@@ -727,6 +823,16 @@ void by_act(int act, F f) {
   }
 }
 
+template <class F>
+void by_held(const Held &h, F f) {
+  const std::integral_constant<int, 256> few;
+  const std::integral_constant<int, 512> many;
+  const std::integral_constant<int, 2> two;
+  const std::integral_constant<int, kHeld> all;
+  if (h.threads == 256) h.held == 2 ? f(few, two) : f(few, all);
+  else h.held == 2 ? f(many, two) : f(many, all);
+}
+
 template <class T>
 hipError_t forward(const wcc_group_norm_desc &d, const NormArgs &g, hipStream_t st) {
   const Plan p = plan_of(d);
@@ -734,16 +840,18 @@ hipError_t forward(const wcc_group_norm_desc &d, const NormArgs &g, hipStream_t 
   const Shape sh = shape_of(d);
   const T *x = static_cast<const T *>(g.x);
   T *y = static_cast<T *>(g.y);
-  if (const int take = g.codes ? p.take_kept : p.take) {
+  const Held held = g.codes ? p.held_kept : p.held;
+  if (const int take = held.take) {
     const unsigned n = (unsigned)(d.samples * ((d.groups + take - 1) / take));
-    const int lanes = held_lanes(d, take, VecOf<T>::N);
+    const int lanes = held_lanes(d, take, VecOf<T>::N, g.codes != nullptr);
     by_act(d.act, [&](auto act) {
-      if (g.codes)
-        norm_held_kernel<T, act(), true>
-            <<<n, kThreads, 0, st>>>(x, g.gamma, g.beta, g.counts, sh, take, lanes, y, g.stats, g.codes, g.steps);
-      else
-        norm_held_kernel<T, act(), false>
-            <<<n, kThreads, 0, st>>>(x, g.gamma, g.beta, g.counts, sh, take, lanes, y, g.stats, nullptr, nullptr);
+      by_held(held, [&](auto threads, auto held) {
+        auto go = [&](auto keep) {
+          norm_held_kernel<T, threads(), held(), act(), keep()>
+              <<<n, threads(), 0, st>>>(x, g.gamma, g.beta, g.counts, sh, take, lanes, y, g.stats, g.codes, g.steps);
+        };
+        g.codes ? go(std::true_type()) : go(std::false_type());
+      });
     });
     return hipGetLastError();
   }
@@ -772,13 +880,16 @@ hipError_t backward(const wcc_group_norm_desc &d, const NormArgs &g, hipStream_t
   const T *dy = static_cast<const T *>(g.dy);
   const dim3 grid((unsigned)(p.chunks * d.samples), p.cols);
   const bool wide = g.dgamma || g.dbeta;
-  const int take = KEPT ? p.take_kept : p.take;
+  const Held held = KEPT ? p.held_kept : p.held;
+  const int take = held.take;
   if (take && d.samples > 0) {
     const unsigned n = (unsigned)(d.samples * ((d.groups + take - 1) / take));
-    const int lanes = held_lanes(d, take, VecOf<T>::N);
+    const int lanes = held_lanes(d, take, VecOf<T>::N, KEPT);
     by_act(d.act, [&](auto act) {
-      norm_grad_held_kernel<T, act(), KEPT><<<n, kThreads, 0, st>>>(in, dy, g.gamma, g.beta, g.stats, g.counts, sh, s.chan, take, lanes,
-                                                                   static_cast<T *>(g.dx), g.dgamma, g.dbeta);
+      by_held(held, [&](auto threads, auto held) {
+        norm_grad_held_kernel<T, threads(), held(), act(), KEPT><<<n, threads(), 0, st>>>(
+            in, dy, g.gamma, g.beta, g.stats, g.counts, sh, s.chan, take, lanes, static_cast<T *>(g.dx), g.dgamma, g.dbeta);
+      });
     });
     if (d.samples == 1) return hipGetLastError();
   } else if (d.samples > 0) {

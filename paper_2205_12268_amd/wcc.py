@@ -270,8 +270,9 @@ def _rows(t, rows, width, ld, dtype):
     """Address of a matrix of tokens: [rows, width] of the descriptor's type, rows `ld` elements apart."""
     if t is None:
         return None
-    assert t.is_cuda and tuple(t.shape) == (rows, width) and _DTYPES.get(t.dtype) == dtype, "not the descriptor's matrix"
-    assert (width <= 1 or t.stride(1) == 1) and (rows <= 1 or t.stride(0) == ld), "not the descriptor's row stride"
+    assert t.is_cuda and t.shape == (rows, width) and _DTYPES.get(t.dtype) == dtype, "not the descriptor's matrix"
+    a, b = t.stride()
+    assert (b == 1 or width <= 1) and (a == ld or rows <= 1), "not the descriptor's row stride"
     return t.data_ptr()
 
 
@@ -279,7 +280,7 @@ def _whole(t, shape, dtype):
     """Address of a contiguous tensor of this shape and torch type."""
     if t is None:
         return None
-    assert t.is_cuda and t.is_contiguous() and t.dtype == dtype and tuple(t.shape) == shape, "not the descriptor's tensor"
+    assert t.is_cuda and t.is_contiguous() and t.dtype == dtype and t.shape == shape, "not the descriptor's tensor"
     return t.data_ptr()
 
 
