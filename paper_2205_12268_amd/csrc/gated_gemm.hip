@@ -630,7 +630,7 @@ ProductPlan plan_of(int64_t rows, int64_t C_in, int64_t C_out, int64_t room, int
 
 // The two projections: tiles of 256 x 128 outputs of both where three quarters of the compute units have one and
 // their end is not most of the work, else of 128 x 64 (fp32, few:
-// of 64 x 64); few and long ones in ranges of eight stages and more.
+// of 64 x 64).
 struct GatePlan {
   int bt, bo, splits;
   int64_t stages, chunk;
@@ -642,7 +642,17 @@ GatePlan gate_plan(int64_t rows, int64_t outs, int64_t k, int size) {
   if (size == 2 && p.stages >= 12 && tiles(rows, 256) * tiles(outs, 128) >= 200) p.bt = p.bo = 256;
   if (size == 4 && tiles(rows, 128) * tiles(outs, 64) < 256) p.bt = 64;
   const int64_t n = tiles(rows, p.bt) * tiles(outs, p.bo / 2);
-  const int64_t want = n < 128 ? std::max<int64_t>(std::min<int64_t>({384 / n, p.stages / 8, 16}), 1) : 1;
+  // Ranges for the shortest time by a rough count, in stages: rounds of 256, four for a workgroup's beginning and end, and the join, 4 us and
+  // the sums written and read at 4 TB/s (a stage takes 0.35 us, of fp32 0.93 or 1.86).
+  int64_t want = 1;
+  if (p.bt < 256) {
+    const double stage = size == 2 ? 0.35 : p.bt == 64 ? 0.93 : 1.86, sums = 16e-6 * rows * room_of(outs) / 4 / stage;
+    double best = 0;
+    for (int64_t splits = 1; splits <= 16 && (splits == 1 || p.stages >= 4 * splits); ++splits) {
+      const double time = tiles(n * splits, 256) * (tiles(p.stages, splits) + 4.0) + (splits > 1 ? 4 / stage + sums * splits : 0.0);
+      if (splits == 1 || time < best) best = time, want = splits;
+    }
+  }
   p.chunk = tiles(p.stages, want);
   p.splits = (int)tiles(p.stages, p.chunk);
   return p;
