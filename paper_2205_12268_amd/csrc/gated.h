@@ -167,7 +167,8 @@ template <class T>
 hipError_t gemm_back(const Backward<T> &b, float *part, hipStream_t s);
 
 // The two projections for few rows of bf16 (gated_thin.hip), operands as above.
+size_t thin_gate_parts(int64_t rows, int64_t outs, int64_t k);
 hipError_t thin_gate(const Gate<bf16_t> &p, int act, bool back, const Side<bf16_t> &x, const bf16_t *w_gate, const bf16_t *w_up, int64_t ldw,
-                     int64_t k, hipStream_t s);
+                     int64_t k, float *part, hipStream_t s);
 
 }  // namespace wcc

@@ -100,6 +100,7 @@ Plan plan_of(const wcc_gated_desc &g, bool backward) {
   p.back = p.gemm || (size == 2 && g.rows <= kThin && g.C_in % each == 0 && products >= 1 << 20);
   if (!p.gemm) p.copy_x = p.copy_w = false;
   size_t parts = tile_gate_parts(g.rows, g.C_out, g.C_in, size), at = 0;  // (tensors at odd addresses take these tiles)
+  if (size == 2 && g.rows <= kThin) parts = std::max(parts, thin_gate_parts(g.rows, g.C_out, p.k));
   if (p.gemm) parts = std::max(parts, gemm_gate_parts(g.rows, g.C_out, p.k, size));
   if (backward) at += up((size_t)g.rows * p.parts * 2 * p.room * size);
   p.x = at;
@@ -165,7 +166,7 @@ hipError_t prepare(const wcc_gated_desc &d, const Plan &p, const GatedArgs &g, b
 template <class T>
 hipError_t gate_of(const wcc_gated_desc &d, const Plan &p, const Gate<T> &gate, bool back, const Operands<T> &o, float *part, hipStream_t s) {
   if constexpr (sizeof(T) == 2) {
-    if (d.rows <= kThin && o.takes) return thin_gate(gate, d.act, back, o.x, o.wg, o.wu, o.ldw, p.k, s);
+    if (d.rows <= kThin && o.takes) return thin_gate(gate, d.act, back, o.x, o.wg, o.wu, o.ldw, p.k, part, s);
   }
   if (p.gemm && o.takes && !(back && p.parts == 2)) return gemm_gate<T>(gate, d.act, back, o.x, o.wg, o.wu, o.ldw, p.k, part, s);
   return tile_gate<T>(gate, d.act, back, o.x, o.wg, o.wu, o.ldw, d.C_in, part, s);

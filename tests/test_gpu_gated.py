@@ -79,6 +79,7 @@ SIZES = [  # rows, C_in, C_out, padding, shift
     (1, 1, 1, 0, 0), (1, 64, 64, 0, 0), (2, 3, 5, 1, 1), (1, 2048, 520, 0, 0), (3, 512, 96, 0, 0), (7, 129, 63, 0, 3), (16, 256, 128, 8, 0),
     (17, 1024, 272, 0, 0), (33, 1000, 137, 3, 1), (64, 320, 640, 0, 0), (65, 64, 257, 0, 0), (100, 72, 96, 8, 8), (130, 512, 384, 0, 0),
     (257, 200, 300, 0, 0), (300, 256, 520, 8, 0), (520, 640, 264, 0, 0), (600, 96, 48, 0, 1), (1000, 40, 24, 0, 0),
+    (2, 4104, 88, 0, 0), (20, 5000, 72, 8, 0), (64, 4360, 33, 0, 0),
 ]
 
 
