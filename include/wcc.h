@@ -502,7 +502,7 @@ typedef struct {
 } wcc_gated_desc;
 
 /* Workspace of the calls below for this descriptor (a multiple of 256).  With more than 2^23 tiles of
- * 128 rows by 64 channels: WCC_ERR_UNSUPPORTED. */
+ * 128 rows by 64 channels or of 64 C_in by 64 C_out: WCC_ERR_UNSUPPORTED. */
 wcc_status wcc_gated_workspace_bytes(const wcc_gated_desc *desc, size_t *bytes);
 
 /* codes and steps (both or neither) receive g and u as wcc_rows_keep keeps rows of C_out values, from

@@ -38,9 +38,9 @@ wcc_status check(const wcc_gated_desc *d) {
   if (!real_type(d->dtype) || bad_act(d->act)) return WCC_ERR_DTYPE;
   if (d->rows < 0 || d->rows > kMostRows || d->C_in < 1 || d->C_in > kMostWidth || d->C_out < 1 || d->C_out > kMostWidth) return WCC_ERR_SHAPE;
   if (bad_stride(d->ldx, d->C_in) || bad_stride(d->ldy, d->C_out)) return WCC_ERR_SHAPE;
-  // (tiles are counted in 32 bits, of 128 rows by 64 outputs)
-  if (((d->rows + 127) / 128) * (int64_t)((d->C_out + 63) / 64) > kMostGroups || ((d->rows + 127) / 128) * (int64_t)((d->C_in + 63) / 64) > kMostGroups)
-    return WCC_ERR_UNSUPPORTED;
+  // (a launch has fewer than 2^24 workgroups of 256)
+  const int64_t rows = (d->rows + 127) / 128, in = (d->C_in + 63) / 64, out = (d->C_out + 63) / 64;
+  if (rows * out > kMostGroups || rows * in > kMostGroups || in * out > kMostGroups) return WCC_ERR_UNSUPPORTED;
   return WCC_OK;
 }
 

@@ -440,24 +440,33 @@ __global__ __launch_bounds__(256) void norm_grad_sums_kernel(Input<T, KEPT> in, 
 }
 
 // ---- backward: the second pass -----------------------------------------------------------------------------
-// dgamma and dbeta of a channel, over the samples (and SHORT, their chunks) in their order
-template <bool SHORT>
-__device__ __forceinline__ void affine_grad(int c, const Shape &d, const Sums &s, float *dgamma, float *dbeta) {
-  if (c >= d.C) return;
-  const double2 *p = (SHORT ? s.part : s.chan) + c;
-  const int n = d.samples * (SHORT ? s.chunks : 1);
+// dgamma and dbeta of a channel: n pairs of sums of it, `stride` rows of C apart, in their order
+__device__ __forceinline__ double2 sum_of(const double2 *p, int n, int64_t stride) {
   double2 a = {0.0, 0.0};
 #pragma unroll 8
   for (int i = 0; i < n; ++i) {
-    const double2 v = p[(int64_t)i * d.C];
+    const double2 v = p[i * stride];
     a.x += v.x, a.y += v.y;
   }
+  return a;
+}
+__device__ __forceinline__ void affine_grad(int c, int C, const double2 *p, int n, int64_t stride, float *dgamma, float *dbeta) {
+  if (c >= C) return;
+  const double2 a = sum_of(p + c, n, stride);
   if (dbeta) dbeta[c] = (float)a.x;
   if (dgamma) dgamma[c] = (float)a.y;
 }
-template <bool SHORT>
-__global__ __launch_bounds__(256) void norm_affine_grad_kernel(Shape d, Sums s, float *__restrict__ dgamma, float *__restrict__ dbeta) {
-  affine_grad<SHORT>(blockIdx.x * 256 + threadIdx.x, d, s, dgamma, dbeta);
+__global__ __launch_bounds__(256) void norm_affine_grad_kernel(const double2 *__restrict__ p, int C, int n, int64_t stride,
+                                                               float *__restrict__ dgamma, float *__restrict__ dbeta) {
+  affine_grad(blockIdx.x * 256 + threadIdx.x, C, p, n, stride, dgamma, dbeta);
+}
+// Many samples: `each` of them joined in the place of their first.
+constexpr int kFewSamples = 64;
+__global__ __launch_bounds__(256) void norm_samples_kernel(double2 *chan, int C, int samples, int each) {
+  const int c = blockIdx.x * 256 + threadIdx.x, first = blockIdx.y * each;
+  if (c >= C) return;
+  double2 *p = chan + (int64_t)first * C + c;
+  *p = sum_of(p, min(each, samples - first), C);
 }
 
 // (workgroups past `tiles` do dgamma and dbeta)
@@ -469,7 +478,8 @@ __global__ __launch_bounds__(256) void norm_grad_apply_kernel(Input<T, KEPT> in,
   constexpr int VE = VecOf<T>::N;
   __shared__ std::conditional_t<SHORT, ShortRoom, char> room;
   if ((int)blockIdx.x >= tiles) {
-    if (blockIdx.y == 0) affine_grad<SHORT>((blockIdx.x - tiles) * 256 + threadIdx.x, d, s, dgamma, dbeta);
+    if (blockIdx.y == 0)
+      affine_grad((blockIdx.x - tiles) * 256 + threadIdx.x, d.C, SHORT ? s.part : s.chan, d.samples * (SHORT ? s.chunks : 1), d.C, dgamma, dbeta);
     return;
   }
   const Place<VE> at(tiles - 1 - blockIdx.x, d, s, counts, lanes);
@@ -789,7 +799,7 @@ Plan plan_of(const wcc_group_norm_desc &d) {
   p.chunks = (int)std::max<int64_t>((d.pixels + p.chunk - 1) / p.chunk, 1);
   p.few = p.chunks <= joined;
   p.part = 0;
-  p.group = up((size_t)d.samples * p.chunks * d.C * sizeof(double2));
+  p.group = p.held.take && p.held_kept.take ? 0 : up((size_t)d.samples * p.chunks * d.C * sizeof(double2));
   p.chan = p.group + up((size_t)d.samples * d.groups * sizeof(float4));
   p.bytes = p.chan + up((size_t)d.samples * d.C * sizeof(double2));
   return p;
@@ -879,7 +889,7 @@ hipError_t backward(const wcc_group_norm_desc &d, const NormArgs &g, hipStream_t
   const Input<T, KEPT> in{static_cast<const T *>(g.x), d.ldx, g.codes, g.steps, (int)kept_blocks(d.C)};
   const T *dy = static_cast<const T *>(g.dy);
   const dim3 grid((unsigned)(p.chunks * d.samples), p.cols);
-  const bool wide = g.dgamma || g.dbeta;
+  const bool wide = g.dgamma || g.dbeta, fused = wide && (p.few || d.samples <= kFewSamples);  // (beside dx's tiles)
   const Held held = KEPT ? p.held_kept : p.held;
   const int take = held.take;
   if (take && d.samples > 0) {
@@ -893,7 +903,7 @@ hipError_t backward(const wcc_group_norm_desc &d, const NormArgs &g, hipStream_t
     });
     if (d.samples == 1) return hipGetLastError();
   } else if (d.samples > 0) {
-    const int n = p.chunks * d.samples, more = wide ? (d.C + 255) / 256 : 0;
+    const int n = p.chunks * d.samples, more = fused ? (d.C + 255) / 256 : 0;
     by_act(d.act, [&](auto act) {
       norm_grad_sums_kernel<T, act(), KEPT><<<grid, 256, 0, st>>>(in, dy, g.gamma, g.beta, g.stats, g.counts, sh, s, p.lanes);
       if (!p.few) norm_join_kernel<true><<<(unsigned)(d.groups * d.samples), 256, 0, st>>>(g.counts, sh, s, g.gamma, g.stats, join_lanes(d));
@@ -907,12 +917,19 @@ hipError_t backward(const wcc_group_norm_desc &d, const NormArgs &g, hipStream_t
         norm_grad_apply_kernel<T, act(), KEPT, false>
             <<<both, 256, 0, st>>>(in, dy, g.gamma, g.beta, g.counts, sh, s, p.lanes, n, dx, g.stats, g.dgamma, g.dbeta);
     });
-    if (g.dx) return hipGetLastError();
+    if (g.dx && (fused || !wide)) return hipGetLastError();
   }
   if (wide) {
     const unsigned n = (unsigned)((d.C + 255) / 256);
-    if (p.few && !take) norm_affine_grad_kernel<true><<<n, 256, 0, st>>>(sh, s, g.dgamma, g.dbeta);
-    else norm_affine_grad_kernel<false><<<n, 256, 0, st>>>(sh, s, g.dgamma, g.dbeta);
+    if (p.few && !take) {
+      norm_affine_grad_kernel<<<n, 256, 0, st>>>(s.part, d.C, d.samples * p.chunks, d.C, g.dgamma, g.dbeta);
+    } else if (d.samples <= kFewSamples) {
+      norm_affine_grad_kernel<<<n, 256, 0, st>>>(s.chan, d.C, d.samples, d.C, g.dgamma, g.dbeta);
+    } else {
+      const int each = std::max((d.samples + 255) / 256, 16), left = (d.samples + each - 1) / each;
+      norm_samples_kernel<<<dim3(n, left), 256, 0, st>>>(s.chan, d.C, d.samples, each);
+      norm_affine_grad_kernel<<<n, 256, 0, st>>>(s.chan, d.C, left, (int64_t)each * d.C, g.dgamma, g.dbeta);
+    }
   }
   return hipGetLastError();
 }

@@ -24,7 +24,7 @@ def test_group_norm_descriptors(kw, status):
 @pytest.mark.parametrize("kw,status", [
     (dict(rows=-1), SHAPE), (dict(rows=1 << 31), SHAPE), (dict(C_in=0), SHAPE), (dict(C_out=0), SHAPE), (dict(C_in=(1 << 20) + 1), SHAPE),
     (dict(ldx=15), SHAPE), (dict(ldy=23), SHAPE), (dict(act=9), DTYPE), (dict(dtype=wcc.I4), DTYPE),
-    (dict(rows=(1 << 31) - 1, C_out=64 * 1024), UNSUPPORTED), (dict(rows=(1 << 31) - 1, C_in=64 * 1024), UNSUPPORTED),
+    (dict(C_in=1 << 18, C_out=1 << 18), UNSUPPORTED), (dict(rows=(1 << 31) - 1, C_out=64 * 1024), UNSUPPORTED), (dict(rows=(1 << 31) - 1, C_in=64 * 1024), UNSUPPORTED),
 ])
 def test_gated_descriptors(kw, status):
     base = dict(rows=5, C_in=16, C_out=24, dtype=wcc.F32)

@@ -293,6 +293,21 @@ def test_no_samples(ctx):
     assert not bool(dgamma.any()) and not bool(dbeta.any()) and CODE["f32"] == wcc.F32
 
 
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [(65, 3, 40, 4), (1500, 2, 24, 3), (300, 1, 520, 1), (70, 1200, 8, 1), (100, 40, 1300, 2)], ids=str)
+def test_many_samples(ctx, t, size):
+    """More samples than one thread adds up: on maps that registers hold, and on others."""
+    samples, pixels, C, groups = size
+    x, gamma, beta, _, dy = inputs(samples, pixels, C, t, sum(size))
+    got = forward(ctx, x, samples, groups, "silu", gamma, beta, None)
+    want = group_norm(x, samples, groups, gamma, beta, None, EPS, "silu", dy)
+    near(got["y"], want["y"], t == "bf16")
+    for some in (("dx", "dgamma", "dbeta"), ("dgamma", "dbeta")):
+        grads = backward(ctx, x, None, samples, groups, "silu", gamma, beta, None, got["stats"], dy, want=some)
+        for k in some:
+            near(grads[k], want[k], t == "bf16" and k == "dx", k)
+
+
 HELD = [  # samples, pixels, C, groups: what a workgroup's registers hold, and what is just too large for them
     (2, 4096, 8, 1), (2, 4097, 8, 1), (1, 1024, 32, 4), (1, 1025, 32, 4), (3, 128, 256, 32), (1, 64, 512, 1), (1, 64, 520, 1), (300, 4, 128, 32),
     (2, 2000, 64, 64), (7, 9, 480, 5), (1, 2048, 24, 2), (1, 8192, 4, 4),
