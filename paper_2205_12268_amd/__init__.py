@@ -7,9 +7,10 @@ Sub-modules
 ``wcc``    thin ctypes binding over ``csrc/libwcc.so`` (argument marshalling only).
 ``synth``  seeded synthetic inputs (holds none of the method's arithmetic).
 ``head``   example: a class head with low-rank adapters on a layer's maps.
+``block``  example: a trained block on a layer's maps, in front of the head.
 
 Nothing is imported eagerly so that ``synth`` can be used without the
 compiled library being present.
 """
 
-__all__ = ["wcc", "synth", "head"]
+__all__ = ["wcc", "synth", "head", "block"]

@@ -4,9 +4,10 @@ together, as a program uses them.
 A row is a pixel of the layer's output map, its channels last.  All images go through one frozen projection; each image's customer
 has a low-rank adapter beside it.  The adapters are tuned by distillation from the teacher's best logits of every pixel
 (``wcc_adapter_forward``, ``wcc_distill_forward`` with the gradient in place of the logits, ``wcc_adapter_backward``), then pixels
-are answered with a class, its log probability, the entropy and the alternatives (``wcc_token_scores``).
+are answered with a class, its log probability, the entropy and the alternatives (``wcc_token_scores``).  With ``--block`` the maps go
+through a trained block first (``block.GatedBlock``), which learns from the gradient of the head's input.
 
-    python -m paper_2205_12268_amd.head [--steps 30]
+    python -m paper_2205_12268_amd.head [--steps 30] [--block]
 """
 from __future__ import annotations
 
@@ -14,7 +15,7 @@ import argparse
 
 import torch
 
-from . import synth, wcc
+from . import block, synth, wcc
 
 
 class AdaptedHead:
@@ -49,11 +50,11 @@ class AdaptedHead:
         self.ctx.wcc_adapter_forward(d, x, self.w, adapter_of_row, self.a16, self.b16, None, None, out)
         return out
 
-    def step(self, x, adapter_of_row, t_idx, t_logit, rate: float) -> torch.Tensor:
-        """One step of gradient descent on the adapters; the losses of the rows before it, on the device."""
+    def step(self, x, adapter_of_row, t_idx, t_logit, rate: float, dx=None) -> torch.Tensor:
+        """One step of gradient descent on the adapters; the losses of the rows before it, on the device.  dx: takes the gradient of x."""
         y = self.project(x, adapter_of_row, self.logits)
         self.ctx.wcc_distill_forward(self.loss_desc, y, t_idx, t_logit, self.loss, None, self.weight, y)  # y: its gradient now
-        self.ctx.wcc_adapter_backward(self.desc, x, self.w, adapter_of_row, self.a16, self.b16, None, None, y, None, self.da, self.db)
+        self.ctx.wcc_adapter_backward(self.desc, x, self.w, adapter_of_row, self.a16, self.b16, None, None, y, dx, self.da, self.db)
         self.a -= rate * self.da
         self.b -= rate * self.db
         self._copies()
@@ -85,7 +86,7 @@ def maps_of_a_layer(ctx: wcc.Context, images: int, channels: int, side: int) -> 
 
 
 def demo(steps: int = 30, images: int = 4, side: int = 32, channels: int = 96, classes: int = 1000, rank: int = 8, teacher: int = 16,
-         rate: float = 3.0, say=print):
+         rate: float = 3.0, say=print, with_block: bool = False):
     """Losses of every step, and the answers to four pixels."""
     ctx = wcc.Context(0)
     rows = maps_of_a_layer(ctx, images, channels, side)
@@ -100,11 +101,20 @@ def demo(steps: int = 30, images: int = 4, side: int = 32, channels: int = 96, c
     t_logit, t_idx = t_logit.contiguous(), t_idx.int().contiguous()
 
     head = AdaptedHead(ctx, w, images, rank, n, teacher, temperature=2.0)
+    front = block.GatedBlock(ctx, images, side * side, channels, 2 * channels, channels // 8) if with_block else None
+    maps, dx = rows, torch.empty_like(rows) if front else None
     losses = []
     for i in range(steps):
-        losses.append(float(head.step(rows, of_row, t_idx, t_logit, rate).mean()))
+        if front:
+            rows = front.forward(maps)
+        losses.append(float(head.step(rows, of_row, t_idx, t_logit, rate, dx).mean()))
+        if front:
+            front.backward(dx)
+            front.step(rate / 3)
         if i % 10 == 0 or i == steps - 1:
             say(f"step {i}: loss {losses[-1]:.4f}")
+    if front:
+        rows = front.forward(maps)
     pick = torch.arange(images, device="cuda") * (side * side) + 5
     answers = head.answer(rows[pick], of_row[pick], t_idx[pick, 0].contiguous(), 3)
     torch.cuda.synchronize()
@@ -118,4 +128,6 @@ def demo(steps: int = 30, images: int = 4, side: int = 32, channels: int = 96, c
 if __name__ == "__main__":
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("--steps", type=int, default=30)
-    demo(ap.parse_args().steps)
+    ap.add_argument("--block", action="store_true", help="a trained block before the head")
+    args = ap.parse_args()
+    demo(args.steps, rate=1.0 if args.block else 3.0, with_block=args.block)
