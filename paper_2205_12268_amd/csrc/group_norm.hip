@@ -161,11 +161,36 @@ struct Place {
 // gamma and beta of a thread's channels; 1 and 0 where there are none
 template <int VE>
 __device__ __forceinline__ void affine(const float *gamma, const float *beta, int c0, int C, float (&g)[VE], float (&b)[VE]) {
+  typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+  const bool whole = c0 + VE <= C;
+  auto take = [&](const float *p, float none, float(&v)[VE]) {
+    if (!p) {
 #pragma unroll
-  for (int j = 0; j < VE; ++j) {
-    const int c = min(c0 + j, C - 1);
-    g[j] = gamma ? gamma[c] : 1.f;
-    b[j] = beta ? beta[c] : 0.f;
+      for (int j = 0; j < VE; ++j) v[j] = none;
+    } else if (whole) {
+#pragma unroll
+      for (int j = 0; j < VE; j += 4) {
+        const f32x4_any q = *reinterpret_cast<const f32x4_any *>(p + c0 + j);
+        v[j] = q[0], v[j + 1] = q[1], v[j + 2] = q[2], v[j + 3] = q[3];
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < VE; ++j) v[j] = p[min(c0 + j, C - 1)];
+    }
+  };
+  take(gamma, 1.f, g), take(beta, 0.f, b);
+}
+// use(j, load(group)) for the channels c + j of a thread, groups up to `last`: one load where they are all of one group
+template <int VE, class L, class U>
+__device__ __forceinline__ void by_groups(int c, int per, int last, L load, U use) {
+  GroupOf of(c, per);
+  if (per % VE == 0) {
+    const auto q = load(min(of.g, last));
+#pragma unroll
+    for (int j = 0; j < VE; ++j) use(j, q);
+  } else {
+#pragma unroll
+    for (int j = 0; j < VE; ++j) use(j, load(min(of.next(), last)));
   }
 }
 
@@ -353,15 +378,13 @@ __global__ __launch_bounds__(256) void norm_apply_kernel(const T *x, const float
   if (at.ty >= at.rows || c0 >= (KEEP ? blocks * kKept : d.C)) return;
   float g[VE], b[VE], mean[VE];
   affine<VE>(gamma, beta, c0, d.C, g, b);
-  GroupOf of(c0, d.per);
-#pragma unroll
-  for (int j = 0; j < VE; ++j) {
-    const int group = min(of.next(), d.groups - 1);
-    float4 q;
-    if constexpr (SHORT) q = room.group[group];
-    else q = s.group[(int64_t)at.sample * d.groups + group];
-    mean[j] = q.x, g[j] *= q.y;
-  }
+  by_groups<VE>(
+      c0, d.per, d.groups - 1,
+      [&](int group) {
+        if constexpr (SHORT) return room.group[group];
+        else return s.group[(int64_t)at.sample * d.groups + group];
+      },
+      [&](int j, const float4 &q) { mean[j] = q.x, g[j] *= q.y; });
   const int64_t row0 = (int64_t)at.sample * d.pixels;
   const Columns<T> cols(c0, d.C - c0, d.C, d.C % (KEEP ? kKept : VE) != 0);
   for (int64_t t = at.begin; t < at.end; t += 4 * at.rows) {
@@ -401,12 +424,10 @@ __global__ __launch_bounds__(256) void norm_grad_sums_kernel(Input<T, KEPT> in, 
   if (at.ty < at.rows && c0 < d.C) {
     float g[VE], b[VE], mean[VE], rstd[VE];
     affine<VE>(gamma, beta, c0, d.C, g, b);
-    GroupOf of(c0, d.per);
-#pragma unroll
-    for (int j = 0; j < VE; ++j) {
-      const int64_t q = 2 * ((int64_t)at.sample * d.groups + min(of.next(), d.groups - 1));
-      mean[j] = stats[q], rstd[j] = stats[q + 1], g[j] *= rstd[j];
-    }
+    const float *own = stats + 2 * (int64_t)at.sample * d.groups;
+    by_groups<VE>(
+        c0, d.per, d.groups - 1, [&](int group) { return float2{own[2 * group], own[2 * group + 1]}; },
+        [&](int j, const float2 &q) { mean[j] = q.x, rstd[j] = q.y, g[j] *= q.y; });
     const int64_t row0 = (int64_t)at.sample * d.pixels;
     const Columns<T> cols(c0, d.C - c0, d.C, d.C % VE != 0);
     for (int64_t t = at.begin; t < at.end; t += 4 * at.rows) {
@@ -489,14 +510,16 @@ __global__ __launch_bounds__(256) void norm_grad_apply_kernel(Input<T, KEPT> in,
   float g[VE], b[VE];
   float4 q[VE];
   affine<VE>(gamma, beta, c0, d.C, g, b);
-  GroupOf of(c0, d.per);
-#pragma unroll
-  for (int j = 0; j < VE; ++j) {
-    const int group = min(of.next(), d.groups - 1);
-    if constexpr (SHORT) q[j] = room.group[group];
-    else q[j] = s.group[(int64_t)at.sample * d.groups + group];
-    g[j] *= q[j].y, q[j].z *= q[j].y, q[j].w *= q[j].y * q[j].y;  // dx = gamma rstd dz - rstd m1 - (x - mean) rstd^2 m2
-  }
+  by_groups<VE>(
+      c0, d.per, d.groups - 1,
+      [&](int group) {
+        float4 v;
+        if constexpr (SHORT) v = room.group[group];
+        else v = s.group[(int64_t)at.sample * d.groups + group];
+        v.z *= v.y, v.w *= v.y * v.y;  // dx = gamma rstd dz - rstd m1 - (x - mean) rstd^2 m2
+        return v;
+      },
+      [&](int j, const float4 &v) { q[j] = v, g[j] *= v.y; });
   const int64_t row0 = (int64_t)at.sample * d.pixels;
   const Columns<T> cols(c0, d.C - c0, d.C, d.C % VE != 0);
   for (int64_t t = at.begin; t < at.end; t += 4 * at.rows) {
@@ -623,12 +646,9 @@ __global__ __launch_bounds__(NT) void norm_held_kernel(const T *x, const float *
   const int blocks = (d.C + kKept - 1) / kKept;
   const bool mine = KEEP ? at.ty < at.rows && at.c0 < blocks * kKept : at.left > 0;
   if (!mine) return;
-  GroupOf of(at.col * VE, d.per);
-#pragma unroll
-  for (int j = 0; j < VE; ++j) {
-    const float2 q = stat_room[min(of.next(), at.groups - 1)];
-    mean[j] = q.x, g[j] *= q.y;
-  }
+  by_groups<VE>(
+      at.col * VE, d.per, at.groups - 1, [&](int group) { return stat_room[group]; },
+      [&](int j, const float2 &q) { mean[j] = q.x, g[j] *= q.y; });
 #pragma unroll
   for (int i = 0; i < HELD; ++i) {
     if (at.ty + (int64_t)i * at.rows >= at.n) break;
@@ -670,12 +690,10 @@ __global__ __launch_bounds__(NT) void norm_grad_held_kernel(Input<T, KEPT> in, c
   }
   float g[VE], b[VE], mean[VE], rstd[VE];
   affine<VE>(gamma, beta, at.c0, d.C, g, b);
-  GroupOf of(at.col * VE, d.per), of_sums = of;
-#pragma unroll
-  for (int j = 0; j < VE; ++j) {
-    const int64_t q = 2 * ((int64_t)at.sample * d.groups + at.first + min(of.next(), at.groups - 1));
-    mean[j] = stats[q], rstd[j] = stats[q + 1], g[j] *= rstd[j];
-  }
+  const float *own = stats + 2 * ((int64_t)at.sample * d.groups + at.first);
+  by_groups<VE>(
+      at.col * VE, d.per, at.groups - 1, [&](int group) { return float2{own[2 * group], own[2 * group + 1]}; },
+      [&](int j, const float2 &q) { mean[j] = q.x, rstd[j] = q.y, g[j] *= q.y; });
   const double per = 1.0 / (double)max(at.n * d.per, (int64_t)1);
   double sum[VE] = {}, dot[VE] = {};
 #pragma unroll
@@ -713,11 +731,9 @@ __global__ __launch_bounds__(NT) void norm_grad_held_kernel(Input<T, KEPT> in, c
       [&](int c) { return gamma ? (double)gamma[first + c] : 1.0; });
   if (!dx || at.left <= 0) return;
   float m1[VE], m2[VE];
-#pragma unroll
-  for (int j = 0; j < VE; ++j) {
-    const double2 q = all[min(of_sums.next(), at.groups - 1)];
-    m1[j] = rstd[j] * (float)(q.x * per), m2[j] = rstd[j] * rstd[j] * (float)(q.y * per);
-  }
+  by_groups<VE>(
+      at.col * VE, d.per, at.groups - 1, [&](int group) { return float2{(float)(all[group].x * per), (float)(all[group].y * per)}; },
+      [&](int j, const float2 &q) { m1[j] = rstd[j] * q.x, m2[j] = rstd[j] * rstd[j] * q.y; });
 #pragma unroll
   for (int i = 0; i < HELD; ++i) {
     if (!at.there(i)) break;
