@@ -804,10 +804,11 @@ Plan plan_of(const wcc_group_norm_desc &d) {
   p.lanes = (int)std::min<int64_t>(vectors, 64);  // (1 KiB a pixel; with all of a wide map's a workgroup had one pixel at a time, and many chunks)
   p.cols = (int)((vectors + p.lanes - 1) / p.lanes);
   const int rows = 256 / p.lanes;
-  // Chunks: as many as give every compute unit eight workgroups, of eight pixels a thread at least; four where there are few, as long as the
+  // Chunks: as many as give every compute unit four workgroups (512 to 4096 of them take 40 to 42 us for 8 x 16384 x 256), of eight pixels a
+  // thread at least; four where there are few, as long as the
   // second pass can join them by itself: up to 2048 pairs of sums, two workgroups a compute unit.
   const int64_t fours = std::max<int64_t>((d.pixels + 4 * rows - 1) / (4 * rows), 1), eights = (fours + 1) / 2;
-  const int64_t each = std::max<int64_t>((int64_t)d.samples * p.cols, 1), want = std::max<int64_t>(2048 / each, 1);
+  const int64_t each = std::max<int64_t>((int64_t)d.samples * p.cols, 1), want = std::max<int64_t>(1024 / each, 1);
   const int64_t joined = d.C <= kShort ? std::min<int64_t>(2048 / d.C, 512 / each) : 0;
   int64_t n = std::min(eights, want);
   if (n < joined) n = std::min({fours, want, joined});
