@@ -537,7 +537,7 @@ __device__ __forceinline__ void product_tile(const Job<T> &job, int64_t block, u
 
 // dx's tiles, the longer ones, before the weights'
 template <class T, int BT, int BO, bool TWO>
-__global__ __launch_bounds__(256, BO == 128 && BT <= 128 ? 2 : 1) void product_gemm_kernel(Job<T> dx, Job<T> dw) {
+__global__ __launch_bounds__(256, BO == 64 ? 4 : BO == 128 ? 2 : 1) void product_gemm_kernel(Job<T> dx, Job<T> dw) {
   __shared__ __align__(1024) unsigned char xs0[BT * kLine], ws0[BO * kLine], xs1[BT * kLine], ws1[BO * kLine];
   const int64_t b = blockIdx.x;
   if (b < dx.blocks) product_tile<T, BT, BO, false, TWO>(dx, in_runs(b, dx.blocks), xs0, ws0, xs1, ws1);
@@ -583,7 +583,7 @@ hipError_t by_act(int act, F f) {
 }
 
 // How the products of a backward pass are cut.  dx: rows x C_in over 2 room; the weights' gradients, both: 2 C_out x C_in over the rows.
-// Each workgroup has about as many stages as there are for every place (256, or 512 of the smaller tiles).
+// Each workgroup has about as many stages as there are for every place (256, or 512 and 1024 of the smaller tiles).
 struct ProductPlan {
   int bt, bo;
   struct Part {
@@ -604,11 +604,13 @@ ProductPlan plan_of(int64_t rows, int64_t C_in, int64_t C_out, int64_t room, int
   p.bt = p.bo = 128;
   // (the larger ones where three quarters of the compute units have one, and four fifths of them lie within the results)
   if (size == 2 && tiles_of(256, 256, dx, dw) >= 200 && 5 * C_in * (rows + 2 * C_out) >= 4 * 65536 * (dx + dw)) p.bt = p.bo = 256;
-  if (size == 4 && tiles_of(128, 128, dx, dw) < 384) p.bt = 64;
+  // (fp32: the smaller ones where the larger are few, and where a fifth of those would lie past C_in, 40000 rows 160 <-> 960 in 928 us against
+  // 1123; 8192 rows 320 <-> 640 take 222 in them and 219 in the larger, 4096 rows 512 <-> 2048 426 and 409, 1024 <-> 2048 820 and 762)
+  if (size == 4 && (tiles_of(128, 128, dx, dw) < 192 || 5 * C_in <= 4 * 128 * tiles(C_in, 128))) p.bt = p.bo = 64;
   tiles_of(p.bt, p.bo, dx, dw);
   // Ranges for the shortest time by a rough count: a workgroup takes its stages and as much as four for its beginning and end; more of them
   // than there are places wait.
-  const int64_t slots = p.bt == 256 ? 256 : 512, mean = std::max<int64_t>(tiles(dx * p.dx.stages + dw * p.dw.stages, slots), 4);
+  const int64_t slots = p.bt == 256 ? 256 : p.bt == 64 ? 1024 : 512, mean = std::max<int64_t>(tiles(dx * p.dx.stages + dw * p.dw.stages, slots), 4);
   int64_t best = 0;
   for (int i = 0; i < 16; ++i) {
     const int64_t has = mean + i * mean / 8;
@@ -752,7 +754,7 @@ hipError_t gemm_back(const Backward<T> &b, float *part, hipStream_t s) {
     else if (b.parts == 2) product_gemm_kernel<T, 128, 128, true><<<n, 256, 0, s>>>(dx, dw);
     else product_gemm_kernel<T, 128, 128, false><<<n, 256, 0, s>>>(dx, dw);
   } else {
-    if (p.bt == 64) product_gemm_kernel<T, 64, 128, false><<<n, 256, 0, s>>>(dx, dw);
+    if (p.bt == 64) product_gemm_kernel<T, 64, 64, false><<<n, 256, 0, s>>>(dx, dw);
     else product_gemm_kernel<T, 128, 128, false><<<n, 256, 0, s>>>(dx, dw);
   }
   const bool join_dx = dx.splits > 1, join_dw = dw.splits > 1;
