@@ -272,12 +272,12 @@ __global__ __launch_bounds__(256) void norm_sums_kernel(const T *__restrict__ x,
 // ---- the chunks joined -----------------------------------------------------------------------------------------
 // A workgroup for each group of a sample: a power of two (`lanes`, 64 at most) of channels side by side, the other threads over the
 // chunks.  BACK: m1 and m2 beside the statistics, and chan is left.
-template <bool BACK>
-__global__ __launch_bounds__(256) void norm_join_kernel(const int32_t *__restrict__ counts, Shape d, Sums s, const float *__restrict__ gamma,
+template <bool BACK, int NT>
+__global__ __launch_bounds__(NT) void norm_join_kernel(const int32_t *__restrict__ counts, Shape d, Sums s, const float *__restrict__ gamma,
                                                         float *__restrict__ stats, int lanes) {
-  __shared__ double2 room[4][64];
+  __shared__ double2 room[NT / 64][64];
   const int group = blockIdx.x % d.groups, sample = blockIdx.x / d.groups, tid = threadIdx.x, lane = tid & 63;
-  const int rows = 256 / lanes, col = tid % lanes, ty = tid / lanes;
+  const int rows = NT / lanes, col = tid % lanes, ty = tid / lanes;
   const int64_t n = pixels_of(counts, d.pixels, sample);
   const int chunks = (int)min((int64_t)s.chunks, (n + s.chunk - 1) / s.chunk);
   const double per = 1.0 / (double)max(n * d.per, (int64_t)1);
@@ -299,7 +299,7 @@ __global__ __launch_bounds__(256) void norm_join_kernel(const int32_t *__restric
     if (tid < lanes && c < d.per) {
       a = {0.0, 0.0};
 #pragma unroll
-      for (int w = 0; w < 4; ++w) a.x += room[w][lane].x, a.y += room[w][lane].y;
+      for (int w = 0; w < NT / 64; ++w) a.x += room[w][lane].x, a.y += room[w][lane].y;
       if constexpr (BACK) {
         s.chan[(int64_t)sample * d.C + group * d.per + c] = a;
         const double w = gamma ? gamma[group * d.per + c] : 1.f;
@@ -804,11 +804,13 @@ Plan plan_of(const wcc_group_norm_desc &d) {
   p.lanes = (int)std::min<int64_t>(vectors, 64);  // (1 KiB a pixel; with all of a wide map's a workgroup had one pixel at a time, and many chunks)
   p.cols = (int)((vectors + p.lanes - 1) / p.lanes);
   const int rows = 256 / p.lanes;
-  // Chunks: as many as give every compute unit four workgroups (512 to 4096 of them take 40 to 42 us for 8 x 16384 x 256), of eight pixels a
-  // thread at least; four where there are few, as long as the
-  // second pass can join them by itself: up to 2048 pairs of sums, two workgroups a compute unit.
+  // Chunks: as many as give every compute unit four workgroups (512 to 4096 of them take 40 to 42 us for 8 x 16384 x 256), two where the
+  // join would have more than 32768 pairs of sums to read for a group (512 KB: 500 chunks of 120 channels take it 15 us), of eight pixels a
+  // thread at least; four where there are few, as long as the second pass can join them by itself: up to 2048 pairs of sums, two workgroups a
+  // compute unit.
   const int64_t fours = std::max<int64_t>((d.pixels + 4 * rows - 1) / (4 * rows), 1), eights = (fours + 1) / 2;
-  const int64_t each = std::max<int64_t>((int64_t)d.samples * p.cols, 1), want = std::max<int64_t>(1024 / each, 1);
+  const int64_t each = std::max<int64_t>((int64_t)d.samples * p.cols, 1);
+  const int64_t want = std::max<int64_t>({std::min<int64_t>(1024 / each, 32768 / (d.C / d.groups)), 512 / each, 1});
   const int64_t joined = d.C <= kShort ? std::min<int64_t>(2048 / d.C, 512 / each) : 0;
   int64_t n = std::min(eights, want);
   if (n < joined) n = std::min({fours, want, joined});
@@ -860,6 +862,15 @@ void by_held(const Held &h, F f) {
   else h.held == 2 ? f(many, two) : f(many, all);
 }
 
+// The chunks joined: by 1024 threads a group where it has many pairs of sums, which a few workgroups would take long to read.
+template <bool BACK>
+void join(const wcc_group_norm_desc &d, const Plan &p, const NormArgs &g, const Shape &sh, const Sums &s, hipStream_t st) {
+  const unsigned n = (unsigned)(d.groups * d.samples);
+  const float *gamma = BACK ? g.gamma : nullptr;
+  if ((int64_t)p.chunks * (d.C / d.groups) > 2048) norm_join_kernel<BACK, 1024><<<n, 1024, 0, st>>>(g.counts, sh, s, gamma, g.stats, join_lanes(d));
+  else norm_join_kernel<BACK, 256><<<n, 256, 0, st>>>(g.counts, sh, s, gamma, g.stats, join_lanes(d));
+}
+
 template <class T>
 hipError_t forward(const wcc_group_norm_desc &d, const NormArgs &g, hipStream_t st) {
   const Plan p = plan_of(d);
@@ -884,7 +895,7 @@ hipError_t forward(const wcc_group_norm_desc &d, const NormArgs &g, hipStream_t 
   }
   const dim3 grid((unsigned)(p.chunks * d.samples), p.cols);
   norm_sums_kernel<T><<<grid, 256, 0, st>>>(x, g.counts, sh, s, p.lanes);
-  if (!p.few) norm_join_kernel<false><<<(unsigned)(d.groups * d.samples), 256, 0, st>>>(g.counts, sh, s, nullptr, g.stats, join_lanes(d));
+  if (!p.few) join<false>(d, p, g, sh, s, st);
   by_act(d.act, [&](auto act) {
     auto go = [&](auto keep, auto few) {
       norm_apply_kernel<T, act(), keep(), few()>
@@ -923,7 +934,7 @@ hipError_t backward(const wcc_group_norm_desc &d, const NormArgs &g, hipStream_t
     const int n = p.chunks * d.samples, more = fused ? (d.C + 255) / 256 : 0;
     by_act(d.act, [&](auto act) {
       norm_grad_sums_kernel<T, act(), KEPT><<<grid, 256, 0, st>>>(in, dy, g.gamma, g.beta, g.stats, g.counts, sh, s, p.lanes);
-      if (!p.few) norm_join_kernel<true><<<(unsigned)(d.groups * d.samples), 256, 0, st>>>(g.counts, sh, s, g.gamma, g.stats, join_lanes(d));
+      if (!p.few) join<true>(d, p, g, sh, s, st);
       if (!g.dx) return;
       const dim3 both((unsigned)(n + more), p.cols);
       T *dx = static_cast<T *>(g.dx);

@@ -80,7 +80,7 @@ SIZES = [  # samples, pixels, C, groups, padding, shift, counts
     (1, 1, 1, 1, 0, 0, None), (1, 64, 1, 1, 0, 0, None), (2, 50, 3, 1, 1, 1, None), (1, 256, 96, 8, 0, 0, None), (3, 100, 40, 5, 0, 0, None),
     (2, 37, 24, 24, 3, 2, None), (4, 33, 96, 32, 0, 0, [33, 5, 0, 40]), (2, 500, 64, 2, 8, 0, [500, 123]), (1, 3000, 32, 4, 0, 0, None),
     (2, 20, 2200, 11, 0, 0, None), (1, 40, 700, 1, 5, 1, None), (5, 1, 512, 2, 0, 0, [1, 0, 1, -3, 1]), (1, 5000, 20, 4, 0, 8, None),
-    (40, 70, 16, 2, 0, 0, None),
+    (40, 70, 16, 2, 0, 0, None), (2, 4097, 360, 3, 0, 0, [4097, 2050]), (1, 900, 1200, 1, 8, 0, None),  # (many pairs of sums to a group)
 ]
 
 
