@@ -6,7 +6,8 @@
 namespace wcc {
 namespace {
 
-// dg and du from what the projections are kept as: a lane has 16 bytes of dy.  Bound by memory.
+// dg and du from what the projections are kept as: a lane has 16 bytes of dy.  Bound by memory: 4096 x 5632 bf16 in 33 us,
+// 5.6 TB/s.
 template <class T, int ACT>
 __global__ __launch_bounds__(256) void kept_slopes_kernel(Gate<T> p) {
   constexpr int VE = VecOf<T>::N;
@@ -50,23 +51,27 @@ __global__ __launch_bounds__(256) void zeros_kernel(uint16_t *p, int64_t n) {
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = 0;
 }
 
-// Matrices of bf16 copied to rows of a stride that 16-byte loads take, zeros behind their width.  Three at most in one launch.
+// Matrices copied to rows of a stride that 16-byte loads take, zeros behind their width.  Three at most in one launch.
+template <class T>
 struct Copy {
-  const bf16_t *from;
-  bf16_t *to;
+  const T *from;
+  T *to;
   int64_t ld, rows;
 };
+template <class T>
 struct Copies {
-  Copy c[3];
+  Copy<T> c[3];
   int width;
   int64_t room;
 };
-__global__ __launch_bounds__(256) void copy_kernel(Copies a) {
-  const Copy c = a.c[blockIdx.y];
-  const int64_t per_row = a.room / 8;
+template <class T>
+__global__ __launch_bounds__(256) void copy_kernel(Copies<T> a) {
+  constexpr int VE = VecOf<T>::N;
+  const Copy<T> c = a.c[blockIdx.y];
+  const int64_t per_row = a.room / VE;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < c.rows * per_row; i += (int64_t)gridDim.x * 256) {
-    const int64_t t = i / per_row, e = (i - t * per_row) * 8;
-    *reinterpret_cast<u32x4 *>(c.to + t * a.room + e) = load_part<bf16_t>(c.from + t * c.ld + e, (int)(a.width - e));
+    const int64_t t = i / per_row, e = (i - t * per_row) * VE;
+    *reinterpret_cast<u32x4 *>(c.to + t * a.room + e) = load_part<T>(c.from + t * c.ld + e, (int)(a.width - e));
   }
 }
 
@@ -76,7 +81,6 @@ size_t up(size_t v) { return (v + 255) / 256 * 256; }
 // they have to be copied; sums of ranges of k.
 struct Plan {
   bool gemm, copy_x, copy_w;  // tiles fed straight from memory
-  bool back;                  // the same for the products of the backward pass
   int parts;                  // of dg and du
   size_t d, x, w, part, bytes;
   int64_t room, ldx, k;  // of d's halves; of rows and weights that were copied; C_in in whole chunks of 16 bytes
@@ -84,21 +88,24 @@ struct Plan {
 
 constexpr int kThin = 64;  // rows of few
 
-// Tiles fed straight from memory from 2^25 products on (fp32: any); bf16 rows or weights that 16-byte loads do not take are copied for it
-// from 2^27 on, fp32 ones go by way of registers.
+// A backward pass has its products in tiles fed straight from memory, rows and weights that 16-byte loads do not take copied for it: as many
+// launches as by way of registers or fewer, and 1.2 to 2.5 times as fast from 2^13 products on (65 rows 64 <-> 64 bf16 14.8 us against
+// 31.0, 777 rows 1000 <-> 1537 at odd strides 43.8 and 102, in fp32 173 and 312; 30 rows 4001 <-> 8000 234 and 252; one row 3001 <-> 5001,
+// all copies, 166 and 163).  A pair of projections has less to win: bf16 from 2^25 products on (128 rows 128 -> 256, 2^23, 4.6 us and
+// 4.4, 256 -> 256 5.4 and 7.1), with copies from 2^27 on (500 rows 301 -> 743 9.3 and 11.2, 512 rows 33 -> 64 6.3 and 4.5), fp32 always, with
+// copies from 3 * 2^27 on (777 rows 333 -> 1000 21.9 and 26.7, 300 rows 301 -> 743 18.1 and 13.4).
 Plan plan_of(const wcc_gated_desc &g, bool backward) {
   Plan p = {};
   const int size = g.dtype == WCC_F32 ? 4 : 2;
   const double products = 2.0 * g.rows * g.C_in * g.C_out;
-  p.room = room_of(g.C_out), p.ldx = room_of(g.C_in), p.k = (g.C_in + 7) / 8 * 8;
   const int each = 16 / size;
+  p.room = room_of(g.C_out), p.ldx = room_of(g.C_in), p.k = (g.C_in + each - 1) / each * each;
   p.copy_w = g.C_in % each != 0, p.copy_x = p.copy_w || g.ldx % each != 0;
-  p.gemm = size == 2 ? g.rows > kThin && products >= (p.copy_x ? 1 << 27 : 1 << 25) : !p.copy_x;
-  if (size == 4) p.copy_x = p.copy_w = false, p.k = g.C_in;
+  const bool thin = size == 2 && g.rows <= kThin;
+  const double least = size == 2 ? (p.copy_x && !backward ? 1 << 27 : 1 << 25) : p.copy_x && !backward ? 3 << 27 : 0;
+  p.gemm = !thin && products >= least;
   p.parts = size == 2 && g.rows * (int64_t)g.C_out < kFew ? 2 : 1;
-  // (few rows, whose products are bound by the weights and their gradients: any that 16-byte loads take)
-  p.back = p.gemm || (size == 2 && g.rows <= kThin && g.C_in % each == 0 && products >= 1 << 20);
-  if (!p.gemm) p.copy_x = p.copy_w = false;
+  if (!backward && !p.gemm) p.copy_x = p.copy_w = false;
   size_t parts = tile_gate_parts(g.rows, g.C_out, g.C_in, size), at = 0;  // (tensors at odd addresses take these tiles)
   if (size == 2 && g.rows <= kThin) parts = std::max(parts, thin_gate_parts(g.rows, g.C_out, p.k));
   if (p.gemm) parts = std::max(parts, gemm_gate_parts(g.rows, g.C_out, p.k, size));
@@ -109,8 +116,8 @@ Plan plan_of(const wcc_gated_desc &g, bool backward) {
   if (p.copy_w) at += 2 * up((size_t)g.C_out * p.ldx * size);
   p.part = at;
   if (backward) {
-    if (p.back) parts = std::max(parts, gemm_back_parts(g.rows, g.C_in, g.C_out, p.parts, size));
-    parts = std::max({parts, tile_product_parts(g.rows, g.C_in, g.C_out, 1, size), tile_product_parts(g.C_out, g.C_in, g.rows, 2, size)});
+    parts = std::max({parts, gemm_back_parts(g.rows, g.C_in, g.C_out, p.parts, size), tile_product_parts(g.rows, g.C_in, g.C_out, 1, size),
+                      tile_product_parts(g.C_out, g.C_in, g.rows, 2, size)});
   }
   p.bytes = p.part + up(parts);
   return p;
@@ -138,25 +145,23 @@ hipError_t prepare(const wcc_gated_desc &d, const Plan &p, const GatedArgs &g, b
     if ((e = launch_restore(r, k, s)) != hipSuccess) return e;
     o.x = Side<T>{static_cast<const T *>(k.back), p.ldx, d.rows};
   }
-  if constexpr (sizeof(T) == 2) {
-    Copies c = {};
-    int n = 0;
-    c.width = d.C_in, c.room = p.ldx;
-    if (x_used && g.x && p.copy_x) {
-      T *to = reinterpret_cast<T *>(g.ws + p.x);
-      c.c[n++] = Copy{o.x.p, to, d.ldx, d.rows};
-      o.x = Side<T>{to, p.ldx, d.rows};
-    }
-    if (w_used && p.copy_w) {
-      T *to = reinterpret_cast<T *>(g.ws + p.w), *next = reinterpret_cast<T *>(g.ws + p.w + up((size_t)d.C_out * p.ldx * sizeof(T)));
-      c.c[n++] = Copy{o.wg, to, d.C_in, d.C_out}, c.c[n++] = Copy{o.wu, next, d.C_in, d.C_out};
-      o.wg = to, o.wu = next, o.ldw = p.ldx;
-    }
-    if (n > 0) {
-      const int64_t most = std::max<int64_t>(d.rows, d.C_out) * (p.ldx / 8);
-      copy_kernel<<<dim3((unsigned)std::min<int64_t>((most + 255) / 256, 2048), n), 256, 0, s>>>(c);
-      e = hipGetLastError();
-    }
+  Copies<T> c = {};
+  int n = 0;
+  c.width = d.C_in, c.room = p.ldx;
+  if (x_used && g.x && p.copy_x) {
+    T *to = reinterpret_cast<T *>(g.ws + p.x);
+    c.c[n++] = Copy<T>{o.x.p, to, d.ldx, d.rows};
+    o.x = Side<T>{to, p.ldx, d.rows};
+  }
+  if (w_used && p.copy_w) {
+    T *to = reinterpret_cast<T *>(g.ws + p.w), *next = reinterpret_cast<T *>(g.ws + p.w + up((size_t)d.C_out * p.ldx * sizeof(T)));
+    c.c[n++] = Copy<T>{o.wg, to, d.C_in, d.C_out}, c.c[n++] = Copy<T>{o.wu, next, d.C_in, d.C_out};
+    o.wg = to, o.wu = next, o.ldw = p.ldx;
+  }
+  if (n > 0) {
+    const int64_t most = std::max<int64_t>(d.rows, d.C_out) * (p.ldx / VecOf<T>::N);
+    copy_kernel<T><<<dim3((unsigned)std::min<int64_t>((most + 255) / 256, 2048), n), 256, 0, s>>>(c);
+    e = hipGetLastError();
   }
   if (x_used) o.takes = gemm_takes(o.x.p, o.x.s, p.k, sizeof(T));
   if (w_used) o.takes = o.takes && gemm_takes(o.wg, o.ldw, p.k, sizeof(T)) && gemm_takes(o.wu, o.ldw, p.k, sizeof(T));
@@ -214,7 +219,7 @@ hipError_t backward(const wcc_gated_desc &d, const GatedArgs &g, hipStream_t s) 
   }
   if (e != hipSuccess) return e;
   const T *dg = gate.d, *du = gate.d + p.room;
-  if (p.back && o.takes) {
+  if (o.takes) {
     const Backward<T> b{dg, p.room, d.rows, p.parts, o.wg, o.wu, o.ldw, o.x.p, o.x.s, p.k, d.C_in, d.C_out, static_cast<T *>(g.dx), d.ldx,
                         static_cast<T *>(g.dw_gate), static_cast<T *>(g.dw_up)};
     return gemm_back<T>(b, part, s);

@@ -12,6 +12,9 @@
 // Maps that one workgroup's registers hold (a sample, some of its groups) take one launch.  Larger ones take three: sums of chunks of
 // pixels by channel; a small one that joins them; a second pass that goes backwards over the chunks, so that it begins with what
 // the caches hold; where the chunks are few, the second pass joins them and there are two.  Bound by memory: the second pass reads again what the first has read.
+// 8 x 16384 x 256 bf16, 32 groups, silu: 40 us forward (13 the first pass, 5.3 TB/s; 5 the join; 22 the second); x to codes beside y 30 in place
+// of 22; backward from codes 29, 5 and 31 (3.5 and 5.5 TB/s: in its first pass the slopes take as long as the loads).  One map of 256
+// pixels and 96 channels, by registers: 7, nearly all of it the way of one load, the statistics and one store.
 #include "block.h"
 
 namespace wcc {

