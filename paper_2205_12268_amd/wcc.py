@@ -266,28 +266,33 @@ _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
 _TORCH = {F32: torch.float32, BF16: torch.bfloat16}
 
 
-def _rows(t, rows, width, ld, dtype):
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _rows(t, rows, width, ld, dtype, device=None):
     """Address of a matrix of tokens: [rows, width] of the descriptor's type, rows `ld` elements apart."""
     if t is None:
         return None
-    assert t.is_cuda and t.shape == (rows, width) and _DTYPES.get(t.dtype) == dtype, "not the descriptor's matrix"
+    assert (t.is_cuda if device is None else t.get_device() == device), "not on the context's device"
+    assert t.shape == (rows, width) and _DTYPES.get(t.dtype) == dtype, "not the descriptor's matrix"
     a, b = t.stride()
     assert (b == 1 or width <= 1) and (a == ld or rows <= 1), "not the descriptor's row stride"
     return t.data_ptr()
 
 
-def _whole(t, shape, dtype):
+def _whole(t, shape, dtype, device=None):
     """Address of a contiguous tensor of this shape and torch type."""
     if t is None:
         return None
-    assert t.is_cuda and t.is_contiguous() and t.dtype == dtype and t.shape == shape, "not the descriptor's tensor"
+    assert (t.is_cuda if device is None else t.get_device() == device), "not on the context's device"
+    assert t.is_contiguous() and t.dtype == dtype and t.shape == shape, "not the descriptor's tensor"
     return t.data_ptr()
 
 
-def _kept(codes, steps, lead, width):
+def _kept(codes, steps, lead, width, device):
     """Addresses of rows in 8 bits: codes [*lead, whole blocks of width], steps [*lead, blocks]."""
     room = kept_room(width)
-    return _whole(codes, (*lead, room), torch.int8), _whole(steps, (*lead, room // KEPT_BLOCK), torch.uint8)
+    return _whole(codes, (*lead, room), torch.int8, device), _whole(steps, (*lead, room // KEPT_BLOCK), torch.uint8, device)
 
 
 # (the current stream's handle without an object around it, which costs 2.5 us a call)
@@ -436,42 +441,47 @@ class Context:
             _rows(dlogits, d.rows, d.V, d.ld_grad, d.dtype), _stream()), "wcc_distill_backward")
 
     # ---- a block on rows ----
+    def _own_stream(self):
+        device = _current_device()
+        assert device == self.device, "the current device is not the context's"
+        return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(device)
+
     def wcc_rows_keep(self, desc, x, codes, steps):
-        d = desc
-        _check(lib().wcc_rows_keep(self._h, C.byref(d), _rows(x, d.rows, d.width, d.ld, d.dtype), *_kept(codes, steps, (d.rows,), d.width),
-                                   _stream()), "wcc_rows_keep")
+        d, dev = desc, self.device
+        _check(lib().wcc_rows_keep(self._h, C.byref(d), _rows(x, d.rows, d.width, d.ld, d.dtype, dev),
+                                   *_kept(codes, steps, (d.rows,), d.width, dev), self._own_stream()), "wcc_rows_keep")
 
     def wcc_rows_restore(self, desc, codes, steps, x):
-        d = desc
-        _check(lib().wcc_rows_restore(self._h, C.byref(d), *_kept(codes, steps, (d.rows,), d.width),
-                                      _rows(x, d.rows, d.width, d.ld, d.dtype), _stream()), "wcc_rows_restore")
+        d, dev = desc, self.device
+        _check(lib().wcc_rows_restore(self._h, C.byref(d), *_kept(codes, steps, (d.rows,), d.width, dev),
+                                      _rows(x, d.rows, d.width, d.ld, d.dtype, dev), self._own_stream()), "wcc_rows_restore")
 
     def wcc_group_norm_forward(self, desc, x, gamma, beta, counts, y, stats=None, codes=None, steps=None):
-        d, f, rows = desc, torch.float32, desc.samples * desc.pixels
+        d, dev, f, rows = desc, self.device, torch.float32, desc.samples * desc.pixels
         _check(lib().wcc_group_norm_forward(
-            self._h, C.byref(d), _rows(x, rows, d.C, d.ldx, d.dtype), _whole(gamma, (d.C,), f), _whole(beta, (d.C,), f),
-            _whole(counts, (d.samples,), torch.int32), _rows(y, rows, d.C, d.ldy, d.dtype), _whole(stats, (d.samples, d.groups, 2), f),
-            *_kept(codes, steps, (rows,), d.C), _stream()), "wcc_group_norm_forward")
+            self._h, C.byref(d), _rows(x, rows, d.C, d.ldx, d.dtype, dev), _whole(gamma, (d.C,), f, dev), _whole(beta, (d.C,), f, dev),
+            _whole(counts, (d.samples,), torch.int32, dev), _rows(y, rows, d.C, d.ldy, d.dtype, dev),
+            _whole(stats, (d.samples, d.groups, 2), f, dev), *_kept(codes, steps, (rows,), d.C, dev), self._own_stream()), "wcc_group_norm_forward")
 
     def wcc_group_norm_backward(self, desc, x, codes, steps, gamma, beta, counts, stats, dy, dx=None, dgamma=None, dbeta=None):
-        d, f, rows = desc, torch.float32, desc.samples * desc.pixels
+        d, dev, f, rows = desc, self.device, torch.float32, desc.samples * desc.pixels
         _check(lib().wcc_group_norm_backward(
-            self._h, C.byref(d), _rows(x, rows, d.C, d.ldx, d.dtype), *_kept(codes, steps, (rows,), d.C), _whole(gamma, (d.C,), f),
-            _whole(beta, (d.C,), f), _whole(counts, (d.samples,), torch.int32), _whole(stats, (d.samples, d.groups, 2), f),
-            _rows(dy, rows, d.C, d.ldy, d.dtype), _rows(dx, rows, d.C, d.ldx, d.dtype), _whole(dgamma, (d.C,), f),
-            _whole(dbeta, (d.C,), f), _stream()), "wcc_group_norm_backward")
+            self._h, C.byref(d), _rows(x, rows, d.C, d.ldx, d.dtype, dev), *_kept(codes, steps, (rows,), d.C, dev), _whole(gamma, (d.C,), f, dev),
+            _whole(beta, (d.C,), f, dev), _whole(counts, (d.samples,), torch.int32, dev), _whole(stats, (d.samples, d.groups, 2), f, dev),
+            _rows(dy, rows, d.C, d.ldy, d.dtype, dev), _rows(dx, rows, d.C, d.ldx, d.dtype, dev), _whole(dgamma, (d.C,), f, dev),
+            _whole(dbeta, (d.C,), f, dev), self._own_stream()), "wcc_group_norm_backward")
 
     def wcc_gated_forward(self, desc, x, w_gate, w_up, y, codes=None, steps=None):
-        d, t = desc, _TORCH[desc.dtype]
+        d, dev, t = desc, self.device, _TORCH[desc.dtype]
         _check(lib().wcc_gated_forward(
-            self._h, C.byref(d), _rows(x, d.rows, d.C_in, d.ldx, d.dtype), _whole(w_gate, (d.C_out, d.C_in), t),
-            _whole(w_up, (d.C_out, d.C_in), t), _rows(y, d.rows, d.C_out, d.ldy, d.dtype), *_kept(codes, steps, (2, d.rows), d.C_out),
-            _stream()), "wcc_gated_forward")
+            self._h, C.byref(d), _rows(x, d.rows, d.C_in, d.ldx, d.dtype, dev), _whole(w_gate, (d.C_out, d.C_in), t, dev),
+            _whole(w_up, (d.C_out, d.C_in), t, dev), _rows(y, d.rows, d.C_out, d.ldy, d.dtype, dev),
+            *_kept(codes, steps, (2, d.rows), d.C_out, dev), self._own_stream()), "wcc_gated_forward")
 
     def wcc_gated_backward(self, desc, x, x_codes, x_steps, w_gate, w_up, codes, steps, dy, dx=None, dw_gate=None, dw_up=None):
-        d, t = desc, _TORCH[desc.dtype]
+        d, dev, t = desc, self.device, _TORCH[desc.dtype]
         _check(lib().wcc_gated_backward(
-            self._h, C.byref(d), _rows(x, d.rows, d.C_in, d.ldx, d.dtype), *_kept(x_codes, x_steps, (d.rows,), d.C_in),
-            _whole(w_gate, (d.C_out, d.C_in), t), _whole(w_up, (d.C_out, d.C_in), t), *_kept(codes, steps, (2, d.rows), d.C_out),
-            _rows(dy, d.rows, d.C_out, d.ldy, d.dtype), _rows(dx, d.rows, d.C_in, d.ldx, d.dtype),
-            _whole(dw_gate, (d.C_out, d.C_in), t), _whole(dw_up, (d.C_out, d.C_in), t), _stream()), "wcc_gated_backward")
+            self._h, C.byref(d), _rows(x, d.rows, d.C_in, d.ldx, d.dtype, dev), *_kept(x_codes, x_steps, (d.rows,), d.C_in, dev),
+            _whole(w_gate, (d.C_out, d.C_in), t, dev), _whole(w_up, (d.C_out, d.C_in), t, dev), *_kept(codes, steps, (2, d.rows), d.C_out, dev),
+            _rows(dy, d.rows, d.C_out, d.ldy, d.dtype, dev), _rows(dx, d.rows, d.C_in, d.ldx, d.dtype, dev),
+            _whole(dw_gate, (d.C_out, d.C_in), t, dev), _whole(dw_up, (d.C_out, d.C_in), t, dev), self._own_stream()), "wcc_gated_backward")

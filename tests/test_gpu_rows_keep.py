@@ -156,3 +156,20 @@ def test_no_rows(ctx):
     ctx.wcc_rows_keep(d, None, None, None)
     ctx.wcc_rows_restore(d, None, None, None)
     assert CODE["bf16"] == wcc.BF16
+
+
+def test_another_device_is_refused(ctx, monkeypatch):
+    """Tensors, or a context, of another device than the current one."""
+    x = torch.ones((3, 40), device="cuda")
+    d = wcc.make_rows_desc(3, 40, wcc.F32)
+    codes, steps = torch.zeros((3, 64), dtype=torch.int8, device="cuda"), torch.zeros((3, 2), dtype=torch.uint8, device="cuda")
+    with monkeypatch.context() as m:
+        m.setattr(wcc, "_current_device", lambda: 1)
+        with pytest.raises(AssertionError, match="the current device"):
+            ctx.wcc_rows_keep(d, x, codes, steps)
+    with monkeypatch.context() as m:
+        m.setattr(ctx, "device", 1)
+        with pytest.raises(AssertionError, match="not on the context's device"):
+            ctx.wcc_rows_keep(d, x, codes, steps)
+    ctx.wcc_rows_keep(d, x, codes, steps)
+    assert int(codes[0, 0]) == 64
