@@ -481,6 +481,8 @@ wcc_status wcc_group_norm_forward(wcc_ctx *ctx, const wcc_group_norm_desc *desc,
  * dz = dy act'(z), and the means taken over a group as above:
  *   dx = rstd (gamma dz - mean(gamma dz) - xh mean(gamma dz xh))
  *   dgamma = sum dz xh, dbeta = sum dz over all samples and pixels   (fp32, written whole)
+ * The mean is the fp32 value that stats holds: where it is far above the spread, xh is off by up to
+ * 2^-24 |mean| rstd here (the forward call keeps what it rounds off).
  * dx may be dy if ldx = ldy. */
 wcc_status wcc_group_norm_backward(wcc_ctx *ctx, const wcc_group_norm_desc *desc,
                                    const void *x /*nullable*/, const int8_t *codes, const uint8_t *steps,

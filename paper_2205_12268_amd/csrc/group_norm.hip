@@ -6,8 +6,10 @@
 // x (backward) is the tensor, or the values that its codes stand for, with the statistics of the tensor.
 //
 // A thread owns a vector of 16 bytes of channels and walks over pixels, so that sums are by channel and groups may have any size.  The
-// sums of x and x^2 are fp64: products of fp32 values are exact there, so that a mean far above the spread costs nothing that a
-// shift would have to bring back.
+// statistics come from fp64 sums of x - s and its square, s the first pixel's value of the group's first channel: the variance of n
+// values is at least (s - mean)^2 / n, so what the mean takes from the squares leaves an error of n 2^-53 at most (of x itself, mean^2 /
+// var 2^-53: 10^-4 for a mean of 10^4 beside a spread of 0.05).  The mean is kept as a fp32 value and the rest that it rounds off, so y is as near for a
+// mean far above the spread.  The backward pass has the rounded mean of `stats` alone: its xh are off by up to 2^-24 |mean| rstd.
 //
 // Maps that one workgroup's registers hold (a sample, some of its groups) take one launch.  Larger ones take three: sums of chunks of
 // pixels by channel; a small one that joins them; a second pass that goes backwards over the chunks, so that it begins with what
@@ -29,7 +31,7 @@ struct Shape {
 // What is kept in the workspace.
 struct Sums {
   double2 *part;  // [samples][chunks][C]
-  float4 *group;  // [samples][groups]: mean, rstd, m1, m2
+  float4 *group;  // [samples][groups]: forward: mean, rstd, the mean's rest, s (from the first pass); backward: mean, rstd, m1, m2
   double2 *chan;  // [samples][C]: backward, sums over a sample
   int chunks;
   int64_t chunk;  // pixels of one
@@ -39,14 +41,16 @@ __device__ __forceinline__ int64_t pixels_of(const int32_t *counts, int64_t pixe
   return counts ? min((int64_t)max(counts[sample], 0), pixels) : pixels;
 }
 
-// mean and rstd from the sums of values and of their squares, by 1 / their number.  The reciprocal root is the hardware's, two steps of
-// Newton's behind it.
-__device__ __forceinline__ float2 stat_of(const double2 &s, double per, float eps) {
-  const double mean = s.x * per, rest = s.y * per - mean * mean, v = (rest < 0.0 ? 0.0 : rest) + (double)eps;  // (NaN stays)
+// mean, rstd and the mean's rest from the sums of values less s and of their squares, by 1 / their number.  The reciprocal root is the
+// hardware's, two steps of Newton's behind it.
+__device__ __forceinline__ float4 stat_of(const double2 &sum, double per, float s, float eps) {
+  const double off = sum.x * per, rest = sum.y * per - off * off, v = (rest < 0.0 ? 0.0 : rest) + (double)eps;  // (NaN stays)
   double r = __builtin_amdgcn_rsq(v);
   r = r * fma(-0.5 * v * r, r, 1.5);
   r = r * fma(-0.5 * v * r, r, 1.5);
-  return float2{(float)mean, (float)r};
+  const double mean = (double)s + off;
+  const float near = (float)mean;
+  return float4{near, (float)r, (float)(mean - (double)near), 0.f};
 }
 
 // The groups of neighbouring channels from c on, by one division.
@@ -250,9 +254,16 @@ __global__ __launch_bounds__(256) void norm_sums_kernel(const T *__restrict__ x,
   constexpr int VE = VecOf<T>::N;
   __shared__ Room<256, VE> room;
   const Place<VE> at(blockIdx.x, d, s, counts, lanes);
+  const T *p = x + (int64_t)at.sample * d.pixels * d.ldx;
+  if (at.chunk == 0) {  // (what joins the chunks may find x overwritten by y)
+    const bool some = pixels_of(counts, d.pixels, at.sample) > 0;
+    for (int g = blockIdx.y * 256 + threadIdx.x; g < d.groups; g += gridDim.y * 256)
+      s.group[(int64_t)at.sample * d.groups + g].w = some ? widen(p[g * d.per]) : 0.f;
+  }
   double sum[VE] = {}, sq[VE] = {};
-  if (at.ty < at.rows && at.c0 < d.C) {
-    const T *p = x + (int64_t)at.sample * d.pixels * d.ldx;
+  if (at.ty < at.rows && at.c0 < d.C && at.begin < at.end) {
+    double first[VE];
+    by_groups<VE>(at.c0, d.per, d.groups - 1, [&](int g) { return widen(p[g * d.per]); }, [&](int j, float q) { first[j] = q; });
     const Columns<T> cols(at.c0, d.C - at.c0, d.C, d.C % VE != 0);
     for (int64_t t = at.begin; t < at.end; t += 4 * at.rows) {
       u32x4 v[4];
@@ -263,7 +274,7 @@ __global__ __launch_bounds__(256) void norm_sums_kernel(const T *__restrict__ x,
         v[u] = cols.fix(v[u]);
 #pragma unroll
         for (int j = 0; j < VE; ++j) {
-          const double f = elem<T>(v[u], j);
+          const double f = elem<T>(v[u], j) - first[j];
           sum[j] += f, sq[j] = fma(f, f, sq[j]);
         }
       }
@@ -284,6 +295,7 @@ __global__ __launch_bounds__(NT) void norm_join_kernel(const int32_t *__restrict
   const int64_t n = pixels_of(counts, d.pixels, sample);
   const int chunks = (int)min((int64_t)s.chunks, (n + s.chunk - 1) / s.chunk);
   const double per = 1.0 / (double)max(n * d.per, (int64_t)1);
+  const float first = BACK ? 0.f : s.group[blockIdx.x].w;
   double2 all = {0.0, 0.0};
   for (int c0 = 0; c0 < d.per; c0 += lanes) {
     const int c = c0 + col;
@@ -319,8 +331,8 @@ __global__ __launch_bounds__(NT) void norm_join_kernel(const int32_t *__restrict
   if constexpr (BACK) {
     s.group[at] = float4{stats[2 * at], stats[2 * at + 1], (float)(all.x * per), (float)(all.y * per)};
   } else {
-    const float2 q = stat_of(all, per, d.eps);
-    s.group[at] = float4{q.x, q.y, 0.f, 0.f};
+    const float4 q = stat_of(all, per, first, d.eps);
+    s.group[at] = q;
     if (stats) stats[2 * at] = q.x, stats[2 * at + 1] = q.y;
   }
 }
@@ -338,6 +350,9 @@ __device__ __forceinline__ void join_short(int sample, bool first, int64_t n, co
   const int chunks = (int)min((int64_t)s.chunks, (n + s.chunk - 1) / s.chunk);
   const double per = 1.0 / (double)max(n * d.per, (int64_t)1);
   const int parts = max(256 / d.C, 1);
+  if constexpr (!BACK) {
+    for (int g = threadIdx.x; g < d.groups; g += 256) room.group[g].w = s.group[(int64_t)sample * d.groups + g].w;
+  }
   for (int i = threadIdx.x; i < parts * d.C; i += 256) {
     const int c = i % d.C;
     const double2 *p = s.part + (int64_t)sample * s.chunks * d.C + c;
@@ -358,8 +373,8 @@ __device__ __forceinline__ void join_short(int sample, bool first, int64_t n, co
     if constexpr (BACK) {
       room.group[g] = float4{stats[2 * at], stats[2 * at + 1], (float)(room.all[g].x * per), (float)(room.all[g].y * per)};
     } else {
-      const float2 q = stat_of(room.all[g], per, d.eps);
-      room.group[g] = float4{q.x, q.y, 0.f, 0.f};
+      const float4 q = stat_of(room.all[g], per, room.group[g].w, d.eps);
+      room.group[g] = q;
       if (stats && first) stats[2 * at] = q.x, stats[2 * at + 1] = q.y;
     }
   }
@@ -387,7 +402,7 @@ __global__ __launch_bounds__(256) void norm_apply_kernel(const T *x, const float
         if constexpr (SHORT) return room.group[group];
         else return s.group[(int64_t)at.sample * d.groups + group];
       },
-      [&](int j, const float4 &q) { mean[j] = q.x, g[j] *= q.y; });
+      [&](int j, const float4 &q) { mean[j] = q.x, g[j] *= q.y, b[j] = fmaf(-q.z, g[j], b[j]); });
   const int64_t row0 = (int64_t)at.sample * d.pixels;
   const Columns<T> cols(c0, d.C - c0, d.C, d.C % (KEEP ? kKept : VE) != 0);
   for (int64_t t = at.begin; t < at.end; t += 4 * at.rows) {
@@ -621,7 +636,13 @@ __global__ __launch_bounds__(NT) void norm_held_kernel(const T *x, const float *
   const HeldPlace<T, NT> at(d, counts, take, lanes);
   u32x4 v[HELD];
   const Columns<T> cols = at.columns(d);
-  if (at.n > 0) cols.load(v, [&](int i) { return x + at.some_row(i) * d.ldx; });
+  const T *top = x + at.row0 * d.ldx + at.first * d.per;
+  float first[VE] = {};
+  if (at.n > 0) {
+    cols.load(v, [&](int i) { return x + at.some_row(i) * d.ldx; });
+    by_groups<VE>(at.col * VE, d.per, at.groups - 1, [&](int g) { return widen(top[g * d.per]); }, [&](int j, float q) { first[j] = q; });
+  }
+  const float own_first = at.n > 0 ? widen(top[min((int)threadIdx.x, at.groups - 1) * d.per]) : 0.f;
 #pragma unroll
   for (int i = 0; i < HELD; ++i) v[i] = at.there(i) ? cols.fix(v[i]) : u32x4{};
   float g[VE], b[VE], mean[VE];
@@ -629,16 +650,18 @@ __global__ __launch_bounds__(NT) void norm_held_kernel(const T *x, const float *
   const double per = 1.0 / (double)max(at.n * d.per, (int64_t)1);
   double sum[VE] = {}, sq[VE] = {};
 #pragma unroll
-  for (int i = 0; i < HELD; ++i)
+  for (int i = 0; i < HELD; ++i) {
+    if (!at.there(i)) break;
 #pragma unroll
     for (int j = 0; j < VE; ++j) {
-      const double f = elem<T>(v[i], j);
+      const double f = (double)elem<T>(v[i], j) - (double)first[j];
       sum[j] += f, sq[j] = fma(f, f, sq[j]);
     }
+  }
   join_held<T, NT>(at, d.per, sum, sq, room, col_room, all, [](int, double2) {}, [](int) { return 1.0; });
-  float2 *stat_room = reinterpret_cast<float2 *>(col_room);  // (read by nobody any more)
-  for (int g = threadIdx.x; g < at.groups; g += NT) {
-    const float2 q = stat_of(all[g], per, d.eps);
+  float4 *stat_room = reinterpret_cast<float4 *>(col_room);  // (read by nobody any more)
+  if (const int g = threadIdx.x; g < at.groups) {            // (a group for each thread at most)
+    const float4 q = stat_of(all[g], per, own_first, d.eps);
     stat_room[g] = q;
     if (stats) {
       float *p = stats + 2 * ((int64_t)at.sample * d.groups + at.first + g);
@@ -651,7 +674,7 @@ __global__ __launch_bounds__(NT) void norm_held_kernel(const T *x, const float *
   if (!mine) return;
   by_groups<VE>(
       at.col * VE, d.per, at.groups - 1, [&](int group) { return stat_room[group]; },
-      [&](int j, const float2 &q) { mean[j] = q.x, g[j] *= q.y; });
+      [&](int j, const float4 &q) { mean[j] = q.x, g[j] *= q.y, b[j] = fmaf(-q.z, g[j], b[j]); });
 #pragma unroll
   for (int i = 0; i < HELD; ++i) {
     if (at.ty + (int64_t)i * at.rows >= at.n) break;
