@@ -777,6 +777,9 @@ __global__ __launch_bounds__(NT) void norm_grad_held_kernel(Input<T, KEPT> in, c
 }
 
 // ---- host ---------------------------------------------------------------------------------------------------
+// A launch has fewer than 2^32 threads.
+bool launches(int64_t workgroups, int threads) { return workgroups * threads < (int64_t)1 << 32; }
+
 // Groups of a workgroup whose registers hold their sample, and its threads.
 struct Held {
   int take, threads, held;  // take 0: no workgroup's registers do; held: vectors of a thread, at most
@@ -809,7 +812,7 @@ Held held_of(const wcc_group_norm_desc &d, int VE, bool kept) {
     if (width > 512) break;
     const int lanes = held_lanes(d, take, VE, kept);
     for (const int threads : {256, 512}) {
-      if (width > threads || lanes > threads) continue;
+      if (width > threads || lanes > threads || !launches((int64_t)d.samples * ((d.groups + take - 1) / take), threads)) continue;
       const int64_t most = (d.pixels + threads / lanes - 1) / (threads / lanes);
       if (most > kHeld) continue;
       best = Held{take, threads, most <= 2 ? 2 : kHeld};
@@ -888,12 +891,13 @@ void by_held(const Held &h, F f) {
   else h.held == 2 ? f(many, two) : f(many, all);
 }
 
-// The chunks joined: by 1024 threads a group where it has many pairs of sums, which a few workgroups would take long to read.
+// The chunks joined: by 1024 threads a group where it has many pairs of sums, which a few workgroups would take long to read (and as many
+// workgroups as a launch of these does not have are not few).
 template <bool BACK>
 void join(const wcc_group_norm_desc &d, const Plan &p, const NormArgs &g, const Shape &sh, const Sums &s, hipStream_t st) {
   const unsigned n = (unsigned)(d.groups * d.samples);
   const float *gamma = BACK ? g.gamma : nullptr;
-  if ((int64_t)p.chunks * (d.C / d.groups) > 2048) norm_join_kernel<BACK, 1024><<<n, 1024, 0, st>>>(g.counts, sh, s, gamma, g.stats, join_lanes(d));
+  if ((int64_t)p.chunks * (d.C / d.groups) > 2048 && launches(n, 1024)) norm_join_kernel<BACK, 1024><<<n, 1024, 0, st>>>(g.counts, sh, s, gamma, g.stats, join_lanes(d));
   else norm_join_kernel<BACK, 256><<<n, 256, 0, st>>>(g.counts, sh, s, gamma, g.stats, join_lanes(d));
 }
 
