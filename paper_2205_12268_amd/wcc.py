@@ -227,6 +227,8 @@ def kept_room(width: int) -> int:
 
 
 def _workspace_of(desc) -> int:
+    if isinstance(desc, RowsDesc):  # (its calls need none)
+        return 0
     call = {BlockDesc: "wcc_block_workspace_bytes", AdapterDesc: "wcc_adapter_workspace_bytes",
             ScoresDesc: "wcc_scores_workspace_bytes", DistillDesc: "wcc_distill_workspace_bytes",
             GroupNormDesc: "wcc_group_norm_workspace_bytes", GatedDesc: "wcc_gated_workspace_bytes"}.get(type(desc), "wcc_workspace_bytes")
