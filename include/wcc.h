@@ -499,9 +499,11 @@ typedef struct {
   int32_t C_in, C_out;     /* 1 .. 2^20                                                           */
   int32_t act;             /* wcc_act                                                             */
   int32_t dtype;           /* WCC_F32 or WCC_BF16                                                */
-  int32_t train;           /* 0: the workspace holds the forward call alone; else both            */
+  int32_t train;           /* 0: the workspace holds the forward call alone; else both; see below */
   int64_t ldx, ldy;        /* row strides of x and dx, of y and dy: < 2^31                        */
 } wcc_gated_desc;
+/* A value of `train`: both calls, and of bf16 the gradients with dg and du in 16 bits. */
+#define WCC_TRAIN_FINE 2
 
 /* Workspace of the calls below for this descriptor (a multiple of 256).  With more than 2^23 tiles of
  * 128 rows by 64 channels or of 64 C_in by 64 C_out: WCC_ERR_UNSUPPORTED. */
@@ -517,8 +519,9 @@ wcc_status wcc_gated_forward(wcc_ctx *ctx, const wcc_gated_desc *desc, const voi
  *   dg = dy u act'(g), du = dy act(g)
  *   dx = w_gate^T dg + w_up^T du      dw_gate = sum_t dg x^T      dw_up = sum_t du x^T
  * x is x or, with x NULL, the values that x_codes and x_steps stand for; g and u are those that codes
- * and steps stand for, or made again with codes NULL.  bf16: dg and du are rounded to bf16 on their
- * way into the products.  x (or its codes) may be NULL if codes are given and dw_gate and dw_up are
+ * and steps stand for, or made again with codes NULL.  bf16: dg and du are rounded on their way into
+ * the products, to bf16's 8 bits, or to 16 where rows * C_out < 2^17 or train is WCC_TRAIN_FINE (which
+ * takes up to 2.5 times as long and twice the room for them).  x (or its codes) may be NULL if codes are given and dw_gate and dw_up are
  * NULL, the weights if codes are given and dx is NULL.  Outputs overlap no input. */
 wcc_status wcc_gated_backward(wcc_ctx *ctx, const wcc_gated_desc *desc, const void *x,
                               const int8_t *x_codes, const uint8_t *x_steps, const void *w_gate,

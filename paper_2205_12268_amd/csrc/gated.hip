@@ -82,6 +82,7 @@ size_t up(size_t v) { return (v + 255) / 256 * 256; }
 struct Plan {
   bool gemm, copy_x, copy_w;  // tiles fed straight from memory
   int parts;                  // of dg and du
+  bool few;                   // they are two because dg and du are few
   size_t d, x, w, part, bytes;
   int64_t room, ldx, k;  // of d's halves; of rows and weights that were copied; C_in in whole chunks of 16 bytes
 };
@@ -93,7 +94,9 @@ constexpr int kThin = 64;  // rows of few
 // 31.0, 777 rows 1000 <-> 1537 at odd strides 43.8 and 102, in fp32 173 and 312; 30 rows 4001 <-> 8000 234 and 252; one row 3001 <-> 5001,
 // all copies, 166 and 163).  A pair of projections has less to win: bf16 from 2^25 products on (128 rows 128 -> 256, 2^23, 4.6 us and
 // 4.4, 256 -> 256 5.4 and 7.1), with copies from 2^27 on (500 rows 301 -> 743 9.3 and 11.2, 512 rows 33 -> 64 6.3 and 4.5), fp32 always, with
-// copies from 3 * 2^27 on (777 rows 333 -> 1000 21.9 and 26.7, 300 rows 301 -> 743 18.1 and 13.4).
+// copies from 3 * 2^27 on (777 rows 333 -> 1000 21.9 and 26.7, 300 rows 301 -> 743 18.1 and 13.4).  Made again for few dg and du (kFew) they
+// stay in tiles by way of registers: whole backward passes of 100 rows 1024 <-> 640 take 27 us so and 32, 1000 rows 1001 <-> 120 40 and 45, 1000 rows
+// 4096 <-> 130 60 and 57.
 Plan plan_of(const wcc_gated_desc &g, bool backward) {
   Plan p = {};
   const int size = g.dtype == WCC_F32 ? 4 : 2;
@@ -104,7 +107,8 @@ Plan plan_of(const wcc_gated_desc &g, bool backward) {
   const bool thin = size == 2 && g.rows <= kThin;
   const double least = size == 2 ? (p.copy_x && !backward ? 1 << 27 : 1 << 25) : p.copy_x && !backward ? 3 << 27 : 0;
   p.gemm = !thin && products >= least;
-  p.parts = size == 2 && g.rows * (int64_t)g.C_out < kFew ? 2 : 1;
+  p.few = size == 2 && g.rows * (int64_t)g.C_out < kFew;
+  p.parts = size == 2 && (p.few || g.train == WCC_TRAIN_FINE) ? 2 : 1;
   if (!backward && !p.gemm) p.copy_x = p.copy_w = false;
   size_t parts = tile_gate_parts(g.rows, g.C_out, g.C_in, size), at = 0;  // (tensors at odd addresses take these tiles)
   if (size == 2 && g.rows <= kThin) parts = std::max(parts, thin_gate_parts(g.rows, g.C_out, p.k));
@@ -173,7 +177,7 @@ hipError_t gate_of(const wcc_gated_desc &d, const Plan &p, const Gate<T> &gate, 
   if constexpr (sizeof(T) == 2) {
     if (d.rows <= kThin && o.takes) return thin_gate(gate, d.act, back, o.x, o.wg, o.wu, o.ldw, p.k, part, s);
   }
-  if (p.gemm && o.takes && !(back && p.parts == 2)) return gemm_gate<T>(gate, d.act, back, o.x, o.wg, o.wu, o.ldw, p.k, part, s);
+  if (p.gemm && o.takes && !(back && p.few)) return gemm_gate<T>(gate, d.act, back, o.x, o.wg, o.wu, o.ldw, p.k, part, s);
   return tile_gate<T>(gate, d.act, back, o.x, o.wg, o.wu, o.ldw, d.C_in, part, s);
 }
 

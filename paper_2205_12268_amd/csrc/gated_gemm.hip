@@ -290,8 +290,9 @@ __device__ __forceinline__ void leave(const unsigned char *lds, F f) {
 }
 
 // ---- the two projections -------------------------------------------------------------------------------------
-// PARTS: a range of k, whose sums go to part [splits][rows][2][room].
-template <class T, int BT, int BO, int ACT, bool BACK, bool PARTS>
+// PARTS: a range of k, whose sums go to part [splits][rows][2][room].  NP: parts of dg and du in d (known here: a loop over p.parts makes
+// the one that nearly all calls have 1 to 2 % slower, 560 to 571 us for 4096 rows 2048 <-> 2 x 5632).
+template <class T, int BT, int BO, int ACT, bool BACK, bool PARTS, int NP = 1>
 __global__ __launch_bounds__(256, BO == 128 ? 2 : 1) void gate_gemm_kernel(Gate<T> p, Operand x, Operand w, int64_t tiles_t, int tiles_o,
                                                                          int64_t chunk, float *__restrict__ part) {
   using G = Gemm<T, BT, BO, false, false, false, true, false>;
@@ -362,40 +363,57 @@ __global__ __launch_bounds__(256, BO == 128 ? 2 : 1) void gate_gemm_kernel(Gate<
   for (int r = 0; r < ET; ++r) {
     const int64_t t = tw + r * 32 + ln;
     unsigned char *second = own + 32 * Row;
+    if constexpr (BACK) {
+#pragma unroll 1
+      for (int part = 0; part < NP; ++part) {
+        int outs = p.outs;
+        if constexpr (NP > 1) asm volatile("" : "+s"(outs));  // (comparisons with it made anew for each part, or they would be held for both)
 #pragma unroll
-    for (int j = 0; j < Pairs; ++j) {
-      const f32x16 &ga = acc[2 * j][r], &ua = acc[2 * j + 1][r];  // (lines behind the last are 0)
-      if constexpr (BACK) {
-        const int o = ow + j * 32;
+        for (int j = 0; j < Pairs; ++j) {
+          const f32x16 &ga = acc[2 * j][r], &ua = acc[2 * j + 1][r];  // (lines behind the last are 0)
+          const int o = ow + j * 32;
 #pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-          const int at = o + result_line(i, half);
-          float dg[4], du[4];
-          uint2 top = {0, 0};
-          if (t < p.rows && at < p.outs) {
-            const bf16_t *q = p.dy + t * p.ldy + at;
-                  if (at + 4 <= p.outs) {
-              const u32x2_any v = *reinterpret_cast<const u32x2_any *>(q);
-              top = uint2{v.x, v.y};
-            } else {
-              top.x = q[0];
-              if (at + 1 < p.outs) top.x |= (uint32_t)q[1] << 16;
-              if (at + 2 < p.outs) top.y = q[2];
+          for (int i = 0; i < 16; i += 4) {
+            const int at = o + result_line(i, half);
+            float dg[4], du[4];
+            uint2 top = {0, 0};
+            if (t < p.rows && at < outs) {
+              const bf16_t *q = p.dy + t * p.ldy + at;
+              if (at + 4 <= outs) {
+                const u32x2_any v = *reinterpret_cast<const u32x2_any *>(q);
+                top = uint2{v.x, v.y};
+              } else {
+                top.x = q[0];
+                if (at + 1 < outs) top.x |= (uint32_t)q[1] << 16;
+                if (at + 2 < outs) top.y = q[2];
+              }
             }
-          }
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            float v, s;
-            act_of<bf16_t, ACT>(ga[i + k], v, s);
-            const uint32_t word = k < 2 ? top.x : top.y;
-            const float dy = __uint_as_float(k & 1 ? word & 0xffff0000u : word << 16);
-            dg[k] = dy * ua[i + k] * s, du[k] = dy * v;
-            if (at + k >= p.outs) dg[k] = du[k] = 0.f;  // (what lies behind is 0)
+            for (int k = 0; k < 4; ++k) {
+              float v, s;
+              act_of<bf16_t, ACT>(ga[i + k], v, s);
+              const uint32_t word = k < 2 ? top.x : top.y;
+              const float dy = __uint_as_float(k & 1 ? word & 0xffff0000u : word << 16);
+              dg[k] = dy * ua[i + k] * s, du[k] = dy * v;
+              if (at + k >= outs) dg[k] = du[k] = 0.f;  // (what lies behind is 0)
+              if (part > 0) dg[k] = left_of(dg[k], narrow<bf16_t>(dg[k])), du[k] = left_of(du[k], narrow<bf16_t>(du[k]));
+            }
+            put<Row>(own, ln, j * 8 + (i >> 1) + half, narrow4(dg[0], dg[1], dg[2], dg[3]));
+            put<Row>(second, ln, j * 8 + (i >> 1) + half, narrow4(du[0], du[1], du[2], du[3]));
           }
-          put<Row>(own, ln, j * 8 + (i >> 1) + half, narrow4(dg[0], dg[1], dg[2], dg[3]));
-          put<Row>(second, ln, j * 8 + (i >> 1) + half, narrow4(du[0], du[1], du[2], du[3]));
         }
-      } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          leave<Row>(h ? second : own, [&](int row, int b, const u32x4 &v) {
+            const int o = ow + b / 2;
+            if (tw + r * 32 + row < p.rows && o < p.room)
+              *reinterpret_cast<u32x4 *>(p.d + (((tw + r * 32 + row) * NP + part) * 2 + h) * p.room + o) = v;
+          });
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < Pairs; ++j) {
+        const f32x16 &ga = acc[2 * j][r], &ua = acc[2 * j + 1][r];  // (lines behind the last are 0)
         if (p.codes) {
           uint32_t m[2] = {0, 0};
 #pragma unroll
@@ -429,16 +447,6 @@ __global__ __launch_bounds__(256, BO == 128 ? 2 : 1) void gate_gemm_kernel(Gate<
           put<Row>(own, ln, j * 8 + (i >> 1) + half, narrow4(f[0], f[1], f[2], f[3]));
         }
       }
-    }
-    if constexpr (BACK) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        leave<Row>(h ? second : own, [&](int row, int b, const u32x4 &v) {
-          const int o = ow + b / 2;
-          if (tw + r * 32 + row < p.rows && o < p.room)
-            *reinterpret_cast<u32x4 *>(p.d + ((tw + r * 32 + row) * 2 + h) * p.room + o) = v;
-        });
-    } else {
       leave<Row>(own, [&](int row, int b, const u32x4 &v) {
         const int o = ow + b / 2;
         if (tw + r * 32 + row < p.rows && o < p.outs) store_part<bf16_t>(p.y + (tw + r * 32 + row) * p.ldy + o, p.outs - o, v);
@@ -691,6 +699,8 @@ hipError_t gemm_gate(const Gate<T> &p, int act, bool back, const Side<T> &x, con
       const unsigned n = (unsigned)(tiles_t * tiles_o * plan.splits);
       if (plan.splits > 1) {
         if constexpr (BO == 128 && ACT == WCC_ACT_NONE) gate_gemm_kernel<T, BT, BO, ACT, false, true><<<n, 256, 0, s>>>(p, xo, wo, tiles_t, tiles_o, plan.chunk, part);
+      } else if (back && sizeof(T) == 2 && p.parts == 2) {
+        if constexpr (sizeof(T) == 2) gate_gemm_kernel<T, BT, BO, ACT, true, false, 2><<<n, 256, 0, s>>>(p, xo, wo, tiles_t, tiles_o, 0, nullptr);
       } else if (back) {
         gate_gemm_kernel<T, BT, BO, ACT, true, false><<<n, 256, 0, s>>>(p, xo, wo, tiles_t, tiles_o, 0, nullptr);
       } else {

@@ -19,6 +19,7 @@ STATIC_SCRATCH_BYTES = 64 << 20  # WCC_STATIC_SCRATCH_BYTES of wcc.h
 NORM_L1, NORM_L2 = 0, 1
 ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU = 0, 1, 2, 3
 KEPT_BLOCK = 32  # WCC_KEPT_BLOCK of wcc.h
+TRAIN_FINE = 2  # WCC_TRAIN_FINE of wcc.h
 STAGES = ("haar_fwd", "norm_select", "gather", "pointwise", "scatter_ihaar", "event_pair",
           "depthwise")
 
@@ -218,7 +219,8 @@ def make_group_norm_desc(samples, pixels, Cc, groups, dtype, act=ACT_NONE, eps=1
 
 
 def make_gated_desc(rows, C_in, C_out, dtype, act=ACT_SILU, train=False, ldx=None, ldy=None) -> GatedDesc:
-    return GatedDesc(rows, C_in, C_out, act, dtype, int(bool(train)), C_in if ldx is None else ldx, C_out if ldy is None else ldy)
+    """train: False, True, or TRAIN_FINE."""
+    return GatedDesc(rows, C_in, C_out, act, dtype, int(train) if train == TRAIN_FINE else int(bool(train)), C_in if ldx is None else ldx, C_out if ldy is None else ldy)
 
 
 def kept_room(width: int) -> int:
