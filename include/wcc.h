@@ -521,8 +521,9 @@ wcc_status wcc_gated_forward(wcc_ctx *ctx, const wcc_gated_desc *desc, const voi
  * x is x or, with x NULL, the values that x_codes and x_steps stand for; g and u are those that codes
  * and steps stand for, or made again with codes NULL.  bf16: dg and du are rounded on their way into
  * the products, to bf16's 8 bits, or to 16 where rows * C_out < 2^17 or train is WCC_TRAIN_FINE (which
- * takes up to 2.5 times as long and twice the room for them).  x (or its codes) may be NULL if codes are given and dw_gate and dw_up are
- * NULL, the weights if codes are given and dx is NULL.  Outputs overlap no input. */
+ * takes up to 2.5 times as long, and twice the room for them).  x (or its codes) may be NULL if codes
+ * are given and dw_gate and dw_up are NULL, the weights if codes are given and dx is NULL.  Outputs
+ * overlap no input. */
 wcc_status wcc_gated_backward(wcc_ctx *ctx, const wcc_gated_desc *desc, const void *x,
                               const int8_t *x_codes, const uint8_t *x_steps, const void *w_gate,
                               const void *w_up, const int8_t *codes, const uint8_t *steps,

@@ -60,7 +60,8 @@ class GatedBlock:
         return self.out
 
     def backward(self, dout: torch.Tensor, counts=None) -> torch.Tensor:
-        """The gradient of the input for a gradient of the output; those of the weights are left in `grads`."""
+        """The gradient of the input for a gradient of the output; those of the weights are left in `grads`.  Rows that `counts` leaves out
+        take part in them with an input of 0, so `dout` has to be finite there too."""
         ctx, m, g = self.ctx, self.masters, self.grads
         ctx.wcc_adapter_backward(self.down, None, self.w_down, None, None, None, None, None, dout, self.dh)
         ctx.wcc_gated_backward(self.gated, None, *self.n_kept, self.w_gate, self.w_up, *self.h_kept, self.dh, self.dn, g["w_gate"], g["w_up"])

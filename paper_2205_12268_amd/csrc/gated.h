@@ -133,6 +133,7 @@ struct Product {
 size_t tile_gate_parts(int64_t rows, int64_t outs, int64_t k, int size);
 size_t tile_product_parts(int64_t rows, int64_t lines, int64_t k, int batches, int size);
 
+// (all three ways to a pair of projections leave as many parts of dg and du as p.parts says)
 template <class T>
 hipError_t tile_gate(const Gate<T> &p, int act, bool back, const Side<T> &x, const T *w_gate, const T *w_up, int64_t ldw, int64_t k,
                      float *part, hipStream_t s);
@@ -142,7 +143,7 @@ hipError_t join_gate(const Gate<T> &p, int act, bool back, int splits, const flo
 template <class T, bool AT>
 hipError_t tile_product(const Product<T> &p, float *part, hipStream_t s);
 
-// Many rows (gated_gemm.hip).  Operands whose k or lines are contiguous and 16 bytes a load: pointers and strides are multiples.
+// Straight from memory (gated_gemm.hip).  Operands whose k or lines are contiguous and 16 bytes a load: pointers and strides are multiples.
 bool gemm_takes(const void *p, int64_t ld, int64_t width, int size);
 size_t gemm_gate_parts(int64_t rows, int64_t outs, int64_t k, int size);
 template <class T>

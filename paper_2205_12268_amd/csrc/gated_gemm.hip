@@ -1,9 +1,10 @@
-// The products of the gated block for many rows of bf16: the matrix cores fed from LDS, which loads go to straight from memory.
+// The products of the gated block fed straight from memory: projections of many rows (bf16, from 2^25 products on) or of any (fp32), and all
+// products of a backward pass, down to one row, wherever operands begin on 16 bytes and their lines lie a multiple of it apart.
 //
-// A workgroup of four waves has BT x BO results and two stages of 64 k in LDS; loads (16 bytes a lane) go there without passing
-// registers.  A wave's operands of a whole stage fit its registers beside the results, so a stage's half of LDS is free after a quarter
-// of its products: from there on the loads of the stage after the next go out, one between every few products.  Two barriers a stage:
-// LDS is read; the next stage is there.
+// A workgroup of four waves has BT x BO results and two stages of 128 bytes of k (64 bf16, 32 fp32) in LDS; loads (16 bytes a lane) go
+// there without passing registers.  A wave's operands of a whole stage fit its registers beside the results, so a stage's half of LDS is
+// free after a quarter of its products: from there on the loads of the stage after the next go out, one between every few products.  Two
+// barriers a stage: LDS is read; the next stage is there.
 // LDS has no padding (such a load writes 1 KiB in a row), so the 16-byte chunks of a line are exchanged by a key of the line, at the load
 // by choosing which chunk of memory a lane asks for: the lines that a read takes at once are on different banks.  Operands come
 // either with k contiguous, or with their lines contiguous (the weights for dx; both for the weights' gradients): LDS holds lines of k then
@@ -11,11 +12,13 @@
 // Loads go through buffer descriptors that end where the operand does: what lies behind the last line or the last k is 0 without a
 // branch, and the stages past the last are loads of nothing.
 //
-// Bound by the matrix cores, whose clock falls to 1.65 GHz under them: 8192 rows 2048 -> 2 x 8192 bf16 take 424 to 487 us by card and
-// temperature (1.3 to 1.13 PFLOP/s; the library's product by itself, without activation and join, 426), 69 % of the cycles a product.  The
-// gradients of 4096 rows 2048 <-> 2 x 5632, dx and the weights', 365 (1.03 PFLOP/s; the library's two 344): there operands whose lines are
-// contiguous take twice as many reads of LDS, and a product is on its way in 47 % of the cycles.  Four stages of 128-wide tiles in
-// place of two, and tiles of 64 rows, were slower.
+// bf16 is bound by the matrix cores, whose clock falls to 1.65 GHz under them: 8192 rows 2048 -> 2 x 8192 bf16 take 424 to 487 us by card
+// and temperature (1.3 to 1.13 PFLOP/s; the library's product by itself, without activation and join, 426), 69 % of the cycles a product.
+// The gradients of 4096 rows 2048 <-> 2 x 5632, dx and the weights', 365 (1.03 PFLOP/s; the library's two 344): there operands whose lines
+// are contiguous take twice as many reads of LDS, and a product is on its way in 47 % of the cycles; the ends of these 256-wide tiles, a
+// bf16 and a fp32 one in one kernel, spill 178 registers, which shows in 108 MB written for 63 MB of results.  Four stages of 128-wide
+// tiles in place of two, and tiles of 64 rows, were slower.  fp32: 8192 rows 2048 <-> 2048 3010 us backward, projections too (137 of 153
+// TFLOP/s); 1156 rows 160 -> 2 x 960 17.5 for 4.6 of products, 285 tiles of five stages on 256 compute units.
 #include <algorithm>
 
 #include "gated.h"

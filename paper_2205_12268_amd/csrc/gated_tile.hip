@@ -1,4 +1,6 @@
 // The products of the gated block in tiles of 128 (or 64) x 128 through LDS by way of registers: any type, alignment and stride.
+// Projections come here that are too small for tiles fed straight from memory to win, or whose copies would cost more than they give; the
+// gradients' products (tile_product) only where a tensor does not begin on 16 bytes or a row is 4 MiB and longer.
 //
 // Four waves of 64 (32) x 64 results; stages of 128 bytes of k (64 bf16 or 32 fp32), two in LDS, the next one's loads in flight while one is
 // multiplied.  LDS lines are 144 bytes apart, which spreads the 16-byte reads of 32 lines over all banks.  Where lines are contiguous

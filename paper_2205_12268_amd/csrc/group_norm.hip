@@ -6,17 +6,19 @@
 // x (backward) is the tensor, or the values that its codes stand for, with the statistics of the tensor.
 //
 // A thread owns a vector of 16 bytes of channels and walks over pixels, so that sums are by channel and groups may have any size.  The
-// statistics come from fp64 sums of x - s and its square, s the first pixel's value of the group's first channel: the variance of n
-// values is at least (s - mean)^2 / n, so what the mean takes from the squares leaves an error of n 2^-53 at most (of x itself, mean^2 /
-// var 2^-53: 10^-4 for a mean of 10^4 beside a spread of 0.05).  The mean is kept as a fp32 value and the rest that it rounds off, so y is as near for a
-// mean far above the spread.  The backward pass has the rounded mean of `stats` alone: its xh are off by up to 2^-24 |mean| rstd.
+// statistics come from fp64 sums of x - s and its square, s the first pixel's value of the group's first channel: the variance of n values
+// is at least (s - mean)^2 / n, so what the mean takes from the squares leaves an error of about n 2^-53 at most (with s = 0 it is mean^2 /
+// var 2^-53 and its growth over the sums: 10^-4 for a mean of 10^4 beside a spread of 0.05).  The mean is kept as a fp32 value and the rest
+// that it rounds off, so y is as near for a mean far above the spread.  The backward pass has the rounded mean of `stats` alone: its xh are
+// off by up to 2^-24 |mean| rstd.
 //
 // Maps that one workgroup's registers hold (a sample, some of its groups) take one launch.  Larger ones take three: sums of chunks of
-// pixels by channel; a small one that joins them; a second pass that goes backwards over the chunks, so that it begins with what
-// the caches hold; where the chunks are few, the second pass joins them and there are two.  Bound by memory: the second pass reads again what the first has read.
-// 8 x 16384 x 256 bf16, 32 groups, silu: 40 us forward (13 the first pass, 5.3 TB/s; 5 the join; 22 the second); x to codes beside y 30 in place
-// of 22; backward from codes 29, 5 and 31 (3.5 and 5.5 TB/s: in its first pass the slopes take as long as the loads).  One map of 256
-// pixels and 96 channels, by registers: 7, nearly all of it the way of one load, the statistics and one store.
+// pixels by channel; a small one that joins them; a second pass that goes backwards over the chunks, so that it begins with what the caches
+// hold; where the chunks are few, the second pass joins them and there are two.  Bound by memory: the second pass reads again what the
+// first has read. 8 x 16384 x 256 bf16, 32 groups, silu: 47 to 49 us forward on inputs in turn (19.6 the first pass, 3.4 TB/s beside the y
+// of the call before, which is still leaving the caches, and 13 without; 4.8 the join; 22.8 the second, 5.9 TB/s); x to codes beside y 31
+// in place of 23; backward from codes 29, 5 and 32 (3.5 and 5.3 TB/s: in its first pass the slopes take as long as the loads).  One map of
+// 256 pixels and 96 channels, by registers: 7, nearly all of it the way of one load, the statistics and one store.
 #include "block.h"
 
 namespace wcc {
